@@ -86,7 +86,8 @@ typedef enum {
     ZKDL_ETOOBIG = -6 /* the input exceeds the fixed work memory of an allocation-free entry point */
 } zkdl_err;
 
-typedef enum { ZKDL_I32 = 0, ZKDL_I64 = 1, ZKDL_FR_LE = 2 } zkdl_dtype;
+/* The first three are what field tensors are made of; the others are for the 8-bit layers (zkdl_mat). */
+typedef enum { ZKDL_I32 = 0, ZKDL_I64 = 1, ZKDL_FR_LE = 2, ZKDL_I8 = 3, ZKDL_F32 = 4, ZKDL_F16 = 5, ZKDL_BF16 = 6 } zkdl_dtype;
 
 typedef struct zkdl_ctx zkdl_ctx;               /* device id + borrowed hipStream_t + scratch */
 typedef struct zkdl_tensor zkdl_tensor;         /* device tensor: Fr (SoA limb planes, Montgomery) or borrowed integers */
@@ -551,6 +552,74 @@ int hyrax_verify(zkdl_ctx* ctx, const zkdl_commit_key* key, const uint8_t* commi
 /* Re-derives the constants of the base-field arithmetic on the host and checks the unreduced point additions, the
  * endomorphism's constant and the split of a scalar against plain computations; ZKDL_OK if they match. */
 int zkdl_commit_selfcheck(void);
+
+/* ---- 8-bit layers: the integers that a proof is about ------------------------
+ * A quantised network's layer Z = A W with A, W in 8 bits and Z in 32: quantisation, the norm between layers, and the
+ * integer products of the three families (Example FCNN: forward A W, gradA G_Z W^T, gradW A^T G_Z).  The int32
+ * accumulators are what sumcheck_matmul proves of the same integers.
+ *
+ * A zkdl_mat is a stack of `stack` matrices [rows, cols] in device memory; entry (s, i, j) lies at
+ * data + (s * stack_stride + i * row_stride + j) items of dtype.  Any sizes below 2^31 (no powers of two), zero among
+ * them; any strides for inputs (0 repeats a row or a matrix), for outputs no item twice: row_stride >= cols, stack_stride
+ * >= (rows - 1) row_stride + cols where stack > 1; no alignment beyond the items'.  Outputs must not overlap inputs or
+ * one another.
+ * These calls enqueue their kernels on the context's stream and return without waiting; scratch comes from the
+ * context.  Under stream capture a call of the same sizes has to have run before, and the context is not trimmed while
+ * the graph is in use.  Errors: ZKDL_EINVAL for a null pointer, a wrong type or shape; ZKDL_ETOOBIG for sums that could
+ * leave 32 bits; ZKDL_ENOMEM, ZKDL_EHIP. */
+typedef struct {
+    void* data;
+    uint64_t stack, rows, cols;
+    uint64_t row_stride, stack_stride; /* in items */
+    int32_t dtype;                     /* zkdl_dtype */
+    int32_t reserved;                  /* 0 */
+} zkdl_mat;
+
+/* zkdl_quantize_i8: symmetric 8-bit quantisation of x (ZKDL_F32 / F16 / BF16), one scale for each row (axis 1: the maximum
+ * is taken along the columns) or for each column (axis 0).  With v = x m (m: `mult`, or 1) and a = max |v|:
+ *   scale = a / 127,  q = v (127 / a) rounded to nearest, halves to even, so q in [-127, 127] and v ~ q scale.
+ * All in 32 bits; a = 0 gives q = 0 and scale 0; a row (column) that holds a NaN or an infinity, or whose products with
+ * m overflow, gives q = 0 and scale NaN.  mult: stack x cols (axis 1) or stack x rows (axis 0) floats along the axis of
+ * the maximum, or NULL: the scale of a product's other operand, folded in before a gradient is quantised.
+ * q: ZKDL_I8, shape of x.  scale: stack x rows (axis 1) or stack x cols (axis 0) floats.  values (may be NULL): q scale
+ * in the type of x, shape of x. */
+int zkdl_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale,
+                     const zkdl_mat* values);
+
+/* zkdl_rmsnorm_i8: root-mean-square norm over the columns with the residual's addition in front and an 8-bit output:
+ *   h = x + residual (residual may be NULL),  rstd = (mean_j h_j^2 + eps)^(-1/2),  y_j = h_j rstd weight_j,
+ * y quantised as by zkdl_quantize_i8 with axis 1.  A row's rstd is one factor of all its y and leaves q as it is: q is
+ * quantised from h weight, and scale is a rstd / 127.  weight: cols items of type weight_dtype, ZKDL_F32 or x's.
+ * eps: positive, normal, finite.  Stacks of one.  rstd (rows floats), total (h in x's type) and values (q scale in x's
+ * type) may be NULL.  h is summed in 32 bits and not rounded before the norm. */
+int zkdl_rmsnorm_i8(zkdl_ctx* ctx, const zkdl_mat* x, const zkdl_mat* residual, const void* weight, int weight_dtype,
+                    float eps, const zkdl_mat* q, float* scale, float* rstd, const zkdl_mat* total, const zkdl_mat* values);
+
+/* zkdl_rmsnorm_i8_backward: gradients of zkdl_rmsnorm_i8, the rounding passed straight through.  dy: gradient of y;
+ * h: the summed stream (total, or x where there was no residual); rstd: as returned; dtotal: gradient of total from its
+ * other uses, or NULL.  With n = h rstd:
+ *   dx_j = rstd (w_j dy_j - n_j mean_i(w_i dy_i n_i)) + dtotal_j  (gradient of x and of the residual alike),
+ *   dweight_j = sum over the rows of dy_j n_j (cols floats; may be NULL).
+ * dy, h, dtotal and dx have one type.  Sums in 32 bits, in an order that depends on the sizes alone. */
+int zkdl_rmsnorm_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* h, const void* weight, int weight_dtype,
+                             const float* rstd, const zkdl_mat* dtotal, const zkdl_mat* dx, float* dweight);
+
+/* zkdl_matmul_i8: out[s] = op(a[s]) op(b[s]) for ZKDL_I8 a, b; op() transposes the stored matrices where trans_a /
+ * trans_b is set.  op(a): [M, K], op(b): [K, N], out: [M, N].  Accumulators are exact 32-bit integers: K <= 2^17 - 1
+ * (ZKDL_ETOOBIG).  out of type ZKDL_I32: the accumulators (a_scale, b_scale NULL).  out of type ZKDL_F32 / F16 / BF16:
+ * (acc a_scale[s, i]) b_scale[s, j], each step in 32 bits and rounded to out's type at the end; a scale that is NULL
+ * stands for 1. */
+int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int trans_a, int trans_b, const float* a_scale,
+                   const float* b_scale, const zkdl_mat* out);
+
+/* zkdl_matmul_i8_backward: gradients of Y = (a a_scale) (w w_scale), a [M, K], w stored [K, N] or, with trans_w, [N, K],
+ * a_scale [M], w_scale [N], from dy [M, N] by two 8-bit products on the integers of the forward pass:
+ *   da = t . (q op(w)^T),   q, t = dy w_scale quantised for each row,
+ *   dw = (a^T p) . u,       p, u = a_scale dy quantised for each column,
+ * the rounding of a, w and of dy passed straight through.  da: dy's type, [M, K]; dw: ZKDL_F32, stored as w is.  Either
+ * may be NULL.  Stacks of equal depth.  M, N <= 2^17 - 1 (ZKDL_ETOOBIG). */
+int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w,
+                            const float* a_scale, const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw);
 
 /* ---- per-kernel timing (for callers that measure; paper-independent) -------
  * While enabled, the launches of the kernel classes below are bracketed by HIP

@@ -7,7 +7,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
-ZKDL_I32, ZKDL_I64, ZKDL_FR_LE = 0, 1, 2
+ZKDL_I32, ZKDL_I64, ZKDL_FR_LE, ZKDL_I8, ZKDL_F32, ZKDL_F16, ZKDL_BF16 = 0, 1, 2, 3, 4, 5, 6
 ERRORS = {0: "ok", -1: "ZKDL_EINVAL", -2: "ZKDL_ERANGE", -3: "ZKDL_ENOMEM", -4: "ZKDL_EHIP",
           -5: "ZKDL_ESMALL", -6: "ZKDL_ETOOBIG"}
 
@@ -24,6 +24,7 @@ EXPORTED_SYMBOLS = [
     "zkdl_ctx_profile_enable", "zkdl_ctx_profile_reset", "zkdl_ctx_profile_read", "zkdl_selfbench",
     "zkdl_commit_key_create", "zkdl_commit_key_destroy", "zkdl_commit_key_generators", "hyrax_commit", "hyrax_open",
     "zkdl_commit_selfcheck", "aggregate_verify", "zkdl_host_aggregate_verify",
+    "zkdl_quantize_i8", "zkdl_rmsnorm_i8", "zkdl_rmsnorm_i8_backward", "zkdl_matmul_i8", "zkdl_matmul_i8_backward",
 ]
 
 PROF_CLASSES = {"sc_round_fused": 0, "sc_round_first": 1, "partial_eval": 2, "zk_bin": 3, "zk_lin": 4,
@@ -47,6 +48,12 @@ class FcnnWitness(C.Structure):
 class Claim(C.Structure):
     _fields_ = [("tensor", C.c_uint32), ("nseg", C.c_uint32), ("seg_off", C.c_uint32 * 4),
                 ("seg_len", C.c_uint32 * 4), ("value", C.c_uint8 * 32)]
+
+
+class Mat(C.Structure):
+    """zkdl_mat: a stack of matrices in device memory."""
+    _fields_ = [("data", C.c_void_p), ("stack", C.c_uint64), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("row_stride", C.c_uint64), ("stack_stride", C.c_uint64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 CLAIM_TENSORS = ["A", "W", "GZ", "Z", "ZR", "GA", "GW", "A_RELU", "GZ_RELU", "GZ_NEXT", "W_NEXT", "AUX",
@@ -112,6 +119,11 @@ def load_library():
         "zkdl_commit_selfcheck": [],
         "aggregate_verify": [vp, vp, sz, vp, C.POINTER(i), vp, psz, vp, psz],
         "zkdl_host_aggregate_verify": [vp, sz, vp, C.POINTER(i), vp, psz, vp, psz],
+        "zkdl_quantize_i8": [vp, vp, i, vp, vp, vp, vp],
+        "zkdl_rmsnorm_i8": [vp, vp, vp, vp, i, C.c_float, vp, vp, vp, vp, vp],
+        "zkdl_rmsnorm_i8_backward": [vp, vp, vp, vp, i, vp, vp, vp, vp],
+        "zkdl_matmul_i8": [vp, vp, vp, i, i, vp, vp, vp],
+        "zkdl_matmul_i8_backward": [vp, vp, vp, vp, i, vp, vp, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -147,6 +159,7 @@ class Context:
             stream = torch.cuda.current_stream(device).cuda_stream
         self.handle = C.c_void_p()
         self.device = device
+        self.stream = int(stream)
         _check(lib.zkdl_ctx_create(C.byref(self.handle), device, C.c_void_p(stream)), "zkdl_ctx_create")
 
     def profile(self, on=True, reset=True):
@@ -661,3 +674,188 @@ def aggregate_verify(ctx, proof, tr):
                  value=int.from_bytes(bytes(c.value), "little"))
             for c in claims[:ncl.value]]
     return out
+
+
+# ---- 8-bit layers ----------------------------------------------------------------------------------------------------
+# Operators on CUDA tensors of the context's device: two-dimensional, or three-dimensional stacks where said.  They enqueue
+# their kernels on the context's stream and return without waiting.  Where the current stream is another one, each of the
+# two waits for the other, so that inputs and outputs are the current stream's as with any torch operator.
+
+_DTYPES = None
+
+
+def _dtypes():
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: ZKDL_F32, torch.float16: ZKDL_F16, torch.bfloat16: ZKDL_BF16, torch.int8: ZKDL_I8,
+                   torch.int32: ZKDL_I32}
+    return _DTYPES
+
+
+def _mat(ctx, t, what, dims=(2, 3)):
+    """(descriptor, transposed): a stack whose rows or, transposed, columns are adjacent in memory."""
+    code = _dtypes().get(t.dtype)
+    if code is None or not t.is_cuda or t.get_device() != ctx.device or t.dim() not in dims:
+        raise ValueError(f"{what}: a {' or '.join(str(d) for d in dims)}-dimensional tensor on device {ctx.device} of a type "
+                         f"the operator knows is needed, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    sh, st = t.shape, t.stride()
+    stack, ss = (sh[0], st[0]) if len(sh) == 3 else (1, 0)
+    if st[-1] == 1 or sh[-1] <= 1:
+        return Mat(t.data_ptr(), stack, sh[-2], sh[-1], st[-2], ss, code, 0), False
+    if st[-2] == 1 or sh[-2] <= 1:
+        return Mat(t.data_ptr(), stack, sh[-1], sh[-2], st[-1], ss, code, 0), True
+    raise ValueError(f"{what}: neither rows nor columns are adjacent in memory (strides {tuple(st)})")
+
+
+def _rows(ctx, t, what, dims=(2, 3)):
+    m, turned = _mat(ctx, t, what, dims)
+    if turned:
+        raise ValueError(f"{what}: the entries of a row have to be adjacent in memory (strides {tuple(t.stride())})")
+    return m
+
+
+def _vec(ctx, t, shape, what, dtype=None):
+    """Address of a contiguous vector (or a stack of them) of 32-bit floats, or of `dtype`."""
+    import torch
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype not in (torch.float32, dtype) or not t.is_cuda or t.get_device() != ctx.device \
+            or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous float32 tensor of shape {tuple(shape)} on device {ctx.device} is needed, not "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+class _OnStream:
+    """Orders a call on the context's stream against the current one where the two differ: the context's stream waits for
+    what the current one has been given, and the current one for the call."""
+
+    def __init__(self, ctx):
+        import torch
+        self.other = None
+        now = torch.cuda.current_stream(ctx.device)
+        if now.cuda_stream != ctx.stream:
+            self.now = now
+            self.other = torch.cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else torch.cuda.default_stream(ctx.device)
+            self.other.wait_stream(now)
+
+    def done(self):
+        if self.other is not None:
+            self.now.wait_stream(self.other)
+
+
+def _codes_like(x):
+    """8-bit integers in the shape of x whose rows start at multiples of 16 bytes, as the products like them."""
+    import torch
+    n = x.shape[-1]
+    return torch.empty(x.shape[:-1] + ((n + 15) // 16 * 16,), dtype=torch.int8, device=x.device)[..., :n]
+
+
+def quantize_i8(ctx, x, axis=-1, mult=None, values=False):
+    """x [.., M, N] (float32, float16, bfloat16) -> dict(q, scale, values): 8-bit integers q with x mult ~ q scale.
+    axis: the axis that shares a scale: -1 a scale for each row, -2 a scale for each column.  mult: None or float32
+    factors along that axis.  values: also q scale in the type of x.  (zkdl_quantize_i8)"""
+    import torch
+    mx = _rows(ctx, x, "x")
+    if axis not in (-1, -2):
+        raise ValueError("axis: -1 (a scale for each row) or -2 (a scale for each column)")
+    lead = tuple(x.shape[:-2])
+    m, n = x.shape[-2:]
+    pm = _vec(ctx, mult, lead + ((n,) if axis == -1 else (m,)), "mult")
+    on = _OnStream(ctx)
+    q = _codes_like(x)
+    scale = torch.empty(lead + ((m,) if axis == -1 else (n,)), dtype=torch.float32, device=x.device)
+    v = torch.empty(x.shape, dtype=x.dtype, device=x.device) if values else None
+    _check(load_library().zkdl_quantize_i8(ctx.handle, C.byref(mx), 1 if axis == -1 else 0, pm, C.byref(_rows(ctx, q, "q")),
+                                           scale.data_ptr(), C.byref(_rows(ctx, v, "values")) if values else None),
+           "zkdl_quantize_i8", ctx)
+    on.done()
+    return dict(q=q, scale=scale, values=v)
+
+
+def rmsnorm_i8(ctx, x, weight, residual=None, eps=1e-6, values=False):
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight, in 8 bits with a scale for each row.  x [M, N]; weight [N]
+    in the type of x or float32.  Returns dict(q, scale, rstd, total, values): total = h in the type of x (None without a
+    residual: x itself), values = q scale if asked for.  (zkdl_rmsnorm_i8)"""
+    import torch
+    mx = _rows(ctx, x, "x", (2,))
+    mr = _rows(ctx, residual, "residual", (2,)) if residual is not None else None
+    m, n = x.shape
+    pw = _vec(ctx, weight, (n,), "weight", x.dtype)
+    on = _OnStream(ctx)
+    q = _codes_like(x)
+    stats = torch.empty((2, m), dtype=torch.float32, device=x.device)
+    total = torch.empty((m, n), dtype=x.dtype, device=x.device) if residual is not None else None
+    v = torch.empty((m, n), dtype=x.dtype, device=x.device) if values else None
+    _check(load_library().zkdl_rmsnorm_i8(ctx.handle, C.byref(mx), C.byref(mr) if mr is not None else None, pw,
+                                          _dtypes()[weight.dtype], eps, C.byref(_rows(ctx, q, "q")), stats.data_ptr(),
+                                          stats.data_ptr() + 4 * m, C.byref(_rows(ctx, total, "total")) if total is not None else None,
+                                          C.byref(_rows(ctx, v, "values")) if values else None), "zkdl_rmsnorm_i8", ctx)
+    on.done()
+    return dict(q=q, scale=stats[0], rstd=stats[1], total=total, values=v)
+
+
+def rmsnorm_i8_backward(ctx, dy, h, weight, rstd, dtotal=None):
+    """Gradients of rmsnorm_i8: dy [M, N] of the normalised output, h the summed stream (total, or x without a residual),
+    rstd as returned, dtotal of the summed stream's other uses.  Returns dict(dx, dweight): dx belongs to x and to the
+    residual, dweight is float32.  (zkdl_rmsnorm_i8_backward)"""
+    import torch
+    mdy, mh = _rows(ctx, dy, "dy", (2,)), _rows(ctx, h, "h", (2,))
+    mt = _rows(ctx, dtotal, "dtotal", (2,)) if dtotal is not None else None
+    m, n = dy.shape
+    pw = _vec(ctx, weight, (n,), "weight", dy.dtype)
+    ps = _vec(ctx, rstd, (m,), "rstd")
+    on = _OnStream(ctx)
+    dx = torch.empty((m, n), dtype=dy.dtype, device=dy.device)
+    dw = torch.empty((n,), dtype=torch.float32, device=dy.device)
+    _check(load_library().zkdl_rmsnorm_i8_backward(ctx.handle, C.byref(mdy), C.byref(mh), pw, _dtypes()[weight.dtype], ps,
+                                                   C.byref(mt) if mt is not None else None, C.byref(_rows(ctx, dx, "dx")),
+                                                   dw.data_ptr()), "zkdl_rmsnorm_i8_backward", ctx)
+    on.done()
+    return dict(dx=dx, dweight=dw)
+
+
+def matmul_i8(ctx, a, b, a_scale=None, b_scale=None, trans_a=False, trans_b=False, dtype=None):
+    """op(a) op(b) of int8 matrices [.., M, K], [.., K, N] (stored transposed where trans_a / trans_b says so; transposed
+    views do as well).  dtype int32 (the default without scales): the exact accumulators; float32, float16 or bfloat16 (the
+    default with scales): acc a_scale[.., i] b_scale[.., j].  (zkdl_matmul_i8)"""
+    import torch
+    ma, ta = _mat(ctx, a, "a")
+    mb, tb = _mat(ctx, b, "b")
+    if a.dim() != b.dim():
+        raise ValueError("a and b: two matrices or two stacks")
+    lead = tuple(a.shape[:-2])
+    m, n = a.shape[-1 if trans_a else -2], b.shape[-2 if trans_b else -1]
+    if dtype is None:
+        dtype = torch.int32 if a_scale is None and b_scale is None else torch.bfloat16
+    pa, pb = _vec(ctx, a_scale, lead + (m,), "a_scale"), _vec(ctx, b_scale, lead + (n,), "b_scale")
+    on = _OnStream(ctx)
+    out = torch.empty(lead + (m, n), dtype=dtype, device=a.device)
+    _check(load_library().zkdl_matmul_i8(ctx.handle, C.byref(ma), C.byref(mb), int(bool(trans_a) != ta), int(bool(trans_b) != tb),
+                                         pa, pb, C.byref(_rows(ctx, out, "out"))), "zkdl_matmul_i8", ctx)
+    on.done()
+    return out
+
+
+def matmul_i8_backward(ctx, dy, a, a_scale, w, w_scale, trans_w=False, need_da=True, need_dw=True):
+    """Gradients of (a a_scale) (w w_scale), a [.., M, K], w [.., K, N] (trans_w: [.., N, K]), from dy [.., M, N] by two 8-bit
+    products on the forward's integers.  Returns dict(da, dw): da in the type of dy, dw float32 in the layout of w.
+    (zkdl_matmul_i8_backward)"""
+    import torch
+    mdy, ma, mw = _rows(ctx, dy, "dy"), _rows(ctx, a, "a"), _rows(ctx, w, "w")
+    if not dy.dim() == a.dim() == w.dim():
+        raise ValueError("dy, a and w: three matrices or three stacks")
+    lead = tuple(dy.shape[:-2])
+    pa, pw = _vec(ctx, a_scale, lead + (dy.shape[-2],), "a_scale"), _vec(ctx, w_scale, lead + (dy.shape[-1],), "w_scale")
+    if pa is None or pw is None:
+        raise ValueError("a_scale and w_scale are needed")
+    on = _OnStream(ctx)
+    da = torch.empty(a.shape, dtype=dy.dtype, device=dy.device) if need_da else None
+    dw = torch.empty(w.shape, dtype=torch.float32, device=dy.device) if need_dw else None
+    _check(load_library().zkdl_matmul_i8_backward(ctx.handle, C.byref(mdy), C.byref(ma), C.byref(mw), int(bool(trans_w)), pa, pw,
+                                                  C.byref(_rows(ctx, da, "da")) if need_da else None,
+                                                  C.byref(_rows(ctx, dw, "dw")) if need_dw else None),
+           "zkdl_matmul_i8_backward", ctx)
+    on.done()
+    return dict(da=da, dw=dw)

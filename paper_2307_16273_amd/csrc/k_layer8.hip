@@ -1,0 +1,641 @@
+// Quantisation to 8 bits and the norm between 8-bit layers (zkdl_quantize_i8, zkdl_rmsnorm_i8, zkdl_rmsnorm_i8_backward).
+// Every kernel here is bound by memory: a value costs a few instructions and 2 to 9 bytes, so a row is read once, kept in
+// registers while its maximum (and mean square) is reduced, and written once.
+#include <float.h>
+
+#include "layer8.cuh"
+
+// ---------------------------------------------------------------------------
+// Rows: v = (x [+ residual]) * w, largest |v| of the row, q = rint(v * 127 / that).
+// A row belongs to G threads (a wave, or a block of four) and each of them keeps ITEMS vectors of 8 values; ITEMS = 0 is
+// for rows too long for the registers, which are read twice.
+// ---------------------------------------------------------------------------
+struct L8RowArgs {
+    uint64_t rows, per_stack;     // rows in all, rows of a matrix
+    uint32_t cols;
+    const void* w;                // norm: cols weights; else cols multipliers for each matrix, or null
+    int w_f32;                    // w is 32 bits (else the values' type)
+    uint64_t w_stack;             // items of w for each matrix
+    float eps;
+    float* scale;
+    float* rstd;
+};
+
+template <class T>
+static __device__ __forceinline__ void l8_weights(const L8RowArgs& a, uint64_t s, uint32_t j, int n, float (&f)[8]) {
+    if (!a.w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 1.f;
+    } else if (a.w_f32) {
+        l8_load((const float*)a.w + s * a.w_stack + j, n, f);
+    } else {
+        l8_load((const T*)a.w + s * a.w_stack + j, n, f);
+    }
+}
+
+// sum and maximum over the G threads of a row
+template <int G>
+static __device__ __forceinline__ void l8_row_reduce(float& sum, uint32_t& top) {
+    sum = l8_wave_sum(sum);
+    top = l8_wave_max(top);
+    if constexpr (G > 64) {
+        __shared__ float s_sum[G / 64];
+        __shared__ uint32_t s_top[G / 64];
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            s_sum[threadIdx.x >> 6] = sum;
+            s_top[threadIdx.x >> 6] = top;
+        }
+        __syncthreads();
+        sum = 0.f;
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < G / 64; ++i) {
+            sum += s_sum[i];
+            top = max(top, s_top[i]);
+        }
+    }
+}
+
+template <class T, bool NORM, int G, int ITEMS>
+__global__ __launch_bounds__(256) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
+                                                 L8Mat<T> values) {
+    constexpr int GROUPS = 256 / G;
+    const uint32_t t = threadIdx.x % G;
+    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    // all groups of a block take as many turns: the reductions of a block-wide group meet at barriers
+    for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
+        const uint64_t r = r0 + threadIdx.x / G;
+        if (GROUPS > 1 && r >= a.rows) continue;
+        const uint64_t s = r / a.per_stack, m = r % a.per_stack;
+        const T* xr = x.p + s * x.ss + m * x.rs;
+        const T* rr = res.p ? res.p + s * res.ss + m * res.rs : nullptr;
+        T* tr = total.p ? total.p + s * total.ss + m * total.rs : nullptr;
+        float keep[ITEMS ? ITEMS : 1][8];
+        float ss = 0.f;
+        uint32_t top = 0;
+        auto sum_at = [&](uint32_t j, float (&h)[8]) {
+            const int n = (int)min(a.cols - j, 8u);
+            l8_load(xr + j, n, h);
+            if (NORM && rr) {
+                float b[8];
+                l8_load(rr + j, n, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[i] += b[i];
+            }
+        };
+        auto first = [&](uint32_t j, float (&v)[8]) {
+            const int n = (int)min(a.cols - j, 8u);
+            sum_at(j, v);
+            if (NORM) {
+                if (tr) l8_store(tr + j, n, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+            }
+            if (a.w) {
+                float w[8];
+                l8_weights<T>(a, s, j, n, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= w[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, l8_mag(v[i]));
+        };
+        if constexpr (ITEMS > 0) {
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const uint32_t j = (k * G + t) * 8;
+                if (j < a.cols) first(j, keep[k]);
+            }
+        } else {
+            for (uint32_t j = t * 8; j < a.cols; j += G * 8) first(j, keep[0]);
+        }
+        l8_row_reduce<G>(ss, top);
+        float rstd = 1.f;
+        if (NORM) {
+            if (l8_mag(ss) >= L8_INF) {      // the squares left the range (or an input did): once more, 2^-80 smaller
+                float again = 0.f;
+                uint32_t unused = 0;
+                for (uint32_t j = t * 8; j < a.cols; j += G * 8) {
+                    float h[8];
+                    sum_at(j, h);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float y = h[i] * 0x1p-80f;
+                        again = fmaf(y, y, again);
+                    }
+                }
+                l8_row_reduce<G>(again, unused);
+                rstd = 0x1p-80f / sqrtf(again / (float)a.cols);
+            } else {
+                rstd = 1.f / sqrtf(ss / (float)a.cols + a.eps);
+            }
+        }
+        const L8Quant c = l8_quant(top);
+        float scale = __uint_as_float(top) / 127.f;
+        if (NORM) scale = __uint_as_float(top) * rstd / 127.f;
+        if (!c.finite) scale = __uint_as_float(0x7fc00000u);
+        if (t == 0) {
+            a.scale[r] = scale;
+            if (NORM && a.rstd) a.rstd[r] = rstd;
+        }
+        int8_t* qr = q.p + s * q.ss + m * q.rs;
+        T* vr = values.p ? values.p + s * values.ss + m * values.rs : nullptr;
+        auto second = [&](uint32_t j, float (&v)[8]) {
+            const int n = (int)min(a.cols - j, 8u);
+            int iq[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[i], c);
+            l8_store_q(qr + j, n, iq);
+            if (vr) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = (float)iq[i] * scale;
+                l8_store(vr + j, n, v);
+            }
+        };
+        if constexpr (ITEMS > 0) {
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const uint32_t j = (k * G + t) * 8;
+                if (j < a.cols) second(j, keep[k]);
+            }
+        } else {
+            for (uint32_t j = t * 8; j < a.cols; j += G * 8) {
+                float v[8], w[8];
+                sum_at(j, v);
+                if (a.w) {
+                    l8_weights<T>(a, s, j, (int)min(a.cols - j, 8u), w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] *= w[i];
+                }
+                second(j, v);
+            }
+        }
+    }
+}
+
+// zeros by a kernel and not by a memory operation: the calls may be captured into a graph
+__global__ __launch_bounds__(256) void k_l8_zero(float* p, uint64_t n) {
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < n; i += gridDim.x * 256ull) p[i] = 0.f;
+}
+
+// blocks of a launch that walks over `units` of work: enough to fill the device several times over
+static unsigned l8_grid(uint64_t units) { return (unsigned)(units < 65536 ? units : 65536); }
+
+template <class T, bool NORM>
+static void l8_launch_rows(zkdl_ctx* ctx, const L8RowArgs& a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
+                           L8Mat<T> values) {
+    const uint32_t n = a.cols;
+#define L8_ROWS(G, ITEMS) \
+    hipLaunchKernelGGL((k_l8_rows<T, NORM, G, ITEMS>), dim3(l8_grid(l8_ceil(a.rows, 256 / G))), dim3(256), 0, ctx->stream, a, x, res, q, total, values)
+    if (n <= 512) L8_ROWS(64, 1);
+    else if (n <= 1024) L8_ROWS(64, 2);
+    else if (n <= 2048) L8_ROWS(256, 1);
+    else if (n <= 4096) L8_ROWS(256, 2);
+    else if (n <= 8192) L8_ROWS(256, 4);
+    else if (n <= 16384) L8_ROWS(256, 8);
+    else L8_ROWS(256, 0);
+#undef L8_ROWS
+}
+
+// ---------------------------------------------------------------------------
+// Columns: a block looks at 64 columns x a chunk of rows; largest magnitudes of the chunks, then the values once more (they
+// come from the last-level cache for anything below 256 MB).  A chunk that is a whole column needs no second launch.
+// ---------------------------------------------------------------------------
+constexpr int L8_COL_T = 8, L8_COL_R = 32;      // 8 threads of 8 columns, 32 rows at a time
+struct L8ColArgs {
+    uint64_t rows, chunk;         // chunk: rows of a block
+    uint32_t cols, chunks;
+    const float* mult;            // rows for each matrix, or null
+    uint32_t* part;               // [stack][chunks][cols] largest magnitudes
+    float* scale;                 // [stack][cols]
+};
+
+template <class T>
+static __device__ __forceinline__ void l8_col_values(const L8ColArgs& a, const L8Mat<const T>& x, uint64_t s, uint64_t m, uint32_t j, int n,
+                                                     float (&v)[8]) {
+    l8_load(x.p + s * x.ss + m * x.rs + j, n, v);
+    if (a.mult) {
+        const float f = a.mult[s * a.rows + m];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= f;
+    }
+}
+
+// MODE 0: largest magnitudes of a chunk -> part; 1: quantise a chunk; 2: both, the chunk being all rows
+template <class T, int MODE>
+__global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, L8Mat<int8_t> q, L8Mat<T> values) {
+    __shared__ uint32_t s_top[L8_COL_R][L8_COL_T * 8 + 1];
+    const uint32_t tx = threadIdx.x % L8_COL_T, ty = threadIdx.x / L8_COL_T;
+    const uint32_t c0 = blockIdx.x * (L8_COL_T * 8), j = c0 + tx * 8;
+    const uint64_t s = blockIdx.z;
+    const uint64_t lo = blockIdx.y * a.chunk, hi = min(lo + a.chunk, a.rows);
+    const bool live = j < a.cols;
+    const int n = live ? (int)min(a.cols - j, 8u) : 0;
+    uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (MODE != 1) {
+        if (live)
+            for (uint64_t m = lo + ty; m < hi; m += L8_COL_R) {
+                float v[8];
+                l8_col_values(a, x, s, m, j, n, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top[i] = max(top[i], l8_mag(v[i]));
+            }
+    } else if (live) {
+        for (uint32_t k = ty; k < a.chunks; k += L8_COL_R)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) top[i] = max(top[i], a.part[(s * a.chunks + k) * a.cols + j + i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s_top[ty][tx * 8 + i] = top[i];
+    __syncthreads();
+    if (threadIdx.x < L8_COL_T * 8) {
+        uint32_t b = 0;
+        for (int k = 0; k < L8_COL_R; ++k) b = max(b, s_top[k][threadIdx.x]);
+        s_top[0][threadIdx.x] = b;
+        if (c0 + threadIdx.x < a.cols) {
+            if (MODE == 0) a.part[(s * a.chunks + blockIdx.y) * a.cols + c0 + threadIdx.x] = b;
+            else if (blockIdx.y == 0) a.scale[s * a.cols + c0 + threadIdx.x] = b < L8_INF ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+        }
+    }
+    if (MODE == 0) return;
+    __syncthreads();
+    if (!live) return;
+    L8Quant c[8];
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = s_top[0][tx * 8 + i];
+        c[i] = l8_quant(b);
+        scale[i] = c[i].finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+    }
+    for (uint64_t m = lo + ty; m < hi; m += L8_COL_R) {
+        float v[8];
+        l8_col_values(a, x, s, m, j, n, v);
+        int iq[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[i], c[i]);
+        l8_store_q(q.p + s * q.ss + m * q.rs + j, n, iq);
+        if (values.p) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)iq[i] * scale[i];
+            l8_store(values.p + s * values.ss + m * values.rs + j, n, v);
+        }
+    }
+}
+
+template <class T>
+static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values) {
+    L8ColArgs a;
+    a.rows = x->rows;
+    a.cols = (uint32_t)x->cols;
+    a.mult = mult;
+    a.scale = scale;
+    a.part = nullptr;
+    const uint64_t tiles = l8_ceil(x->cols, L8_COL_T * 8);
+    // the grid's axes hold 65535 blocks: matrices of a longer stack go in launches of their own
+    for (uint64_t s0 = 0; s0 < x->stack; s0 += 65535) {
+        const uint64_t ns = x->stack - s0 < 65535 ? x->stack - s0 : 65535;
+        // four blocks for each compute unit, of 64 rows and more
+        uint64_t chunks = l8_ceil(1024, tiles * ns);
+        if (chunks > l8_ceil(x->rows, 64)) chunks = l8_ceil(x->rows, 64);
+        if (chunks < 1) chunks = 1;
+        a.chunk = l8_ceil(l8_ceil(x->rows, chunks), L8_COL_R) * L8_COL_R;
+        a.chunks = (uint32_t)l8_ceil(x->rows, a.chunk);
+        L8Mat<const T> mx = l8_mat<const T>(x);
+        L8Mat<int8_t> mq = l8_mat<int8_t>(q);
+        L8Mat<T> mv = l8_mat<T>(values);
+        mx.p += s0 * mx.ss;
+        mq.p += s0 * mq.ss;
+        if (mv.p) mv.p += s0 * mv.ss;
+        a.mult = mult ? mult + s0 * x->rows : nullptr;
+        a.scale = scale + s0 * x->cols;
+        const dim3 grid((unsigned)tiles, a.chunks, (unsigned)ns);
+        if (a.chunks == 1) {
+            hipLaunchKernelGGL((k_l8_cols<T, 2>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+            continue;
+        }
+        a.part = (uint32_t*)zk_alloc(ctx, ns * a.chunks * x->cols * 4);
+        if (!a.part) return ZKDL_ENOMEM;
+        hipLaunchKernelGGL((k_l8_cols<T, 0>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+        hipLaunchKernelGGL((k_l8_cols<T, 1>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+        zk_free(ctx, a.part);
+    }
+    return ZKDL_OK;
+}
+
+template <class T>
+static int l8_quantize(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values) {
+    if (axis == 0) return l8_quant_cols<T>(ctx, x, mult, q, scale, values);
+    L8RowArgs a = {};
+    a.rows = x->stack * x->rows;
+    a.per_stack = x->rows;
+    a.cols = (uint32_t)x->cols;
+    a.w = mult;
+    a.w_f32 = 1;
+    a.w_stack = x->cols;
+    a.scale = scale;
+    l8_launch_rows<T, false>(ctx, a, l8_mat<const T>(x), L8Mat<const T>{nullptr, 0, 0}, l8_mat<int8_t>(q), L8Mat<T>{nullptr, 0, 0}, l8_mat<T>(values));
+    return ZKDL_OK;
+}
+
+int zk_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values) {
+    switch (x->dtype) {
+        case ZKDL_F32: return l8_quantize<float>(ctx, x, axis, mult, q, scale, values);
+        case ZKDL_F16: return l8_quantize<__half>(ctx, x, axis, mult, q, scale, values);
+        default: return l8_quantize<bf16_t>(ctx, x, axis, mult, q, scale, values);
+    }
+}
+
+extern "C" int zkdl_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale,
+                                const zkdl_mat* values) try {
+    if (!ctx || !l8_mat_ok(x, false) || !l8_mat_ok(q, true) || !l8_is_float(x->dtype) || q->dtype != ZKDL_I8 || !l8_same_shape(x, q) ||
+        (axis != 0 && axis != 1))
+        return ZKDL_EINVAL;
+    if (values && (!l8_mat_ok(values, true) || values->dtype != x->dtype || !l8_same_shape(x, values))) return ZKDL_EINVAL;
+    const uint64_t scales = x->stack * (axis ? x->rows : x->cols);
+    if (scales && !scale) return ZKDL_EINVAL;
+    if (axis == 0 && x->cols >= (uint64_t)1 << 30) return ZKDL_ETOOBIG;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    if (scales && (axis ? x->cols : x->rows) == 0) {        // scales of nothing
+        hipLaunchKernelGGL(k_l8_zero, dim3(l8_grid(l8_ceil(scales, 256))), dim3(256), 0, ctx->stream, scale, scales);
+        ZK_HIP(ctx, hipGetLastError());
+        return ZKDL_OK;
+    }
+    if (!scales) return ZKDL_OK;
+    const int rc = zk_quantize_i8(ctx, x, axis, mult, q, scale, values);
+    if (rc != ZKDL_OK) return rc;
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+extern "C" int zkdl_rmsnorm_i8(zkdl_ctx* ctx, const zkdl_mat* x, const zkdl_mat* residual, const void* weight, int weight_dtype, float eps,
+                               const zkdl_mat* q, float* scale, float* rstd, const zkdl_mat* total, const zkdl_mat* values) try {
+    if (!ctx || !l8_mat_ok(x, false) || !l8_mat_ok(q, true) || !l8_is_float(x->dtype) || q->dtype != ZKDL_I8 || !l8_same_shape(x, q) ||
+        x->stack != 1)
+        return ZKDL_EINVAL;
+    if (residual && (!l8_mat_ok(residual, false) || residual->dtype != x->dtype || !l8_same_shape(x, residual))) return ZKDL_EINVAL;
+    for (const zkdl_mat* o : {total, values})
+        if (o && (!l8_mat_ok(o, true) || o->dtype != x->dtype || !l8_same_shape(x, o))) return ZKDL_EINVAL;
+    if (weight_dtype != ZKDL_F32 && weight_dtype != x->dtype) return ZKDL_EINVAL;
+    if (!(eps >= FLT_MIN) || !(eps <= FLT_MAX)) return ZKDL_EINVAL;
+    if (x->rows == 0) return ZKDL_OK;
+    if (x->cols == 0 || !weight || !scale) return ZKDL_EINVAL;      // the mean over no entries is no number
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    L8RowArgs a = {};
+    a.rows = a.per_stack = x->rows;
+    a.cols = (uint32_t)x->cols;
+    a.w = weight;
+    a.w_f32 = weight_dtype == ZKDL_F32;
+    a.eps = eps;
+    a.scale = scale;
+    a.rstd = rstd;
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        l8_launch_rows<T, true>(ctx, a, l8_mat<const T>(x), l8_mat<const T>(residual), l8_mat<int8_t>(q), l8_mat<T>(total), l8_mat<T>(values));
+    };
+    if (x->dtype == ZKDL_F32) go(float{});
+    else if (x->dtype == ZKDL_F16) go(__half{});
+    else go(bf16_t{});
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of the norm.  A group of G threads walks over rows with fixed columns for each thread, so that its share of
+// dweight stays in registers; the blocks' shares are summed by a second kernel, always in the same order.
+// ---------------------------------------------------------------------------
+struct L8BackArgs {
+    uint64_t rows;
+    uint32_t cols;
+    const void* w;
+    int w_f32;
+    const float* rstd;
+    float* part;        // [blocks][cols], or null
+};
+
+template <class T, int G, int ITEMS>
+__global__ __launch_bounds__(256) void k_l8_norm_back(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h, L8Mat<const T> dt, L8Mat<T> dx) {
+    constexpr int GROUPS = 256 / G;
+    const uint32_t t = threadIdx.x % G;
+    L8RowArgs wa = {};
+    wa.w = a.w;
+    wa.w_f32 = a.w_f32;
+    float dw[ITEMS][8] = {};
+    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    const float over = 1.f / (float)a.cols;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
+        const uint64_t m = r0 + threadIdx.x / G;
+        if (GROUPS > 1 && m >= a.rows) continue;
+        const float rstd = a.rstd[m];
+        float g[ITEMS][8], n[ITEMS][8];
+        float dot = 0.f;
+        uint32_t unused = 0;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint32_t j = (k * G + t) * 8;
+            if (j < a.cols) {
+                const int c = (int)min(a.cols - j, 8u);
+                float w[8];
+                l8_load(dy.p + m * dy.rs + j, c, g[k]);
+                l8_load(h.p + m * h.rs + j, c, n[k]);
+                l8_weights<T>(wa, 0, j, c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    n[k][i] *= rstd;
+                    dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
+                    g[k][i] *= w[i];
+                    dot = fmaf(g[k][i], n[k][i], dot);
+                }
+            }
+        }
+        l8_row_reduce<G>(dot, unused);
+        dot *= over;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint32_t j = (k * G + t) * 8;
+            if (j < a.cols) {
+                const int c = (int)min(a.cols - j, 8u);
+                float d[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-n[k][i], dot, g[k][i]);
+                if (dt.p) {
+                    float e[8];
+                    l8_load(dt.p + m * dt.rs + j, c, e);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] += e[i];
+                }
+                l8_store(dx.p + m * dx.rs + j, c, d);
+            }
+        }
+    }
+    if (!a.part) return;
+    if constexpr (GROUPS > 1) {
+        __shared__ float s_dw[GROUPS][G * ITEMS * 8];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s_dw[threadIdx.x / G][(k * G + t) * 8 + i] = dw[k][i];
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < a.cols; j += 256) {
+            float s = 0.f;
+            for (int k = 0; k < GROUPS; ++k) s += s_dw[k][j];
+            a.part[(uint64_t)blockIdx.x * a.cols + j] = s;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint32_t j = (k * G + t) * 8;
+            if (j < a.cols) l8_store(a.part + (uint64_t)blockIdx.x * a.cols + j, (int)min(a.cols - j, 8u), dw[k]);
+        }
+    }
+}
+
+// Rows too long for the registers: dx with the row read twice, and dweight by columns.
+template <class T>
+__global__ __launch_bounds__(256) void k_l8_norm_back_long(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h, L8Mat<const T> dt, L8Mat<T> dx) {
+    L8RowArgs wa = {};
+    wa.w = a.w;
+    wa.w_f32 = a.w_f32;
+    const float over = 1.f / (float)a.cols;
+    for (uint64_t m = blockIdx.x; m < a.rows; m += gridDim.x) {
+        const float rstd = a.rstd[m];
+        float dot = 0.f;
+        uint32_t unused = 0;
+        auto at = [&](uint32_t j, int c, float (&g)[8], float (&n)[8]) {
+            float w[8];
+            l8_load(dy.p + m * dy.rs + j, c, g);
+            l8_load(h.p + m * h.rs + j, c, n);
+            l8_weights<T>(wa, 0, j, c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] *= rstd;
+                g[i] *= w[i];
+            }
+        };
+        for (uint32_t j = threadIdx.x * 8; j < a.cols; j += 2048) {
+            float g[8], n[8];
+            at(j, (int)min(a.cols - j, 8u), g, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot = fmaf(g[i], n[i], dot);
+        }
+        l8_row_reduce<256>(dot, unused);
+        dot *= over;
+        for (uint32_t j = threadIdx.x * 8; j < a.cols; j += 2048) {
+            const int c = (int)min(a.cols - j, 8u);
+            float g[8], n[8];
+            at(j, c, g, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = rstd * fmaf(-n[i], dot, g[i]);
+            if (dt.p) {
+                float e[8];
+                l8_load(dt.p + m * dt.rs + j, c, e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] += e[i];
+            }
+            l8_store(dx.p + m * dx.rs + j, c, g);
+        }
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_l8_dweight_long(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h) {
+    const uint64_t j = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (j >= a.cols) return;
+    const int c = (int)min(a.cols - j, (uint64_t)8);
+    float dw[8] = {};
+    for (uint64_t m = blockIdx.y; m < a.rows; m += gridDim.y) {
+        float g[8], n[8];
+        l8_load(dy.p + m * dy.rs + j, c, g);
+        l8_load(h.p + m * h.rs + j, c, n);
+        const float rstd = a.rstd[m];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[i] = fmaf(g[i], n[i] * rstd, dw[i]);
+    }
+    l8_store(a.part + blockIdx.y * (uint64_t)a.cols + j, c, dw);
+}
+
+// out[j] = sum over the blocks' shares: 64 columns x 16 runs of shares, the runs' sums added in their order
+__global__ __launch_bounds__(1024) void k_l8_sum_shares(const float* part, uint32_t shares, uint32_t cols, float* out) {
+    __shared__ float s[16][64];
+    const uint32_t tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    for (uint64_t j0 = (uint64_t)blockIdx.x * 64; j0 < cols; j0 += gridDim.x * 64ull) {
+        const uint64_t j = j0 + tx;
+        float x = 0.f;
+        if (j < cols)
+            for (uint32_t k = ty; k < shares; k += 16) x += part[(uint64_t)k * cols + j];
+        __syncthreads();
+        s[ty][tx] = x;
+        __syncthreads();
+        if (ty == 0 && j < cols) {
+            x = 0.f;
+            for (int k = 0; k < 16; ++k) x += s[k][tx];
+            out[j] = x;
+        }
+    }
+}
+
+template <class T>
+static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const zkdl_mat* h, const zkdl_mat* dt, const zkdl_mat* dx, float* dweight) {
+    const uint32_t n = a.cols;
+    const bool wave = n <= 1024, regs = n <= 16384;
+    uint64_t blocks = l8_ceil(a.rows, wave ? 4 : 1);
+    if (blocks > 1024) blocks = 1024;
+    const uint64_t col_rows = a.rows < 64 ? a.rows : 64;
+    if (dweight) {
+        a.part = (float*)zk_alloc(ctx, (regs ? blocks : col_rows) * n * 4);
+        if (!a.part) return ZKDL_ENOMEM;
+    }
+    const L8Mat<const T> mdy = l8_mat<const T>(dy), mh = l8_mat<const T>(h), mdt = l8_mat<const T>(dt);
+    const L8Mat<T> mdx = l8_mat<T>(dx);
+#define L8_BACK(G, ITEMS) hipLaunchKernelGGL((k_l8_norm_back<T, G, ITEMS>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx)
+    if (n <= 512) L8_BACK(64, 1);
+    else if (n <= 1024) L8_BACK(64, 2);
+    else if (n <= 2048) L8_BACK(256, 1);
+    else if (n <= 4096) L8_BACK(256, 2);
+    else if (n <= 8192) L8_BACK(256, 4);
+    else if (n <= 16384) L8_BACK(256, 8);
+    else {
+        hipLaunchKernelGGL((k_l8_norm_back_long<T>), dim3(l8_grid(a.rows)), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx);
+        if (dweight) hipLaunchKernelGGL((k_l8_dweight_long<T>), dim3((unsigned)l8_ceil(n, 2048), (unsigned)col_rows), dim3(256), 0, ctx->stream, a, mdy, mh);
+    }
+#undef L8_BACK
+    if (dweight)
+        hipLaunchKernelGGL(k_l8_sum_shares, dim3(l8_grid(l8_ceil(n, 64))), dim3(1024), 0, ctx->stream, a.part, (uint32_t)(regs ? blocks : col_rows), n, dweight);
+    zk_free(ctx, a.part);
+    return ZKDL_OK;
+}
+
+extern "C" int zkdl_rmsnorm_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* h, const void* weight, int weight_dtype,
+                                        const float* rstd, const zkdl_mat* dtotal, const zkdl_mat* dx, float* dweight) try {
+    if (!ctx || !l8_mat_ok(dy, false) || !l8_mat_ok(h, false) || !l8_mat_ok(dx, true) || !l8_is_float(dy->dtype) || h->dtype != dy->dtype ||
+        dx->dtype != dy->dtype || !l8_same_shape(dy, h) || !l8_same_shape(dy, dx) || dy->stack != 1)
+        return ZKDL_EINVAL;
+    if (dtotal && (!l8_mat_ok(dtotal, false) || dtotal->dtype != dy->dtype || !l8_same_shape(dy, dtotal))) return ZKDL_EINVAL;
+    if ((weight_dtype != ZKDL_F32 && weight_dtype != dy->dtype) || dy->cols == 0 || !weight) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    if (dy->rows == 0) {
+        if (dweight) hipLaunchKernelGGL(k_l8_zero, dim3(l8_grid(l8_ceil(dy->cols, 256))), dim3(256), 0, ctx->stream, dweight, dy->cols);
+        ZK_HIP(ctx, hipGetLastError());
+        return ZKDL_OK;
+    }
+    if (!rstd) return ZKDL_EINVAL;
+    L8BackArgs a = {dy->rows, (uint32_t)dy->cols, weight, weight_dtype == ZKDL_F32, rstd, nullptr};
+    int rc;
+    if (dy->dtype == ZKDL_F32) rc = l8_norm_back<float>(ctx, a, dy, h, dtotal, dx, dweight);
+    else if (dy->dtype == ZKDL_F16) rc = l8_norm_back<__half>(ctx, a, dy, h, dtotal, dx, dweight);
+    else rc = l8_norm_back<bf16_t>(ctx, a, dy, h, dtotal, dx, dweight);
+    if (rc != ZKDL_OK) return rc;
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}

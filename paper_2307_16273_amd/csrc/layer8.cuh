@@ -1,0 +1,162 @@
+// What the kernels of the 8-bit layers (k_layer8.hip, k_matmul8.hip) share: matrices as kernels see them, items of the three
+// floating types, reductions over a wave.
+#pragma once
+#include <hip/hip_fp16.h>
+
+#include "zkdl_internal.h"
+
+enum L8Type { L8_F32 = 0, L8_F16 = 1, L8_BF16 = 2 };
+struct bf16_t {
+    uint16_t v;
+};
+
+// A stack of matrices: item (s, i, j) at p + s * ss + i * rs + j.
+template <class T>
+struct L8Mat {
+    T* p;
+    uint64_t rs, ss;
+};
+template <class T>
+static inline L8Mat<T> l8_mat(const zkdl_mat* m) {
+    L8Mat<T> r = {nullptr, 0, 0};
+    if (m) {
+        r.p = (T*)m->data;
+        r.rs = m->row_stride;
+        r.ss = m->stack_stride;
+    }
+    return r;
+}
+
+static __device__ __forceinline__ float l8_f32(float x) { return x; }
+static __device__ __forceinline__ float l8_f32(__half x) { return __half2float(x); }
+static __device__ __forceinline__ float l8_f32(bf16_t x) { return __uint_as_float((uint32_t)x.v << 16); }
+// One rounding, to nearest even, where a result leaves for memory.
+static __device__ __forceinline__ void l8_put(float x, float& o) { o = x; }
+static __device__ __forceinline__ void l8_put(float x, __half& o) {
+    asm("" : "+v"(x));      // a 32-bit value of its own: a product in front would be rounded once, to 16 bits, otherwise
+    o = __float2half(x);
+}
+static __device__ __forceinline__ void l8_put(float x, bf16_t& o) {
+    const uint32_t u = __float_as_uint(x);
+    o.v = (uint16_t)((u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+// Eight adjacent items, at any address: the memory system takes 16 bytes at once also where they are not aligned.
+template <class T>
+struct __attribute__((packed, aligned(1))) L8Vec {
+    T v[8];
+};
+// f[0..8) = p[0..n), zeros behind
+template <class T>
+static __device__ __forceinline__ void l8_load(const T* p, int n, float (&f)[8]) {
+    if (n >= 8) {
+        const L8Vec<T> x = *(const L8Vec<T>*)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = l8_f32(x.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? l8_f32(p[i]) : 0.f;
+    }
+}
+template <class T>
+static __device__ __forceinline__ void l8_store(T* p, int n, const float (&f)[8]) {
+    L8Vec<T> x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        T o;
+        l8_put(f[i], o);
+        x.v[i] = o;
+    }
+    if (n >= 8) {
+        *(L8Vec<T>*)p = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = x.v[i];
+    }
+}
+struct __attribute__((packed, aligned(1))) L8Bytes {
+    uint32_t lo, hi;
+};
+static __device__ __forceinline__ void l8_store_q(int8_t* p, int n, const int (&q)[8]) {
+    L8Bytes w;
+    w.lo = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24;
+    w.hi = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24;
+    if (n >= 8) {
+        *(L8Bytes*)p = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (int8_t)q[i];
+    }
+}
+
+// |x| as a number whose order as an integer is that of the magnitudes, infinity above all finite ones and NaN above that.
+static __device__ __forceinline__ uint32_t l8_mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+constexpr uint32_t L8_INF = 0x7f800000u;
+
+// How the values of a row (column) whose largest magnitude is `top` become 8-bit integers.
+struct L8Quant {
+    float pre, inv;     // q = rint((v * pre) * inv)
+    bool finite;
+};
+static __device__ __forceinline__ L8Quant l8_quant(uint32_t top) {
+    L8Quant r;
+    r.finite = top < L8_INF;
+    const float a = __uint_as_float(top);
+    // 127 / a overflows for the smallest a; times 2^100 both stay normal, exactly
+    r.pre = a < 0x1p-100f ? 0x1p100f : 1.f;
+    r.inv = top == 0 || !r.finite ? 0.f : 127.f / (a * r.pre);
+    return r;
+}
+static __device__ __forceinline__ int l8_round(float v, const L8Quant& c) {
+    return c.finite ? (int)rintf(v * c.pre * c.inv) : 0;
+}
+
+static __device__ __forceinline__ float l8_wave_sum(float x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+static __device__ __forceinline__ uint32_t l8_wave_max(uint32_t x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d, 64));
+    return x;
+}
+
+// ---- host side -------------------------------------------------------------------
+// The context's device is the current one while this lives: its stream may be the device's default one.
+struct L8Device {
+    int before = -1;
+    hipError_t err;
+    explicit L8Device(const zkdl_ctx* ctx) {
+        int now = -1;
+        err = hipGetDevice(&now);
+        if (err == hipSuccess && now != ctx->device) {
+            err = hipSetDevice(ctx->device);
+            if (err == hipSuccess) before = now;
+        }
+    }
+    ~L8Device() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+static inline bool l8_is_float(int dtype) { return dtype == ZKDL_F32 || dtype == ZKDL_F16 || dtype == ZKDL_BF16; }
+// A matrix that a kernel can address; an output's items are all different ones.
+static inline bool l8_mat_ok(const zkdl_mat* m, bool output) {
+    if (!m || m->reserved != 0) return false;
+    const uint64_t lim = (uint64_t)1 << 31, far = (uint64_t)1 << 40;
+    if (m->rows >= lim || m->cols >= lim || m->stack >= lim) return false;
+    if (m->rows == 0 || m->cols == 0 || m->stack == 0) return true;
+    if (!m->data || (m->rows > 1 && m->row_stride >= far) || (m->stack > 1 && m->stack_stride >= far)) return false;
+    if (!output) return true;
+    return (m->rows == 1 || m->row_stride >= m->cols) && (m->stack == 1 || m->stack_stride >= (m->rows - 1) * m->row_stride + m->cols);
+}
+static inline bool l8_same_shape(const zkdl_mat* a, const zkdl_mat* b) {
+    return a->stack == b->stack && a->rows == b->rows && a->cols == b->cols;
+}
+static inline uint64_t l8_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// ---- k_layer8.hip ------------------------------------------------------------------
+// zkdl_quantize_i8 behind its checks, on matrices with entries
+int zk_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values);

@@ -1,0 +1,543 @@
+"""The 8-bit layer operators against their definitions in 64 bits.
+
+u = 2^-24 is the unit roundoff of 32-bit floats; a sum of t terms one after the other and a tree of 12 levels over them has a
+relative error of at most (t + 12) u on the sum of the magnitudes, t being the terms that one thread adds."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def normal(g, shape, dtype=torch.float32, scale=1.0):
+    return (torch.randn(shape, generator=g) * scale).to(dtype)
+
+
+def codes(g, shape):
+    q = torch.randint(-128, 128, shape, generator=g, dtype=torch.int32)
+    return q.to(torch.int8)
+
+
+def unaligned(t, pad_cols=5, offset=3):
+    """The same matrix (or stack) on the GPU in a larger buffer: odd row stride, odd address."""
+    shape = list(t.shape)
+    wide = shape[:-1] + [shape[-1] + pad_cols]
+    n = int(np.prod(wide))
+    buf = torch.empty(n + offset + 16, dtype=t.dtype, device="cuda")
+    v = buf[offset:offset + n].view(wide)[..., :shape[-1]]
+    v.copy_(t)
+    return v
+
+
+def threads_terms(cols):
+    """Entries of a row that one thread adds up."""
+    return max(64, 8 * -(-cols // 2048))
+
+
+def check_codes(v, axis, q, scale, what):
+    """q and scale against v (64 bits): a rounding in 32 bits may move 127 v / max by three roundings."""
+    v = v.double()
+    top = v.abs().amax(axis, keepdim=True) if v.shape[axis] else torch.zeros_like(v.sum(axis, keepdim=True))
+    assert torch.all((scale.double() - top.squeeze(axis) / 127).abs() <= 3 * U * top.squeeze(axis) / 127 + 2.0 ** -149), what
+    ideal = torch.where(top > 0, v * 127 / torch.where(top > 0, top, torch.ones_like(top)), torch.zeros_like(v))
+    q = q.double()
+    assert torch.all((q - ideal).abs() <= 0.5 + 127 * 4 * U), what
+    assert torch.all(q.abs() <= 127), what
+
+
+QUANT_SHAPES = [(1, 1), (1, 7), (3, 512), (5, 513), (2, 1025), (70, 64), (4, 2049), (33, 4100), (130, 66), (2, 8200),
+                (1, 16400), (257, 1000), (2, 3, 65), (3, 70, 129)]
+
+
+@pytest.mark.parametrize("shape", QUANT_SHAPES, ids=str)
+@pytest.mark.parametrize("axis", [-1, -2])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_quantize(lib, ctx, shape, axis, dtype):
+    g = gen(len(shape) * 1000 + shape[-1])
+    x = normal(g, shape, TYPES[dtype], 3.0)
+    if shape[-2] > 2:
+        x[..., 1, :] = 0                       # an empty row
+    if shape[-1] > 4:
+        x[..., 2] = 0                          # an empty column
+    mult = torch.rand(shape[:-2] + (shape[axis],), generator=g) + 0.1 if shape[-1] % 2 else None
+    wide = mult.unsqueeze(-2 if axis == -1 else -1) if mult is not None else None
+    v = x.float() * wide if mult is not None else x.float()      # the operator's v: one rounding, the values' own
+    for where in (lambda t: t.cuda(), unaligned):
+        got = lib.quantize_i8(ctx, where(x), axis=axis, mult=mult.cuda() if mult is not None else None, values=True)
+        q, scale = got["q"].cpu(), got["scale"].cpu()
+        check_codes(v, axis, q, scale, (shape, axis, dtype))
+        back = (q.float() * scale.unsqueeze(axis)).to(TYPES[dtype])
+        assert torch.equal(got["values"].cpu(), back)
+
+
+def test_quantize_range_of_the_inputs(lib, ctx):
+    """Magnitudes from the smallest to the largest of the type, infinities and NaN: a row of its own each."""
+    rows = [[2.0 ** -149, 0, -2.0 ** -149, 2.0 ** -149], [2.0 ** -149 * 127, 2.0 ** -149, 0, -2.0 ** -148],
+            [2.0 ** -101, 2.0 ** -108, -2.0 ** -102, 0], [2.0 ** -126, 2.0 ** -100, 2.0 ** -99, 1e-30],
+            [3.4e38, -3.4e38, 1e30, 1.7e38], [0.0, -0.0, 0.0, 0.0],
+            [1.0, float("inf"), 2.0, 3.0], [1.0, 2.0, float("nan"), 3.0], [float("-inf"), float("nan"), 0.0, 1.0]]
+    x = torch.tensor(rows, dtype=torch.float32)
+    for axis, t in ((-1, x), (-2, x.t().contiguous())):
+        got = lib.quantize_i8(ctx, t.cuda(), axis=axis, values=True)
+        q, scale = got["q"].cpu(), got["scale"].cpu()
+        q = q if axis == -1 else q.t()
+        check_codes(x[:6], -1, q[:6], scale[:6], axis)
+        assert torch.all(torch.isnan(scale[6:])) and torch.all(q[6:] == 0)
+        assert torch.all(torch.isnan(got["values"].cpu()[6:] if axis == -1 else got["values"].cpu()[:, 6:]))
+    # a product with the multiplier that overflows counts as the infinity it is
+    got = lib.quantize_i8(ctx, torch.tensor([[1e30, 1.0]], device="cuda"), mult=torch.tensor([1e30, 1.0], device="cuda"))
+    assert torch.isnan(got["scale"]).all() and (got["q"] == 0).all()
+
+
+def test_quantize_ties_go_to_even(lib, ctx):
+    """With a maximum of 127 the quotients are the inputs themselves."""
+    x = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, 126.5, -125.5, 3.49999, 3.50001]])
+    want = torch.tensor([[127, 0, 2, 2, 0, -2, 126, -126, 3, 4]], dtype=torch.int8)
+    assert torch.equal(lib.quantize_i8(ctx, x.cuda())["q"].cpu(), want)
+    assert torch.equal(lib.quantize_i8(ctx, x.t().contiguous().cuda(), axis=-2)["q"].cpu(), want.t())
+
+
+NORM_SHAPES = [(1, 1), (1, 4096), (3, 17), (7, 512), (6, 700), (5, 1001), (130, 1024), (3, 2048), (2, 4095), (9, 5000),
+               (2, 9000), (2, 16384), (3, 20001)]
+
+
+@pytest.mark.parametrize("shape", NORM_SHAPES, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("residual", [False, True])
+def test_rmsnorm(lib, ctx, shape, dtype, residual):
+    t = TYPES[dtype]
+    g = gen(shape[1] + residual)
+    x, r = normal(g, shape, t, 2.0), normal(g, shape, t)
+    w32 = 1 + 0.3 * torch.randn(shape[1], generator=g)
+    if shape[0] > 2:
+        x[1] = 0
+        r[1] = 0
+    eps = 1e-5
+    for where, w in ((lambda a: a.cuda(), w32.to(t)), (unaligned, w32)):
+        got = lib.rmsnorm_i8(ctx, where(x), w.cuda(), residual=where(r) if residual else None, eps=eps, values=True)
+        h = x.float() + r.float() if residual else x.float()
+        hd = h.double()
+        rstd = (hd.square().mean(1) + eps) ** -0.5
+        sum_err = (threads_terms(shape[1]) + 16) * U
+        assert torch.all((got["rstd"].cpu().double() - rstd).abs() <= (sum_err / 2 + 4 * U) * rstd)
+        # scale and codes: v = h w is rounded once, and rstd is the row's factor
+        v = h * w.float()
+        top = v.double().abs().amax(1)
+        assert torch.all((got["scale"].cpu().double() - top * rstd / 127).abs() <= (sum_err + 8 * U) * top * rstd / 127)
+        q = got["q"].cpu()
+        check_codes(v, 1, q, top.float() / 127, (shape, dtype))
+        y = hd * rstd[:, None] * w.double()
+        assert torch.all((q.double() * got["scale"].cpu().double()[:, None] - y).abs()
+                         <= (0.5 + 127 * (sum_err + 10 * U)) * (top * rstd / 127)[:, None])
+        assert torch.equal(got["values"].cpu(), (q.float() * got["scale"].cpu()[:, None]).to(t))
+        if residual:
+            assert torch.equal(got["total"].cpu(), h.to(t))
+        else:
+            assert got["total"] is None
+
+
+def test_rmsnorm_range_of_the_inputs(lib, ctx):
+    """Squares that leave the range of 32 bits, rows of zeros, infinities and NaN."""
+    n = 300
+    g = gen(3)
+    x = normal(g, (6, n))
+    x[0] *= 1e25
+    x[1] *= 1e-30
+    x[2] = 0
+    x[3] *= 3e37
+    x[4, 7] = float("inf")
+    x[5, 299] = float("nan")
+    w = torch.ones(n)
+    got = lib.rmsnorm_i8(ctx, x.cuda(), w.cuda(), eps=1e-6)
+    xd = x.double()[:4]
+    rstd = (xd.square().mean(1) + 1e-6) ** -0.5
+    sum_err = (64 + 20) * U
+    assert torch.all((got["rstd"][:4].cpu().double() - rstd).abs() <= sum_err * rstd + 2.0 ** -149)
+    top = xd.abs().amax(1)
+    assert torch.all((got["scale"][:4].cpu().double() - top * rstd / 127).abs() <= sum_err * top * rstd / 127 + 2.0 ** -149 * top)
+    check_codes(x[:4], 1, got["q"][:4].cpu(), (top / 127).float(), "range")
+    assert torch.all(torch.isnan(got["scale"][4:])) and torch.all(got["q"][4:] == 0)
+
+
+def norm64(x, w, eps):
+    return x * w / torch.sqrt(x.square().mean(-1, keepdim=True) + eps)
+
+
+@pytest.mark.parametrize("shape", NORM_SHAPES + [(1500, 130), (2100, 2100)], ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rmsnorm_backward(lib, ctx, shape, dtype):
+    t, eps = TYPES[dtype], 1e-5
+    g = gen(shape[0] + 7 * shape[1])
+    h, dy, dt = normal(g, shape, t, 2.0), normal(g, shape, t, 0.1), normal(g, shape, t, 0.1)
+    w = (1 + 0.3 * torch.randn(shape[1], generator=g)).to(t)
+    if shape[0] > 2:
+        h[1] = 0
+        dy[2] = 0
+    rstd = ((h.double().square().mean(1) + eps) ** -0.5).float()
+    for where, extra in ((lambda a: a.cuda(), dt), (unaligned, None)):
+        got = lib.rmsnorm_i8_backward(ctx, where(dy), where(h), w.cuda(), rstd.cuda(), where(extra) if extra is not None else None)
+        r = rstd.double()[:, None]
+        n, gw = h.double() * r, dy.double() * w.double()
+        dot = (gw * n).mean(1, keepdim=True)
+        dx = r * (gw - n * dot)
+        err = r * (4 * U * gw.abs() + n.abs() * ((threads_terms(shape[1]) + 20) * U * (gw * n).abs().mean(1, keepdim=True) + 4 * U * dot.abs()))
+        if extra is not None:
+            dx = dx + extra.double()
+            err = err + U * (dx.abs() + err)
+        err = err + HALF_ULP[t] * (dx.abs() + err) + TINY[t]
+        assert torch.all((got["dx"].cpu().double() - dx).abs() <= err)
+        dwe = (shape[0] + 20) * U * (dy.double() * n).abs().sum(0)
+        assert torch.all((got["dweight"].cpu().double() - (dy.double() * n).sum(0)).abs() <= dwe + 2.0 ** -149)
+
+
+def test_rmsnorm_backward_is_the_slope_of_the_norm(lib, ctx):
+    """Central differences of the norm in 64 bits: step d leaves an error of the order d^2, 1e-8 here, next to 32-bit results."""
+    g = gen(11)
+    m, n, eps, d = 4, 37, 1e-4, 1e-4
+    x, w, dy = torch.randn((m, n), generator=g).double(), (1 + 0.2 * torch.randn(n, generator=g)).double(), torch.randn((m, n), generator=g).double()
+    x, w, dy = (v.float().double() for v in (x, w, dy))
+    rstd = (x.square().mean(1) + eps) ** -0.5
+    got = lib.rmsnorm_i8_backward(ctx, dy.float().cuda(), x.float().cuda(), w.float().cuda(), rstd.float().cuda())
+    slope = torch.empty_like(x)
+    for j in range(n):
+        e = torch.zeros(n, dtype=torch.float64)
+        e[j] = d
+        slope[:, j] = ((norm64(x + e, w, eps) - norm64(x - e, w, eps)) * dy).sum(1) / (2 * d)
+    assert torch.allclose(got["dx"].cpu().double(), slope, rtol=0, atol=1e-5)
+    dw = torch.stack([((norm64(x, w + d * torch.eye(n)[j].double(), eps) - norm64(x, w - d * torch.eye(n)[j].double(), eps)) * dy).sum() / (2 * d)
+                      for j in range(n)])
+    assert torch.allclose(got["dweight"].cpu().double(), dw, rtol=0, atol=1e-5)
+
+
+def product64(a, b):
+    """Exact: products below 2^14 and fewer than 2^17 of them, in 64-bit floats."""
+    return a.double() @ b.double()
+
+
+# M, K, N: single tokens, edges of tiles of 16, 64, 128 and 256, primes, long and short sums
+MM_SHAPES = [(1, 1, 1), (1, 64, 16), (1, 4096, 257), (1, 1000, 130), (2, 17, 33), (3, 129, 64), (5, 4096, 512), (16, 256, 256), (15, 130, 1),
+             (17, 63, 65), (31, 640, 48), (33, 1024, 1000), (64, 64, 64), (65, 127, 129), (64, 1024, 1024), (100, 2048, 96), (127, 512, 255),
+             (128, 128, 128), (129, 1040, 272), (200, 96, 640), (255, 385, 257), (256, 256, 256), (257, 272, 1040), (300, 16, 700),
+             (512, 2048, 512), (777, 1008, 1024), (1024, 5, 1024), (1000, 1001, 999), (1, 16, 5000), (40, 8208, 80), (2049, 144, 520)]
+
+
+def stored(t, turned):
+    return t.mT.contiguous() if turned else t
+
+
+@pytest.mark.parametrize("ta,tb", [(False, False), (False, True), (True, False), (True, True)], ids=["nn", "nt", "tn", "tt"])
+@pytest.mark.parametrize("shape", MM_SHAPES, ids=str)
+def test_matmul(lib, ctx, shape, ta, tb):
+    m, k, n = shape
+    g = gen(m * 31 + k * 7 + n)
+    a, b = codes(g, (m, k)), codes(g, (k, n))
+    want = product64(a, b)
+    sa, sb = torch.rand(m, generator=g) + 0.5, (torch.rand(n, generator=g) + 0.5) / 128
+    sa[m // 2] = 0
+    scaled = want * sa.double()[:, None] * sb.double()[None, :]
+    for where in (lambda t: t.cuda(), unaligned):
+        pa, pb = where(stored(a, ta)), where(stored(b, tb))
+        got = lib.matmul_i8(ctx, pa, pb, trans_a=ta, trans_b=tb)
+        assert got.dtype == torch.int32 and torch.equal(got.cpu().double(), want)
+        dtype = [torch.float32, torch.bfloat16, torch.float16][(m + n) % 3]
+        got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=dtype).cpu().double()
+        tol = 3.1 * U * scaled.abs() + HALF_ULP[dtype] * 1.001 * scaled.abs() + TINY[dtype]
+        over = scaled.abs() > (65504 if dtype == torch.float16 else 3e38)
+        assert torch.all(((got - scaled).abs() <= tol) | over)
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 256, 64), (8, 64, 256, 128), (5, 33, 100, 70), (2, 130, 1024, 384), (300, 4, 8, 4), (3, 0, 8, 4)], ids=str)
+@pytest.mark.parametrize("ta,tb", [(False, False), (False, True), (True, False)])
+def test_matmul_stacks(lib, ctx, shape, ta, tb):
+    s, m, k, n = shape
+    g = gen(s + m + k + n)
+    a, b = codes(g, (s, m, k)), codes(g, (s, k, n))
+    sa, sb = torch.rand((s, m), generator=g), torch.rand((s, n), generator=g)
+    want = product64(a, b)
+    for where in (lambda t: t.cuda(), unaligned):
+        pa, pb = where(stored(a, ta)), where(stored(b, tb))
+        assert torch.equal(lib.matmul_i8(ctx, pa, pb, trans_a=ta, trans_b=tb).cpu().double(), want)
+        got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=torch.float32).cpu().double()
+        scaled = want * sa.double()[..., :, None] * sb.double()[..., None, :]
+        assert torch.all((got - scaled).abs() <= 4 * U * scaled.abs())
+
+
+def test_matmul_views(lib, ctx):
+    """Transposed views, one weight matrix repeated over the stack, rows taken in steps, a scale left out."""
+    g = gen(5)
+    a, b = codes(g, (4, 96, 160)), codes(g, (160, 80))
+    one = b.cuda().expand(4, 160, 80)
+    assert torch.equal(lib.matmul_i8(ctx, a.cuda(), one).cpu().double(), product64(a, b))
+    assert torch.equal(lib.matmul_i8(ctx, a.cuda()[0], stored(b, True).cuda().t()).cpu().double(), product64(a[0], b))
+    assert torch.equal(lib.matmul_i8(ctx, a.cuda()[0].t(), b.cuda(), trans_a=True).cpu().double(), product64(a[0], b))
+    assert torch.equal(lib.matmul_i8(ctx, a.cuda()[0, ::3], b.cuda()).cpu().double(), product64(a[0, ::3], b))
+    row = a[0, :1].cuda().expand(96, 160)
+    assert torch.equal(lib.matmul_i8(ctx, row, b.cuda()).cpu().double(), product64(a[0, :1].expand(96, 160), b))
+    sb = torch.rand(80, generator=g)
+    got = lib.matmul_i8(ctx, a.cuda()[0], b.cuda(), None, sb.cuda(), dtype=torch.float32).cpu().double()
+    want = product64(a[0], b) * sb.double()
+    assert torch.all((got - want).abs() <= 3 * U * want.abs())
+
+
+def test_matmul_extremes(lib, ctx):
+    """The largest sums that 32 bits hold, the empty sum, empty sides, scales that are no numbers."""
+    k = 2 ** 17 - 1
+    a, b = torch.full((2, k), -128, dtype=torch.int8, device="cuda"), torch.full((k, 3), -128, dtype=torch.int8, device="cuda")
+    assert torch.all(lib.matmul_i8(ctx, a, b) == k * 2 ** 14)
+    b.fill_(127)
+    assert torch.all(lib.matmul_i8(ctx, a, b.t().contiguous(), trans_b=True) == -128 * 127 * k)
+    none = lib.matmul_i8(ctx, a[:, :0], b[:0])
+    assert none.shape == (2, 3) and torch.all(none == 0)
+    assert lib.matmul_i8(ctx, a[:0], b).shape == (0, 3) and lib.matmul_i8(ctx, a, b[:, :0]).shape == (2, 0)
+    sa = torch.tensor([float("nan"), 1.0], device="cuda")
+    got = lib.matmul_i8(ctx, a[:, :64], b[:64], sa, torch.ones(3, device="cuda"), dtype=torch.bfloat16)
+    assert torch.all(torch.isnan(got[0])) and torch.all(torch.isfinite(got[1]))
+
+
+def test_offsets_beyond_32_bits(lib, ctx):
+    """Rows and matrices further apart than 2^31 items."""
+    far = 2 ** 31 + 48
+    buf = torch.empty(2 * far + 4096, dtype=torch.int8, device="cuda")
+    a = buf.as_strided((3, 160), (far, 1))
+    g = gen(9)
+    ca, cb = codes(g, (3, 160)), codes(g, (160, 64))
+    a.copy_(ca)
+    assert torch.equal(lib.matmul_i8(ctx, a, cb.cuda()).cpu().double(), product64(ca, cb))
+    assert torch.equal(lib.matmul_i8(ctx, a, ca.cuda(), trans_a=True).cpu().double(), product64(ca.t(), ca))
+    st = buf.as_strided((2, 16, 160), (far, 160, 1))
+    cs = codes(g, (2, 16, 160))
+    st.copy_(cs)
+    assert torch.equal(lib.matmul_i8(ctx, st, cs.cuda(), trans_b=True).cpu().double(), product64(cs, cs.mT))
+    x = buf.view(torch.bfloat16).as_strided((3, 100), (far // 2, 1))
+    cx = normal(g, (3, 100), torch.bfloat16)
+    x.copy_(cx)
+    got = lib.rmsnorm_i8(ctx, x, torch.ones(100, device="cuda"))
+    assert torch.equal(got["q"].cpu(), lib.rmsnorm_i8(ctx, cx.cuda(), torch.ones(100, device="cuda"))["q"].cpu())
+
+
+BACK_SHAPES = [(1, 64, 32), (16, 256, 256), (33, 100, 70), (64, 1024, 128), (130, 257, 515), (4, 16, 1)]
+
+
+def codes32(v, axis):
+    """The operator's quantisation in its own 32-bit steps."""
+    top = v.abs().amax(axis, keepdim=True)
+    inv = torch.where(top > 0, torch.full_like(top, 127.0) / top, torch.zeros_like(top))
+    return torch.round(v * inv), top.double() / 127
+
+
+@pytest.mark.parametrize("shape", BACK_SHAPES, ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_matmul_backward(lib, ctx, shape, trans_w, dtype):
+    m, k, n = shape
+    t = TYPES[dtype]
+    g = gen(m + k + n)
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1
+    dy = normal(g, (m, n), t, 0.1)
+    if m > 3:
+        dy[2] = 0
+    got = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w)
+    q, tq = codes32(dy.float() * sw, 1)
+    p, u = codes32(dy.float() * sa[:, None], 0)
+    da, dw = product64(q, w.t()) * tq, product64(a.t(), p) * u
+    if trans_w:
+        dw = dw.t()
+    assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs() + 1.001 * HALF_ULP[t] * da.abs() + TINY[t])
+    assert torch.all((got["dw"].cpu().double() - dw).abs() <= 6 * U * dw.abs())
+    # against the gradients of (a sa)(w sw) themselves: a rounding of the gradient is off by half a step at most
+    fa, fw = a.double() * sa.double()[:, None], w.double() * sw.double()
+    da64, dw64 = dy.double() @ fw.t(), fa.t() @ dy.double()
+    assert torch.all((got["da"].cpu().double() - da64).abs() <= 0.501 * tq * w.double().abs().sum(1) + 2 * HALF_ULP[t] * da64.abs() + TINY[t])
+    off = 0.501 * u * a.double().abs().sum(0)[:, None]
+    gw = got["dw"].cpu().double()
+    assert torch.all(((gw.t() if trans_w else gw) - dw64).abs() <= off + 8 * U * dw64.abs())
+    # either gradient alone
+    one = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w, need_da=False)
+    assert one["da"] is None and torch.equal(one["dw"], got["dw"])
+    one = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w, need_dw=False)
+    assert one["dw"] is None and torch.equal(one["da"], got["da"])
+
+
+def test_matmul_backward_is_the_slope_of_the_product(lib, ctx):
+    """The product is linear in either factor, so differences of any step give its slope; the 8-bit gradient is within half a
+    step of each quantised entry."""
+    g = gen(21)
+    m, k, n = 5, 12, 9
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw, dy = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1, normal(g, (m, n))
+    got = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), w.cuda(), sw.cuda())
+
+    def loss(fa, fw):
+        return float(((fa @ fw) * dy.double()).sum())
+
+    fa, fw = a.double() * sa.double()[:, None], w.double() * sw.double()
+    tq = (dy * sw).double().abs().amax(1) / 127
+    for i in range(m):
+        for j in range(k):
+            e = torch.zeros_like(fa)
+            e[i, j] = 1
+            off = 0.501 * float(tq[i] * w.double()[j].abs().sum()) + 1e-5
+            assert abs(float(got["da"][i, j]) - (loss(fa + e, fw) - loss(fa - e, fw)) / 2) <= off
+    u = (dy * sa[:, None]).double().abs().amax(0) / 127
+    for i in range(k):
+        for j in range(n):
+            e = torch.zeros_like(fw)
+            e[i, j] = 1
+            off = 0.501 * float(u[j] * a.double()[:, i].abs().sum()) + 1e-4
+            assert abs(float(got["dw"][i, j]) - (loss(fa, fw + e) - loss(fa, fw - e)) / 2) <= off
+
+
+def test_same_results_every_time(lib, ctx):
+    g = gen(8)
+    x, w = normal(g, (515, 1000), torch.bfloat16).cuda(), torch.ones(1000, device="cuda")
+    dy = normal(g, (515, 1000), torch.bfloat16).cuda()
+    rstd = torch.rand(515, generator=g).cuda()
+    one, two = (lib.rmsnorm_i8_backward(ctx, dy, x, w, rstd) for _ in range(2))
+    assert torch.equal(one["dx"], two["dx"]) and torch.equal(one["dweight"], two["dweight"])
+    a, b = codes(g, (70, 5000)).cuda(), codes(g, (5000, 90)).cuda()
+    assert torch.equal(lib.matmul_i8(ctx, a, b), lib.matmul_i8(ctx, a, b))
+
+
+def test_on_another_stream(lib, ctx):
+    """Inputs made on the current stream just before the call, results used there just after, the context's stream being
+    another; and a context of a stream of its own."""
+    g = gen(2)
+    a0, b = codes(g, (300, 2000)).cuda(), codes(g, (2000, 256)).cuda()
+    want = product64(a0.cpu(), b.cpu())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    own = lib.Context(0, stream=side.cuda_stream)
+    for c, on in ((ctx, side), (own, torch.cuda.default_stream()), (own, side)):
+        with torch.cuda.stream(on):
+            big = torch.randn(4096, 4096, device="cuda")
+            for _ in range(3):
+                big = big @ big                     # keeps the stream busy while the host goes on
+            a = a0.clone()
+            got = lib.matmul_i8(c, a, b).clone()
+            del a
+            torch.zeros(300, 2000, dtype=torch.int8, device="cuda")
+        torch.cuda.synchronize()
+        assert torch.equal(got.cpu().double(), want)
+    own.close()
+
+
+def test_in_a_graph(lib):
+    """A norm and a layer, forward and backward, captured once and replayed on new inputs with other work in between."""
+    g = gen(4)
+    side = torch.cuda.Stream()
+    own = lib.Context(0, stream=side.cuda_stream)
+    x = normal(g, (70, 512), torch.bfloat16).cuda()
+    w = torch.ones(512, device="cuda")
+    wq = codes(g, (512, 384)).cuda()
+    sw = torch.rand(384, generator=g).cuda()
+    dy = normal(g, (70, 384), torch.bfloat16).cuda()
+
+    def layer():
+        n = lib.rmsnorm_i8(own, x, w)
+        y = lib.matmul_i8(own, n["q"], wq, n["scale"], sw, dtype=torch.float32)
+        d = lib.matmul_i8_backward(own, dy, n["q"], n["scale"], wq, sw)
+        e = lib.rmsnorm_i8_backward(own, d["da"], x, w, n["rstd"])
+        return n["scale"], y, d["dw"], e["dx"], e["dweight"]
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        layer()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = layer()
+    for k in range(4):
+        torch.cuda.synchronize()
+        x.copy_(normal(g, (70, 512), torch.bfloat16, 1.0 + k))
+        dy.copy_(normal(g, (70, 384), torch.bfloat16, 1.0 + k))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        with torch.cuda.stream(side):
+            eager = layer()
+        torch.cuda.synchronize()
+        for p, q in zip(got, eager):
+            assert torch.equal(p, q)
+    del graph
+    own.close()
+
+
+def test_refusals(lib, ctx):
+    f, i8 = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, dtype=torch.int8, device="cuda")
+    one4, one8 = torch.ones(4, device="cuda"), torch.ones(8, device="cuda")
+    with pytest.raises(ValueError):
+        lib.quantize_i8(ctx, f.cpu())
+    with pytest.raises(ValueError):
+        lib.quantize_i8(ctx, f.double())
+    with pytest.raises(ValueError):
+        lib.quantize_i8(ctx, f.t())                            # rows not adjacent
+    with pytest.raises(ValueError):
+        lib.quantize_i8(ctx, f, axis=0)
+    with pytest.raises(ValueError):
+        lib.quantize_i8(ctx, f, mult=one4)                     # as many as columns
+    with pytest.raises(lib.ZkdlError):
+        lib.quantize_i8(ctx, i8)                               # not a floating type
+    with pytest.raises(ValueError):
+        lib.rmsnorm_i8(ctx, f, one4)
+    with pytest.raises(ValueError):
+        lib.rmsnorm_i8(ctx, f, one8.half())
+    with pytest.raises(lib.ZkdlError):
+        lib.rmsnorm_i8(ctx, f, one8, residual=f.half())
+    with pytest.raises(lib.ZkdlError):
+        lib.rmsnorm_i8(ctx, f, one8, residual=f[:3])
+    for eps in (0.0, -1.0, float("nan"), float("inf"), 1e-42):
+        with pytest.raises(lib.ZkdlError):
+            lib.rmsnorm_i8(ctx, f, one8, eps=eps)
+    with pytest.raises(lib.ZkdlError):
+        lib.rmsnorm_i8(ctx, f[:, :0], one8[:0])
+    with pytest.raises(lib.ZkdlError):
+        lib.rmsnorm_i8_backward(ctx, f, f.half(), one8, one4)
+    with pytest.raises(ValueError):
+        lib.rmsnorm_i8_backward(ctx, f, f, one8, one8)
+    with pytest.raises(lib.ZkdlError):
+        lib.matmul_i8(ctx, i8, i8)                             # 8 and 4
+    with pytest.raises(lib.ZkdlError):
+        lib.matmul_i8(ctx, f, f, trans_b=True)
+    with pytest.raises(lib.ZkdlError):
+        lib.matmul_i8(ctx, i8, i8, one4, one4, trans_b=True, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        lib.matmul_i8(ctx, i8, i8, one8, one4, trans_b=True)
+    with pytest.raises(ValueError):
+        lib.matmul_i8(ctx, i8[:, ::2], i8[:, ::2], trans_b=True)
+    with pytest.raises(ValueError):
+        lib.matmul_i8(ctx, i8, i8[None], trans_b=True)
+    long = torch.zeros(1, 2 ** 17, dtype=torch.int8, device="cuda")
+    with pytest.raises(lib.ZkdlError):
+        lib.matmul_i8(ctx, long, long, trans_b=True)
+    with pytest.raises(ValueError):
+        lib.matmul_i8_backward(ctx, f, i8, None, i8, one8)
+    with pytest.raises(lib.ZkdlError):
+        lib.matmul_i8_backward(ctx, torch.zeros(4, 9, device="cuda"), i8, one4, i8, torch.ones(9, device="cuda"))
+    # and after all that the context serves the next call
+    assert torch.equal(lib.matmul_i8(ctx, i8, i8, trans_b=True), torch.zeros(4, 4, dtype=torch.int32, device="cuda"))
+
+
+def test_empty_matrices(lib, ctx):
+    f = torch.zeros(4, 8, device="cuda")
+    one8 = torch.ones(8, device="cuda")
+    assert torch.equal(lib.quantize_i8(ctx, f[:, :0])["scale"], torch.zeros(4, device="cuda"))
+    assert torch.equal(lib.quantize_i8(ctx, f[:0], axis=-2)["scale"], torch.zeros(8, device="cuda"))
+    assert lib.quantize_i8(ctx, f[:0])["q"].shape == (0, 8)
+    assert lib.rmsnorm_i8(ctx, f[:0], one8)["q"].shape == (0, 8)
+    got = lib.rmsnorm_i8_backward(ctx, f[:0], f[:0], one8, one8[:0])
+    assert got["dx"].shape == (0, 8) and torch.equal(got["dweight"], torch.zeros(8, device="cuda"))
+    i8 = torch.zeros(0, 8, dtype=torch.int8, device="cuda")
+    w = torch.ones(8, 5, dtype=torch.int8, device="cuda")
+    got = lib.matmul_i8_backward(ctx, torch.zeros(0, 5, device="cuda"), i8, one8[:0], w, one8[:5])
+    assert got["da"].shape == (0, 8) and torch.equal(got["dw"], torch.zeros(8, 5, device="cuda"))
