@@ -16,30 +16,69 @@ struct M8Args {
     void* out;
     uint64_t o_rs, o_ss;               // items
     int o_type;                        // zkdl_dtype
+    int o_vec;                         // four adjacent items may be stored at once
     const float *sa, *sb;
     uint32_t M, N, K;
 };
 
-// the block's tile: matrix, first row, first column
+// The block's tile: matrix, first row, first column.  Blocks go round the eight dies; each die takes a run of tiles that lie together,
+// eight rows of tiles at a time, so that its L2 serves a tile's neighbours.
 static __device__ __forceinline__ void m8_tile(const M8Args& p, uint32_t bm, uint32_t bn, uint64_t& s, uint32_t& m0, uint32_t& n0) {
-    const uint32_t gm = (p.M + bm - 1) / bm, gn = (p.N + bn - 1) / bn, t = blockIdx.x % (gm * gn);
-    s = blockIdx.x / (gm * gn);
-    m0 = t / gn * bm;
-    n0 = t % gn * bn;
+    const uint32_t gm = (p.M + bm - 1) / bm, gn = (p.N + bn - 1) / bn, run = gridDim.x / 8;
+    uint32_t id = blockIdx.x;
+    if (id < run * 8) id = id % 8 * run + id / 8;
+    s = id / (gm * gn);
+    id %= gm * gn;
+    const uint32_t first = id / (8 * gn) * 8, rows = min(gm - first, 8u), at = id - first * gn;
+    m0 = (first + at % rows) * bm;
+    n0 = at / rows * bn;
 }
 
-static __device__ __forceinline__ void m8_store(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, int acc) {
+// Four adjacent columns of a row: (acc sa) sb, each product rounded to 32 bits, and once more to out's type.
+static __device__ __forceinline__ void m8_store4(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, const v4i& acc, float sa, const float (&sb)[4]) {
+    if (i >= p.M || j >= p.N) return;
     const uint64_t at = s * p.o_ss + i * p.o_rs + j;
+    const int n = (int)min(p.N - j, 4u);
     if (p.o_type == ZKDL_I32) {
-        ((int*)p.out)[at] = acc;
+        int* o = (int*)p.out + at;
+        if (n == 4 && p.o_vec) {
+            *(v4i*)o = acc;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < n) o[e] = acc[e];
+        }
         return;
     }
-    float f = (float)acc;
-    if (p.sa) f *= p.sa[s * p.M + i];
-    if (p.sb) f *= p.sb[s * p.N + j];
-    if (p.o_type == ZKDL_F32) l8_put(f, ((float*)p.out)[at]);
-    else if (p.o_type == ZKDL_F16) l8_put(f, ((__half*)p.out)[at]);
-    else l8_put(f, ((bf16_t*)p.out)[at]);
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = (float)acc[e] * sa * sb[e];
+    auto put = [&](auto t) {
+        using T = decltype(t);
+        struct alignas(4 * sizeof(T)) Four {
+            T v[4];
+        } x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l8_put(f[e], x.v[e]);
+        T* o = (T*)p.out + at;
+        if (n == 4 && p.o_vec) {
+            *(Four*)o = x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < n) o[e] = x.v[e];
+        }
+    };
+    if (p.o_type == ZKDL_F32) put(float{});
+    else if (p.o_type == ZKDL_F16) put(__half{});
+    else put(bf16_t{});
+}
+static __device__ __forceinline__ float m8_row_scale(const M8Args& p, uint64_t s, uint32_t i) {
+    return p.sa && i < p.M ? p.sa[s * p.M + i] : 1.f;
+}
+static __device__ __forceinline__ void m8_col_scales(const M8Args& p, uint64_t s, uint32_t j, float (&f)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = p.sb && j + e < p.N ? p.sb[s * p.N + j + e] : 1.f;
 }
 
 struct __attribute__((packed, aligned(1))) M8Bytes {
@@ -106,31 +145,296 @@ __global__ __launch_bounds__(256) void k_m8_any(M8Args p) {
 #pragma unroll
             for (int y = 0; y < 2; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
     }
-    // the tile comes out turned: a lane has four adjacent columns of one row
+    // the products come out turned: a lane has four adjacent columns of one row
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int y = 0; y < 2; ++y) {
+        const uint32_t j = n0 + wn + y * 16 + g * 4;
+        float sb[4];
+        m8_col_scales(p, s, j, sb);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+        for (int x = 0; x < 2; ++x) {
             const uint32_t i = m0 + wm + x * 16 + i16;
+            m8_store4(p, s, i, j, acc[x][y], m8_row_scale(p, s, i), sb);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles whose operands lie at multiples of 16 bytes: the memory system writes them into LDS by itself (16 bytes a lane, in
+// the order of the lanes), a stage of 128 k while the one before it is multiplied.  A lane chooses which 16 bytes it fetches, so
+// that the rows of a fragment lie in different banks: chunk c of row r stands at c ^ swizzle(r).
+// ---------------------------------------------------------------------------
+static __device__ __align__(16) const uint32_t m8_zeros[4] = {0, 0, 0, 0};
+typedef const __attribute__((address_space(1))) void* glb_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// An operand's tile: R rows of op(A) (columns of op(B)), BK = 128 k, for T threads.  TURN: memory runs along the rows.
+template <int R, bool TURN, int T>
+struct M8Tile {
+    static constexpr int BK = 128, BYTES = R * BK, LOADS = BYTES / 16 / T, CHUNKS = (TURN ? R : BK) / 16;
+    uint32_t off[LOADS];
+    // The banks hold 256 bytes, and a quarter wave's reads are to cover them: 16 rows' chunks of 16 bytes each, of two
+    // groups of lanes
+    static __device__ __forceinline__ uint32_t swizzle(uint32_t r) {
+        if (!TURN) return (r >> 1) & 7;
+        if (CHUNKS >= 16) return (r & 7) | ((r >> 4) & 1) << 3;
+        if (CHUNKS == 8) return ((r >> 1) & 3) | ((r >> 4) & 1) << 2;
+        return ((r >> 2) & 1) | ((r >> 4) & 1) << 1;
+    }
+    static __device__ __forceinline__ void place(uint32_t i, uint32_t t, uint32_t& r, uint32_t& c) {
+        const uint32_t at = i * T + t;
+        r = at / CHUNKS;
+        c = ((at % CHUNKS) ^ swizzle(r)) * 16;
+    }
+    // rows: how many of the tile's there are; the last ones stand in for those that are not (their sums are not stored)
+    __device__ __forceinline__ void init(uint32_t t, uint64_t rs, uint32_t rows) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t j = n0 + wn + y * 16 + g * 4 + e;
-                if (i < p.M && j < p.N) m8_store(p, s, i, j, acc[x][y][e]);
+        for (int i = 0; i < LOADS; ++i) {
+            uint32_t r, c;
+            place(i, t, r, c);
+            off[i] = TURN ? (uint32_t)(r * rs) + min(c, rows - 16) : (uint32_t)(min(r, rows - 1) * rs) + c;
+        }
+    }
+    __device__ __forceinline__ void load(const int8_t* p, int8_t* lds, uint32_t w) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_global_load_lds((glb_ptr)(p + off[i]), (lds_ptr)(lds + (i * T + w * 64) * 16), 16, 0, 0);
+    }
+    // the last stage: zeros from k = `left` on
+    __device__ __forceinline__ void load_part(const int8_t* p, int8_t* lds, uint32_t w, uint32_t t, uint32_t left) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            uint32_t r, c;
+            place(i, t, r, c);
+            const int8_t* q = (TURN ? r : c) < left ? p + off[i] : (const int8_t*)m8_zeros;
+            __builtin_amdgcn_global_load_lds((glb_ptr)q, (lds_ptr)(lds + (i * T + w * 64) * 16), 16, 0, 0);
+        }
+    }
+    // the fragment of rows at .. at + 15, k from 64 kk on
+    static __device__ __forceinline__ v4i frag(const int8_t* lds, uint32_t at, int kk, uint32_t g, uint32_t i16) {
+        if constexpr (!TURN) {
+            const uint32_t r = at + i16;
+            return *(const v4i*)(lds + r * BK + (((kk * 4 + g) ^ swizzle(r)) * 16));
+        } else {
+            v4i f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t r = kk * 64 + 16 * g + 8 * h + (i16 >> 1);
+                const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i*)(lds + r * R + (((at >> 4) ^ swizzle(r)) * 16) + (i16 & 1) * 8));
+                f[2 * h] = y[0];
+                f[2 * h + 1] = y[1];
+            }
+            return f;
+        }
+    }
+};
+
+template <int BM, int BN, int WM, int WN, int STAGES, bool AT, bool BT>
+__global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
+    constexpr int T = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
+    using OA = M8Tile<BM, AT, T>;
+    using OB = M8Tile<BN, BT, T>;
+    constexpr int STAGE = OA::BYTES + OB::BYTES, LOADS = OA::LOADS + OB::LOADS;
+    __shared__ __align__(16) int8_t lds[STAGES * STAGE];
+    const uint32_t t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), g = l >> 4, i16 = l & 15;
+    uint64_t s;
+    uint32_t m0, n0;
+    m8_tile(p, BM, BN, s, m0, n0);
+    const uint32_t wm = w / WN * (BM / WM), wn = w % WN * (BN / WN);
+    OA oa;
+    OB ob;
+    oa.init(t, p.a_rs, min(p.M - m0, (uint32_t)BM));
+    ob.init(t, p.b_rs, min(p.N - n0, (uint32_t)BN));
+    const int8_t* pa = p.a + s * p.a_ss + (AT ? (uint64_t)m0 : m0 * p.a_rs);
+    const int8_t* pb = p.b + s * p.b_ss + (BT ? (uint64_t)n0 : n0 * p.b_rs);
+    const uint64_t step_a = AT ? 128 * p.a_rs : 128, step_b = BT ? 128 * p.b_rs : 128;
+    const uint32_t stages = (p.K + 127) / 128;
+    uint32_t ahead = 0, in = 0, out = 0;
+    auto load = [&]() {
+        if (ahead < stages) {
+            int8_t* q = lds + in * STAGE;
+            const uint32_t left = p.K - ahead * 128;
+            if (left >= 128) {
+                oa.load(pa, q, w);
+                ob.load(pb, q + OA::BYTES, w);
+            } else {
+                oa.load_part(pa, q, w, t, left);
+                ob.load_part(pb, q + OA::BYTES, w, t, left);
+            }
+            pa += step_a;
+            pb += step_b;
+            in = in == STAGES - 1 ? 0 : in + 1;
+        }
+        ++ahead;
+    };
+    v4i acc[FM][FN] = {};
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) load();
+    for (uint32_t k = 0; k < stages; ++k) {
+        // stage k has landed when no more is under way than the stages behind it; then everybody has also left stage k - 1
+        if (STAGES > 2 && stages - 1 - k >= STAGES - 2) {
+            constexpr int V = (STAGES - 2) * LOADS;
+            static_assert(V < 64, "counts to 63");
+            __builtin_amdgcn_s_waitcnt(0x0f70 | (V & 15) | (V >> 4) << 14);
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        load();
+        const int8_t* la = lds + out * STAGE;
+        const int8_t* lb = la + OA::BYTES;
+        out = out == STAGES - 1 ? 0 : out + 1;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            v4i fa[FM], fb[FN];
+#pragma unroll
+            for (int y = 0; y < FN; ++y) fb[y] = OB::frag(lb, wn + y * 16, kk, g, i16);
+#pragma unroll
+            for (int x = 0; x < FM; ++x) fa[x] = OA::frag(la, wm + x * 16, kk, g, i16);
+            __builtin_amdgcn_s_setprio(1);      // the wave whose operands are there goes first: the others read meanwhile
+#pragma unroll
+            for (int x = 0; x < FM; ++x)
+#pragma unroll
+                for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < FN; ++y) {
+        const uint32_t j = n0 + wn + y * 16 + g * 4;
+        float sb[4];
+        m8_col_scales(p, s, j, sb);
+#pragma unroll
+        for (int x = 0; x < FM; ++x) {
+            const uint32_t i = m0 + wm + x * 16 + i16;
+            m8_store4(p, s, i, j, acc[x][y], m8_row_scale(p, s, i), sb);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows (a batch of tokens): bound by reading op(B) once.  A block has 16 FM rows and 16 NC columns and its eight waves share out
+// k, 64 at a time; operands go straight into registers (op(B) through a wave's own piece of LDS where it has to be turned), many
+// loads under way at once, and the waves' sums are added at the end.
+// ---------------------------------------------------------------------------
+template <int FM, int NC, int U, bool AT, bool BT>
+__global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
+    constexpr int W = 8, BYTES = 1024 * NC;      // of a wave's tile of 64 k
+    __shared__ __align__(16) int8_t turn[BT ? W * BYTES : 16];
+    __shared__ __align__(16) int sums[W][FM * NC][64][4];
+    const uint32_t t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), g = l >> 4, i16 = l & 15;
+    uint64_t s;
+    uint32_t m0, n0;
+    m8_tile(p, 16 * FM, 16 * NC, s, m0, n0);
+    const int8_t *a = p.a + s * p.a_ss, *b = p.b + s * p.b_ss;
+    v4i acc[FM][NC] = {};
+    const uint32_t steps = (p.K + 63) / 64;
+    int8_t* mine = turn + (BT ? w * BYTES : 0);
+    for (uint32_t k0 = w; k0 < steps; k0 += W * U) {
+        v4i fa[U][FM], fb[U][NC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t k = (k0 + u * W) * 64;
+#pragma unroll
+            for (int y = 0; y < NC; ++y) {
+                if (BT) {       // 64 rows of k, 16 NC columns each: lane's piece
+                    const uint32_t at = y * 64 + l, r = at / NC, c = at % NC * 16;
+                    fb[u][y] = m8_fetch(b, p.b_rs, k + r, p.K, n0 + c, p.N);
+                } else {
+                    fb[u][y] = m8_fetch(b, p.b_rs, n0 + y * 16 + i16, p.N, k + g * 16, p.K);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < FM; ++x) {
+                if (AT) {
+                    const uint32_t i = m0 + x * 16 + i16;
+                    v4i f = {0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t kk = k + g * 16 + e;
+                        if (i < p.M && kk < p.K) f[e / 4] |= (int)((uint32_t)(uint8_t)a[kk * p.a_rs + i] << (8 * (e % 4)));
+                    }
+                    fa[u][x] = f;
+                } else {
+                    fa[u][x] = m8_fetch(a, p.a_rs, m0 + x * 16 + i16, p.M, k + g * 16, p.K);
+                }
             }
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            v4i f[NC];
+            if (BT) {
+                // a wave's own LDS: its operations there keep their order
+#pragma unroll
+                for (int y = 0; y < NC; ++y) *(v4i*)(mine + (y * 64 + l) * 16) = fb[u][y];
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int y = 0; y < NC; ++y)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t r = 16 * g + 8 * h + (i16 >> 1);
+                        const v2i z = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i*)(mine + r * (16 * NC) + y * 16 + (i16 & 1) * 8));
+                        f[y][2 * h] = z[0];
+                        f[y][2 * h + 1] = z[1];
+                    }
+                asm volatile("" ::: "memory");
+            } else {
+#pragma unroll
+                for (int y = 0; y < NC; ++y) f[y] = fb[u][y];
+            }
+#pragma unroll
+            for (int x = 0; x < FM; ++x)
+#pragma unroll
+                for (int y = 0; y < NC; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f[y], fa[u][x], acc[x][y], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < NC; ++y) *(v4i*)sums[w][x * NC + y][l] = acc[x][y];
+    __syncthreads();
+    // fragment f of the sums goes to wave f (mod 8)
+#pragma unroll
+    for (int f0 = 0; f0 < FM * NC; f0 += W) {
+        const uint32_t f = f0 + w;
+        if (f < FM * NC) {
+            v4i v = {0, 0, 0, 0};
+#pragma unroll
+            for (int q = 0; q < W; ++q) v += *(const v4i*)sums[q][f][l];
+            const uint32_t i = m0 + f / NC * 16 + i16, j = n0 + f % NC * 16 + g * 4;
+            float sb[4];
+            m8_col_scales(p, s, j, sb);
+            m8_store4(p, s, i, j, v, m8_row_scale(p, s, i), sb);
+        }
+    }
 }
 
 // a launch's blocks are counted in 32 bits of threads
-constexpr uint64_t M8_MAX_TILES = (uint64_t)1 << 24;
+constexpr uint64_t M8_MAX_TILES = (uint64_t)1 << 23;
 
-static int m8_launch(zkdl_ctx* ctx, const M8Args& p, bool at, bool bn, uint64_t stack) {
-    const uint64_t tiles = l8_ceil(p.M, 64) * l8_ceil(p.N, 64);
-    if (tiles >= M8_MAX_TILES || stack >= M8_MAX_TILES || tiles * stack >= M8_MAX_TILES) return ZKDL_ETOOBIG;
-    const dim3 grid((unsigned)(tiles * stack));
-    if (at && bn) hipLaunchKernelGGL((k_m8_any<true, true>), grid, dim3(256), 0, ctx->stream, p);
-    else if (at) hipLaunchKernelGGL((k_m8_any<true, false>), grid, dim3(256), 0, ctx->stream, p);
-    else if (bn) hipLaunchKernelGGL((k_m8_any<false, true>), grid, dim3(256), 0, ctx->stream, p);
-    else hipLaunchKernelGGL((k_m8_any<false, false>), grid, dim3(256), 0, ctx->stream, p);
+template <bool AT, bool BT>
+static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, bool whole) {
+    int bm = 64, bn = 64, threads = 256;
+    void (*kernel)(M8Args) = k_m8_any<AT, BT>;
+    auto tiles = [&](uint64_t m, uint64_t n) { return l8_ceil(p.M, m) * l8_ceil(p.N, n) * stack; };
+    if (p.M <= 16) {
+        constexpr int NC = BT ? 2 : 1;
+        kernel = k_m8_few<1, NC, 8, AT, BT>;
+        bm = 16, bn = 16 * NC, threads = 512;
+    } else if (whole) {
+        if (tiles(256, 256) >= 200) {
+            kernel = k_m8_tile<256, 256, 2, 4, 2, AT, BT>;
+            bm = bn = 256, threads = 512;
+        } else if (tiles(128, 128) >= 200) {
+            kernel = k_m8_tile<128, 128, 2, 2, 2, AT, BT>;
+            bm = bn = 128;
+        } else {
+            kernel = k_m8_tile<64, 64, 2, 2, 4, AT, BT>;
+        }
+    }
+    if (l8_ceil(p.M, bm) * l8_ceil(p.N, bn) >= M8_MAX_TILES || stack >= M8_MAX_TILES || tiles(bm, bn) >= M8_MAX_TILES) return ZKDL_ETOOBIG;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(bm, bn)), dim3(threads), 0, ctx->stream, p);
     return ZKDL_OK;
 }
 
@@ -154,7 +458,18 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
     p.M = (uint32_t)out->rows;
     p.N = (uint32_t)out->cols;
     p.K = (uint32_t)(trans_a ? a->rows : a->cols);
-    return m8_launch(ctx, p, trans_a != 0, trans_b == 0, out->stack);
+    const uint64_t item = out->dtype == ZKDL_I32 || out->dtype == ZKDL_F32 ? 4 : 2;
+    p.o_vec = p.o_rs % 4 == 0 && (out->stack == 1 || p.o_ss % 4 == 0) && (uintptr_t)p.out % (4 * item) == 0;
+    // operands that k_m8_tile can fetch: whole 16 bytes along memory, and rows of a tile within 32 bits
+    auto whole = [&](const zkdl_mat* m) {
+        return (uintptr_t)m->data % 16 == 0 && m->row_stride % 16 == 0 && (m->stack == 1 || m->stack_stride % 16 == 0) && m->cols % 16 == 0 &&
+               m->row_stride < (uint64_t)1 << 23;
+    };
+    const bool w = p.K > 0 && whole(a) && whole(b);
+    if (trans_a && !trans_b) return m8_launch<true, true>(ctx, p, out->stack, w);
+    if (trans_a) return m8_launch<true, false>(ctx, p, out->stack, w);
+    if (!trans_b) return m8_launch<false, true>(ctx, p, out->stack, w);
+    return m8_launch<false, false>(ctx, p, out->stack, w);
 }
 
 // sums of this many products of magnitude 2^14 stay within 31 bits

@@ -541,3 +541,19 @@ def test_empty_matrices(lib, ctx):
     w = torch.ones(8, 5, dtype=torch.int8, device="cuda")
     got = lib.matmul_i8_backward(ctx, torch.zeros(0, 5, device="cuda"), i8, one8[:0], w, one8[:5])
     assert got["da"].shape == (0, 8) and torch.equal(got["dw"], torch.zeros(8, 5, device="cuda"))
+
+
+# enough tiles of 256 x 256 and of 128 x 128 to fill the device; edges in all three directions, whole 16 bytes for either layout
+@pytest.mark.parametrize("ta,tb", [(False, False), (False, True), (True, False), (True, True)], ids=["nn", "nt", "tn", "tt"])
+@pytest.mark.parametrize("shape", [(3696, 400, 3600), (2000, 144, 1840), (4096, 16, 4096), (1600, 1024, 2064)], ids=str)
+def test_matmul_large_tiles(lib, ctx, shape, ta, tb):
+    m, k, n = shape
+    g = gen(m + k + n)
+    a, b = codes(g, (m, k)), codes(g, (k, n))
+    want = product64(a, b)
+    pa, pb = stored(a, ta).cuda(), stored(b, tb).cuda()
+    assert torch.equal(lib.matmul_i8(ctx, pa, pb, trans_a=ta, trans_b=tb).cpu().double(), want)
+    sa, sb = torch.rand(m, generator=g) + 0.5, torch.rand(n, generator=g) + 0.5
+    got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=torch.bfloat16).cpu().double()
+    scaled = want * sa.double()[:, None] * sb.double()[None, :]
+    assert torch.all((got - scaled).abs() <= (4 * U + 1.001 * HALF_ULP[torch.bfloat16]) * scaled.abs())
