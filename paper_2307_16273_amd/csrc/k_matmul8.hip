@@ -34,51 +34,76 @@ static __device__ __forceinline__ void m8_tile(const M8Args& p, uint32_t bm, uin
     n0 = at / rows * bn;
 }
 
-// Four adjacent columns of a row: (acc sa) sb, each product rounded to 32 bits, and once more to out's type.
-static __device__ __forceinline__ void m8_store4(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, const v4i& acc, float sa, const float (&sb)[4]) {
-    if (i >= p.M || j >= p.N) return;
-    const uint64_t at = s * p.o_ss + i * p.o_rs + j;
-    const int n = (int)min(p.N - j, 4u);
-    if (p.o_type == ZKDL_I32) {
-        int* o = (int*)p.out + at;
-        if (n == 4 && p.o_vec) {
-            *(v4i*)o = acc;
-        } else {
+template <class T>
+struct alignas(4 * sizeof(T)) M8Four {
+    T v[4];
+};
+// Four adjacent columns of a row: the accumulators, or (acc sa) sb, each product rounded to 32 bits and once more to out's type.
+template <class T>
+static __device__ __forceinline__ void m8_store4(T* o, int n, bool vec, const v4i& acc, float sa, const float (&sb)[4]) {
+    M8Four<T> x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) o[e] = acc[e];
-        }
-        return;
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (__is_same(T, int)) x.v[e] = acc[e];
+        else l8_put((float)acc[e] * sa * sb[e], x.v[e]);
     }
-    float f[4];
+    if (vec && n >= 4) {
+        *(M8Four<T>*)o = x;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = (float)acc[e] * sa * sb[e];
-    auto put = [&](auto t) {
-        using T = decltype(t);
-        struct alignas(4 * sizeof(T)) Four {
-            T v[4];
-        } x;
+        for (int e = 0; e < 4; ++e)
+            if (e < n) o[e] = x.v[e];
+    }
+}
+// A wave's fragments, 16 rows and 16 columns apart; the lane's first row and column are (i, j): the products come out turned, so that a
+// lane has four adjacent columns of one row.  inside: no fragment crosses an edge and items may be stored by fours.  All scales are read
+// before the first store: a load behind stores waits for them.
+template <class T, int FM, int FN>
+static __device__ __forceinline__ void m8_store_as(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, bool inside, const v4i (&acc)[FM][FN]) {
+    float sa[FM], sb[FN][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) l8_put(f[e], x.v[e]);
-        T* o = (T*)p.out + at;
-        if (n == 4 && p.o_vec) {
-            *(Four*)o = x;
-        } else {
+    for (int x = 0; x < FM; ++x) sa[x] = 1.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) o[e] = x.v[e];
+    for (int y = 0; y < FN; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sb[y][e] = 1.f;
+    if constexpr (!__is_same(T, int)) {
+        if (p.sa) {
+            const float* q = p.sa + s * p.M;
+#pragma unroll
+            for (int x = 0; x < FM; ++x) sa[x] = q[min(i + x * 16, p.M - 1)];
         }
-    };
-    if (p.o_type == ZKDL_F32) put(float{});
-    else if (p.o_type == ZKDL_F16) put(__half{});
-    else put(bf16_t{});
-}
-static __device__ __forceinline__ float m8_row_scale(const M8Args& p, uint64_t s, uint32_t i) {
-    return p.sa && i < p.M ? p.sa[s * p.M + i] : 1.f;
-}
-static __device__ __forceinline__ void m8_col_scales(const M8Args& p, uint64_t s, uint32_t j, float (&f)[4]) {
+        if (p.sb) {
+            const float* q = p.sb + s * p.N;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = p.sb && j + e < p.N ? p.sb[s * p.N + j + e] : 1.f;
+            for (int y = 0; y < FN; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sb[y][e] = q[min(j + y * 16 + e, p.N - 1)];
+        }
+    }
+    T* o = (T*)p.out + s * p.o_ss + i * p.o_rs + j;
+    if (inside) {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FN; ++y) m8_store4(o + x * 16 * p.o_rs + y * 16, 4, true, acc[x][y], sa[x], sb[y]);
+    } else {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FN; ++y)
+                if (i + x * 16 < p.M && j + y * 16 < p.N)
+                    m8_store4(o + x * 16 * p.o_rs + y * 16, (int)min(p.N - j - y * 16, 4u), p.o_vec != 0, acc[x][y], sa[x], sb[y]);
+    }
+}
+template <int FM, int FN>
+static __device__ __forceinline__ void m8_store_tile(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, bool inside, const v4i (&acc)[FM][FN]) {
+    switch (p.o_type) {
+        case ZKDL_I32: m8_store_as<int>(p, s, i, j, inside, acc); break;
+        case ZKDL_F32: m8_store_as<float>(p, s, i, j, inside, acc); break;
+        case ZKDL_F16: m8_store_as<__half>(p, s, i, j, inside, acc); break;
+        default: m8_store_as<bf16_t>(p, s, i, j, inside, acc);
+    }
 }
 
 struct __attribute__((packed, aligned(1))) M8Bytes {
@@ -145,18 +170,7 @@ __global__ __launch_bounds__(256) void k_m8_any(M8Args p) {
 #pragma unroll
             for (int y = 0; y < 2; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
     }
-    // the products come out turned: a lane has four adjacent columns of one row
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        const uint32_t j = n0 + wn + y * 16 + g * 4;
-        float sb[4];
-        m8_col_scales(p, s, j, sb);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint32_t i = m0 + wm + x * 16 + i16;
-            m8_store4(p, s, i, j, acc[x][y], m8_row_scale(p, s, i), sb);
-        }
-    }
+    m8_store_tile<2, 2>(p, s, m0 + wm + i16, n0 + wn + g * 4, false, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -300,17 +314,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
             __builtin_amdgcn_s_setprio(0);
         }
     }
-#pragma unroll
-    for (int y = 0; y < FN; ++y) {
-        const uint32_t j = n0 + wn + y * 16 + g * 4;
-        float sb[4];
-        m8_col_scales(p, s, j, sb);
-#pragma unroll
-        for (int x = 0; x < FM; ++x) {
-            const uint32_t i = m0 + wm + x * 16 + i16;
-            m8_store4(p, s, i, j, acc[x][y], m8_row_scale(p, s, i), sb);
-        }
-    }
+    m8_store_tile<FM, FN>(p, s, m0 + wm + i16, n0 + wn + g * 4, p.o_vec && m0 + BM <= p.M && n0 + BN <= p.N, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -399,13 +403,10 @@ __global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
     for (int f0 = 0; f0 < FM * NC; f0 += W) {
         const uint32_t f = f0 + w;
         if (f < FM * NC) {
-            v4i v = {0, 0, 0, 0};
+            v4i v[1][1] = {};
 #pragma unroll
-            for (int q = 0; q < W; ++q) v += *(const v4i*)sums[q][f][l];
-            const uint32_t i = m0 + f / NC * 16 + i16, j = n0 + f % NC * 16 + g * 4;
-            float sb[4];
-            m8_col_scales(p, s, j, sb);
-            m8_store4(p, s, i, j, v, m8_row_scale(p, s, i), sb);
+            for (int q = 0; q < W; ++q) v[0][0] += *(const v4i*)sums[q][f][l];
+            m8_store_tile<1, 1>(p, s, m0 + f / NC * 16 + i16, n0 + f % NC * 16 + g * 4, false, v);
         }
     }
 }

@@ -36,10 +36,7 @@ static __device__ __forceinline__ void l8_put(float x, __half& o) {
     asm("" : "+v"(x));      // a 32-bit value of its own: a product in front would be rounded once, to 16 bits, otherwise
     o = __float2half(x);
 }
-static __device__ __forceinline__ void l8_put(float x, bf16_t& o) {
-    const uint32_t u = __float_as_uint(x);
-    o.v = (uint16_t)((u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-}
+static __device__ __forceinline__ void l8_put(float x, bf16_t& o) { o.v = __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 // Eight adjacent items, at any address: the memory system takes 16 bytes at once also where they are not aligned.
 template <class T>
