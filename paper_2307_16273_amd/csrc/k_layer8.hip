@@ -7,8 +7,9 @@
 
 // ---------------------------------------------------------------------------
 // Rows: v = (x [+ residual]) * w, largest |v| of the row, q = rint(v * 127 / that).
-// A row belongs to G threads (a wave, or a block of four) and each of them keeps ITEMS vectors of 8 values; ITEMS = 0 is
-// for rows too long for the registers, which are read twice.
+// A row belongs to G threads (a wave, or a block) and each of them keeps ITEMS vectors of 8 values, all of whose loads are
+// under way before the first is looked at; ITEMS = 0 is for rows too long for the registers, which are read twice, and for
+// rows of fewer than 8.
 // ---------------------------------------------------------------------------
 struct L8RowArgs {
     uint64_t rows, per_stack;     // rows in all, rows of a matrix
@@ -32,6 +33,9 @@ static __device__ __forceinline__ void l8_weights(const L8RowArgs& a, uint64_t s
         l8_load((const T*)a.w + s * a.w_stack + j, n, f);
     }
 }
+
+// threads of a block: four waves, or one group if that is larger
+constexpr int l8_threads(int group) { return group < 256 ? 256 : group; }
 
 // sum and maximum over the G threads of a row
 template <int G>
@@ -57,10 +61,31 @@ static __device__ __forceinline__ void l8_row_reduce(float& sum, uint32_t& top) 
     }
 }
 
+// the mean square's root when the squares left the range (or an input did): once more, 2^-80 smaller
+template <class T, int G>
+static __device__ __forceinline__ float l8_rstd_again(const T* x, const T* r, uint32_t cols, uint32_t t) {
+    float again = 0.f;
+    uint32_t unused = 0;
+#pragma unroll 1
+    for (uint32_t j = t * 8; j < cols; j += G * 8) {
+        float h[8], b[8] = {};
+        const int n = (int)min(cols - j, 8u);
+        l8_load(x + j, n, h);
+        if (r) l8_load(r + j, n, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = (h[i] + b[i]) * 0x1p-80f;
+            again = fmaf(y, y, again);
+        }
+    }
+    l8_row_reduce<G>(again, unused);
+    return 0x1p-80f / sqrtf(again / (float)cols);
+}
+
 template <class T, bool NORM, int G, int ITEMS>
-__global__ __launch_bounds__(256) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
+__global__ __launch_bounds__(l8_threads(G)) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
                                                  L8Mat<T> values) {
-    constexpr int GROUPS = 256 / G;
+    constexpr int GROUPS = l8_threads(G) / G;
     const uint32_t t = threadIdx.x % G;
     const uint64_t step = (uint64_t)gridDim.x * GROUPS;
     // all groups of a block take as many turns: the reductions of a block-wide group meet at barriers
@@ -69,68 +94,78 @@ __global__ __launch_bounds__(256) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, 
         if (GROUPS > 1 && r >= a.rows) continue;
         const uint64_t s = r / a.per_stack, m = r % a.per_stack;
         const T* xr = x.p + s * x.ss + m * x.rs;
-        const T* rr = res.p ? res.p + s * res.ss + m * res.rs : nullptr;
-        T* tr = total.p ? total.p + s * total.ss + m * total.rs : nullptr;
+        const T* rr = NORM && res.p ? res.p + s * res.ss + m * res.rs : nullptr;
+        T* tr = NORM && total.p ? total.p + s * total.ss + m * total.rs : nullptr;
         float keep[ITEMS ? ITEMS : 1][8];
         float ss = 0.f;
         uint32_t top = 0;
-        auto sum_at = [&](uint32_t j, float (&h)[8]) {
-            const int n = (int)min(a.cols - j, 8u);
-            l8_load(xr + j, n, h);
-            if (NORM && rr) {
-                float b[8];
-                l8_load(rr + j, n, b);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[i] += b[i];
-            }
-        };
-        auto first = [&](uint32_t j, float (&v)[8]) {
-            const int n = (int)min(a.cols - j, 8u);
-            sum_at(j, v);
-            if (NORM) {
-                if (tr) l8_store(tr + j, n, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
-            }
-            if (a.w) {
-                float w[8];
-                l8_weights<T>(a, s, j, n, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= w[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, l8_mag(v[i]));
-        };
         if constexpr (ITEMS > 0) {
+            L8At at[ITEMS];
+            L8Vec<T> xv[ITEMS], rv[ITEMS], wt[ITEMS];
+            L8Vec<float> wf[ITEMS];
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const uint32_t j = (k * G + t) * 8;
-                if (j < a.cols) first(j, keep[k]);
+                at[k] = l8_at((k * G + t) * 8, a.cols);
+                xv[k] = l8_raw(xr + at[k].start);
+            }
+            if (NORM && rr) {
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) rv[k] = l8_raw(rr + at[k].start);
+            }
+            if (a.w && a.w_f32) {
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) wf[k] = l8_raw((const float*)a.w + s * a.w_stack + at[k].start);
+            } else if (NORM && a.w) {
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) wt[k] = l8_raw((const T*)a.w + at[k].start);
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                float(&v)[8] = keep[k];
+                l8_floats(xv[k], v);
+                if (NORM) {
+                    if (rr) {
+                        float b[8];
+                        l8_floats(rv[k], b);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] += b[i];
+                    }
+                    if (tr && at[k].live) l8_store(tr + at[k].start, 8, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ss = fmaf(v[i], (uint32_t)i < at[k].dup ? 0.f : v[i], ss);
+                }
+                if (a.w) {
+                    float w[8];
+                    if (a.w_f32) l8_floats(wf[k], w);
+                    else if (NORM) l8_floats(wt[k], w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] *= w[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, l8_mag(v[i]));
             }
         } else {
-            for (uint32_t j = t * 8; j < a.cols; j += G * 8) first(j, keep[0]);
+            for (uint32_t j = t * 8; j < a.cols; j += G * 8) {
+                const int n = (int)min(a.cols - j, 8u);
+                float v[8], w[8];
+                l8_load(xr + j, n, v);
+                if (rr) {
+                    l8_load(rr + j, n, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += w[i];
+                }
+                if (tr) l8_store(tr + j, n, v);
+                l8_weights<T>(a, s, j, n, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (NORM) ss = fmaf(v[i], v[i], ss);
+                    top = max(top, l8_mag(v[i] * w[i]));
+                }
+            }
         }
         l8_row_reduce<G>(ss, top);
         float rstd = 1.f;
-        if (NORM) {
-            if (l8_mag(ss) >= L8_INF) {      // the squares left the range (or an input did): once more, 2^-80 smaller
-                float again = 0.f;
-                uint32_t unused = 0;
-                for (uint32_t j = t * 8; j < a.cols; j += G * 8) {
-                    float h[8];
-                    sum_at(j, h);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float y = h[i] * 0x1p-80f;
-                        again = fmaf(y, y, again);
-                    }
-                }
-                l8_row_reduce<G>(again, unused);
-                rstd = 0x1p-80f / sqrtf(again / (float)a.cols);
-            } else {
-                rstd = 1.f / sqrtf(ss / (float)a.cols + a.eps);
-            }
-        }
+        if (NORM) rstd = l8_mag(ss) >= L8_INF ? l8_rstd_again<T, G>(xr, rr, a.cols, t) : 1.f / sqrtf(ss / (float)a.cols + a.eps);
         const L8Quant c = l8_quant(top);
         float scale = __uint_as_float(top) / 127.f;
         if (NORM) scale = __uint_as_float(top) * rstd / 127.f;
@@ -141,8 +176,7 @@ __global__ __launch_bounds__(256) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, 
         }
         int8_t* qr = q.p + s * q.ss + m * q.rs;
         T* vr = values.p ? values.p + s * values.ss + m * values.rs : nullptr;
-        auto second = [&](uint32_t j, float (&v)[8]) {
-            const int n = (int)min(a.cols - j, 8u);
+        auto second = [&](uint32_t j, int n, float (&v)[8]) {
             int iq[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[i], c);
@@ -156,19 +190,23 @@ __global__ __launch_bounds__(256) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, 
         if constexpr (ITEMS > 0) {
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const uint32_t j = (k * G + t) * 8;
-                if (j < a.cols) second(j, keep[k]);
+                const L8At p = l8_at((k * G + t) * 8, a.cols);
+                if (p.live) second(p.start, 8, keep[k]);
             }
         } else {
             for (uint32_t j = t * 8; j < a.cols; j += G * 8) {
+                const int n = (int)min(a.cols - j, 8u);
                 float v[8], w[8];
-                sum_at(j, v);
-                if (a.w) {
-                    l8_weights<T>(a, s, j, (int)min(a.cols - j, 8u), w);
+                l8_load(xr + j, n, v);
+                if (rr) {
+                    l8_load(rr + j, n, w);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= w[i];
+                    for (int i = 0; i < 8; ++i) v[i] += w[i];
                 }
-                second(j, v);
+                l8_weights<T>(a, s, j, n, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= w[i];
+                second(j, n, v);
             }
         }
     }
@@ -186,15 +224,17 @@ template <class T, bool NORM>
 static void l8_launch_rows(zkdl_ctx* ctx, const L8RowArgs& a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
                            L8Mat<T> values) {
     const uint32_t n = a.cols;
-#define L8_ROWS(G, ITEMS) \
-    hipLaunchKernelGGL((k_l8_rows<T, NORM, G, ITEMS>), dim3(l8_grid(l8_ceil(a.rows, 256 / G))), dim3(256), 0, ctx->stream, a, x, res, q, total, values)
-    if (n <= 512) L8_ROWS(64, 1);
+#define L8_ROWS(G, ITEMS)                                                                                                              \
+    hipLaunchKernelGGL((k_l8_rows<T, NORM, G, ITEMS>), dim3(l8_grid(l8_ceil(a.rows, l8_threads(G) / G))), dim3(l8_threads(G)), 0, ctx->stream, a, x, \
+                       res, q, total, values)
+    if (n < 8) L8_ROWS(64, 0);
+    else if (n <= 512) L8_ROWS(64, 1);
     else if (n <= 1024) L8_ROWS(64, 2);
     else if (n <= 2048) L8_ROWS(256, 1);
     else if (n <= 4096) L8_ROWS(256, 2);
-    else if (n <= 8192) L8_ROWS(256, 4);
-    else if (n <= 16384) L8_ROWS(256, 8);
-    else L8_ROWS(256, 0);
+    else if (n <= 8192) L8_ROWS(512, 2);
+    else if (n <= 16384) L8_ROWS(1024, 2);
+    else L8_ROWS(1024, 0);
 #undef L8_ROWS
 }
 
@@ -211,14 +251,41 @@ struct L8ColArgs {
     float* scale;                 // [stack][cols]
 };
 
-template <class T>
-static __device__ __forceinline__ void l8_col_values(const L8ColArgs& a, const L8Mat<const T>& x, uint64_t s, uint64_t m, uint32_t j, int n,
-                                                     float (&v)[8]) {
-    l8_load(x.p + s * x.ss + m * x.rs + j, n, v);
-    if (a.mult) {
-        const float f = a.mult[s * a.rows + m];
+// f(m, v) for the thread's rows m, m + 32, .. < hi; four rows are read before the first of them is looked at
+template <class T, class F>
+static __device__ __forceinline__ void l8_col_walk(const L8ColArgs& a, const L8Mat<const T>& x, uint64_t s, uint64_t m, uint64_t hi, uint32_t j, F f) {
+    const T* p = x.p + s * x.ss + j;
+    const float* mu = a.mult ? a.mult + s * a.rows : nullptr;
+    if (j + 8 <= a.cols) {
+        for (; m < hi; m += 4 * L8_COL_R) {
+            L8Vec<T> v[4];
+            float w[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= f;
+            for (int k = 0; k < 4; ++k) v[k] = l8_raw(p + min(m + k * L8_COL_R, hi - 1) * x.rs);
+            if (mu) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = mu[min(m + k * L8_COL_R, hi - 1)];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (m + k * L8_COL_R >= hi) break;
+                float g[8];
+                l8_floats(v[k], g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= w[k];
+                f(m + k * L8_COL_R, g);
+            }
+        }
+    } else {
+        for (; m < hi; m += L8_COL_R) {
+            float g[8];
+            l8_load(p + m * x.rs, (int)(a.cols - j), g);
+            if (mu) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= mu[m];
+            }
+            f(m, g);
+        }
     }
 }
 
@@ -235,12 +302,10 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
     uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (MODE != 1) {
         if (live)
-            for (uint64_t m = lo + ty; m < hi; m += L8_COL_R) {
-                float v[8];
-                l8_col_values(a, x, s, m, j, n, v);
+            l8_col_walk(a, x, s, lo + ty, hi, j, [&](uint64_t, float(&v)[8]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top[i] = max(top[i], l8_mag(v[i]));
-            }
+            });
     } else if (live) {
         for (uint32_t k = ty; k < a.chunks; k += L8_COL_R)
 #pragma unroll
@@ -270,9 +335,7 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
         c[i] = l8_quant(b);
         scale[i] = c[i].finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
     }
-    for (uint64_t m = lo + ty; m < hi; m += L8_COL_R) {
-        float v[8];
-        l8_col_values(a, x, s, m, j, n, v);
+    l8_col_walk(a, x, s, lo + ty, hi, j, [&](uint64_t m, float(&v)[8]) {
         int iq[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[i], c[i]);
@@ -282,7 +345,7 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
             for (int i = 0; i < 8; ++i) v[i] = (float)iq[i] * scale[i];
             l8_store(values.p + s * values.ss + m * values.rs + j, n, v);
         }
-    }
+    });
 }
 
 template <class T>
@@ -422,13 +485,19 @@ struct L8BackArgs {
 };
 
 template <class T, int G, int ITEMS>
-__global__ __launch_bounds__(256) void k_l8_norm_back(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h, L8Mat<const T> dt, L8Mat<T> dx) {
-    constexpr int GROUPS = 256 / G;
+__global__ __launch_bounds__(l8_threads(G)) void k_l8_norm_back(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h, L8Mat<const T> dt, L8Mat<T> dx) {
+    constexpr int GROUPS = l8_threads(G) / G;
     const uint32_t t = threadIdx.x % G;
     L8RowArgs wa = {};
     wa.w = a.w;
     wa.w_f32 = a.w_f32;
-    float dw[ITEMS][8] = {};
+    float dw[ITEMS][8] = {}, w[ITEMS][8];
+    L8At at[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        at[k] = l8_at((k * G + t) * 8, a.cols);
+        l8_weights<T>(wa, 0, at[k].start, 8, w[k]);
+    }
     const uint64_t step = (uint64_t)gridDim.x * GROUPS;
     const float over = 1.f / (float)a.cols;
     for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
@@ -438,42 +507,41 @@ __global__ __launch_bounds__(256) void k_l8_norm_back(L8BackArgs a, L8Mat<const 
         float g[ITEMS][8], n[ITEMS][8];
         float dot = 0.f;
         uint32_t unused = 0;
+        L8Vec<T> gv[ITEMS], hv[ITEMS], ev[ITEMS];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) gv[k] = l8_raw(dy.p + m * dy.rs + at[k].start);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) hv[k] = l8_raw(h.p + m * h.rs + at[k].start);
+        if (dt.p) {
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) ev[k] = l8_raw(dt.p + m * dt.rs + at[k].start);
+        }
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t j = (k * G + t) * 8;
-            if (j < a.cols) {
-                const int c = (int)min(a.cols - j, 8u);
-                float w[8];
-                l8_load(dy.p + m * dy.rs + j, c, g[k]);
-                l8_load(h.p + m * h.rs + j, c, n[k]);
-                l8_weights<T>(wa, 0, j, c, w);
+            l8_floats(gv[k], g[k]);
+            l8_floats(hv[k], n[k]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    n[k][i] *= rstd;
-                    dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
-                    g[k][i] *= w[i];
-                    dot = fmaf(g[k][i], n[k][i], dot);
-                }
+            for (int i = 0; i < 8; ++i) {
+                n[k][i] *= rstd;
+                dw[k][i] = fmaf(g[k][i], n[k][i], dw[k][i]);
+                g[k][i] *= w[k][i];
+                dot = fmaf(g[k][i], (uint32_t)i < at[k].dup ? 0.f : n[k][i], dot);
             }
         }
         l8_row_reduce<G>(dot, unused);
         dot *= over;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t j = (k * G + t) * 8;
-            if (j < a.cols) {
-                const int c = (int)min(a.cols - j, 8u);
-                float d[8];
+            float d[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-n[k][i], dot, g[k][i]);
-                if (dt.p) {
-                    float e[8];
-                    l8_load(dt.p + m * dt.rs + j, c, e);
+            for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-n[k][i], dot, g[k][i]);
+            if (dt.p) {
+                float e[8];
+                l8_floats(ev[k], e);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] += e[i];
-                }
-                l8_store(dx.p + m * dx.rs + j, c, d);
+                for (int i = 0; i < 8; ++i) d[i] += e[i];
             }
+            if (at[k].live) l8_store(dx.p + m * dx.rs + at[k].start, 8, d);
         }
     }
     if (!a.part) return;
@@ -482,19 +550,18 @@ __global__ __launch_bounds__(256) void k_l8_norm_back(L8BackArgs a, L8Mat<const 
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s_dw[threadIdx.x / G][(k * G + t) * 8 + i] = dw[k][i];
+            for (int i = 0; i < 8; ++i)
+                if (at[k].live) s_dw[threadIdx.x / G][at[k].start + i] = dw[k][i];
         __syncthreads();
-        for (uint32_t j = threadIdx.x; j < a.cols; j += 256) {
+        for (uint32_t j = threadIdx.x; j < a.cols; j += l8_threads(G)) {
             float s = 0.f;
             for (int k = 0; k < GROUPS; ++k) s += s_dw[k][j];
             a.part[(uint64_t)blockIdx.x * a.cols + j] = s;
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t j = (k * G + t) * 8;
-            if (j < a.cols) l8_store(a.part + (uint64_t)blockIdx.x * a.cols + j, (int)min(a.cols - j, 8u), dw[k]);
-        }
+        for (int k = 0; k < ITEMS; ++k)
+            if (at[k].live) l8_store(a.part + (uint64_t)blockIdx.x * a.cols + at[k].start, 8, dw[k]);
     }
 }
 
@@ -562,21 +629,23 @@ __global__ __launch_bounds__(256) void k_l8_dweight_long(L8BackArgs a, L8Mat<con
     l8_store(a.part + blockIdx.y * (uint64_t)a.cols + j, c, dw);
 }
 
-// out[j] = sum over the blocks' shares: 64 columns x 16 runs of shares, the runs' sums added in their order
+// out[j] = sum over the blocks' shares: 32 columns x 32 runs of shares, the runs' sums added in their order
 __global__ __launch_bounds__(1024) void k_l8_sum_shares(const float* part, uint32_t shares, uint32_t cols, float* out) {
-    __shared__ float s[16][64];
-    const uint32_t tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    for (uint64_t j0 = (uint64_t)blockIdx.x * 64; j0 < cols; j0 += gridDim.x * 64ull) {
+    __shared__ float s[32][33];
+    const uint32_t tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    for (uint64_t j0 = (uint64_t)blockIdx.x * 32; j0 < cols; j0 += gridDim.x * 32ull) {
         const uint64_t j = j0 + tx;
         float x = 0.f;
-        if (j < cols)
-            for (uint32_t k = ty; k < shares; k += 16) x += part[(uint64_t)k * cols + j];
+        if (j < cols) {
+#pragma unroll 8
+            for (uint32_t k = ty; k < shares; k += 32) x += part[(uint64_t)k * cols + j];
+        }
         __syncthreads();
         s[ty][tx] = x;
         __syncthreads();
         if (ty == 0 && j < cols) {
             x = 0.f;
-            for (int k = 0; k < 16; ++k) x += s[k][tx];
+            for (int k = 0; k < 32; ++k) x += s[k][tx];
             out[j] = x;
         }
     }
@@ -585,9 +654,9 @@ __global__ __launch_bounds__(1024) void k_l8_sum_shares(const float* part, uint3
 template <class T>
 static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const zkdl_mat* h, const zkdl_mat* dt, const zkdl_mat* dx, float* dweight) {
     const uint32_t n = a.cols;
-    const bool wave = n <= 1024, regs = n <= 16384;
+    const bool wave = n <= 1024, regs = n >= 8 && n <= 16384;
     uint64_t blocks = l8_ceil(a.rows, wave ? 4 : 1);
-    if (blocks > 1024) blocks = 1024;
+    if (blocks > 768) blocks = 768;
     const uint64_t col_rows = a.rows < 64 ? a.rows : 64;
     if (dweight) {
         a.part = (float*)zk_alloc(ctx, (regs ? blocks : col_rows) * n * 4);
@@ -595,20 +664,20 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
     }
     const L8Mat<const T> mdy = l8_mat<const T>(dy), mh = l8_mat<const T>(h), mdt = l8_mat<const T>(dt);
     const L8Mat<T> mdx = l8_mat<T>(dx);
-#define L8_BACK(G, ITEMS) hipLaunchKernelGGL((k_l8_norm_back<T, G, ITEMS>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx)
-    if (n <= 512) L8_BACK(64, 1);
+#define L8_BACK(G, ITEMS) \
+    hipLaunchKernelGGL((k_l8_norm_back<T, G, ITEMS>), dim3((unsigned)blocks), dim3(l8_threads(G)), 0, ctx->stream, a, mdy, mh, mdt, mdx)
+    if (!regs) {
+        hipLaunchKernelGGL((k_l8_norm_back_long<T>), dim3(l8_grid(a.rows)), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx);
+        if (dweight) hipLaunchKernelGGL((k_l8_dweight_long<T>), dim3((unsigned)l8_ceil(n, 2048), (unsigned)col_rows), dim3(256), 0, ctx->stream, a, mdy, mh);
+    } else if (n <= 512) L8_BACK(64, 1);
     else if (n <= 1024) L8_BACK(64, 2);
     else if (n <= 2048) L8_BACK(256, 1);
     else if (n <= 4096) L8_BACK(256, 2);
-    else if (n <= 8192) L8_BACK(256, 4);
-    else if (n <= 16384) L8_BACK(256, 8);
-    else {
-        hipLaunchKernelGGL((k_l8_norm_back_long<T>), dim3(l8_grid(a.rows)), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx);
-        if (dweight) hipLaunchKernelGGL((k_l8_dweight_long<T>), dim3((unsigned)l8_ceil(n, 2048), (unsigned)col_rows), dim3(256), 0, ctx->stream, a, mdy, mh);
-    }
+    else if (n <= 8192) L8_BACK(512, 2);
+    else L8_BACK(1024, 2);
 #undef L8_BACK
     if (dweight)
-        hipLaunchKernelGGL(k_l8_sum_shares, dim3(l8_grid(l8_ceil(n, 64))), dim3(1024), 0, ctx->stream, a.part, (uint32_t)(regs ? blocks : col_rows), n, dweight);
+        hipLaunchKernelGGL(k_l8_sum_shares, dim3(l8_grid(l8_ceil(n, 32))), dim3(1024), 0, ctx->stream, a.part, (uint32_t)(regs ? blocks : col_rows), n, dweight);
     zk_free(ctx, a.part);
     return ZKDL_OK;
 }

@@ -55,6 +55,28 @@ static __device__ __forceinline__ void l8_load(const T* p, int n, float (&f)[8])
         for (int i = 0; i < 8; ++i) f[i] = i < n ? l8_f32(p[i]) : 0.f;
     }
 }
+// The eight items that a thread at column j of a row of `cols` >= 8 looks at: those from j on, or the row's last eight, of which
+// the first `dup` belong to another thread (all of them where j is behind the end).  So every load takes eight items, none waits for
+// a branch, and what two threads write twice is the same.
+struct L8At {
+    uint32_t start, dup;
+    bool live;
+};
+static __device__ __forceinline__ L8At l8_at(uint32_t j, uint32_t cols) {
+    L8At r;
+    r.start = min(j, cols - 8);
+    r.dup = j - r.start;
+    r.live = j < cols;
+    return r;
+}
+template <class T>
+static __device__ __forceinline__ L8Vec<T> l8_raw(const T* p) { return *(const L8Vec<T>*)p; }
+template <class T>
+static __device__ __forceinline__ void l8_floats(const L8Vec<T>& x, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = l8_f32(x.v[i]);
+}
+
 template <class T>
 static __device__ __forceinline__ void l8_store(T* p, int n, const float (&f)[8]) {
     L8Vec<T> x;
