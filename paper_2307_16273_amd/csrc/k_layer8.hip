@@ -348,6 +348,74 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
     });
 }
 
+// The same with the columns kept in registers between the two looks at them, for up to 2048 rows: 1024 threads have 32 columns, 256 rows
+// at a time.
+constexpr int L8_ONCE_T = 4, L8_ONCE_R = 256, L8_ONCE_ITEMS = 8;
+template <class T, int ITEMS>
+__global__ __launch_bounds__(1024) void k_l8_cols_once(L8ColArgs a, L8Mat<const T> x, L8Mat<int8_t> q, L8Mat<T> values) {
+    __shared__ uint32_t s_top[16][L8_ONCE_T][8];
+    const uint32_t tx = threadIdx.x % L8_ONCE_T, ty = threadIdx.x / L8_ONCE_T;
+    const L8At at = l8_at(blockIdx.x * (L8_ONCE_T * 8) + tx * 8, a.cols);
+    const uint64_t s = blockIdx.z;
+    const T* p = x.p + s * x.ss + at.start;
+    const float* mu = a.mult ? a.mult + s * a.rows : nullptr;
+    L8Vec<T> raw[ITEMS];
+    float w[ITEMS], v[ITEMS][8];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) raw[k] = l8_raw(p + min(ty + (uint64_t)k * L8_ONCE_R, a.rows - 1) * x.rs);
+    if (mu) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) w[k] = mu[min(ty + (uint64_t)k * L8_ONCE_R, a.rows - 1)];
+    }
+    uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        l8_floats(raw[k], v[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (mu) v[k][i] *= w[k];
+            top[i] = max(top[i], l8_mag(v[k][i]));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int d = L8_ONCE_T; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], d, 64));
+    }
+    if ((threadIdx.x & 63) < L8_ONCE_T) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_top[threadIdx.x >> 6][tx][i] = top[i];
+    }
+    __syncthreads();
+    L8Quant c[8];
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) b = max(b, s_top[k][tx][i]);
+        c[i] = l8_quant(b);
+        scale[i] = c[i].finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+    }
+    if (!at.live) return;
+    if (ty == 0) l8_store(a.scale + s * a.cols + at.start, 8, scale);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const uint64_t m = ty + (uint64_t)k * L8_ONCE_R;
+        if (m >= a.rows) break;
+        int iq[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[k][i], c[i]);
+        l8_store_q(q.p + s * q.ss + m * q.rs + at.start, 8, iq);
+        if (values.p) {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = (float)iq[i] * scale[i];
+            l8_store(values.p + s * values.ss + m * values.rs + at.start, 8, f);
+        }
+    }
+}
+
 template <class T>
 static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values) {
     L8ColArgs a;
@@ -375,6 +443,16 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
         a.mult = mult ? mult + s0 * x->rows : nullptr;
         a.scale = scale + s0 * x->cols;
         const dim3 grid((unsigned)tiles, a.chunks, (unsigned)ns);
+        if (x->cols >= 8 && x->rows <= L8_ONCE_R * L8_ONCE_ITEMS) {
+            const dim3 once((unsigned)l8_ceil(x->cols, L8_ONCE_T * 8), 1, (unsigned)ns);
+#define L8_ONCE(ITEMS) hipLaunchKernelGGL((k_l8_cols_once<T, ITEMS>), once, dim3(1024), 0, ctx->stream, a, mx, mq, mv)
+            if (x->rows <= L8_ONCE_R) L8_ONCE(1);
+            else if (x->rows <= 2 * L8_ONCE_R) L8_ONCE(2);
+            else if (x->rows <= 4 * L8_ONCE_R) L8_ONCE(4);
+            else L8_ONCE(8);
+#undef L8_ONCE
+            continue;
+        }
         if (a.chunks == 1) {
             hipLaunchKernelGGL((k_l8_cols<T, 2>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
             continue;
@@ -419,7 +497,7 @@ extern "C" int zkdl_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, cons
     if (values && (!l8_mat_ok(values, true) || values->dtype != x->dtype || !l8_same_shape(x, values))) return ZKDL_EINVAL;
     const uint64_t scales = x->stack * (axis ? x->rows : x->cols);
     if (scales && !scale) return ZKDL_EINVAL;
-    if (axis == 0 && x->cols >= (uint64_t)1 << 30) return ZKDL_ETOOBIG;
+    if (axis == 0 && x->cols >= (uint64_t)1 << 27) return ZKDL_ETOOBIG;     // a launch's threads are counted in 32 bits
     L8Device dev(ctx);
     ZK_HIP(ctx, dev.err);
     if (scales && (axis ? x->cols : x->rows) == 0) {        // scales of nothing
