@@ -127,52 +127,6 @@ static __device__ __forceinline__ v4i m8_fetch(const int8_t* p, uint64_t rs, uin
     return x;
 }
 
-// 64 x 64 entries a block, four waves of 32 x 32; tiles of 64 k go through registers into LDS, so any address and any edge
-// will do.  AT: op(A) runs along m in memory, BN: op(B) along n.
-constexpr int M8_PITCH = 80;     // bytes of a tile's row in LDS: 64 and 16 that keep the rows' banks apart
-template <bool AT, bool BN>
-__global__ __launch_bounds__(256) void k_m8_any(M8Args p) {
-    __shared__ __align__(16) int8_t s_a[64 * M8_PITCH], s_b[64 * M8_PITCH];
-    const uint32_t t = threadIdx.x, l = t & 63, w = t >> 6, g = l >> 4, i16 = l & 15;
-    uint64_t s;
-    uint32_t m0, n0;
-    m8_tile(p, 64, 64, s, m0, n0);
-    const uint32_t wm = (w >> 1) * 32, wn = (w & 1) * 32;
-    const int8_t *a = p.a + s * p.a_ss, *b = p.b + s * p.b_ss;
-    v4i acc[2][2] = {};
-    for (uint32_t k0 = 0; k0 < p.K; k0 += 64) {
-        const uint32_t r = t >> 2, c = (t & 3) * 16;
-        const v4i va = AT ? m8_fetch(a, p.a_rs, k0 + r, p.K, m0 + c, p.M) : m8_fetch(a, p.a_rs, m0 + r, p.M, k0 + c, p.K);
-        const v4i vb = BN ? m8_fetch(b, p.b_rs, k0 + r, p.K, n0 + c, p.N) : m8_fetch(b, p.b_rs, n0 + r, p.N, k0 + c, p.K);
-        __syncthreads();
-        *(v4i*)(s_a + r * M8_PITCH + c) = va;
-        *(v4i*)(s_b + r * M8_PITCH + c) = vb;
-        __syncthreads();
-        v4i fa[2], fb[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            auto frag = [&](bool turned, int8_t* tile, uint32_t at) {
-                if (!turned) return *(const v4i*)(tile + (at + i16) * M8_PITCH + g * 16);
-                v4i f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i*)(tile + (16 * g + 8 * h + (i16 >> 1)) * M8_PITCH + at + (i16 & 1) * 8));
-                    f[2 * h] = y[0];
-                    f[2 * h + 1] = y[1];
-                }
-                return f;
-            };
-            fa[x] = frag(AT, s_a, wm + x * 16);
-            fb[x] = frag(BN, s_b, wn + x * 16);
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
-    }
-    m8_store_tile<2, 2>(p, s, m0 + wm + i16, n0 + wn + g * 4, false, acc);
-}
-
 // ---------------------------------------------------------------------------
 // Tiles whose operands lie at multiples of 16 bytes: the memory system writes them into LDS by itself (16 bytes a lane, in
 // the order of the lanes), a stage of 128 k while the one before it is multiplied.  A lane chooses which 16 bytes it fetches, so
@@ -200,13 +154,14 @@ struct M8Tile {
         r = at / CHUNKS;
         c = ((at % CHUNKS) ^ swizzle(r)) * 16;
     }
-    // rows: how many of the tile's there are; the last ones stand in for those that are not (their sums are not stored)
+    // rows: how many of the tile's there are; the last ones stand in for those that are not (their sums are not stored).  Along memory
+    // they come in whole 16s.
     __device__ __forceinline__ void init(uint32_t t, uint64_t rs, uint32_t rows) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             uint32_t r, c;
             place(i, t, r, c);
-            off[i] = TURN ? (uint32_t)(r * rs) + min(c, rows - 16) : (uint32_t)(min(r, rows - 1) * rs) + c;
+            off[i] = TURN ? (uint32_t)(r * rs) + min(c, ((rows + 15) & ~15u) - 16) : (uint32_t)(min(r, rows - 1) * rs) + c;
         }
     }
     __device__ __forceinline__ void load(const int8_t* p, int8_t* lds, uint32_t w) const {
@@ -318,125 +273,191 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows (a batch of tokens): bound by reading op(B) once.  A block has 16 FM rows and 16 NC columns and its eight waves share out
-// k, 64 at a time; operands go straight into registers (op(B) through a wave's own piece of LDS where it has to be turned), many
-// loads under way at once, and the waves' sums are added at the end.
+// Small products, any address: bound by latency and by reading the operands once.  A block has 16 FM rows and 16 FN columns and its eight
+// waves share out k, 64 at a time; U such steps are under way at once, straight into registers (through a wave's own piece of LDS where an
+// operand has to be turned), and the waves' sums are added at the end.
 // ---------------------------------------------------------------------------
-template <int FM, int NC, int U, bool AT, bool BT>
+
+// A wave's share of one operand: F fragments of 16 rows of op(A) (columns of op(B)) from `at` on.  Loads wait for no branch: what lies
+// behind an edge is read from inside the matrix and shifted out (along k) or never stored (rows).
+template <int F, bool TURN>
+struct M8Few {
+    const int8_t* p;
+    uint64_t rs;
+    uint32_t at, rows, K, l;
+    // whether that holds: at least 16 k, and whole pieces of 16 rows where memory runs along them
+    __device__ __forceinline__ bool plain() const { return TURN ? at + 16 * F <= rows : K >= 16; }
+    __device__ __forceinline__ void load(uint32_t k, v4i (&f)[F]) const {
+#pragma unroll
+        for (int x = 0; x < F; ++x) {
+            const int8_t* q;
+            if (TURN) {
+                const uint32_t piece = x * 64 + l;
+                q = p + min(k + piece / F, K - 1) * rs + at + piece % F * 16;
+            } else {
+                q = p + min(at + x * 16 + (l & 15), rows - 1) * rs + min(k + (l >> 4) * 16, K - 16);
+            }
+            const M8Bytes y = *(const M8Bytes*)q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[x][i] = (int)y.v[i];
+        }
+    }
+    __device__ __forceinline__ void load_guarded(uint32_t k, v4i (&f)[F]) const {
+#pragma unroll
+        for (int x = 0; x < F; ++x) {
+            const uint32_t piece = x * 64 + l;
+            f[x] = TURN ? m8_fetch(p, rs, k + piece / F, K, at + piece % F * 16, rows)
+                        : m8_fetch(p, rs, at + x * 16 + (l & 15), rows, k + (l >> 4) * 16, K);
+        }
+    }
+    // the last, partial step of load(): entries from K on become zeros
+    __device__ __forceinline__ void cut(uint32_t k, v4i (&f)[F]) const {
+#pragma unroll
+        for (int x = 0; x < F; ++x) {
+            if (TURN) {
+                if (k + (x * 64 + l) / F >= K) f[x] = v4i{0, 0, 0, 0};
+            } else {
+                const uint32_t from = k + (l >> 4) * 16, sh = from + 16 > K ? from + 16 - K : 0;     // bytes too many
+                const uint64_t lo = (uint32_t)f[x][0] | (uint64_t)(uint32_t)f[x][1] << 32, hi = (uint32_t)f[x][2] | (uint64_t)(uint32_t)f[x][3] << 32;
+                uint64_t nl = lo, nh = hi;
+                if (sh >= 16) nl = nh = 0;
+                else if (sh >= 8) nl = hi >> (8 * (sh - 8)), nh = 0;
+                else if (sh) nl = lo >> (8 * sh) | hi << (64 - 8 * sh), nh = hi >> (8 * sh);
+                f[x] = v4i{(int)(uint32_t)nl, (int)(uint32_t)(nl >> 32), (int)(uint32_t)nh, (int)(uint32_t)(nh >> 32)};
+            }
+        }
+    }
+    // turned: from pieces of rows of k to fragments, by way of the wave's own LDS, whose operations keep their order
+    static __device__ __forceinline__ void turn(int8_t* mine, uint32_t l, v4i (&f)[F]) {
+        if (!TURN) return;
+        const uint32_t g = l >> 4, i16 = l & 15;
+#pragma unroll
+        for (int x = 0; x < F; ++x) *(v4i*)(mine + (x * 64 + l) * 16) = f[x];
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int x = 0; x < F; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v2i z = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i*)(mine + (16 * g + 8 * h + (i16 >> 1)) * (16 * F) + x * 16 + (i16 & 1) * 8));
+                f[x][2 * h] = z[0];
+                f[x][2 * h + 1] = z[1];
+            }
+        asm volatile("" ::: "memory");
+    }
+};
+
+template <int FM, int FN, int U, bool AT, bool BT>
 __global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
-    constexpr int W = 8, BYTES = 1024 * NC;      // of a wave's tile of 64 k
-    __shared__ __align__(16) int8_t turn[BT ? W * BYTES : 16];
-    __shared__ __align__(16) int sums[W][FM * NC][64][4];
+    constexpr int W = 8, TURN_A = AT ? 1024 * FM : 0, TURN_B = BT ? 1024 * FN : 0, SUMS = FM * FN * 1024;
+    __shared__ __align__(16) int8_t lds[W * (SUMS > TURN_A + TURN_B ? SUMS : TURN_A + TURN_B)];
     const uint32_t t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), g = l >> 4, i16 = l & 15;
     uint64_t s;
     uint32_t m0, n0;
-    m8_tile(p, 16 * FM, 16 * NC, s, m0, n0);
-    const int8_t *a = p.a + s * p.a_ss, *b = p.b + s * p.b_ss;
-    v4i acc[FM][NC] = {};
+    m8_tile(p, 16 * FM, 16 * FN, s, m0, n0);
+    const M8Few<FM, AT> a = {p.a + s * p.a_ss, p.a_rs, m0, p.M, p.K, l};
+    const M8Few<FN, BT> b = {p.b + s * p.b_ss, p.b_rs, n0, p.N, p.K, l};
+    int8_t *turn_a = lds + w * (TURN_A + TURN_B), *turn_b = turn_a + TURN_A;
+    v4i acc[FM][FN] = {};
     const uint32_t steps = (p.K + 63) / 64;
-    int8_t* mine = turn + (BT ? w * BYTES : 0);
-    for (uint32_t k0 = w; k0 < steps; k0 += W * U) {
-        v4i fa[U][FM], fb[U][NC];
+    auto mul = [&](v4i(&fa)[FM], v4i(&fb)[FN]) {
+        M8Few<FM, AT>::turn(turn_a, l, fa);
+        M8Few<FN, BT>::turn(turn_b, l, fb);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t k = (k0 + u * W) * 64;
+        for (int x = 0; x < FM; ++x)
 #pragma unroll
-            for (int y = 0; y < NC; ++y) {
-                if (BT) {       // 64 rows of k, 16 NC columns each: lane's piece
-                    const uint32_t at = y * 64 + l, r = at / NC, c = at % NC * 16;
-                    fb[u][y] = m8_fetch(b, p.b_rs, k + r, p.K, n0 + c, p.N);
-                } else {
-                    fb[u][y] = m8_fetch(b, p.b_rs, n0 + y * 16 + i16, p.N, k + g * 16, p.K);
-                }
+            for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
+    };
+    if (a.plain() && b.plain()) {
+        for (uint32_t k0 = w; k0 < steps; k0 += W * U) {
+            v4i fa[U][FM], fb[U][FN];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // (steps behind the end read the last one again: their k is looked at below)
+                const uint32_t k = min(k0 + u * W, steps - 1) * 64;
+                b.load(k, fb[u]);
+                a.load(k, fa[u]);
             }
 #pragma unroll
-            for (int x = 0; x < FM; ++x) {
-                if (AT) {
-                    const uint32_t i = m0 + x * 16 + i16;
-                    v4i f = {0, 0, 0, 0};
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t kk = k + g * 16 + e;
-                        if (i < p.M && kk < p.K) f[e / 4] |= (int)((uint32_t)(uint8_t)a[kk * p.a_rs + i] << (8 * (e % 4)));
-                    }
-                    fa[u][x] = f;
-                } else {
-                    fa[u][x] = m8_fetch(a, p.a_rs, m0 + x * 16 + i16, p.M, k + g * 16, p.K);
+            for (int u = 0; u < U; ++u) {
+                if (k0 + u * W >= steps) break;
+                const uint32_t k = (k0 + u * W) * 64;
+                if (k + 64 > p.K) {
+                    a.cut(k, fa[u]);
+                    b.cut(k, fb[u]);
                 }
+                mul(fa[u], fb[u]);
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            v4i f[NC];
-            if (BT) {
-                // a wave's own LDS: its operations there keep their order
-#pragma unroll
-                for (int y = 0; y < NC; ++y) *(v4i*)(mine + (y * 64 + l) * 16) = fb[u][y];
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int y = 0; y < NC; ++y)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t r = 16 * g + 8 * h + (i16 >> 1);
-                        const v2i z = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i*)(mine + r * (16 * NC) + y * 16 + (i16 & 1) * 8));
-                        f[y][2 * h] = z[0];
-                        f[y][2 * h + 1] = z[1];
-                    }
-                asm volatile("" ::: "memory");
-            } else {
-#pragma unroll
-                for (int y = 0; y < NC; ++y) f[y] = fb[u][y];
-            }
-#pragma unroll
-            for (int x = 0; x < FM; ++x)
-#pragma unroll
-                for (int y = 0; y < NC; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f[y], fa[u][x], acc[x][y], 0, 0, 0);
+    } else {
+        for (uint32_t k0 = w; k0 < steps; k0 += W) {
+            v4i fa[FM], fb[FN];
+            a.load_guarded(k0 * 64, fa);
+            b.load_guarded(k0 * 64, fb);
+            mul(fa, fb);
         }
     }
+    __syncthreads();
 #pragma unroll
     for (int x = 0; x < FM; ++x)
 #pragma unroll
-        for (int y = 0; y < NC; ++y) *(v4i*)sums[w][x * NC + y][l] = acc[x][y];
+        for (int y = 0; y < FN; ++y) *(v4i*)(lds + ((w * FM * FN + x * FN + y) * 64 + l) * 16) = acc[x][y];
     __syncthreads();
     // fragment f of the sums goes to wave f (mod 8)
 #pragma unroll
-    for (int f0 = 0; f0 < FM * NC; f0 += W) {
+    for (int f0 = 0; f0 < FM * FN; f0 += W) {
         const uint32_t f = f0 + w;
-        if (f < FM * NC) {
+        if (f < FM * FN) {
             v4i v[1][1] = {};
 #pragma unroll
-            for (int q = 0; q < W; ++q) v[0][0] += *(const v4i*)sums[q][f][l];
-            m8_store_tile<1, 1>(p, s, m0 + f / NC * 16 + i16, n0 + f % NC * 16 + g * 4, false, v);
+            for (int q = 0; q < W; ++q) v[0][0] += *(const v4i*)(lds + ((q * FM * FN + f) * 64 + l) * 16);
+            m8_store_tile<1, 1>(p, s, m0 + f / FN * 16 + i16, n0 + f % FN * 16 + g * 4, false, v);
         }
+    }
+}
+
+// Rows of whole 16 bytes at multiples of 16, zeros behind the last column: what k_m8_tile can fetch of any matrix.
+struct M8PackArgs {
+    const int8_t* p;
+    uint64_t rs, ss;
+    uint64_t rows, stack, pitch;
+    uint32_t cols;
+};
+__global__ __launch_bounds__(256) void k_m8_pack(M8PackArgs a, int8_t* out) {
+    const uint64_t pieces = a.pitch / 16, n = a.stack * a.rows * pieces;
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < n; i += gridDim.x * 256ull) {
+        const uint64_t row = i / pieces, c = i % pieces * 16;
+        *(v4i*)(out + i * 16) = m8_fetch(a.p + row / a.rows * a.ss, a.rs, (uint32_t)(row % a.rows), (uint32_t)a.rows, (uint32_t)c, a.cols);
     }
 }
 
 // a launch's blocks are counted in 32 bits of threads
 constexpr uint64_t M8_MAX_TILES = (uint64_t)1 << 23;
+enum M8Choice { M8_FEW1, M8_FEW2, M8_FEW4, M8_TILE64, M8_TILE128, M8_TILE256 };
 
 template <bool AT, bool BT>
-static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, bool whole) {
-    int bm = 64, bn = 64, threads = 256;
-    void (*kernel)(M8Args) = k_m8_any<AT, BT>;
-    auto tiles = [&](uint64_t m, uint64_t n) { return l8_ceil(p.M, m) * l8_ceil(p.N, n) * stack; };
-    if (p.M <= 16) {
-        constexpr int NC = BT ? 2 : 1;
-        kernel = k_m8_few<1, NC, 8, AT, BT>;
-        bm = 16, bn = 16 * NC, threads = 512;
-    } else if (whole) {
-        if (tiles(256, 256) >= 200) {
-            kernel = k_m8_tile<256, 256, 2, 4, 2, AT, BT>;
-            bm = bn = 256, threads = 512;
-        } else if (tiles(128, 128) >= 200) {
-            kernel = k_m8_tile<128, 128, 2, 2, 2, AT, BT>;
-            bm = bn = 128;
-        } else {
-            kernel = k_m8_tile<64, 64, 2, 2, 4, AT, BT>;
-        }
-    }
-    if (l8_ceil(p.M, bm) * l8_ceil(p.N, bn) >= M8_MAX_TILES || stack >= M8_MAX_TILES || tiles(bm, bn) >= M8_MAX_TILES) return ZKDL_ETOOBIG;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles(bm, bn)), dim3(threads), 0, ctx->stream, p);
+static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, int choice) {
+    int bm, bn, threads = 512;
+    void (*kernel)(M8Args);
+    if (choice == M8_FEW1) kernel = k_m8_few<1, BT ? 2 : 1, 8, AT, BT>, bm = 16, bn = BT ? 32 : 16;
+    else if (choice == M8_FEW2) kernel = k_m8_few<2, 2, 4, AT, BT>, bm = bn = 32;
+    else if (choice == M8_FEW4) kernel = k_m8_few<4, 4, 2, AT, BT>, bm = bn = 64;
+    else if (choice == M8_TILE64) kernel = k_m8_tile<64, 64, 2, 2, 4, AT, BT>, bm = bn = 64, threads = 256;
+    else if (choice == M8_TILE128) kernel = k_m8_tile<128, 128, 2, 2, 2, AT, BT>, bm = bn = 128, threads = 256;
+    else kernel = k_m8_tile<256, 256, 2, 4, 2, AT, BT>, bm = bn = 256;
+    const uint64_t tiles = l8_ceil(p.M, bm) * l8_ceil(p.N, bn);
+    if (tiles >= M8_MAX_TILES || stack >= M8_MAX_TILES || tiles * stack >= M8_MAX_TILES) return ZKDL_ETOOBIG;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * stack)), dim3(threads), 0, ctx->stream, p);
     return ZKDL_OK;
+}
+
+// Which kernel.  (to be measured)
+static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole) {
+    auto tiles = [&](uint64_t x) { return l8_ceil(m, x) * l8_ceil(n, x) * stack; };
+    if (m <= 16 || n <= 16) return M8_FEW1;
+    if (!whole && tiles(128) * l8_ceil(k, 128) < 4096) return tiles(32) < 2048 ? M8_FEW2 : M8_FEW4;
+    if (tiles(256) >= 200) return M8_TILE256;
+    if (tiles(128) >= 200) return M8_TILE128;
+    return M8_TILE64;
 }
 
 // a and b behind the checks; out may be empty
@@ -444,12 +465,6 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
                       const zkdl_mat* out) {
     if (out->stack == 0 || out->rows == 0 || out->cols == 0) return ZKDL_OK;
     M8Args p;
-    p.a = (const int8_t*)a->data;
-    p.b = (const int8_t*)b->data;
-    p.a_rs = a->row_stride;
-    p.a_ss = a->stack_stride;
-    p.b_rs = b->row_stride;
-    p.b_ss = b->stack_stride;
     p.out = out->data;
     p.o_rs = out->row_stride;
     p.o_ss = out->stack_stride;
@@ -466,11 +481,43 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
         return (uintptr_t)m->data % 16 == 0 && m->row_stride % 16 == 0 && (m->stack == 1 || m->stack_stride % 16 == 0) && m->cols % 16 == 0 &&
                m->row_stride < (uint64_t)1 << 23;
     };
-    const bool w = p.K > 0 && whole(a) && whole(b);
-    if (trans_a && !trans_b) return m8_launch<true, true>(ctx, p, out->stack, w);
-    if (trans_a) return m8_launch<true, false>(ctx, p, out->stack, w);
-    if (!trans_b) return m8_launch<false, true>(ctx, p, out->stack, w);
-    return m8_launch<false, false>(ctx, p, out->stack, w);
+    const bool wa = whole(a), wb = whole(b);
+    const int choice = p.K ? m8_choose(p.M, p.N, p.K, out->stack, wa && wb) : M8_FEW1;
+    zkdl_mat pa = *a, pb = *b;
+    void* packed[2] = {nullptr, nullptr};
+    if (choice >= M8_TILE64) {
+        zkdl_mat* todo[2] = {wa ? nullptr : &pa, wb ? nullptr : &pb};
+        for (int i = 0; i < 2; ++i) {
+            zkdl_mat* m = todo[i];
+            if (!m) continue;
+            const uint64_t pitch = l8_ceil(m->cols, 16) * 16, bytes = m->stack * m->rows * pitch;
+            packed[i] = pitch < (uint64_t)1 << 23 ? zk_alloc(ctx, bytes) : nullptr;
+            if (!packed[i]) {
+                zk_free(ctx, packed[0]);
+                return pitch < (uint64_t)1 << 23 ? ZKDL_ENOMEM : ZKDL_ETOOBIG;
+            }
+            const M8PackArgs args = {(const int8_t*)m->data, m->row_stride, m->stack_stride, m->rows, m->stack, pitch, (uint32_t)m->cols};
+            const uint64_t blocks = l8_ceil(bytes / 16, 256);
+            hipLaunchKernelGGL(k_m8_pack, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, args, (int8_t*)packed[i]);
+            m->data = packed[i];
+            m->row_stride = pitch;
+            m->stack_stride = m->rows * pitch;
+        }
+    }
+    p.a = (const int8_t*)pa.data;
+    p.b = (const int8_t*)pb.data;
+    p.a_rs = pa.row_stride;
+    p.a_ss = pa.stack_stride;
+    p.b_rs = pb.row_stride;
+    p.b_ss = pb.stack_stride;
+    int rc;
+    if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, out->stack, choice);
+    else if (trans_a) rc = m8_launch<true, false>(ctx, p, out->stack, choice);
+    else if (!trans_b) rc = m8_launch<false, true>(ctx, p, out->stack, choice);
+    else rc = m8_launch<false, false>(ctx, p, out->stack, choice);
+    zk_free(ctx, packed[0]);
+    zk_free(ctx, packed[1]);
+    return rc;
 }
 
 // sums of this many products of magnitude 2^14 stay within 31 bits
