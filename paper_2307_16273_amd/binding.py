@@ -1,7 +1,6 @@
 """ctypes binding of libzkdl.so; argument marshalling only."""
 import ctypes as C
 import os
-import struct
 
 import numpy as np
 
@@ -161,8 +160,8 @@ class Context:
         self.handle = C.c_void_p()
         self.device = device
         self.stream = int(stream)
-        self._layers8 = None
         _check(lib.zkdl_ctx_create(C.byref(self.handle), device, C.c_void_p(stream)), "zkdl_ctx_create")
+        self.address = self.handle.value
 
     def profile(self, on=True, reset=True):
         """Per-kernel-class HIP-event timing on this context's stream."""
@@ -213,6 +212,7 @@ class Context:
         if self.handle:
             load_library().zkdl_ctx_destroy(self.handle)
             self.handle = C.c_void_p()
+            self.address = 0
 
     def __del__(self):
         try:
@@ -681,201 +681,90 @@ def aggregate_verify(ctx, proof, tr):
 # ---- 8-bit layers ----------------------------------------------------------------------------------------------------
 # Operators on CUDA tensors of the context's device: two-dimensional, or three-dimensional stacks where said.  They enqueue
 # their kernels on the context's stream and return without waiting.  Where the current stream is another one, each of the
-# two waits for the other, so that inputs and outputs are the current stream's as with any torch operator.
-#
-# A call on a single token is over in a few microseconds on the GPU, and as many go into each tensor that Python makes or
-# looks at: descriptors are packed into memory that the context keeps, and tensors are looked at once.
+# two waits for the other, so that inputs and outputs are the current stream's as with any torch operator.  Tensors are
+# looked at and made in compiled code (csrc/layers8_torch.cpp): for a single token, Python would take longer than the GPU.
 
-_MAT = struct.Struct("=QQQQQQii")
-_MATS = 5                          # descriptors of one call at most
-assert _MAT.size == C.sizeof(Mat)
+_L8 = None
 
 
-class _Layers8:
-    """What the operators of one context keep: torch, the descriptors' memory and addresses, the entry points."""
-
-    def __init__(self, ctx):
-        import torch
+def _layers8():
+    global _L8
+    if _L8 is None:
+        import importlib.machinery
+        import importlib.util
+        import torch  # noqa: F401  (its libraries come first)
+        path = os.path.join(_HERE, "_layers8.so")
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is missing: run `python paper_2307_16273_amd/build.py`")
+        loader = importlib.machinery.ExtensionFileLoader("_layers8", path)
+        mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_layers8", loader))
+        loader.exec_module(mod)
         lib = load_library()
-        self.torch, self.empty = torch, torch.empty
-        self.dtypes = {torch.float32: ZKDL_F32, torch.float16: ZKDL_F16, torch.bfloat16: ZKDL_BF16, torch.int8: ZKDL_I8,
-                       torch.int32: ZKDL_I32}
-        self.device = torch.device("cuda", ctx.device)
-        self.buf = C.create_string_buffer(_MAT.size * _MATS)
-        base = C.addressof(self.buf)
-        self.addr = [base + _MAT.size * k for k in range(_MATS)]
-        self.raw_stream = torch._C._cuda_getCurrentRawStream
-        self.quantize, self.rmsnorm, self.rmsnorm_backward = lib.zkdl_quantize_i8, lib.zkdl_rmsnorm_i8, lib.zkdl_rmsnorm_i8_backward
-        self.matmul, self.matmul_backward = lib.zkdl_matmul_i8, lib.zkdl_matmul_i8_backward
-
-    def put(self, ctx, slot, t, what, either=False):
-        """Describes an input at `slot`: a stack of matrices whose rows or (`either`) columns are adjacent in memory.
-        Returns whether the matrices are described transposed."""
-        sh, code = t.shape, self.dtypes.get(t.dtype)
-        if code is None or not 2 <= len(sh) <= 3 or t.get_device() != ctx.device:
-            raise ValueError(f"{what}: a matrix or a stack of matrices on device {ctx.device} of a type the operator knows is "
-                             f"needed, not {tuple(sh)} {t.dtype} on {t.device}")
-        st = t.stride()
-        stack, ss = (sh[0], st[0]) if len(sh) == 3 else (1, 0)
-        if st[-1] == 1 or sh[-1] <= 1:
-            _MAT.pack_into(self.buf, _MAT.size * slot, t.data_ptr(), stack, sh[-2], sh[-1], st[-2], ss, code, 0)
-            return False
-        if either and (st[-2] == 1 or sh[-2] <= 1):
-            _MAT.pack_into(self.buf, _MAT.size * slot, t.data_ptr(), stack, sh[-1], sh[-2], st[-1], ss, code, 0)
-            return True
-        raise ValueError(f"{what}: the entries of a row have to be adjacent in memory (strides {tuple(st)})")
-
-    def new(self, slot, shape, dtype, pitch=None):
-        """A new tensor of this shape, described at `slot`; pitch: entries from row to row."""
-        cols = shape[-1]
-        t = self.empty(shape if pitch is None or pitch == cols else shape[:-1] + (pitch,), dtype=dtype, device=self.device)
-        rs = cols if pitch is None else pitch
-        rows = shape[-2]
-        _MAT.pack_into(self.buf, _MAT.size * slot, t.data_ptr(), shape[0] if len(shape) == 3 else 1, rows, cols, rs, rows * rs,
-                       self.dtypes[dtype], 0)
-        return t if rs == cols else t[..., :cols]
-
-    def vec(self, ctx, t, shape, what, dtype=None):
-        """Address of a contiguous tensor of 32-bit floats, or of `dtype`."""
-        if t is None:
-            return None
-        if t.shape != shape or (t.dtype is not self.torch.float32 and t.dtype is not dtype) or t.get_device() != ctx.device \
-                or not t.is_contiguous():
-            raise ValueError(f"{what}: a contiguous float32 tensor of shape {tuple(shape)} on device {ctx.device} is needed, not "
-                             f"{tuple(t.shape)} {t.dtype} on {t.device}")
-        return t.data_ptr()
-
-    def call(self, ctx, name, fn, *args):
-        """One entry point, in order with the current stream."""
-        if self.raw_stream(ctx.device) == ctx.stream:
-            rc = fn(ctx.handle, *args)
-        else:
-            cuda = self.torch.cuda
-            now = cuda.current_stream(ctx.device)
-            other = cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else cuda.default_stream(ctx.device)
-            other.wait_stream(now)
-            rc = fn(ctx.handle, *args)
-            now.wait_stream(other)
-        if rc:
-            _check(rc, name, ctx)
+        mod.bind(*(C.cast(fn, C.c_void_p).value for fn in (lib.zkdl_quantize_i8, lib.zkdl_rmsnorm_i8, lib.zkdl_rmsnorm_i8_backward,
+                                                           lib.zkdl_matmul_i8, lib.zkdl_matmul_i8_backward)))
+        _L8 = mod
+    return _L8
 
 
-def _layers8(ctx):
-    k = ctx._layers8
-    if k is None:
-        k = ctx._layers8 = _Layers8(ctx)
-    return k
-
-
-def _pitch(n):
-    """Entries from row to row of new 8-bit matrices: rows start at multiples of 16 bytes, as the products like them."""
-    return (n + 15) & -16
+def _rest(ctx, fn, got, args):
+    """What a call that is not simply done needs: its error raised, or the two streams ordered and the call made."""
+    if got is None:
+        from torch import cuda
+        now = cuda.current_stream(ctx.device)
+        other = cuda.ExternalStream(ctx.stream, device=ctx.device) if ctx.stream else cuda.default_stream(ctx.device)
+        other.wait_stream(now)
+        got = fn(ctx.address, ctx.device, ctx.stream, True, *args)
+        now.wait_stream(other)
+    if type(got) is int:
+        _check(got, "zkdl_" + fn.__name__, ctx)
+    return got
 
 
 def quantize_i8(ctx, x, axis=-1, mult=None, values=False):
     """x [.., M, N] (float32, float16, bfloat16) -> dict(q, scale, values): 8-bit integers q with x mult ~ q scale.
     axis: the axis that shares a scale: -1 a scale for each row, -2 a scale for each column.  mult: None or float32
     factors along that axis.  values: also q scale in the type of x.  (zkdl_quantize_i8)"""
-    k = _layers8(ctx)
-    k.put(ctx, 0, x, "x")
-    if axis != -1 and axis != -2:
-        raise ValueError("axis: -1 (a scale for each row) or -2 (a scale for each column)")
-    sh = tuple(x.shape)
-    n = sh[-1]
-    along, across = (n, sh[-2]) if axis == -1 else (sh[-2], n)
-    pm = k.vec(ctx, mult, sh[:-2] + (along,), "mult")
-    q = k.new(1, sh, k.torch.int8, _pitch(n))
-    scale = k.empty(sh[:-2] + (across,), dtype=k.torch.float32, device=k.device)
-    v = k.new(2, sh, x.dtype) if values else None
-    at = k.addr
-    k.call(ctx, "zkdl_quantize_i8", k.quantize, at[0], 1 if axis == -1 else 0, pm, at[1], scale.data_ptr(), at[2] if values else None)
-    return dict(q=q, scale=scale, values=v)
+    fn = (_L8 or _layers8()).quantize_i8
+    args = (x, axis, mult, bool(values))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
 
 
 def rmsnorm_i8(ctx, x, weight, residual=None, eps=1e-6, values=False):
     """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight, in 8 bits with a scale for each row.  x [M, N]; weight [N]
     in the type of x or float32.  Returns dict(q, scale, rstd, total, values): total = h in the type of x (None without a
     residual: x itself), values = q scale if asked for.  (zkdl_rmsnorm_i8)"""
-    k = _layers8(ctx)
-    sh, t = tuple(x.shape), x.dtype
-    if len(sh) != 2:
-        raise ValueError(f"x: one matrix is needed, not {sh}")
-    k.put(ctx, 0, x, "x")
-    if residual is not None:
-        k.put(ctx, 1, residual, "residual")
-    m, n = sh
-    pw = k.vec(ctx, weight, (n,), "weight", t)
-    f32 = k.torch.float32
-    q = k.new(2, sh, k.torch.int8, _pitch(n))
-    scale, rstd = k.empty(m, dtype=f32, device=k.device), k.empty(m, dtype=f32, device=k.device)
-    total = k.new(3, sh, t) if residual is not None else None
-    v = k.new(4, sh, t) if values else None
-    at = k.addr
-    k.call(ctx, "zkdl_rmsnorm_i8", k.rmsnorm, at[0], at[1] if residual is not None else None, pw, k.dtypes[weight.dtype], eps, at[2],
-           scale.data_ptr(), rstd.data_ptr(), at[3] if residual is not None else None, at[4] if values else None)
-    return dict(q=q, scale=scale, rstd=rstd, total=total, values=v)
+    fn = (_L8 or _layers8()).rmsnorm_i8
+    args = (x, weight, residual, eps, bool(values))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
 
 
 def rmsnorm_i8_backward(ctx, dy, h, weight, rstd, dtotal=None):
     """Gradients of rmsnorm_i8: dy [M, N] of the normalised output, h the summed stream (total, or x without a residual),
     rstd as returned, dtotal of the summed stream's other uses.  Returns dict(dx, dweight): dx belongs to x and to the
     residual, dweight is float32.  (zkdl_rmsnorm_i8_backward)"""
-    k = _layers8(ctx)
-    sh, t = tuple(dy.shape), dy.dtype
-    if len(sh) != 2:
-        raise ValueError(f"dy: one matrix is needed, not {sh}")
-    k.put(ctx, 0, dy, "dy")
-    k.put(ctx, 1, h, "h")
-    if dtotal is not None:
-        k.put(ctx, 2, dtotal, "dtotal")
-    pw, ps = k.vec(ctx, weight, (sh[1],), "weight", t), k.vec(ctx, rstd, (sh[0],), "rstd")
-    dx = k.new(3, sh, t)
-    dw = k.empty(sh[1], dtype=k.torch.float32, device=k.device)
-    at = k.addr
-    k.call(ctx, "zkdl_rmsnorm_i8_backward", k.rmsnorm_backward, at[0], at[1], pw, k.dtypes[weight.dtype], ps,
-           at[2] if dtotal is not None else None, at[3], dw.data_ptr())
-    return dict(dx=dx, dweight=dw)
+    fn = (_L8 or _layers8()).rmsnorm_i8_backward
+    args = (dy, h, weight, rstd, dtotal)
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
 
 
 def matmul_i8(ctx, a, b, a_scale=None, b_scale=None, trans_a=False, trans_b=False, dtype=None):
     """op(a) op(b) of int8 matrices [.., M, K], [.., K, N] (stored transposed where trans_a / trans_b says so; transposed
     views do as well).  dtype int32 (the default without scales): the exact accumulators; float32, float16 or bfloat16 (the
     default with scales): acc a_scale[.., i] b_scale[.., j].  (zkdl_matmul_i8)"""
-    k = _layers8(ctx)
-    ta = k.put(ctx, 0, a, "a", True)
-    tb = k.put(ctx, 1, b, "b", True)
-    sa, sb = tuple(a.shape), tuple(b.shape)
-    if len(sa) != len(sb):
-        raise ValueError("a and b: two matrices or two stacks")
-    lead, m, n = sa[:-2], sa[-1 if trans_a else -2], sb[-2 if trans_b else -1]
-    if dtype is None:
-        dtype = k.torch.int32 if a_scale is None and b_scale is None else k.torch.bfloat16
-    if dtype not in k.dtypes:
-        raise ValueError(f"dtype: int32, float32, float16 or bfloat16, not {dtype}")
-    pa, pb = k.vec(ctx, a_scale, lead + (m,), "a_scale"), k.vec(ctx, b_scale, lead + (n,), "b_scale")
-    out = k.new(2, lead + (m, n), dtype)
-    at = k.addr
-    k.call(ctx, "zkdl_matmul_i8", k.matmul, at[0], at[1], int(bool(trans_a) != ta), int(bool(trans_b) != tb), pa, pb, at[2])
-    return out
+    fn = (_L8 or _layers8()).matmul_i8
+    args = (a, b, a_scale, b_scale, bool(trans_a), bool(trans_b), dtype)
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return _rest(ctx, fn, got, args) if got is None or type(got) is int else got
 
 
 def matmul_i8_backward(ctx, dy, a, a_scale, w, w_scale, trans_w=False, need_da=True, need_dw=True):
     """Gradients of (a a_scale) (w w_scale), a [.., M, K], w [.., K, N] (trans_w: [.., N, K]), from dy [.., M, N] by two 8-bit
     products on the forward's integers.  Returns dict(da, dw): da in the type of dy, dw float32 in the layout of w.
     (zkdl_matmul_i8_backward)"""
-    k = _layers8(ctx)
-    k.put(ctx, 0, dy, "dy")
-    k.put(ctx, 1, a, "a")
-    k.put(ctx, 2, w, "w")
-    sd, sa, sw = tuple(dy.shape), tuple(a.shape), tuple(w.shape)
-    if not len(sd) == len(sa) == len(sw):
-        raise ValueError("dy, a and w: three matrices or three stacks")
-    if a_scale is None or w_scale is None:
-        raise ValueError("a_scale and w_scale are needed")
-    pa, pw = k.vec(ctx, a_scale, sd[:-2] + (sd[-2],), "a_scale"), k.vec(ctx, w_scale, sd[:-2] + (sd[-1],), "w_scale")
-    da = k.new(3, sa, dy.dtype) if need_da else None
-    dw = k.new(4, sw, k.torch.float32) if need_dw else None
-    at = k.addr
-    k.call(ctx, "zkdl_matmul_i8_backward", k.matmul_backward, at[0], at[1], at[2], int(bool(trans_w)), pa, pw,
-           at[3] if need_da else None, at[4] if need_dw else None)
-    return dict(da=da, dw=dw)
+    fn = (_L8 or _layers8()).matmul_i8_backward
+    args = (dy, a, a_scale, w, w_scale, bool(trans_w), bool(need_da), bool(need_dw))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)

@@ -1,4 +1,4 @@
-"""Builds libzkdl.so (the C-ABI HIP library) for gfx950 with hipcc, in-tree."""
+"""Builds libzkdl.so (the C-ABI HIP library) for gfx950 with hipcc, and _layers8.so (Python's side of its 8-bit layers), in-tree."""
 import os
 import subprocess
 import sys
@@ -20,10 +20,30 @@ def _compile(src):
     return src, obj, r
 
 
+MODULE = os.path.join(HERE, "_layers8.so")      # Python's side of the 8-bit layers, against the installed torch
+
+
+def _module():
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    inc = [f"-I{d}" for d in cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/opt/rocm/include"]]
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, os.path.join(CSRC, "layers8_torch.cpp"),
+           "-o", MODULE, f"-L{lib}", f"-Wl,-rpath,{lib}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+    return subprocess.run(cmd, capture_output=True, text=True)
+
+
 def build(verbose=True):
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as ex:
+        module = ex.submit(_module)
         results = list(ex.map(_compile, SOURCES))
+        r = module.result()
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed on layers8_torch.cpp")
     objs = []
     for src, obj, r in results:
         if r.returncode != 0:

@@ -16,7 +16,6 @@ struct M8Args {
     void* out;
     uint64_t o_rs, o_ss;               // items
     int o_type;                        // zkdl_dtype
-    int o_vec;                         // four adjacent items may be stored at once
     const float *sa, *sb;
     uint32_t M, N, K;
 };
@@ -35,19 +34,21 @@ static __device__ __forceinline__ void m8_tile(const M8Args& p, uint32_t bm, uin
 }
 
 template <class T>
-struct alignas(4 * sizeof(T)) M8Four {
+struct __attribute__((packed, aligned(1))) M8Four {      // at any address
     T v[4];
 };
 // Four adjacent columns of a row: the accumulators, or (acc sa) sb, each product rounded to 32 bits and once more to out's type.
 template <class T>
-static __device__ __forceinline__ void m8_store4(T* o, int n, bool vec, const v4i& acc, float sa, const float (&sb)[4]) {
+static __device__ __forceinline__ void m8_store4(T* o, int n, const v4i& acc, float sa, const float (&sb)[4]) {
     M8Four<T> x;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if constexpr (__is_same(T, int)) x.v[e] = acc[e];
-        else l8_put((float)acc[e] * sa * sb[e], x.v[e]);
+        T y;
+        if constexpr (__is_same(T, int)) y = acc[e];
+        else l8_put((float)acc[e] * sa * sb[e], y);
+        x.v[e] = y;
     }
-    if (vec && n >= 4) {
+    if (n >= 4) {
         *(M8Four<T>*)o = x;
     } else {
 #pragma unroll
@@ -56,7 +57,7 @@ static __device__ __forceinline__ void m8_store4(T* o, int n, bool vec, const v4
     }
 }
 // A wave's fragments, 16 rows and 16 columns apart; the lane's first row and column are (i, j): the products come out turned, so that a
-// lane has four adjacent columns of one row.  inside: no fragment crosses an edge and items may be stored by fours.  All scales are read
+// lane has four adjacent columns of one row.  inside: no fragment crosses an edge.  All scales are read
 // before the first store: a load behind stores waits for them.
 template <class T, int FM, int FN>
 static __device__ __forceinline__ void m8_store_as(const M8Args& p, uint64_t s, uint32_t i, uint32_t j, bool inside, const v4i (&acc)[FM][FN]) {
@@ -86,14 +87,14 @@ static __device__ __forceinline__ void m8_store_as(const M8Args& p, uint64_t s, 
 #pragma unroll
         for (int x = 0; x < FM; ++x)
 #pragma unroll
-            for (int y = 0; y < FN; ++y) m8_store4(o + x * 16 * p.o_rs + y * 16, 4, true, acc[x][y], sa[x], sb[y]);
+            for (int y = 0; y < FN; ++y) m8_store4(o + x * 16 * p.o_rs + y * 16, 4, acc[x][y], sa[x], sb[y]);
     } else {
 #pragma unroll
         for (int x = 0; x < FM; ++x)
 #pragma unroll
             for (int y = 0; y < FN; ++y)
                 if (i + x * 16 < p.M && j + y * 16 < p.N)
-                    m8_store4(o + x * 16 * p.o_rs + y * 16, (int)min(p.N - j - y * 16, 4u), p.o_vec != 0, acc[x][y], sa[x], sb[y]);
+                    m8_store4(o + x * 16 * p.o_rs + y * 16, (int)min(p.N - j - y * 16, 4u), acc[x][y], sa[x], sb[y]);
     }
 }
 template <int FM, int FN>
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
     using OA = M8Tile<BM, AT, T>;
     using OB = M8Tile<BN, BT, T>;
     constexpr int STAGE = OA::BYTES + OB::BYTES, LOADS = OA::LOADS + OB::LOADS;
+    constexpr bool BIG = FM * FN > 16;
     __shared__ __align__(16) int8_t lds[STAGES * STAGE];
     const uint32_t t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), g = l >> 4, i16 = l & 15;
     uint64_t s;
@@ -213,14 +215,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
     OB ob;
     oa.init(t, p.a_rs, min(p.M - m0, (uint32_t)BM));
     ob.init(t, p.b_rs, min(p.N - n0, (uint32_t)BN));
-    const int8_t* pa = p.a + s * p.a_ss + (AT ? (uint64_t)m0 : m0 * p.a_rs);
-    const int8_t* pb = p.b + s * p.b_ss + (BT ? (uint64_t)n0 : n0 * p.b_rs);
     const uint64_t step_a = AT ? 128 * p.a_rs : 128, step_b = BT ? 128 * p.b_rs : 128;
     const uint32_t stages = (p.K + 127) / 128;
+    const int8_t* pa = p.a + s * p.a_ss + (AT ? (uint64_t)m0 : m0 * p.a_rs);
+    const int8_t* pb = p.b + s * p.b_ss + (BT ? (uint64_t)n0 : n0 * p.b_rs);
     uint32_t ahead = 0, in = 0, out = 0;
     auto load = [&]() {
         if (ahead < stages) {
-            int8_t* q = lds + in * STAGE;
+            int8_t* q = lds + in;
             const uint32_t left = p.K - ahead * 128;
             if (left >= 128) {
                 oa.load(pa, q, w);
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
             }
             pa += step_a;
             pb += step_b;
-            in = in == STAGES - 1 ? 0 : in + 1;
+            in = in == (STAGES - 1) * STAGE ? 0 : in + STAGE;
         }
         ++ahead;
     };
@@ -250,26 +252,35 @@ __global__ __launch_bounds__(WM * WN * 64) void k_m8_tile(M8Args p) {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        load();
-        const int8_t* la = lds + out * STAGE;
+        const int8_t* la = lds + out;
         const int8_t* lb = la + OA::BYTES;
-        out = out == STAGES - 1 ? 0 : out + 1;
+        out = out == (STAGES - 1) * STAGE ? 0 : out + STAGE;
+        v4i fa[2][FM], fb[2][FN];
+        auto frags = [&](int q) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            v4i fa[FM], fb[FN];
+            for (int y = 0; y < FN; ++y) fb[q][y] = OB::frag(lb, wn + y * 16, q, g, i16);
 #pragma unroll
-            for (int y = 0; y < FN; ++y) fb[y] = OB::frag(lb, wn + y * 16, kk, g, i16);
-#pragma unroll
-            for (int x = 0; x < FM; ++x) fa[x] = OA::frag(la, wm + x * 16, kk, g, i16);
-            __builtin_amdgcn_s_setprio(1);      // the wave whose operands are there goes first: the others read meanwhile
+            for (int x = 0; x < FM; ++x) fa[q][x] = OA::frag(la, wm + x * 16, q, g, i16);
+        };
+        auto mul = [&](int q) {
+            if (BIG) __builtin_amdgcn_s_setprio(1);      // the wave whose operands are there goes first: the others read meanwhile
 #pragma unroll
             for (int x = 0; x < FM; ++x)
 #pragma unroll
-                for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
-            __builtin_amdgcn_s_setprio(0);
-        }
+                for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[q][y], fa[q][x], acc[x][y], 0, 0, 0);
+            if (BIG) __builtin_amdgcn_s_setprio(0);
+        };
+        // Fragments come before the next stage's loads, whose addresses are worked out while they are on their way; both halves of a
+        // stage's where they fit the registers beside the sums.  8192 x 4096 x 4096, us, loads first / like this: op(A) op(B) along k
+        // 122 / 115, op(B) across 137 / 111, both across 140 / 114; 128 x 128 tiles 135 / 123, 158 / 127, 160 / 131.
+        frags(0);
+        if (!BIG) frags(1);
+        load();
+        mul(0);
+        if (BIG) frags(1);
+        mul(1);
     }
-    m8_store_tile<FM, FN>(p, s, m0 + wm + i16, n0 + wn + g * 4, p.o_vec && m0 + BM <= p.M && n0 + BN <= p.N, acc);
+    m8_store_tile<FM, FN>(p, s, m0 + wm + i16, n0 + wn + g * 4, m0 + BM <= p.M && n0 + BN <= p.N, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -432,37 +443,49 @@ __global__ __launch_bounds__(256) void k_m8_pack(M8PackArgs a, int8_t* out) {
 
 // a launch's blocks are counted in 32 bits of threads
 constexpr uint64_t M8_MAX_TILES = (uint64_t)1 << 23;
-enum M8Choice { M8_FEW1, M8_FEW2, M8_FEW4, M8_TILE64, M8_TILE128, M8_TILE256 };
+enum M8Choice { M8_FEW1, M8_FEW2, M8_TILE64, M8_TILE128, M8_TILE256 };
 
 template <bool AT, bool BT>
 static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, int choice) {
-    int bm, bn, threads = 512;
-    void (*kernel)(M8Args);
-    if (choice == M8_FEW1) kernel = k_m8_few<1, BT ? 2 : 1, 8, AT, BT>, bm = 16, bn = BT ? 32 : 16;
-    else if (choice == M8_FEW2) kernel = k_m8_few<2, 2, 4, AT, BT>, bm = bn = 32;
-    else if (choice == M8_FEW4) kernel = k_m8_few<4, 4, 2, AT, BT>, bm = bn = 64;
-    else if (choice == M8_TILE64) kernel = k_m8_tile<64, 64, 2, 2, 4, AT, BT>, bm = bn = 64, threads = 256;
-    else if (choice == M8_TILE128) kernel = k_m8_tile<128, 128, 2, 2, 2, AT, BT>, bm = bn = 128, threads = 256;
-    else kernel = k_m8_tile<256, 256, 2, 4, 2, AT, BT>, bm = bn = 256;
+    int bm = 0, bn = 0, threads = 0;
+    void (*kernel)(M8Args) = nullptr;
+    auto few = [&](void (*k)(M8Args), int fm, int fn) { kernel = k, bm = 16 * fm, bn = 16 * fn, threads = 512; };
+    auto tile = [&](void (*k)(M8Args), int m, int n, int t) { kernel = k, bm = m, bn = n, threads = t; };
+    switch (choice) {
+        case M8_FEW1: few(k_m8_few<1, BT ? 2 : 1, 8, AT, BT>, 1, BT ? 2 : 1); break;
+        case M8_FEW2: few(k_m8_few<2, 2, 4, AT, BT>, 2, 2); break;
+        case M8_TILE64: tile(k_m8_tile<64, 64, 2, 2, 4, AT, BT>, 64, 64, 256); break;
+        case M8_TILE128: tile(k_m8_tile<128, 128, 2, 2, 2, AT, BT>, 128, 128, 256); break;
+        default: tile(k_m8_tile<256, 256, 2, 4, 2, AT, BT>, 256, 256, 512);
+    }
     const uint64_t tiles = l8_ceil(p.M, bm) * l8_ceil(p.N, bn);
     if (tiles >= M8_MAX_TILES || stack >= M8_MAX_TILES || tiles * stack >= M8_MAX_TILES) return ZKDL_ETOOBIG;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * stack)), dim3(threads), 0, ctx->stream, p);
     return ZKDL_OK;
 }
 
-// Which kernel.  (to be measured)
-static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole) {
+// Which kernel.  whole: both operands can be fetched by k_m8_tile as they are; across: one of them does not run along k.  Times in us on
+// the way back to back, launch included (a launch alone 4):
+//  - up to 16 rows or columns, blocks of 16 (FEW1 / FEW2 / TILE64): 1 x 4096 x 4096 along k 5.7 / 7.5 / 10.8, across 9.2 / 9.2 / 16.5;
+//  - up to 64 with an operand across and a long k, blocks of 32 (FEW2 / TILE64): 64 x 4096 x 4096 11.5 / 17.2, both along k 10.6 / 10.9;
+//    not with more tiles (8 products of 64 x 1024 x 1024 9.9 / 5.4);
+//  - operands that have to be packed first, FEW2 / TILE64 with the packing: 64 x 4001 x 4001 23 / 27, 260 x 515 x 515 13 / 11 (along k),
+//    10 / 12 (one across), 130 x 1001 x 1001 10 / 13, 260 x 1001 x 1001 17 / 13;
+//  - tiles of 64, 128, 256 (4096 x 4096 weights, along k): 256 rows 11 / 27 / 52, 512 16 / 28 / 53, 1024 30 / 30 / 55, 2048 58 / 36 / 57,
+//    4096 114 / 66 / 61, 8192 208 / 128 / 114.  That is by how many fit the 256 compute units at once, two of the smaller ones each:
+static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole, bool across) {
+    const uint64_t few = m < n ? m : n;
+    if (few <= 16) return M8_FEW1;
     auto tiles = [&](uint64_t x) { return l8_ceil(m, x) * l8_ceil(n, x) * stack; };
-    if (m <= 16 || n <= 16) return M8_FEW1;
-    if (!whole && tiles(128) * l8_ceil(k, 128) < 4096) return tiles(32) < 2048 ? M8_FEW2 : M8_FEW4;
-    if (tiles(256) >= 200) return M8_TILE256;
-    if (tiles(128) >= 200) return M8_TILE128;
-    return M8_TILE64;
+    const uint64_t t64 = tiles(64), t128 = tiles(128), t256 = tiles(256), work = m * n * k * stack;
+    if (whole ? few <= 64 && across && k >= 2048 && t64 <= 64 : work <= (uint64_t)1 << (few <= 64 ? 30 : 27)) return M8_FEW2;
+    const uint64_t c64 = t64 <= 256 ? 11 : 15 * l8_ceil(t64, 512), c128 = t128 <= 256 ? 28 : 34 * l8_ceil(t128, 512), c256 = 54 * l8_ceil(t256, 256);
+    return c64 <= c128 && c64 <= c256 ? M8_TILE64 : c128 <= c256 ? M8_TILE128 : M8_TILE256;
 }
 
-// a and b behind the checks; out may be empty
+// a and b behind the checks; out may be empty.  padded 1, 2: a, b is the context's own memory, whose rows go on to a multiple of 16.
 static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int trans_a, int trans_b, const float* sa, const float* sb,
-                      const zkdl_mat* out) {
+                      const zkdl_mat* out, int padded) {
     if (out->stack == 0 || out->rows == 0 || out->cols == 0) return ZKDL_OK;
     M8Args p;
     p.out = out->data;
@@ -474,15 +497,14 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
     p.M = (uint32_t)out->rows;
     p.N = (uint32_t)out->cols;
     p.K = (uint32_t)(trans_a ? a->rows : a->cols);
-    const uint64_t item = out->dtype == ZKDL_I32 || out->dtype == ZKDL_F32 ? 4 : 2;
-    p.o_vec = p.o_rs % 4 == 0 && (out->stack == 1 || p.o_ss % 4 == 0) && (uintptr_t)p.out % (4 * item) == 0;
-    // operands that k_m8_tile can fetch: whole 16 bytes along memory, and rows of a tile within 32 bits
-    auto whole = [&](const zkdl_mat* m) {
-        return (uintptr_t)m->data % 16 == 0 && m->row_stride % 16 == 0 && (m->stack == 1 || m->stack_stride % 16 == 0) && m->cols % 16 == 0 &&
-               m->row_stride < (uint64_t)1 << 23;
+    // Operands that k_m8_tile can fetch: whole 16 bytes along memory, rows of a tile within 32 bits.  Along k one of the two has to end in
+    // zeros or at a multiple of 16: a packed or a turned one does.
+    auto whole = [&](const zkdl_mat* m, bool padded) {
+        return (uintptr_t)m->data % 16 == 0 && m->row_stride % 16 == 0 && (m->stack == 1 || m->stack_stride % 16 == 0) &&
+               (padded || m->cols % 16 == 0) && m->row_stride < (uint64_t)1 << 23;
     };
-    const bool wa = whole(a), wb = whole(b);
-    const int choice = p.K ? m8_choose(p.M, p.N, p.K, out->stack, wa && wb) : M8_FEW1;
+    const bool wa = whole(a, padded == 1), wb = whole(b, padded == 2);
+    const int choice = p.K ? m8_choose(p.M, p.N, p.K, out->stack, wa && wb, trans_a || !trans_b) : M8_FEW1;
     zkdl_mat pa = *a, pb = *b;
     void* packed[2] = {nullptr, nullptr};
     if (choice >= M8_TILE64) {
@@ -535,7 +557,7 @@ extern "C" int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* 
     if (k > M8_MAX_K) return ZKDL_ETOOBIG;
     L8Device dev(ctx);
     ZK_HIP(ctx, dev.err);
-    const int rc = m8_product(ctx, a, b, trans_a, trans_b, a_scale, b_scale, out);
+    const int rc = m8_product(ctx, a, b, trans_a, trans_b, a_scale, b_scale, out, 0);
     if (rc != ZKDL_OK) return rc;
     ZK_HIP(ctx, hipGetLastError());
     return ZKDL_OK;
@@ -565,13 +587,13 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     const zkdl_mat mq = {q, st, m, n, pitch, m * pitch, ZKDL_I8, 0};
     if (rc == ZKDL_OK && da) {
         if (m && n) rc = zk_quantize_i8(ctx, dy, 1, w_scale, &mq, scale, nullptr);
-        if (rc == ZKDL_OK) rc = m8_product(ctx, &mq, w, 0, !trans_w, n ? scale : nullptr, nullptr, da);
+        if (rc == ZKDL_OK) rc = m8_product(ctx, &mq, w, 0, !trans_w, n ? scale : nullptr, nullptr, da, 1);
     }
     if (rc == ZKDL_OK && dw) {
         if (m && n) rc = zk_quantize_i8(ctx, dy, 0, a_scale, &mq, scale, nullptr);
         if (rc == ZKDL_OK) {
-            if (trans_w) rc = m8_product(ctx, &mq, a, 1, 0, m ? scale : nullptr, nullptr, dw);
-            else rc = m8_product(ctx, a, &mq, 1, 0, nullptr, m ? scale : nullptr, dw);
+            if (trans_w) rc = m8_product(ctx, &mq, a, 1, 0, m ? scale : nullptr, nullptr, dw, 1);
+            else rc = m8_product(ctx, a, &mq, 1, 0, nullptr, m ? scale : nullptr, dw, 2);
         }
     }
     zk_free(ctx, scale);
