@@ -348,15 +348,17 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
     });
 }
 
-// The same with the columns kept in registers between the two looks at them, for up to 2048 rows: 1024 threads have 32 columns, 256 rows
-// at a time.
-constexpr int L8_ONCE_T = 4, L8_ONCE_R = 256, L8_ONCE_ITEMS = 8;
-template <class T, int ITEMS>
-__global__ __launch_bounds__(1024) void k_l8_cols_once(L8ColArgs a, L8Mat<const T> x, L8Mat<int8_t> q, L8Mat<T> values) {
-    __shared__ uint32_t s_top[16][L8_ONCE_T][8];
-    const uint32_t tx = threadIdx.x % L8_ONCE_T, ty = threadIdx.x / L8_ONCE_T;
-    const L8At at = l8_at(blockIdx.x * (L8_ONCE_T * 8) + tx * 8, a.cols);
-    const uint64_t s = blockIdx.z;
+// The same with the columns kept in registers between the two looks at them, for up to 2048 rows: a block has 8 CT columns, 256 rows at a
+// time.  CT = 4 reads whole lines; CT = 1 is for matrices of few columns, which would otherwise leave most of the device idle.
+constexpr int L8_ONCE_R = 256, L8_ONCE_ITEMS = 8;
+template <class T, int CT, int ITEMS>
+static __device__ __forceinline__ void l8_cols_once(const L8ColArgs& a, const L8Mat<const T>& x, const L8Mat<int8_t>& q, const L8Mat<T>& values,
+                                                    uint64_t s, uint32_t block) {
+    constexpr int WAVES = CT * L8_ONCE_R / 64;
+    __shared__ uint32_t s_top[WAVES][CT * 8];
+    __shared__ float s_pre[CT * 8], s_inv[CT * 8], s_scale[CT * 8];
+    const uint32_t tx = threadIdx.x % CT, ty = threadIdx.x / CT;
+    const L8At at = l8_at(block * (CT * 8) + tx * 8, a.cols);
     const T* p = x.p + s * x.ss + at.start;
     const float* mu = a.mult ? a.mult + s * a.rows : nullptr;
     L8Vec<T> raw[ITEMS];
@@ -380,24 +382,33 @@ __global__ __launch_bounds__(1024) void k_l8_cols_once(L8ColArgs a, L8Mat<const 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int d = L8_ONCE_T; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], d, 64));
+        for (int d = CT; d < 64; d <<= 1) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], d, 64));
     }
-    if ((threadIdx.x & 63) < L8_ONCE_T) {
+    if ((threadIdx.x & 63) < CT) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s_top[threadIdx.x >> 6][tx][i] = top[i];
+        for (int i = 0; i < 8; ++i) s_top[threadIdx.x >> 6][tx * 8 + i] = top[i];
     }
     __syncthreads();
+    if (threadIdx.x < CT * 8) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) b = max(b, s_top[k][threadIdx.x]);
+        const L8Quant c = l8_quant(b);
+        s_pre[threadIdx.x] = c.pre;
+        s_inv[threadIdx.x] = c.inv;
+        s_scale[threadIdx.x] = c.finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+    }
+    __syncthreads();
+    if (!at.live) return;
     L8Quant c[8];
     float scale[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        uint32_t b = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) b = max(b, s_top[k][tx][i]);
-        c[i] = l8_quant(b);
-        scale[i] = c[i].finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+        scale[i] = s_scale[tx * 8 + i];
+        c[i].pre = s_pre[tx * 8 + i];
+        c[i].inv = s_inv[tx * 8 + i];
+        c[i].finite = scale[i] == scale[i];
     }
-    if (!at.live) return;
     if (ty == 0) l8_store(a.scale + s * a.cols + at.start, 8, scale);
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
@@ -414,6 +425,10 @@ __global__ __launch_bounds__(1024) void k_l8_cols_once(L8ColArgs a, L8Mat<const 
             l8_store(values.p + s * values.ss + m * values.rs + at.start, 8, f);
         }
     }
+}
+template <class T, int CT, int ITEMS>
+__global__ __launch_bounds__(CT * L8_ONCE_R) void k_l8_cols_once(L8ColArgs a, L8Mat<const T> x, L8Mat<int8_t> q, L8Mat<T> values) {
+    l8_cols_once<T, CT, ITEMS>(a, x, q, values, blockIdx.z, blockIdx.x);
 }
 
 template <class T>
@@ -444,12 +459,15 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
         a.scale = scale + s0 * x->cols;
         const dim3 grid((unsigned)tiles, a.chunks, (unsigned)ns);
         if (x->cols >= 8 && x->rows <= L8_ONCE_R * L8_ONCE_ITEMS) {
-            const dim3 once((unsigned)l8_ceil(x->cols, L8_ONCE_T * 8), 1, (unsigned)ns);
-#define L8_ONCE(ITEMS) hipLaunchKernelGGL((k_l8_cols_once<T, ITEMS>), once, dim3(1024), 0, ctx->stream, a, mx, mq, mv)
-            if (x->rows <= L8_ONCE_R) L8_ONCE(1);
-            else if (x->rows <= 2 * L8_ONCE_R) L8_ONCE(2);
-            else if (x->rows <= 4 * L8_ONCE_R) L8_ONCE(4);
-            else L8_ONCE(8);
+#define L8_ONCE(CT, ITEMS) \
+    hipLaunchKernelGGL((k_l8_cols_once<T, CT, ITEMS>), dim3((unsigned)l8_ceil(x->cols, CT * 8), 1, (unsigned)ns), dim3(CT * L8_ONCE_R), 0, ctx->stream, a, mx, mq, mv)
+            if (l8_ceil(x->cols, 32) * ns < 64 && x->rows <= 4 * L8_ONCE_R) {
+                if (x->rows <= 2 * L8_ONCE_R) L8_ONCE(1, 2);
+                else L8_ONCE(1, 4);
+            } else if (x->rows <= L8_ONCE_R) L8_ONCE(4, 1);
+            else if (x->rows <= 2 * L8_ONCE_R) L8_ONCE(4, 2);
+            else if (x->rows <= 4 * L8_ONCE_R) L8_ONCE(4, 4);
+            else L8_ONCE(4, 8);
 #undef L8_ONCE
             continue;
         }
@@ -560,7 +578,49 @@ struct L8BackArgs {
     int w_f32;
     const float* rstd;
     float* part;        // [blocks][cols], or null
+    float* dweight;     // not null: blocks from row_blocks on sum it up by columns
+    uint32_t row_blocks;
 };
+
+// dweight of 64 columns, straight from the gradients: 32 rows at a time
+template <class T>
+static __device__ __forceinline__ void l8_dweight_cols(const L8BackArgs& a, const L8Mat<const T>& dy, const L8Mat<const T>& h, uint32_t block) {
+    __shared__ float s[32][65];
+    const uint32_t tx = threadIdx.x % 8, ty = threadIdx.x / 8;
+    const L8At at = l8_at(block * 64 + tx * 8, a.cols);
+    float dw[8] = {};
+    for (uint64_t m = ty; m < a.rows; m += 128) {
+        L8Vec<T> gv[4], hv[4];
+        float r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t i = min(m + k * 32, a.rows - 1);
+            gv[k] = l8_raw(dy.p + i * dy.rs + at.start);
+            hv[k] = l8_raw(h.p + i * h.rs + at.start);
+            r[k] = a.rstd[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (m + k * 32 >= a.rows) break;
+            float g[8], n[8];
+            l8_floats(gv[k], g);
+            l8_floats(hv[k], n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[i] = fmaf(g[i], n[i] * r[k], dw[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[ty][tx * 8 + i] = dw[i];
+    __syncthreads();
+    if (ty == 0 && at.live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dw[i] = 0.f;
+            for (int k = 0; k < 32; ++k) dw[i] += s[k][tx * 8 + i];
+        }
+        l8_store(a.dweight + at.start, 8, dw);
+    }
+}
 
 template <class T, int G, int ITEMS>
 __global__ __launch_bounds__(l8_threads(G)) void k_l8_norm_back(L8BackArgs a, L8Mat<const T> dy, L8Mat<const T> h, L8Mat<const T> dt, L8Mat<T> dx) {
@@ -569,6 +629,10 @@ __global__ __launch_bounds__(l8_threads(G)) void k_l8_norm_back(L8BackArgs a, L8
     L8RowArgs wa = {};
     wa.w = a.w;
     wa.w_f32 = a.w_f32;
+    if (G <= 256 && blockIdx.x >= a.row_blocks) {
+        l8_dweight_cols(a, dy, h, blockIdx.x - a.row_blocks);
+        return;
+    }
     float dw[ITEMS][8] = {}, w[ITEMS][8];
     L8At at[ITEMS];
 #pragma unroll
@@ -576,7 +640,7 @@ __global__ __launch_bounds__(l8_threads(G)) void k_l8_norm_back(L8BackArgs a, L8
         at[k] = l8_at((k * G + t) * 8, a.cols);
         l8_weights<T>(wa, 0, at[k].start, 8, w[k]);
     }
-    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    const uint64_t step = (uint64_t)a.row_blocks * GROUPS;
     const float over = 1.f / (float)a.cols;
     for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
         const uint64_t m = r0 + threadIdx.x / G;
@@ -736,7 +800,15 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
     uint64_t blocks = l8_ceil(a.rows, wave ? 4 : 1);
     if (blocks > 768) blocks = 768;
     const uint64_t col_rows = a.rows < 64 ? a.rows : 64;
-    if (dweight) {
+    a.row_blocks = (uint32_t)blocks;
+    // The gradients of few rows are summed by columns in blocks of the same launch, which read them once more, from L2; otherwise the blocks'
+    // shares are summed by a second one.  Whole calls (us, second launch / same launch) with 128, 1024, 4096 columns: 64 rows 8.2 / 4.9,
+    // 8.6 / 5.0, 8.5 / 5.0; 512 rows 8.4 / 6.8, 8.4 / 7.2, 11.2 / 8.1; 1024 rows 8.6 / 10.6, 8.4 / 11.3, 14.4 / 14.1.
+    const bool together = dweight && regs && n <= 4096 && a.rows <= 512;
+    if (together) {
+        a.dweight = dweight;
+        blocks += l8_ceil(n, 64);
+    } else if (dweight) {
         a.part = (float*)zk_alloc(ctx, (regs ? blocks : col_rows) * n * 4);
         if (!a.part) return ZKDL_ENOMEM;
     }
@@ -754,7 +826,7 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
     else if (n <= 8192) L8_BACK(512, 2);
     else L8_BACK(1024, 2);
 #undef L8_BACK
-    if (dweight)
+    if (a.part)
         hipLaunchKernelGGL(k_l8_sum_shares, dim3(l8_grid(l8_ceil(n, 32))), dim3(1024), 0, ctx->stream, a.part, (uint32_t)(regs ? blocks : col_rows), n, dweight);
     zk_free(ctx, a.part);
     return ZKDL_OK;
@@ -775,7 +847,7 @@ extern "C" int zkdl_rmsnorm_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const
         return ZKDL_OK;
     }
     if (!rstd) return ZKDL_EINVAL;
-    L8BackArgs a = {dy->rows, (uint32_t)dy->cols, weight, weight_dtype == ZKDL_F32, rstd, nullptr};
+    L8BackArgs a = {dy->rows, (uint32_t)dy->cols, weight, weight_dtype == ZKDL_F32, rstd, nullptr, nullptr, 0};
     int rc;
     if (dy->dtype == ZKDL_F32) rc = l8_norm_back<float>(ctx, a, dy, h, dtotal, dx, dweight);
     else if (dy->dtype == ZKDL_F16) rc = l8_norm_back<__half>(ctx, a, dy, h, dtotal, dx, dweight);

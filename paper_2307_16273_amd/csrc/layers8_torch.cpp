@@ -7,7 +7,7 @@
 // Arguments that do not fit raise ValueError.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
 
 #include "../../include/zkdl.h"
@@ -96,7 +96,7 @@ struct Call {
         return t.data_ptr();
     }
     at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const {
-        return at::empty(sizes, at::TensorOptions().dtype(type).device(c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)device)));
+        return at::Tensor(at::detail::empty_cuda(sizes, type, c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)device), std::nullopt));
     }
     // A new matrix or stack; `pitch`: entries from row to row.
     at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, zkdl_mat* m, int64_t pitch = -1) const {
