@@ -83,13 +83,13 @@ static __device__ __forceinline__ float l8_rstd_again(const T* x, const T* r, ui
 }
 
 template <class T, bool NORM, int G, int ITEMS>
-__global__ __launch_bounds__(l8_threads(G)) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
-                                                 L8Mat<T> values) {
+static __device__ __forceinline__ void l8_rows(const L8RowArgs& a, const L8Mat<const T>& x, const L8Mat<const T>& res, const L8Mat<int8_t>& q,
+                                               const L8Mat<T>& total, const L8Mat<T>& values, uint32_t block, uint32_t blocks) {
     constexpr int GROUPS = l8_threads(G) / G;
     const uint32_t t = threadIdx.x % G;
-    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    const uint64_t step = (uint64_t)blocks * GROUPS;
     // all groups of a block take as many turns: the reductions of a block-wide group meet at barriers
-    for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
+    for (uint64_t r0 = (uint64_t)block * GROUPS; r0 < a.rows; r0 += step) {
         const uint64_t r = r0 + threadIdx.x / G;
         if (GROUPS > 1 && r >= a.rows) continue;
         const uint64_t s = r / a.per_stack, m = r % a.per_stack;
@@ -210,6 +210,12 @@ __global__ __launch_bounds__(l8_threads(G)) void k_l8_rows(L8RowArgs a, L8Mat<co
             }
         }
     }
+}
+
+template <class T, bool NORM, int G, int ITEMS>
+__global__ __launch_bounds__(l8_threads(G)) void k_l8_rows(L8RowArgs a, L8Mat<const T> x, L8Mat<const T> res, L8Mat<int8_t> q, L8Mat<T> total,
+                                                           L8Mat<T> values) {
+    l8_rows<T, NORM, G, ITEMS>(a, x, res, q, total, values, blockIdx.x, gridDim.x);
 }
 
 // zeros by a kernel and not by a memory operation: the calls may be captured into a graph
@@ -565,6 +571,70 @@ extern "C" int zkdl_rmsnorm_i8(zkdl_ctx* ctx, const zkdl_mat* x, const zkdl_mat*
     return ZKDL_OK;
 } catch (...) {
     return ZKDL_ENOMEM;
+}
+
+// ---------------------------------------------------------------------------
+// L8Prepare: blocks for each of its parts
+// ---------------------------------------------------------------------------
+template <class T>
+struct L8PrepareArgs {
+    L8RowArgs rows;
+    L8ColArgs cols;
+    L8Mat<const T> dy;
+    L8Mat<int8_t> q, p;
+    M8PackArgs pack[2];
+    uint32_t first[4];      // first block of the columns, of the two packings, and their end
+};
+template <class T, int G, int ITEMS>
+__global__ __launch_bounds__(256) void k_l8_prepare(L8PrepareArgs<T> a) {
+    const L8Mat<T> none = {nullptr, 0, 0};
+    const uint32_t b = blockIdx.x;
+    if (b < a.first[0]) l8_rows<T, false, G, ITEMS>(a.rows, a.dy, L8Mat<const T>{nullptr, 0, 0}, a.q, none, none, b, a.first[0]);
+    else if (b < a.first[1]) l8_cols_once<T, 1, 4>(a.cols, a.dy, a.p, none, 0, b - a.first[0]);
+    else if (b < a.first[2]) m8_pack(a.pack[0], b - a.first[1], a.first[2] - a.first[1]);
+    else m8_pack(a.pack[1], b - a.first[2], a.first[3] - a.first[2]);
+}
+
+template <class T>
+static void l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
+    L8PrepareArgs<T> a = {};
+    a.rows.rows = a.rows.per_stack = j.dy->rows;
+    a.rows.cols = (uint32_t)j.dy->cols;
+    a.rows.w = j.w_scale;
+    a.rows.w_f32 = 1;
+    a.rows.w_stack = j.dy->cols;
+    a.rows.scale = j.t;
+    a.cols.rows = a.cols.chunk = j.dy->rows;
+    a.cols.cols = (uint32_t)j.dy->cols;
+    a.cols.chunks = 1;
+    a.cols.mult = j.a_scale;
+    a.cols.scale = j.u;
+    a.dy = l8_mat<const T>(j.dy);
+    a.q = l8_mat<int8_t>(j.q);
+    a.p = l8_mat<int8_t>(j.p);
+    const uint64_t n = j.dy->cols;
+    a.first[0] = (uint32_t)l8_ceil(j.dy->rows, n <= 1024 ? 4 : 1);
+    a.first[1] = a.first[0] + (uint32_t)l8_ceil(n, 8);
+    for (int i = 0; i < 2; ++i) {
+        a.pack[i] = j.pack[i];
+        const uint64_t pieces = i < j.packs ? j.pack[i].stack * j.pack[i].rows * (j.pack[i].pitch / 16) : 0, blocks = l8_ceil(pieces, 256);
+        a.first[2 + i] = a.first[1 + i] + (uint32_t)(blocks < 4096 ? blocks : 4096);
+    }
+    if (n <= 512) hipLaunchKernelGGL((k_l8_prepare<T, 64, 1>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
+    else if (n <= 1024) hipLaunchKernelGGL((k_l8_prepare<T, 64, 2>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
+    else hipLaunchKernelGGL((k_l8_prepare<T, 256, 1>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
+}
+
+// rows of one group's registers, columns of a block's, and no more than its scattered reads are worth
+bool zk_prepare_fits(const zkdl_mat* dy) {
+    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 2048 && dy->rows >= 1 && dy->rows <= 4 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)1 << 20;
+}
+void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job) {
+    switch (job.dy->dtype) {
+        case ZKDL_F32: l8_prepare<float>(ctx, job); break;
+        case ZKDL_F16: l8_prepare<__half>(ctx, job); break;
+        default: l8_prepare<bf16_t>(ctx, job);
+    }
 }
 
 // ---------------------------------------------------------------------------

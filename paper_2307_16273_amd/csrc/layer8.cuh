@@ -143,6 +143,44 @@ static __device__ __forceinline__ uint32_t l8_wave_max(uint32_t x) {
     return x;
 }
 
+typedef int v4i __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(1))) M8Bytes {
+    uint32_t v[4];
+};
+// 16 bytes of a stored matrix from (r, c) on, zeros outside rows x cols
+static __device__ __forceinline__ v4i m8_fetch(const int8_t* p, uint64_t rs, uint32_t r, uint32_t rows, uint32_t c, uint32_t cols) {
+    v4i x = {0, 0, 0, 0};
+    if (r < rows && c < cols) {
+        const int8_t* at = p + r * rs + c;
+        if (cols - c >= 16) {
+            const M8Bytes y = *(const M8Bytes*)at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (int)y.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (c + i < cols) x[i / 4] |= (int)((uint32_t)(uint8_t)at[i] << (8 * (i % 4)));
+        }
+    }
+    return x;
+}
+
+// Rows of whole 16 bytes at multiples of 16, zeros behind the last column: what k_m8_tile can fetch of any matrix.
+struct M8PackArgs {
+    const int8_t* p;
+    uint64_t rs, ss;
+    uint64_t rows, stack, pitch;
+    uint32_t cols;
+    int8_t* out;
+};
+static __device__ __forceinline__ void m8_pack(const M8PackArgs& a, uint32_t block, uint32_t blocks) {
+    const uint64_t pieces = a.pitch / 16, n = a.stack * a.rows * pieces;
+    for (uint64_t i = block * 256ull + threadIdx.x; i < n; i += blocks * 256ull) {
+        const uint64_t row = i / pieces, c = i % pieces * 16;
+        *(v4i*)(a.out + i * 16) = m8_fetch(a.p + row / a.rows * a.ss, a.rs, (uint32_t)(row % a.rows), (uint32_t)a.rows, (uint32_t)c, a.cols);
+    }
+}
+
 // ---- host side -------------------------------------------------------------------
 // The context's device is the current one while this lives: its stream may be the device's default one.
 struct L8Device {
@@ -179,3 +217,14 @@ static inline uint64_t l8_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b;
 // ---- k_layer8.hip ------------------------------------------------------------------
 // zkdl_quantize_i8 behind its checks, on matrices with entries
 int zk_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values);
+// What the gradients of a small layer need first, in one launch: dy w_scale quantised by rows (q, t), a_scale dy by columns (p, u), and the
+// matrices that have to be packed for the tiles.
+struct L8Prepare {
+    const zkdl_mat *dy, *q, *p;
+    const float *a_scale, *w_scale;
+    float *t, *u;
+    M8PackArgs pack[2];
+    int packs;
+};
+bool zk_prepare_fits(const zkdl_mat* dy);
+void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job);

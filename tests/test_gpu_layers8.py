@@ -557,3 +557,22 @@ def test_matmul_large_tiles(lib, ctx, shape, ta, tb):
     got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=torch.bfloat16).cpu().double()
     scaled = want * sa.double()[:, None] * sb.double()[None, :]
     assert torch.all((got - scaled).abs() <= (4 * U + 1.001 * HALF_ULP[torch.bfloat16]) * scaled.abs())
+
+
+@pytest.mark.parametrize("shape", [(1, 1100, 130, 515), (1, 2100, 256, 304), (3, 70, 96, 130), (1, 300, 64, 2500), (2, 2, 40, 8)], ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+def test_matmul_backward_by_steps(lib, ctx, shape, trans_w):
+    """Layers that are too large for one launch of all preparations, and stacks: codes by the operator itself, products exact."""
+    s, m, k, n = shape
+    g = gen(sum(shape))
+    lead = (s,) if s > 1 else ()
+    a, w = codes(g, lead + (m, k)), codes(g, lead + (k, n))
+    sa, sw = torch.rand(lead + (m,), generator=g) + 0.1, torch.rand(lead + (n,), generator=g) + 0.1
+    dy = normal(g, lead + (m, n), torch.float32, 0.1)
+    got = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w)
+    q, tq = codes32(dy * sw.unsqueeze(-2), -1)
+    p, u = codes32(dy * sa.unsqueeze(-1), -2)
+    da, dw = product64(q, w.mT) * tq, product64(a.mT, p) * u
+    gw = got["dw"].cpu().double()
+    assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
+    assert torch.all(((gw.mT if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
