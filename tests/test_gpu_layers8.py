@@ -576,3 +576,10 @@ def test_matmul_backward_by_steps(lib, ctx, shape, trans_w):
     gw = got["dw"].cpu().double()
     assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
     assert torch.all(((gw.mT if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
+
+
+def test_training_answering_and_proving_together(lib):
+    from paper_2307_16273_amd.train_quantized import run
+    losses, rows_equal, holds = run(layers=4, width=256, batch=32, steps=6, say=lambda s: None)
+    assert losses[-1] < 0.9 * losses[0] and all(np.isfinite(losses))
+    assert rows_equal and holds
