@@ -585,12 +585,12 @@ struct L8PrepareArgs {
     M8PackArgs pack[2];
     uint32_t first[4];      // first block of the columns, of the two packings, and their end
 };
-template <class T, int G, int ITEMS>
+template <class T, int G, int ITEMS, int COL_ITEMS>
 __global__ __launch_bounds__(256) void k_l8_prepare(L8PrepareArgs<T> a) {
     const L8Mat<T> none = {nullptr, 0, 0};
     const uint32_t b = blockIdx.x;
     if (b < a.first[0]) l8_rows<T, false, G, ITEMS>(a.rows, a.dy, L8Mat<const T>{nullptr, 0, 0}, a.q, none, none, b, a.first[0]);
-    else if (b < a.first[1]) l8_cols_once<T, 1, 4>(a.cols, a.dy, a.p, none, 0, b - a.first[0]);
+    else if (b < a.first[1]) l8_cols_once<T, 1, COL_ITEMS>(a.cols, a.dy, a.p, none, 0, b - a.first[0]);
     else if (b < a.first[2]) m8_pack(a.pack[0], b - a.first[1], a.first[2] - a.first[1]);
     else m8_pack(a.pack[1], b - a.first[2], a.first[3] - a.first[2]);
 }
@@ -620,14 +620,18 @@ static void l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
         const uint64_t pieces = i < j.packs ? j.pack[i].stack * j.pack[i].rows * (j.pack[i].pitch / 16) : 0, blocks = l8_ceil(pieces, 256);
         a.first[2 + i] = a.first[1 + i] + (uint32_t)(blocks < 4096 ? blocks : 4096);
     }
-    if (n <= 512) hipLaunchKernelGGL((k_l8_prepare<T, 64, 1>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
-    else if (n <= 1024) hipLaunchKernelGGL((k_l8_prepare<T, 64, 2>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
-    else hipLaunchKernelGGL((k_l8_prepare<T, 256, 1>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a);
+#define L8_PREPARE(G, ITEMS, COL_ITEMS) hipLaunchKernelGGL((k_l8_prepare<T, G, ITEMS, COL_ITEMS>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a)
+    if (j.dy->rows > 4 * L8_ONCE_R) L8_PREPARE(64, 2, 8);       // then there are at most 1023 columns
+    else if (n <= 512) L8_PREPARE(64, 1, 4);
+    else if (n <= 1024) L8_PREPARE(64, 2, 4);
+    else if (n <= 2048) L8_PREPARE(256, 1, 4);
+    else L8_PREPARE(256, 2, 4);
+#undef L8_PREPARE
 }
 
 // rows of one group's registers, columns of a block's, and no more than its scattered reads are worth
 bool zk_prepare_fits(const zkdl_mat* dy) {
-    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 2048 && dy->rows >= 1 && dy->rows <= 4 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)1 << 20;
+    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 4096 && dy->rows >= 1 && dy->rows <= 8 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)1 << 20;
 }
 void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job) {
     switch (job.dy->dtype) {

@@ -563,7 +563,7 @@ extern "C" int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* 
 }
 
 static int m8_small_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w, const float* a_scale,
-                             const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw, int c_da, int c_dw) {
+                             const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw) {
     const uint64_t m = dy->rows, n = dy->cols, pitch = l8_ceil(n, 16) * 16, codes = l8_ceil(m * pitch, 256) * 256;
     int8_t* mem = (int8_t*)zk_alloc(ctx, 2 * codes + (m + n) * 4);      // q, p, t, u
     if (!mem) return ZKDL_ENOMEM;
@@ -592,7 +592,9 @@ static int m8_small_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* 
         if (trans_w) m8_operands(pair.dw, &p, &pa);
         else m8_operands(pair.dw, &pa, &p);
         pair.da_blocks = (uint32_t)(l8_ceil(da->rows, 64) * l8_ceil(da->cols, 64));
-        if (c_da != M8_TILE64 || c_dw != M8_TILE64) {
+        // (few rows as well: a product of their own kernel costs a launch more)
+        const int c_da = m8_choose(da->rows, da->cols, n, 1, true, false), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false);
+        if (c_da > M8_TILE64 || c_dw > M8_TILE64) {
             rc = trans_w ? m8_launch<false, true>(ctx, pair.da, 1, c_da) : m8_launch<false, false>(ctx, pair.da, 1, c_da);
             if (rc == ZKDL_OK) rc = m8_launch<true, true>(ctx, pair.dw, 1, c_dw);
         } else {
@@ -624,13 +626,10 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     // of 64.  Whole calls (us, a launch for each step / like this), rows x in x out: 33 x 100 x 70 14.3 / 7.8, 64 x 1024 x 1024 15.1 / 9.7,
     // 333 x 1000 x 517 22.3 / 9.6, 1024 x 1024 x 1024 21.9 / 15.8, 1000 x 1000 x 1000 30.7 / 18.4.
     if (da && dw && k && zk_prepare_fits(dy)) {
-        const int c_da = m8_choose(m, k, n, 1, true, false), c_dw = m8_choose(k, n, m, 1, true, false);
-        if (c_da >= M8_TILE64 && c_dw >= M8_TILE64) {
-            const int rc = m8_small_backward(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw, c_da, c_dw);
-            if (rc != ZKDL_OK) return rc;
-            ZK_HIP(ctx, hipGetLastError());
-            return ZKDL_OK;
-        }
+        const int rc = m8_small_backward(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw);
+        if (rc != ZKDL_OK) return rc;
+        ZK_HIP(ctx, hipGetLastError());
+        return ZKDL_OK;
     }
     // the quantised gradient: rows of whole 16 bytes
     const uint64_t pitch = l8_ceil(n ? n : 1, 16) * 16;

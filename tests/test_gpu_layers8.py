@@ -583,3 +583,19 @@ def test_training_answering_and_proving_together(lib):
     losses, rows_equal, holds = run(layers=4, width=256, batch=32, steps=6, say=lambda s: None)
     assert losses[-1] < 0.9 * losses[0] and all(np.isfinite(losses))
     assert rows_equal and holds
+
+
+@pytest.mark.parametrize("shape", [(1, 16, 8), (3, 178, 2816), (8, 67, 1408), (5, 40, 4096), (1728, 832, 16), (2048, 48, 500), (1025, 17, 9), (20, 5000, 33)], ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+def test_matmul_backward_long_and_narrow(lib, ctx, shape, trans_w):
+    m, k, n = shape
+    g = gen(sum(shape))
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw, dy = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1, normal(g, (m, n), torch.float32, 0.1)
+    got = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w)
+    q, tq = codes32(dy * sw, 1)
+    p, u = codes32(dy * sa[:, None], 0)
+    da, dw = product64(q, w.t()) * tq, product64(a.t(), p) * u
+    gw = got["dw"].cpu().double()
+    assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
+    assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
