@@ -253,7 +253,8 @@ struct L8ColArgs {
     uint64_t rows, chunk;         // chunk: rows of a block
     uint32_t cols, chunks;
     const float* mult;            // rows for each matrix, or null
-    uint32_t* part;               // [stack][chunks][cols] largest magnitudes
+    uint32_t* part;               // [stack][parts][cols] largest magnitudes
+    uint32_t parts;
     float* scale;                 // [stack][cols]
 };
 
@@ -313,10 +314,10 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
                 for (int i = 0; i < 8; ++i) top[i] = max(top[i], l8_mag(v[i]));
             });
     } else if (live) {
-        for (uint32_t k = ty; k < a.chunks; k += L8_COL_R)
+        for (uint32_t k = ty; k < a.parts; k += L8_COL_R)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < n) top[i] = max(top[i], a.part[(s * a.chunks + k) * a.cols + j + i]);
+                if (i < n) top[i] = max(top[i], a.part[(s * a.parts + k) * a.cols + j + i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) s_top[ty][tx * 8 + i] = top[i];
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
         for (int k = 0; k < L8_COL_R; ++k) b = max(b, s_top[k][threadIdx.x]);
         s_top[0][threadIdx.x] = b;
         if (c0 + threadIdx.x < a.cols) {
-            if (MODE == 0) a.part[(s * a.chunks + blockIdx.y) * a.cols + c0 + threadIdx.x] = b;
+            if (MODE == 0) a.part[(s * a.parts + blockIdx.y) * a.cols + c0 + threadIdx.x] = b;
             else if (blockIdx.y == 0) a.scale[s * a.cols + c0 + threadIdx.x] = b < L8_INF ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
         }
     }
@@ -437,9 +438,18 @@ __global__ __launch_bounds__(CT * L8_ONCE_R) void k_l8_cols_once(L8ColArgs a, L8
     l8_cols_once<T, CT, ITEMS>(a, x, q, values, blockIdx.z, blockIdx.x);
 }
 
+// four blocks for each compute unit, of 64 rows and more
+static void l8_col_chunks(L8ColArgs& a, uint64_t tiles) {
+    uint64_t chunks = l8_ceil(1024, tiles);
+    if (chunks > l8_ceil(a.rows, 64)) chunks = l8_ceil(a.rows, 64);
+    if (chunks < 1) chunks = 1;
+    a.chunk = l8_ceil(l8_ceil(a.rows, chunks), L8_COL_R) * L8_COL_R;
+    a.chunks = (uint32_t)l8_ceil(a.rows, a.chunk);
+}
+
 template <class T>
 static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, const zkdl_mat* q, float* scale, const zkdl_mat* values) {
-    L8ColArgs a;
+    L8ColArgs a = {};
     a.rows = x->rows;
     a.cols = (uint32_t)x->cols;
     a.mult = mult;
@@ -449,12 +459,8 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
     // the grid's axes hold 65535 blocks: matrices of a longer stack go in launches of their own
     for (uint64_t s0 = 0; s0 < x->stack; s0 += 65535) {
         const uint64_t ns = x->stack - s0 < 65535 ? x->stack - s0 : 65535;
-        // four blocks for each compute unit, of 64 rows and more
-        uint64_t chunks = l8_ceil(1024, tiles * ns);
-        if (chunks > l8_ceil(x->rows, 64)) chunks = l8_ceil(x->rows, 64);
-        if (chunks < 1) chunks = 1;
-        a.chunk = l8_ceil(l8_ceil(x->rows, chunks), L8_COL_R) * L8_COL_R;
-        a.chunks = (uint32_t)l8_ceil(x->rows, a.chunk);
+        l8_col_chunks(a, tiles * ns);
+        a.parts = a.chunks;
         L8Mat<const T> mx = l8_mat<const T>(x);
         L8Mat<int8_t> mq = l8_mat<int8_t>(q);
         L8Mat<T> mv = l8_mat<T>(values);
@@ -571,6 +577,145 @@ extern "C" int zkdl_rmsnorm_i8(zkdl_ctx* ctx, const zkdl_mat* x, const zkdl_mat*
     return ZKDL_OK;
 } catch (...) {
     return ZKDL_ENOMEM;
+}
+
+// ---------------------------------------------------------------------------
+// Both quantisations of a large gradient: by rows (times the columns' scales), and, in the same pass, the largest magnitudes of the columns
+// (times the rows' scales), each thread its own columns over all of its block's rows; then by columns.  The gradient is read twice instead
+// of three times.
+// ---------------------------------------------------------------------------
+template <class T>
+struct L8BothArgs {
+    uint64_t rows;
+    uint32_t cols;
+    const float *row_mult, *col_mult;     // a factor for each row (for the columns' codes), for each column (for the rows')
+    float* scale;                         // of the rows
+    uint32_t* part;                       // [blocks][cols]
+    L8Mat<const T> x;
+    L8Mat<int8_t> q;
+};
+template <class T, int G, int ITEMS>
+__global__ __launch_bounds__(l8_threads(G)) void k_l8_both(L8BothArgs<T> a) {
+    constexpr int GROUPS = l8_threads(G) / G;
+    const uint32_t t = threadIdx.x % G;
+    uint32_t tops[ITEMS][8] = {};
+    float w[ITEMS][8];
+    L8At at[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        at[k] = l8_at((k * G + t) * 8, a.cols);
+        l8_floats(l8_raw(a.col_mult + at[k].start), w[k]);
+    }
+    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += step) {
+        const uint64_t m = r0 + threadIdx.x / G;
+        if (GROUPS > 1 && m >= a.rows) continue;
+        const float f = a.row_mult[m];
+        L8Vec<T> xv[ITEMS];
+        float v[ITEMS][8], unused = 0.f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) xv[k] = l8_raw(a.x.p + m * a.x.rs + at[k].start);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            l8_floats(xv[k], v[k]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                tops[k][i] = max(tops[k][i], l8_mag(v[k][i] * f));
+                v[k][i] *= w[k][i];
+                top = max(top, l8_mag(v[k][i]));
+            }
+        }
+        l8_row_reduce<G>(unused, top);
+        const L8Quant c = l8_quant(top);
+        if (t == 0) a.scale[m] = c.finite ? __uint_as_float(top) / 127.f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            int iq[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[k][i], c);
+            if (at[k].live) l8_store_q(a.q.p + m * a.q.rs + at[k].start, 8, iq);
+        }
+    }
+    if constexpr (GROUPS > 1) {
+        __shared__ uint32_t s_tops[GROUPS][G * ITEMS * 8];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (at[k].live) s_tops[threadIdx.x / G][at[k].start + i] = tops[k][i];
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < a.cols; j += l8_threads(G)) {
+            uint32_t b = 0;
+            for (int k = 0; k < GROUPS; ++k) b = max(b, s_tops[k][j]);
+            a.part[(uint64_t)blockIdx.x * a.cols + j] = b;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+            if (at[k].live) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a.part[(uint64_t)blockIdx.x * a.cols + at[k].start + i] = tops[k][i];
+            }
+    }
+}
+// of the blocks' parts the first: 32 columns x 32 runs of parts
+__global__ __launch_bounds__(1024) void k_l8_max_parts(uint32_t* part, uint32_t parts, uint32_t cols) {
+    __shared__ uint32_t s[32][33];
+    const uint32_t tx = threadIdx.x & 31, ty = threadIdx.x >> 5, j = blockIdx.x * 32 + tx;
+    uint32_t b = 0;
+    if (j < cols) {
+#pragma unroll 8
+        for (uint32_t k = ty; k < parts; k += 32) b = max(b, part[(uint64_t)k * cols + j]);
+    }
+    s[ty][tx] = b;
+    __syncthreads();
+    if (ty == 0 && j < cols) {
+        for (int k = 0; k < 32; ++k) b = max(b, s[k][tx]);
+        part[j] = b;
+    }
+}
+
+template <class T>
+static int l8_both(zkdl_ctx* ctx, const L8Prepare& job) {
+    const zkdl_mat* x = job.dy;
+    L8BothArgs<T> a = {x->rows, (uint32_t)x->cols, job.a_scale, job.w_scale, job.t, nullptr, l8_mat<const T>(x), l8_mat<int8_t>(job.q)};
+    const uint32_t n = a.cols;
+    uint64_t blocks = l8_ceil(a.rows, n <= 1024 ? 4 : 1);
+    if (blocks > 768) blocks = 768;
+    a.part = (uint32_t*)zk_alloc(ctx, blocks * n * 4);
+    if (!a.part) return ZKDL_ENOMEM;
+#define L8_BOTH(G, ITEMS) hipLaunchKernelGGL((k_l8_both<T, G, ITEMS>), dim3((unsigned)blocks), dim3(l8_threads(G)), 0, ctx->stream, a)
+    if (n <= 512) L8_BOTH(64, 1);
+    else if (n <= 1024) L8_BOTH(64, 2);
+    else if (n <= 2048) L8_BOTH(256, 1);
+    else if (n <= 4096) L8_BOTH(256, 2);
+    else if (n <= 8192) L8_BOTH(512, 2);
+    else L8_BOTH(1024, 2);
+#undef L8_BOTH
+    hipLaunchKernelGGL(k_l8_max_parts, dim3((unsigned)l8_ceil(n, 32)), dim3(1024), 0, ctx->stream, a.part, (uint32_t)blocks, n);
+    L8ColArgs c = {};
+    c.rows = a.rows;
+    c.cols = n;
+    c.mult = job.a_scale;
+    c.scale = job.u;
+    c.part = a.part;
+    c.parts = 1;
+    l8_col_chunks(c, l8_ceil(n, L8_COL_T * 8));
+    hipLaunchKernelGGL((k_l8_cols<T, 1>), dim3((unsigned)l8_ceil(n, L8_COL_T * 8), c.chunks, 1), dim3(256), 0, ctx->stream, c, l8_mat<const T>(x),
+                       l8_mat<int8_t>(job.p), L8Mat<T>{nullptr, 0, 0});
+    zk_free(ctx, a.part);
+    return ZKDL_OK;
+}
+// Whole calls of zkdl_matmul_i8_backward (us, three reads / two), rows x in x out: 3000 x 1000 x 1000 55.8 / 57.2, 4096 x 4096 x 4096
+// 157.4 / 155.0, 8192 x 1024 x 1024 77.7 / 65.8; up to 2048 rows the columns' codes need one read anyway (300 x 500 x 8192 45 / 51).
+bool zk_quantize_both_fits(const zkdl_mat* dy) { return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 16384 && dy->rows >= 4096; }
+int zk_quantize_both(zkdl_ctx* ctx, const L8Prepare& job) {
+    switch (job.dy->dtype) {
+        case ZKDL_F32: return l8_both<float>(ctx, job);
+        case ZKDL_F16: return l8_both<__half>(ctx, job);
+        default: return l8_both<bf16_t>(ctx, job);
+    }
 }
 
 // ---------------------------------------------------------------------------

@@ -17,6 +17,7 @@ struct M8Args {
     int o_type;                        // zkdl_dtype
     const float *sa, *sb;
     uint32_t M, N, K;
+    uint32_t all;       // not 0: the matrices of the stack are slices of K out of so many k, the last one what is left
 };
 
 // The block's tile: matrix, first row, first column.  Blocks go round the eight dies; each die takes a run of tiles that lie together,
@@ -187,20 +188,21 @@ static __device__ __forceinline__ void m8_tile_block(const M8Args& p, int8_t* ld
     uint64_t s;
     uint32_t m0, n0;
     m8_tile(p, BM, BN, block, blocks, s, m0, n0);
+    const uint32_t K = p.all ? min(p.K, p.all - (uint32_t)s * p.K) : p.K;
     const uint32_t wm = w / WN * (BM / WM), wn = w % WN * (BN / WN);
     OA oa;
     OB ob;
     oa.init(t, p.a_rs, min(p.M - m0, (uint32_t)BM));
     ob.init(t, p.b_rs, min(p.N - n0, (uint32_t)BN));
     const uint64_t step_a = AT ? 128 * p.a_rs : 128, step_b = BT ? 128 * p.b_rs : 128;
-    const uint32_t stages = (p.K + 127) / 128;
+    const uint32_t stages = (K + 127) / 128;
     const int8_t* pa = p.a + s * p.a_ss + (AT ? (uint64_t)m0 : m0 * p.a_rs);
     const int8_t* pb = p.b + s * p.b_ss + (BT ? (uint64_t)n0 : n0 * p.b_rs);
     uint32_t ahead = 0, in = 0, out = 0;
     auto load = [&]() {
         if (ahead < stages) {
             int8_t* q = lds + in;
-            const uint32_t left = p.K - ahead * 128;
+            const uint32_t left = K - ahead * 128;
             if (left >= 128) {
                 oa.load(pa, q, w);
                 ob.load(pb, q + OA::BYTES, w);
@@ -421,6 +423,29 @@ __global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
     }
 }
 
+// The sums of the slices of a long k, 32-bit integers [slices][M][N]: out = (their sum sa) sb
+__global__ __launch_bounds__(256) void k_m8_join(M8Args p, const int* parts, uint32_t slices) {
+    const uint32_t n4 = (p.N + 3) / 4;
+    const uint64_t n = (uint64_t)p.M * n4, each = (uint64_t)p.M * p.N;
+    for (uint64_t at = blockIdx.x * 256ull + threadIdx.x; at < n; at += gridDim.x * 256ull) {
+        const uint32_t i = (uint32_t)(at / n4), j = (uint32_t)(at % n4) * 4;
+        const int* q = parts + (uint64_t)i * p.N + j;
+        v4i acc[1][1] = {};
+        if (j + 4 <= p.N) {
+#pragma unroll 8
+            for (uint32_t s = 0; s < slices; ++s) {
+                const M8Bytes x = *(const M8Bytes*)(q + s * each);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][e] += (int)x.v[e];
+            }
+        } else {
+            for (uint32_t s = 0; s < slices; ++s)
+                for (uint32_t e = 0; j + e < p.N; ++e) acc[0][0][e] += q[s * each + e];
+        }
+        m8_store_tile<1, 1>(p, 0, i, j, false, acc);
+    }
+}
+
 __global__ __launch_bounds__(256) void k_m8_pack(M8PackArgs a) { m8_pack(a, blockIdx.x, gridDim.x); }
 
 // a launch's blocks are counted in 32 bits of threads
@@ -450,7 +475,7 @@ static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, int choice)
 // the way back to back, launch included (a launch alone 4):
 //  - up to 16 rows or columns, blocks of 16 (FEW1 / FEW2 / TILE64): 1 x 4096 x 4096 along k 5.7 / 7.5 / 10.8, across 9.2 / 9.2 / 16.5;
 //  - up to 64 with an operand across and a long k, blocks of 32 (FEW2 / TILE64): 64 x 4096 x 4096 11.5 / 17.2, both along k 10.6 / 10.9;
-//    not with more tiles (8 products of 64 x 1024 x 1024 9.9 / 5.4);
+//    not with more tiles (8 products of 64 x 1024 x 1024 9.9 / 5.4) or a k that is cut in slices (64 x 8192 x 4096 18 / 12);
 //  - operands that have to be packed first, FEW2 / TILE64 with the packing: 64 x 4001 x 4001 23 / 27, 260 x 515 x 515 13 / 11 (along k),
 //    10 / 12 (one across), 130 x 1001 x 1001 10 / 13, 260 x 1001 x 1001 17 / 13;
 //  - tiles of 64, 128, 256 (4096 x 4096 weights, along k): 256 rows 11 / 27 / 52, 512 16 / 28 / 53, 1024 30 / 30 / 55, 2048 58 / 36 / 57,
@@ -460,9 +485,23 @@ static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool wh
     if (few <= 16) return M8_FEW1;
     auto tiles = [&](uint64_t x) { return l8_ceil(m, x) * l8_ceil(n, x) * stack; };
     const uint64_t t64 = tiles(64), t128 = tiles(128), t256 = tiles(256), work = m * n * k * stack;
-    if (whole ? few <= 64 && across && k >= 2048 && t64 <= 64 : work <= (uint64_t)1 << (few <= 64 ? 30 : 27)) return M8_FEW2;
+    if (whole ? few <= 64 && across && k >= 2048 && k <= 4096 && t64 <= 64 : work <= (uint64_t)1 << (few <= 64 ? 30 : 27)) return M8_FEW2;
     const uint64_t c64 = t64 <= 256 ? 11 : 15 * l8_ceil(t64, 512), c128 = t128 <= 256 ? 28 : 34 * l8_ceil(t128, 512), c256 = 54 * l8_ceil(t256, 256);
     return c64 <= c128 && c64 <= c256 ? M8_TILE64 : c128 <= c256 ? M8_TILE128 : M8_TILE256;
+}
+
+// How many slices of k tiles of 64 are worth, joined by a second launch: few tiles would leave most of the device idle over a long k.
+// Whole calls (us, one launch / slices), both operands along k: 256 x 256 with k = 2048 6.7 / 7.5, 4096 10.6 / 8.2, 8192 18.6 / 8.7, 65536
+// 129 / 15; 512 x 512 with k = 4096 10.6 / 12.0, 8192 18.7 / 13.2; 1024 x 1024 with k = 8192 19.2 / 19.4 (across 30.7 / 26.3), 65536 131 / 100.
+// (A join inside the launch, by the last block of a tile, was no faster: what passes between the dies has to go past their caches.)
+static uint64_t m8_slices(uint64_t m, uint64_t n, uint64_t k) {
+    const uint64_t t64 = l8_ceil(m, 64) * l8_ceil(n, 64), stages = l8_ceil(k, 128);
+    if (stages < (t64 <= 16 ? 32 : 64) || t64 > 256) return 1;
+    uint64_t slices = 512 / t64;
+    if (slices > stages / 4) slices = stages / 4;
+    if (slices < 2) return 1;
+    // every slice has entries: slices of whole stages, as many as those make
+    return l8_ceil(k, l8_ceil(l8_ceil(k, slices), 128) * 128);
 }
 
 // Operands that k_m8_tile can fetch: whole 16 bytes along memory, rows of a tile within 32 bits.  Along k one of the two has to end in
@@ -529,11 +568,37 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
         }
     }
     m8_operands(p, &pa, &pb);
+    uint64_t stack = out->stack;
+    const M8Args joined = p;
+    int* parts = nullptr;
+    const uint64_t slices = choice == M8_TILE64 && stack == 1 ? m8_slices(p.M, p.N, p.K) : 1;
+    if (slices > 1) {
+        parts = (int*)zk_alloc(ctx, slices * p.M * p.N * 4);
+        if (!parts) {
+            zk_free(ctx, packed[0]);
+            zk_free(ctx, packed[1]);
+            return ZKDL_ENOMEM;
+        }
+        stack = slices;
+        p.all = p.K;
+        p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, slices), 128) * 128);
+        p.a_ss = trans_a ? p.K * p.a_rs : p.K;
+        p.b_ss = trans_b ? p.K : p.K * p.b_rs;
+        p.out = parts;
+        p.o_type = ZKDL_I32;
+        p.o_rs = p.N;
+        p.o_ss = (uint64_t)p.M * p.N;
+    }
     int rc;
-    if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, out->stack, choice);
-    else if (trans_a) rc = m8_launch<true, false>(ctx, p, out->stack, choice);
-    else if (!trans_b) rc = m8_launch<false, true>(ctx, p, out->stack, choice);
-    else rc = m8_launch<false, false>(ctx, p, out->stack, choice);
+    if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, stack, choice);
+    else if (trans_a) rc = m8_launch<true, false>(ctx, p, stack, choice);
+    else if (!trans_b) rc = m8_launch<false, true>(ctx, p, stack, choice);
+    else rc = m8_launch<false, false>(ctx, p, stack, choice);
+    if (parts && rc == ZKDL_OK) {
+        const uint64_t blocks = l8_ceil((uint64_t)joined.M * l8_ceil(joined.N, 4), 256);
+        hipLaunchKernelGGL(k_m8_join, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, joined, parts, (uint32_t)slices);
+    }
+    zk_free(ctx, parts);
     zk_free(ctx, packed[0]);
     zk_free(ctx, packed[1]);
     return rc;
@@ -562,7 +627,7 @@ extern "C" int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* 
     return ZKDL_ENOMEM;
 }
 
-static int m8_small_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w, const float* a_scale,
+static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w, const float* a_scale,
                              const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw) {
     const uint64_t m = dy->rows, n = dy->cols, pitch = l8_ceil(n, 16) * 16, codes = l8_ceil(m * pitch, 256) * 256;
     int8_t* mem = (int8_t*)zk_alloc(ctx, 2 * codes + (m + n) * 4);      // q, p, t, u
@@ -576,6 +641,14 @@ static int m8_small_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* 
     job.w_scale = w_scale;
     job.t = (float*)(mem + 2 * codes);
     job.u = job.t + m;
+    if (!zk_prepare_fits(dy)) {
+        int rc = zk_quantize_both(ctx, job);
+        if (rc == ZKDL_OK) rc = m8_product(ctx, &q, w, 0, !trans_w, job.t, nullptr, da, 1);
+        if (rc == ZKDL_OK)
+            rc = trans_w ? m8_product(ctx, &p, a, 1, 0, job.u, nullptr, dw, 1) : m8_product(ctx, a, &p, 1, 0, nullptr, job.u, dw, 2);
+        zk_free(ctx, mem);
+        return rc;
+    }
     zkdl_mat pa = *a, pw = *w;
     int rc = ZKDL_OK;
     for (zkdl_mat* x : {&pa, &pw})
@@ -625,8 +698,8 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     // Both gradients of a small layer: everything in front of the products in one launch, and the products in another where both take tiles
     // of 64.  Whole calls (us, a launch for each step / like this), rows x in x out: 33 x 100 x 70 14.3 / 7.8, 64 x 1024 x 1024 15.1 / 9.7,
     // 333 x 1000 x 517 22.3 / 9.6, 1024 x 1024 x 1024 21.9 / 15.8, 1000 x 1000 x 1000 30.7 / 18.4.
-    if (da && dw && k && zk_prepare_fits(dy)) {
-        const int rc = m8_small_backward(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw);
+    if (da && dw && k && (zk_prepare_fits(dy) || zk_quantize_both_fits(dy))) {
+        const int rc = m8_both_gradients(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw);
         if (rc != ZKDL_OK) return rc;
         ZK_HIP(ctx, hipGetLastError());
         return ZKDL_OK;

@@ -228,3 +228,6 @@ struct L8Prepare {
 };
 bool zk_prepare_fits(const zkdl_mat* dy);
 void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job);
+// the two quantisations alone, for gradients of many rows
+bool zk_quantize_both_fits(const zkdl_mat* dy);
+int zk_quantize_both(zkdl_ctx* ctx, const L8Prepare& job);

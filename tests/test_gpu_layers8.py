@@ -599,3 +599,18 @@ def test_matmul_backward_long_and_narrow(lib, ctx, shape, trans_w):
     gw = got["dw"].cpu().double()
     assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
     assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
+
+
+@pytest.mark.parametrize("ta,tb", [(False, False), (False, True), (True, False), (True, True)], ids=["nn", "nt", "tn", "tt"])
+@pytest.mark.parametrize("shape", [(64, 8192, 64), (80, 8208, 48), (100, 9001, 131), (256, 12000, 130), (1024, 4112, 960), (70, 70001, 70), (64, 4095, 64)], ids=str)
+def test_matmul_long_sums(lib, ctx, shape, ta, tb):
+    m, k, n = shape
+    g = gen(sum(shape))
+    a, b = codes(g, (m, k)), codes(g, (k, n))
+    want = product64(a, b)
+    pa, pb = stored(a, ta).cuda(), stored(b, tb).cuda()
+    assert torch.equal(lib.matmul_i8(ctx, pa, pb, trans_a=ta, trans_b=tb).cpu().double(), want)
+    sa, sb = torch.rand(m, generator=g) + 0.5, torch.rand(n, generator=g) + 0.5
+    got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=torch.float32).cpu().double()
+    scaled = want * sa.double()[:, None] * sb.double()
+    assert torch.all((got - scaled).abs() <= 4 * U * scaled.abs())
