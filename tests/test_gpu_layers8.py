@@ -614,3 +614,66 @@ def test_matmul_long_sums(lib, ctx, shape, ta, tb):
     got = lib.matmul_i8(ctx, pa, pb, sa.cuda(), sb.cuda(), trans_a=ta, trans_b=tb, dtype=torch.float32).cpu().double()
     scaled = want * sa.double()[:, None] * sb.double()
     assert torch.all((got - scaled).abs() <= 4 * U * scaled.abs())
+
+
+@pytest.mark.parametrize("shape", [(4100, 70), (2049, 33), (2048, 40), (5000, 3), (300, 5), (1000, 4097), (513, 24), (2, 3000, 50), (70000, 9)], ids=str)
+@pytest.mark.parametrize("axis", [-1, -2])
+def test_quantize_long_columns(lib, ctx, shape, axis):
+    g = gen(sum(shape))
+    x = normal(g, shape, torch.bfloat16, 2.0)
+    x[..., 1] = 0
+    mult = torch.rand(shape[:-2] + (shape[axis],), generator=g) + 0.1
+    v = x.float() * mult.unsqueeze(-2 if axis == -1 else -1)
+    for where in (lambda t: t.cuda(), unaligned):
+        got = lib.quantize_i8(ctx, where(x), axis=axis, mult=mult.cuda(), values=True)
+        q, scale = got["q"].cpu(), got["scale"].cpu()
+        check_codes(v, axis, q, scale, (shape, axis))
+        assert torch.equal(got["values"].cpu(), (q.float() * scale.unsqueeze(axis)).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("shape", [(4500, 64, 80), (4200, 40, 1500), (4100, 20, 5000), (4097, 17, 9000), (4096, 33, 700), (4100, 24, 2050)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_matmul_backward_many_rows(lib, ctx, shape, dtype):
+    """Both quantisations share a pass over the gradient; an empty row and column, and one that holds an infinity."""
+    m, k, n = shape
+    t = TYPES[dtype]
+    g = gen(sum(shape))
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw, dy = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1, normal(g, (m, n), t, 0.1)
+    dy[7] = 0
+    dy[:, 3] = 0
+    for bad in (False, True):
+        if bad:
+            dy[11, 5] = float("inf")
+        got = lib.matmul_i8_backward(ctx, unaligned(dy) if bad else dy.cuda(), a.cuda(), sa.cuda(), w.cuda(), sw.cuda())
+        q, tq = codes32(dy.float() * sw, 1)
+        p, u = codes32(dy.float() * sa[:, None], 0)
+        if bad:
+            assert torch.all(torch.isnan(got["da"][11])) and torch.all(torch.isnan(got["dw"][:, 5]))
+            q[11], p[:, 5], tq[11], u[:, 5] = 0, 0, 0, 0
+        da, dw = product64(q, w.t()) * tq, product64(a.t(), p) * u
+        ga, gw = got["da"].cpu().double(), got["dw"].cpu().double()
+        if bad:
+            ga[11], gw[:, 5] = 0, 0
+        assert torch.all((ga - da).abs() <= 6 * U * da.abs() + 1.001 * HALF_ULP[t] * da.abs() + TINY[t])
+        assert torch.all((gw - dw).abs() <= 6 * U * dw.abs())
+
+
+@pytest.mark.parametrize("shape", [(5, 7), (3, 8), (600, 1024), (513, 100), (512, 4096), (40, 3), (700, 2000)], ids=str)
+def test_norm_of_narrow_and_tall(lib, ctx, shape):
+    g = gen(sum(shape))
+    x, dy = normal(g, shape, torch.float32, 2.0), normal(g, shape, torch.float32, 0.1)
+    w = 1 + 0.3 * torch.randn(shape[1], generator=g)
+    got = lib.rmsnorm_i8(ctx, x.cuda(), w.cuda(), eps=1e-5)
+    xd = x.double()
+    rstd = (xd.square().mean(1) + 1e-5) ** -0.5
+    assert torch.all((got["rstd"].cpu().double() - rstd).abs() <= (threads_terms(shape[1]) + 20) * U * rstd)
+    check_codes(x * w, 1, got["q"].cpu(), (x * w).abs().amax(1) / 127, shape)
+    r32 = rstd.float()
+    back = lib.rmsnorm_i8_backward(ctx, dy.cuda(), x.cuda(), w.cuda(), r32.cuda())
+    r = r32.double()[:, None]
+    n, gw = xd * r, dy.double() * w.double()
+    dx = r * (gw - n * (gw * n).mean(1, keepdim=True))
+    err = r * (5 * U * gw.abs() + n.abs() * (threads_terms(shape[1]) + 24) * U * (gw * n).abs().mean(1, keepdim=True)) + 2.0 ** -149
+    assert torch.all((back["dx"].cpu().double() - dx).abs() <= err + 2 * U * dx.abs())
+    assert torch.all((back["dweight"].cpu().double() - (dy.double() * n).sum(0)).abs() <= (shape[0] + 20) * U * (dy.double() * n).abs().sum(0))
