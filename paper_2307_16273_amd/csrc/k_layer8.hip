@@ -769,17 +769,22 @@ static void l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
         a.first[2 + i] = a.first[1 + i] + (uint32_t)(blocks < 4096 ? blocks : 4096);
     }
 #define L8_PREPARE(G, ITEMS, COL_ITEMS) hipLaunchKernelGGL((k_l8_prepare<T, G, ITEMS, COL_ITEMS>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a)
-    if (j.dy->rows > 4 * L8_ONCE_R) L8_PREPARE(64, 2, 8);       // then there are at most 1023 columns
-    else if (n <= 512) L8_PREPARE(64, 1, 4);
+    if (j.dy->rows > 4 * L8_ONCE_R) {       // at most 2046 columns
+        if (n <= 1024) L8_PREPARE(64, 2, 8);
+        else L8_PREPARE(256, 1, 8);
+    } else if (n <= 512) L8_PREPARE(64, 1, 4);
     else if (n <= 1024) L8_PREPARE(64, 2, 4);
     else if (n <= 2048) L8_PREPARE(256, 1, 4);
-    else L8_PREPARE(256, 2, 4);
+    else if (n <= 4096) L8_PREPARE(256, 2, 4);
+    else L8_PREPARE(256, 4, 4);
 #undef L8_PREPARE
 }
 
-// rows of one group's registers, columns of a block's, and no more than its scattered reads are worth
+// Rows of one group's registers, columns of a block's, and no more entries than reading the columns eight at a time is worth: whole calls
+// of zkdl_matmul_i8_backward (us, a launch for each step / all in one), rows x in x out: 1024 x 2048 x 2048 34.4 / 34.1, 300 x 500 x 8192
+// 34.7 / 32.7, 512 x 512 x 8192 36 / 40.
 bool zk_prepare_fits(const zkdl_mat* dy) {
-    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 4096 && dy->rows >= 1 && dy->rows <= 8 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)1 << 20;
+    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 8192 && dy->rows >= 1 && dy->rows <= 8 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)5 << 19;
 }
 void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job) {
     switch (job.dy->dtype) {

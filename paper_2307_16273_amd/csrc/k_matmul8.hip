@@ -290,22 +290,34 @@ __global__ __launch_bounds__(256) void k_m8_pair(M8Pair p) {
 // operand has to be turned), and the waves' sums are added at the end.
 // ---------------------------------------------------------------------------
 
+// the 16 bytes moved towards the lower ones by sh, zeros behind them
+static __device__ __forceinline__ v4i m8_shift(const v4i& f, uint32_t sh) {
+    const uint64_t lo = (uint32_t)f[0] | (uint64_t)(uint32_t)f[1] << 32, hi = (uint32_t)f[2] | (uint64_t)(uint32_t)f[3] << 32;
+    uint64_t nl = lo, nh = hi;
+    if (sh >= 16) nl = nh = 0;
+    else if (sh >= 8) nl = hi >> (8 * (sh - 8)), nh = 0;
+    else if (sh) nl = lo >> (8 * sh) | hi << (64 - 8 * sh), nh = hi >> (8 * sh);
+    return v4i{(int)(uint32_t)nl, (int)(uint32_t)(nl >> 32), (int)(uint32_t)nh, (int)(uint32_t)(nh >> 32)};
+}
+
 // A wave's share of one operand: F fragments of 16 rows of op(A) (columns of op(B)) from `at` on.  Loads wait for no branch: what lies
-// behind an edge is read from inside the matrix and shifted out (along k) or never stored (rows).
+// behind an edge is read from inside the matrix and shifted out (along memory) or never stored.
 template <int F, bool TURN>
 struct M8Few {
     const int8_t* p;
     uint64_t rs;
     uint32_t at, rows, K, l;
-    // whether that holds: at least 16 k, and whole pieces of 16 rows where memory runs along them
-    __device__ __forceinline__ bool plain() const { return TURN ? at + 16 * F <= rows : K >= 16; }
+    // whether that holds: at least 16 entries along memory
+    __device__ __forceinline__ bool plain() const { return (TURN ? rows : K) >= 16; }
+    // whether pieces of the tile cross the edge along memory
+    __device__ __forceinline__ bool ragged() const { return TURN && at + 16 * F > rows; }
     __device__ __forceinline__ void load(uint32_t k, v4i (&f)[F]) const {
 #pragma unroll
         for (int x = 0; x < F; ++x) {
             const int8_t* q;
             if (TURN) {
                 const uint32_t piece = x * 64 + l;
-                q = p + min(k + piece / F, K - 1) * rs + at + piece % F * 16;
+                q = p + min(k + piece / F, K - 1) * rs + min(at + piece % F * 16, rows - 16);
             } else {
                 q = p + min(at + x * 16 + (l & 15), rows - 1) * rs + min(k + (l >> 4) * 16, K - 16);
             }
@@ -329,14 +341,17 @@ struct M8Few {
             if (TURN) {
                 if (k + (x * 64 + l) / F >= K) f[x] = v4i{0, 0, 0, 0};
             } else {
-                const uint32_t from = k + (l >> 4) * 16, sh = from + 16 > K ? from + 16 - K : 0;     // bytes too many
-                const uint64_t lo = (uint32_t)f[x][0] | (uint64_t)(uint32_t)f[x][1] << 32, hi = (uint32_t)f[x][2] | (uint64_t)(uint32_t)f[x][3] << 32;
-                uint64_t nl = lo, nh = hi;
-                if (sh >= 16) nl = nh = 0;
-                else if (sh >= 8) nl = hi >> (8 * (sh - 8)), nh = 0;
-                else if (sh) nl = lo >> (8 * sh) | hi << (64 - 8 * sh), nh = hi >> (8 * sh);
-                f[x] = v4i{(int)(uint32_t)nl, (int)(uint32_t)(nl >> 32), (int)(uint32_t)nh, (int)(uint32_t)(nh >> 32)};
+                const uint32_t from = k + (l >> 4) * 16;
+                f[x] = m8_shift(f[x], from + 16 > K ? from + 16 - K : 0);
             }
+        }
+    }
+    // ragged(): the pieces to their places
+    __device__ __forceinline__ void place(v4i (&f)[F]) const {
+#pragma unroll
+        for (int x = 0; x < F; ++x) {
+            const uint32_t from = at + (x * 64 + l) % F * 16;
+            f[x] = m8_shift(f[x], from + 16 > rows ? from + 16 - rows : 0);
         }
     }
     // turned: from pieces of rows of k to fragments, by way of the wave's own LDS, whose operations keep their order
@@ -380,6 +395,7 @@ __global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
             for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[y], fa[x], acc[x][y], 0, 0, 0);
     };
     if (a.plain() && b.plain()) {
+        const bool ragged_a = a.ragged(), ragged_b = b.ragged();
         for (uint32_t k0 = w; k0 < steps; k0 += W * U) {
             v4i fa[U][FM], fb[U][FN];
 #pragma unroll
@@ -397,6 +413,8 @@ __global__ __launch_bounds__(512) void k_m8_few(M8Args p) {
                     a.cut(k, fa[u]);
                     b.cut(k, fb[u]);
                 }
+                if (ragged_a) a.place(fa[u]);
+                if (ragged_b) b.place(fb[u]);
                 mul(fa[u], fb[u]);
             }
         }
@@ -500,7 +518,7 @@ static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool wh
 // (A join inside the launch, by the last block of a tile, was no faster: what passes between the dies has to go past their caches.)
 static uint64_t m8_slices(uint64_t m, uint64_t n, uint64_t k) {
     const uint64_t t64 = l8_ceil(m, 64) * l8_ceil(n, 64), stages = l8_ceil(k, 128);
-    if (stages < (t64 <= 16 ? 32 : 64) || t64 > 256) return 1;
+    if (stages < (t64 <= 16 ? 24 : t64 <= 128 ? 40 : 64) || t64 > 256) return 1;
     uint64_t slices = 512 / t64;
     if (slices > stages / 4) slices = stages / 4;
     if (slices < 2) return 1;
@@ -548,6 +566,37 @@ static void m8_operands(M8Args& p, const zkdl_mat* a, const zkdl_mat* b) {
     p.b_ss = b->stack_stride;
 }
 
+// The product of operands as the chosen kernel wants them, a long k in slices.
+static int m8_run(zkdl_ctx* ctx, M8Args p, bool trans_a, bool trans_b, uint64_t stack, int choice) {
+    const M8Args joined = p;
+    int* parts = nullptr;
+    const uint64_t slices = choice == M8_TILE64 && stack == 1 ? m8_slices(p.M, p.N, p.K) : 1;
+    if (slices > 1) {
+        parts = (int*)zk_alloc(ctx, slices * p.M * p.N * 4);
+        if (!parts) return ZKDL_ENOMEM;
+        stack = slices;
+        p.all = p.K;
+        p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, slices), 128) * 128);
+        p.a_ss = trans_a ? p.K * p.a_rs : p.K;
+        p.b_ss = trans_b ? p.K : p.K * p.b_rs;
+        p.out = parts;
+        p.o_type = ZKDL_I32;
+        p.o_rs = p.N;
+        p.o_ss = (uint64_t)p.M * p.N;
+    }
+    int rc;
+    if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, stack, choice);
+    else if (trans_a) rc = m8_launch<true, false>(ctx, p, stack, choice);
+    else if (!trans_b) rc = m8_launch<false, true>(ctx, p, stack, choice);
+    else rc = m8_launch<false, false>(ctx, p, stack, choice);
+    if (parts && rc == ZKDL_OK) {
+        const uint64_t blocks = l8_ceil((uint64_t)joined.M * l8_ceil(joined.N, 4), 256);
+        hipLaunchKernelGGL(k_m8_join, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, joined, parts, (uint32_t)slices);
+    }
+    zk_free(ctx, parts);
+    return rc;
+}
+
 // a and b behind the checks; out may be empty.  padded 1, 2: a, b is the context's own memory, whose rows go on to a multiple of 16.
 static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int trans_a, int trans_b, const float* sa, const float* sb,
                       const zkdl_mat* out, int padded) {
@@ -572,37 +621,7 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
         }
     }
     m8_operands(p, &pa, &pb);
-    uint64_t stack = out->stack;
-    const M8Args joined = p;
-    int* parts = nullptr;
-    const uint64_t slices = choice == M8_TILE64 && stack == 1 ? m8_slices(p.M, p.N, p.K) : 1;
-    if (slices > 1) {
-        parts = (int*)zk_alloc(ctx, slices * p.M * p.N * 4);
-        if (!parts) {
-            zk_free(ctx, packed[0]);
-            zk_free(ctx, packed[1]);
-            return ZKDL_ENOMEM;
-        }
-        stack = slices;
-        p.all = p.K;
-        p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, slices), 128) * 128);
-        p.a_ss = trans_a ? p.K * p.a_rs : p.K;
-        p.b_ss = trans_b ? p.K : p.K * p.b_rs;
-        p.out = parts;
-        p.o_type = ZKDL_I32;
-        p.o_rs = p.N;
-        p.o_ss = (uint64_t)p.M * p.N;
-    }
-    int rc;
-    if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, stack, choice);
-    else if (trans_a) rc = m8_launch<true, false>(ctx, p, stack, choice);
-    else if (!trans_b) rc = m8_launch<false, true>(ctx, p, stack, choice);
-    else rc = m8_launch<false, false>(ctx, p, stack, choice);
-    if (parts && rc == ZKDL_OK) {
-        const uint64_t blocks = l8_ceil((uint64_t)joined.M * l8_ceil(joined.N, 4), 256);
-        hipLaunchKernelGGL(k_m8_join, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, joined, parts, (uint32_t)slices);
-    }
-    zk_free(ctx, parts);
+    const int rc = m8_run(ctx, p, trans_a != 0, trans_b != 0, out->stack, choice);
     zk_free(ctx, packed[0]);
     zk_free(ctx, packed[1]);
     return rc;
@@ -671,9 +690,10 @@ static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* 
         pair.da_blocks = (uint32_t)(l8_ceil(da->rows, 64) * l8_ceil(da->cols, 64));
         // (few rows as well: a product of their own kernel costs a launch more)
         const int c_da = m8_choose(da->rows, da->cols, n, 1, true, false), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false);
-        if (c_da > M8_TILE64 || c_dw > M8_TILE64) {
-            rc = trans_w ? m8_launch<false, true>(ctx, pair.da, 1, c_da) : m8_launch<false, false>(ctx, pair.da, 1, c_da);
-            if (rc == ZKDL_OK) rc = m8_launch<true, true>(ctx, pair.dw, 1, c_dw);
+        const bool sliced = m8_slices(pair.da.M, pair.da.N, pair.da.K) > 1 || m8_slices(pair.dw.M, pair.dw.N, pair.dw.K) > 1;
+        if (c_da > M8_TILE64 || c_dw > M8_TILE64 || sliced) {
+            rc = m8_run(ctx, pair.da, false, !trans_w, 1, c_da < M8_TILE64 ? M8_TILE64 : c_da);
+            if (rc == ZKDL_OK) rc = m8_run(ctx, pair.dw, true, false, 1, c_dw < M8_TILE64 ? M8_TILE64 : c_dw);
         } else {
             const dim3 grid((unsigned)(pair.da_blocks + l8_ceil(dw->rows, 64) * l8_ceil(dw->cols, 64)));
             if (trans_w) hipLaunchKernelGGL(k_m8_pair<true>, grid, dim3(256), 0, ctx->stream, pair);

@@ -107,9 +107,9 @@ struct Call {
         if (pitch == cols) {
             t = empty(sizes, type);
         } else {
-            c10::SmallVector<int64_t, 3> wide(sizes.begin(), sizes.end());
-            wide[d - 1] = pitch;
-            t = empty(wide, type).narrow(-1, 0, cols);
+            const int64_t strides[3] = {rows * pitch, pitch, 1};
+            t = at::Tensor(at::detail::empty_strided_cuda(sizes, at::IntArrayRef(strides + 3 - d, d), type,
+                                                          c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)device)));
         }
         *m = {t.data_ptr(), d == 3 ? (uint64_t)sizes[0] : 1, (uint64_t)rows, (uint64_t)cols, (uint64_t)pitch, (uint64_t)(rows * pitch), code_of(type), 0};
         return t;

@@ -677,3 +677,31 @@ def test_norm_of_narrow_and_tall(lib, ctx, shape):
     err = r * (5 * U * gw.abs() + n.abs() * (threads_terms(shape[1]) + 24) * U * (gw * n).abs().mean(1, keepdim=True)) + 2.0 ** -149
     assert torch.all((back["dx"].cpu().double() - dx).abs() <= err + 2 * U * dx.abs())
     assert torch.all((back["dweight"].cpu().double() - (dy.double() * n).sum(0)).abs() <= (shape[0] + 20) * U * (dy.double() * n).abs().sum(0))
+
+
+@pytest.mark.parametrize("shape", [(1, 100, 29), (3, 700, 35), (16, 129, 47), (40, 333, 31), (29, 5000, 100), (64, 515, 61), (33, 17, 33), (20, 15, 20), (17, 4100, 17)], ids=str)
+@pytest.mark.parametrize("ta,tb", [(False, False), (False, True), (True, False), (True, True)], ids=["nn", "nt", "tn", "tt"])
+def test_matmul_ragged_edges(lib, ctx, shape, ta, tb):
+    m, k, n = shape
+    g = gen(sum(shape) + 1)
+    a, b = codes(g, (m, k)), codes(g, (k, n))
+    want = product64(a, b)
+    for where in (lambda t: t.cuda(), unaligned, lambda t: unaligned(t, 3, 16)):
+        got = lib.matmul_i8(ctx, where(stored(a, ta)), where(stored(b, tb)), trans_a=ta, trans_b=tb)
+        assert torch.equal(got.cpu().double(), want)
+
+
+@pytest.mark.parametrize("shape", [(3951, 384, 29), (1068, 415, 1339), (3476, 64, 576), (128, 84, 4544), (64, 200, 8192), (2100, 33, 1990), (4095, 20, 1024), (70, 64, 5000)], ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+def test_matmul_backward_in_between(lib, ctx, shape, trans_w):
+    m, k, n = shape
+    g = gen(sum(shape))
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw, dy = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1, normal(g, (m, n), torch.float32, 0.1)
+    got = lib.matmul_i8_backward(ctx, dy.cuda(), a.cuda(), sa.cuda(), stored(w, trans_w).cuda(), sw.cuda(), trans_w=trans_w)
+    q, tq = codes32(dy * sw, 1)
+    p, u = codes32(dy * sa[:, None], 0)
+    da, dw = product64(q, w.t()) * tq, product64(a.t(), p) * u
+    gw = got["dw"].cpu().double()
+    assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
+    assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
