@@ -261,35 +261,47 @@ struct L8ColArgs {
     float* scale;                 // [stack][cols]
 };
 
-// f(m, v) for the thread's rows m, m + 32, .. < hi; four rows are read before the first of them is looked at
-template <class T, class F>
-static __device__ __forceinline__ void l8_col_walk(const L8ColArgs& a, const L8Mat<const T>& x, uint64_t s, uint64_t m, uint64_t hi, uint32_t j, F f) {
+// four rows of a thread: read before the first of them is looked at
+template <class T>
+struct L8ColRows {
+    L8Vec<T> v[4];
+    float w[4];
+    __device__ __forceinline__ void fetch(const L8Mat<const T>& x, const T* p, const float* mu, uint64_t m, uint64_t hi) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = l8_raw(p + min(m + k * L8_COL_R, hi - 1) * x.rs);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = 1.f;
+        if (mu) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = mu[min(m + k * L8_COL_R, hi - 1)];
+        }
+    }
+};
+
+// f(m, v) for the thread's rows m, m + 32, .. < hi.  WIDE: there are 8 columns and more; the last eight of a row start where that many are
+// left (what two threads both have, both write alike), and `first` holds the first four rows.
+template <class T, bool WIDE, class F>
+static __device__ __forceinline__ void l8_col_walk(const L8ColArgs& a, const L8Mat<const T>& x, uint64_t s, uint64_t m, uint64_t hi, uint32_t j,
+                                                   L8ColRows<T> first, F f) {
     const T* p = x.p + s * x.ss + j;
     const float* mu = a.mult ? a.mult + s * a.rows : nullptr;
-    if (j + 8 <= a.cols) {
-        for (; m < hi; m += 4 * L8_COL_R) {
-            L8Vec<T> v[4];
-            float w[4] = {1.f, 1.f, 1.f, 1.f};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = l8_raw(p + min(m + k * L8_COL_R, hi - 1) * x.rs);
-            if (mu) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = mu[min(m + k * L8_COL_R, hi - 1)];
-            }
+    if constexpr (WIDE) {
+        for (bool more = false; m < hi; m += 4 * L8_COL_R, more = true) {
+            if (more) first.fetch(x, p, mu, m, hi);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (m + k * L8_COL_R >= hi) break;
                 float g[8];
-                l8_floats(v[k], g);
+                l8_floats(first.v[k], g);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] *= w[k];
+                for (int i = 0; i < 8; ++i) g[i] *= first.w[k];
                 f(m + k * L8_COL_R, g);
             }
         }
     } else {
         for (; m < hi; m += L8_COL_R) {
             float g[8];
-            l8_load(p + m * x.rs, (int)(a.cols - j), g);
+            l8_load(p + m * x.rs, (int)a.cols, g);
             if (mu) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] *= mu[m];
@@ -300,27 +312,40 @@ static __device__ __forceinline__ void l8_col_walk(const L8ColArgs& a, const L8M
 }
 
 // MODE 0: largest magnitudes of a chunk -> part; 1: quantise a chunk; 2: both, the chunk being all rows
-template <class T, int MODE>
+template <class T, int MODE, bool WIDE>
 __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, L8Mat<int8_t> q, L8Mat<T> values) {
     __shared__ uint32_t s_top[L8_COL_R][L8_COL_T * 8 + 1];
+    __shared__ float s_pre[L8_COL_T * 8], s_inv[L8_COL_T * 8], s_scale[L8_COL_T * 8];
     const uint32_t tx = threadIdx.x % L8_COL_T, ty = threadIdx.x / L8_COL_T;
-    const uint32_t c0 = blockIdx.x * (L8_COL_T * 8), j = c0 + tx * 8;
+    const uint32_t c0 = blockIdx.x * (L8_COL_T * 8);
+    // threadIdx.x < 64 also: the column whose magnitude that thread finishes
+    const uint32_t j = WIDE ? l8_at(c0 + tx * 8, a.cols).start : 0, mine = WIDE ? l8_at(c0 + (threadIdx.x & 56), a.cols).start + (threadIdx.x & 7) : threadIdx.x;
     const uint64_t s = blockIdx.z;
     const uint64_t lo = blockIdx.y * a.chunk, hi = min(lo + a.chunk, a.rows);
-    const bool live = j < a.cols;
-    const int n = live ? (int)min(a.cols - j, 8u) : 0;
+    const bool live = c0 + tx * 8 < a.cols;
+    const int n = WIDE ? 8 : (int)a.cols;
     uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    L8ColRows<T> first;
+    if (WIDE && lo < hi) first.fetch(x, x.p + s * x.ss + j, a.mult ? a.mult + s * a.rows : nullptr, lo + ty, hi);
     if (MODE != 1) {
         if (live)
-            l8_col_walk(a, x, s, lo + ty, hi, j, [&](uint64_t, float(&v)[8]) {
+            l8_col_walk<T, WIDE>(a, x, s, lo + ty, hi, j, first, [&](uint64_t, float(&v)[8]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top[i] = max(top[i], l8_mag(v[i]));
             });
     } else if (live) {
-        for (uint32_t k = ty; k < a.parts; k += L8_COL_R)
+        for (uint32_t k = ty; k < a.parts; k += L8_COL_R) {
+            const uint32_t* p = a.part + (s * a.parts + k) * a.cols + j;
+            if constexpr (WIDE) {
+                const M8Bytes b = *(const M8Bytes*)p, c = *(const M8Bytes*)(p + 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) top[i] = max(top[i], a.part[(s * a.parts + k) * a.cols + j + i]);
+                for (int i = 0; i < 4; ++i) top[i] = max(top[i], b.v[i]), top[4 + i] = max(top[4 + i], c.v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) top[i] = max(top[i], p[i]);
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) s_top[ty][tx * 8 + i] = top[i];
@@ -328,10 +353,16 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
     if (threadIdx.x < L8_COL_T * 8) {
         uint32_t b = 0;
         for (int k = 0; k < L8_COL_R; ++k) b = max(b, s_top[k][threadIdx.x]);
-        s_top[0][threadIdx.x] = b;
-        if (c0 + threadIdx.x < a.cols) {
-            if (MODE == 0) a.part[(s * a.parts + blockIdx.y) * a.cols + c0 + threadIdx.x] = b;
-            else if (blockIdx.y == 0) a.scale[s * a.cols + c0 + threadIdx.x] = b < L8_INF ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+        const bool in = WIDE ? c0 + (threadIdx.x & 56) < a.cols : threadIdx.x < a.cols;
+        if (MODE == 0) {
+            if (in) a.part[(s * a.parts + blockIdx.y) * a.cols + mine] = b;
+        } else {
+            const L8Quant c = l8_quant(b);
+            const float scale = c.finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+            s_pre[threadIdx.x] = c.pre;
+            s_inv[threadIdx.x] = c.inv;
+            s_scale[threadIdx.x] = scale;
+            if (in && blockIdx.y == 0) a.scale[s * a.cols + mine] = scale;
         }
     }
     if (MODE == 0) return;
@@ -341,11 +372,12 @@ __global__ __launch_bounds__(256) void k_l8_cols(L8ColArgs a, L8Mat<const T> x, 
     float scale[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t b = s_top[0][tx * 8 + i];
-        c[i] = l8_quant(b);
-        scale[i] = c[i].finite ? __uint_as_float(b) / 127.f : __uint_as_float(0x7fc00000u);
+        scale[i] = s_scale[tx * 8 + i];
+        c[i].pre = s_pre[tx * 8 + i];
+        c[i].inv = s_inv[tx * 8 + i];
+        c[i].finite = scale[i] == scale[i];
     }
-    l8_col_walk(a, x, s, lo + ty, hi, j, [&](uint64_t m, float(&v)[8]) {
+    l8_col_walk<T, WIDE>(a, x, s, lo + ty, hi, j, first, [&](uint64_t m, float(&v)[8]) {
         int iq[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) iq[i] = l8_round(v[i], c[i]);
@@ -459,6 +491,7 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
     a.scale = scale;
     a.part = nullptr;
     const uint64_t tiles = l8_ceil(x->cols, L8_COL_T * 8);
+    const bool wide = x->cols >= 8;
     // the grid's axes hold 65535 blocks: matrices of a longer stack go in launches of their own
     for (uint64_t s0 = 0; s0 < x->stack; s0 += 65535) {
         const uint64_t ns = x->stack - s0 < 65535 ? x->stack - s0 : 65535;
@@ -473,7 +506,7 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
         a.mult = mult ? mult + s0 * x->rows : nullptr;
         a.scale = scale + s0 * x->cols;
         const dim3 grid((unsigned)tiles, a.chunks, (unsigned)ns);
-        if (x->cols >= 8 && x->rows <= L8_ONCE_R * L8_ONCE_ITEMS) {
+        if (wide && x->rows <= L8_ONCE_R * L8_ONCE_ITEMS) {
 #define L8_ONCE(CT, ITEMS) \
     hipLaunchKernelGGL((k_l8_cols_once<T, CT, ITEMS>), dim3((unsigned)l8_ceil(x->cols, CT * 8), 1, (unsigned)ns), dim3(CT * L8_ONCE_R), 0, ctx->stream, a, mx, mq, mv)
             if (l8_ceil(x->cols, 32) * ns < 64 && x->rows <= 4 * L8_ONCE_R) {
@@ -487,13 +520,13 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
             continue;
         }
         if (a.chunks == 1) {
-            hipLaunchKernelGGL((k_l8_cols<T, 2>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+            hipLaunchKernelGGL((wide ? k_l8_cols<T, 2, true> : k_l8_cols<T, 2, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
             continue;
         }
         a.part = (uint32_t*)zk_alloc(ctx, ns * a.chunks * x->cols * 4);
         if (!a.part) return ZKDL_ENOMEM;
-        hipLaunchKernelGGL((k_l8_cols<T, 0>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
-        hipLaunchKernelGGL((k_l8_cols<T, 1>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+        hipLaunchKernelGGL((wide ? k_l8_cols<T, 0, true> : k_l8_cols<T, 0, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
+        hipLaunchKernelGGL((wide ? k_l8_cols<T, 1, true> : k_l8_cols<T, 1, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
         zk_free(ctx, a.part);
     }
     return ZKDL_OK;
@@ -705,14 +738,12 @@ static int l8_both(zkdl_ctx* ctx, const L8Prepare& job) {
     c.part = a.part;
     c.parts = 1;
     l8_col_chunks(c, l8_ceil(n, L8_COL_T * 8));
-    hipLaunchKernelGGL((k_l8_cols<T, 1>), dim3((unsigned)l8_ceil(n, L8_COL_T * 8), c.chunks, 1), dim3(256), 0, ctx->stream, c, l8_mat<const T>(x),
+    hipLaunchKernelGGL((k_l8_cols<T, 1, true>), dim3((unsigned)l8_ceil(n, L8_COL_T * 8), c.chunks, 1), dim3(256), 0, ctx->stream, c, l8_mat<const T>(x),
                        l8_mat<int8_t>(job.p), L8Mat<T>{nullptr, 0, 0});
     zk_free(ctx, a.part);
     return ZKDL_OK;
 }
-// Whole calls of zkdl_matmul_i8_backward (us, three reads / two), rows x in x out: 3000 x 1000 x 1000 55.8 / 57.2, 4096 x 4096 x 4096
-// 157.4 / 155.0, 8192 x 1024 x 1024 77.7 / 65.8; up to 2048 rows the columns' codes need one read anyway (300 x 500 x 8192 45 / 51).
-bool zk_quantize_both_fits(const zkdl_mat* dy) { return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 16384 && dy->rows >= 4096; }
+bool zk_quantize_both_fits(const zkdl_mat* dy) { return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 16384; }
 int zk_quantize_both(zkdl_ctx* ctx, const L8Prepare& job) {
     switch (job.dy->dtype) {
         case ZKDL_F32: return l8_both<float>(ctx, job);

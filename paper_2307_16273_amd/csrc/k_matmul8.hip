@@ -515,10 +515,12 @@ static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool wh
 // How many slices of k tiles of 64 are worth, joined by a second launch: few tiles would leave most of the device idle over a long k.
 // Whole calls (us, one launch / slices), both operands along k: 256 x 256 with k = 2048 6.7 / 7.5, 4096 10.6 / 8.2, 8192 18.6 / 8.7, 65536
 // 129 / 15; 512 x 512 with k = 4096 10.6 / 12.0, 8192 18.7 / 13.2; 1024 x 1024 with k = 8192 19.2 / 19.4 (across 30.7 / 26.3), 65536 131 / 100.
+// fresh: an operand that the launch before wrote, which comes from farther away: gradients of 64 x 768 x 2944 22.8 / 19.3 (23 stages of one
+// of them), 4000 x 200 x 1000 47 / 41 (32), 4718 x 4544 x 31 51 / 45 (37).
 // (A join inside the launch, by the last block of a tile, was no faster: what passes between the dies has to go past their caches.)
-static uint64_t m8_slices(uint64_t m, uint64_t n, uint64_t k) {
+static uint64_t m8_slices(uint64_t m, uint64_t n, uint64_t k, bool fresh) {
     const uint64_t t64 = l8_ceil(m, 64) * l8_ceil(n, 64), stages = l8_ceil(k, 128);
-    if (stages < (t64 <= 16 ? 24 : t64 <= 128 ? 40 : 64) || t64 > 256) return 1;
+    if (stages < (t64 <= 16 ? (fresh ? 16 : 24) : t64 <= 128 ? (fresh ? 20 : 40) : 64) || t64 > 256) return 1;
     uint64_t slices = 512 / t64;
     if (slices > stages / 4) slices = stages / 4;
     if (slices < 2) return 1;
@@ -544,6 +546,10 @@ static int m8_pack_for(zkdl_ctx* ctx, zkdl_mat* m, M8PackArgs* args) {
     m->stack_stride = m->rows * pitch;
     return ZKDL_OK;
 }
+static void m8_launch_pack(zkdl_ctx* ctx, const M8PackArgs& args) {
+    const uint64_t blocks = l8_ceil(args.stack * args.rows * (args.pitch / 16), 256);
+    hipLaunchKernelGGL(k_m8_pack, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, args);
+}
 static M8Args m8_args(const zkdl_mat* out, uint32_t k, const float* sa, const float* sb) {
     M8Args p = {};
     p.out = out->data;
@@ -566,34 +572,47 @@ static void m8_operands(M8Args& p, const zkdl_mat* a, const zkdl_mat* b) {
     p.b_ss = b->stack_stride;
 }
 
-// The product of operands as the chosen kernel wants them, a long k in slices.
-static int m8_run(zkdl_ctx* ctx, M8Args p, bool trans_a, bool trans_b, uint64_t stack, int choice) {
-    const M8Args joined = p;
+// A product that tiles of 64 take in slices of k: p becomes their stack, whose 32-bit sums `parts` gets and m8_join adds up into what p was.
+struct M8Slices {
+    uint64_t count = 1;
     int* parts = nullptr;
-    const uint64_t slices = choice == M8_TILE64 && stack == 1 ? m8_slices(p.M, p.N, p.K) : 1;
-    if (slices > 1) {
-        parts = (int*)zk_alloc(ctx, slices * p.M * p.N * 4);
-        if (!parts) return ZKDL_ENOMEM;
-        stack = slices;
-        p.all = p.K;
-        p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, slices), 128) * 128);
-        p.a_ss = trans_a ? p.K * p.a_rs : p.K;
-        p.b_ss = trans_b ? p.K : p.K * p.b_rs;
-        p.out = parts;
-        p.o_type = ZKDL_I32;
-        p.o_rs = p.N;
-        p.o_ss = (uint64_t)p.M * p.N;
-    }
-    int rc;
+    M8Args joined;
+};
+static int m8_slice(zkdl_ctx* ctx, M8Args& p, bool trans_a, bool trans_b, bool fresh, M8Slices& s) {
+    s.count = m8_slices(p.M, p.N, p.K, fresh);
+    s.joined = p;
+    if (s.count == 1) return ZKDL_OK;
+    s.parts = (int*)zk_alloc(ctx, s.count * p.M * p.N * 4);
+    if (!s.parts) return ZKDL_ENOMEM;
+    p.all = p.K;
+    p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, s.count), 128) * 128);
+    p.a_ss = trans_a ? p.K * p.a_rs : p.K;
+    p.b_ss = trans_b ? p.K : p.K * p.b_rs;
+    p.out = s.parts;
+    p.o_type = ZKDL_I32;
+    p.o_rs = p.N;
+    p.o_ss = (uint64_t)p.M * p.N;
+    p.sa = p.sb = nullptr;
+    return ZKDL_OK;
+}
+static void m8_join(zkdl_ctx* ctx, const M8Slices& s) {
+    if (!s.parts) return;
+    const uint64_t blocks = l8_ceil((uint64_t)s.joined.M * l8_ceil(s.joined.N, 4), 256);
+    hipLaunchKernelGGL(k_m8_join, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, s.joined, s.parts, (uint32_t)s.count);
+}
+
+// The product of operands as the chosen kernel wants them, a long k in slices.
+static int m8_run(zkdl_ctx* ctx, M8Args p, bool trans_a, bool trans_b, uint64_t stack, bool fresh, int choice) {
+    M8Slices sl;
+    int rc = choice == M8_TILE64 && stack == 1 ? m8_slice(ctx, p, trans_a, trans_b, fresh, sl) : ZKDL_OK;
+    if (rc != ZKDL_OK) return rc;
+    stack *= sl.count;
     if (trans_a && !trans_b) rc = m8_launch<true, true>(ctx, p, stack, choice);
     else if (trans_a) rc = m8_launch<true, false>(ctx, p, stack, choice);
     else if (!trans_b) rc = m8_launch<false, true>(ctx, p, stack, choice);
     else rc = m8_launch<false, false>(ctx, p, stack, choice);
-    if (parts && rc == ZKDL_OK) {
-        const uint64_t blocks = l8_ceil((uint64_t)joined.M * l8_ceil(joined.N, 4), 256);
-        hipLaunchKernelGGL(k_m8_join, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, joined, parts, (uint32_t)slices);
-    }
-    zk_free(ctx, parts);
+    if (rc == ZKDL_OK) m8_join(ctx, sl);
+    zk_free(ctx, sl.parts);
     return rc;
 }
 
@@ -616,12 +635,11 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
                 return rc;
             }
             packed[i] = args.out;
-            const uint64_t blocks = l8_ceil(args.stack * args.rows * (args.pitch / 16), 256);
-            hipLaunchKernelGGL(k_m8_pack, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, ctx->stream, args);
+            m8_launch_pack(ctx, args);
         }
     }
     m8_operands(p, &pa, &pb);
-    const int rc = m8_run(ctx, p, trans_a != 0, trans_b != 0, out->stack, choice);
+    const int rc = m8_run(ctx, p, trans_a != 0, trans_b != 0, out->stack, padded != 0, choice);
     zk_free(ctx, packed[0]);
     zk_free(ctx, packed[1]);
     return rc;
@@ -651,7 +669,7 @@ extern "C" int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* 
 }
 
 static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w, const float* a_scale,
-                             const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw) {
+                             const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw, int c_da, int c_dw) {
     const uint64_t m = dy->rows, n = dy->cols, pitch = l8_ceil(n, 16) * 16, codes = l8_ceil(m * pitch, 256) * 256;
     int8_t* mem = (int8_t*)zk_alloc(ctx, 2 * codes + (m + n) * 4);      // q, p, t, u
     if (!mem) return ZKDL_ENOMEM;
@@ -664,40 +682,51 @@ static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* 
     job.w_scale = w_scale;
     job.t = (float*)(mem + 2 * codes);
     job.u = job.t + m;
-    if (!zk_prepare_fits(dy)) {
-        int rc = zk_quantize_both(ctx, job);
+    const bool one = zk_prepare_fits(dy), tiles64 = c_da <= M8_TILE64 && c_dw <= M8_TILE64;
+    zkdl_mat pa = *a, pw = *w;
+    int rc = ZKDL_OK;
+    if (!one) rc = zk_quantize_both(ctx, job);
+    if (!one && !tiles64) {
         if (rc == ZKDL_OK) rc = m8_product(ctx, &q, w, 0, !trans_w, job.t, nullptr, da, 1);
         if (rc == ZKDL_OK)
             rc = trans_w ? m8_product(ctx, &p, a, 1, 0, job.u, nullptr, dw, 1) : m8_product(ctx, a, &p, 1, 0, nullptr, job.u, dw, 2);
         zk_free(ctx, mem);
         return rc;
     }
-    zkdl_mat pa = *a, pw = *w;
-    int rc = ZKDL_OK;
     for (zkdl_mat* x : {&pa, &pw})
         if (rc == ZKDL_OK && !m8_whole(x, false)) {
             rc = m8_pack_for(ctx, x, &job.pack[job.packs]);
             if (rc == ZKDL_OK) ++job.packs;
         }
     if (rc == ZKDL_OK) {
-        zk_prepare(ctx, job);
+        if (one) zk_prepare(ctx, job);
+        else
+            for (int i = 0; i < job.packs; ++i) m8_launch_pack(ctx, job.pack[i]);
         M8Pair pair;
         pair.da = m8_args(da, (uint32_t)n, job.t, nullptr);
         m8_operands(pair.da, &q, &pw);
         pair.dw = m8_args(dw, (uint32_t)m, trans_w ? job.u : nullptr, trans_w ? nullptr : job.u);
         if (trans_w) m8_operands(pair.dw, &p, &pa);
         else m8_operands(pair.dw, &pa, &p);
-        pair.da_blocks = (uint32_t)(l8_ceil(da->rows, 64) * l8_ceil(da->cols, 64));
-        // (few rows as well: a product of their own kernel costs a launch more)
-        const int c_da = m8_choose(da->rows, da->cols, n, 1, true, false), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false);
-        const bool sliced = m8_slices(pair.da.M, pair.da.N, pair.da.K) > 1 || m8_slices(pair.dw.M, pair.dw.N, pair.dw.K) > 1;
-        if (c_da > M8_TILE64 || c_dw > M8_TILE64 || sliced) {
-            rc = m8_run(ctx, pair.da, false, !trans_w, 1, c_da < M8_TILE64 ? M8_TILE64 : c_da);
-            if (rc == ZKDL_OK) rc = m8_run(ctx, pair.dw, true, false, 1, c_dw < M8_TILE64 ? M8_TILE64 : c_dw);
+        if (!tiles64) {
+            rc = m8_run(ctx, pair.da, false, !trans_w, 1, true, c_da < M8_TILE64 ? M8_TILE64 : c_da);
+            if (rc == ZKDL_OK) rc = m8_run(ctx, pair.dw, true, false, 1, true, c_dw < M8_TILE64 ? M8_TILE64 : c_dw);
         } else {
-            const dim3 grid((unsigned)(pair.da_blocks + l8_ceil(dw->rows, 64) * l8_ceil(dw->cols, 64)));
-            if (trans_w) hipLaunchKernelGGL(k_m8_pair<true>, grid, dim3(256), 0, ctx->stream, pair);
-            else hipLaunchKernelGGL(k_m8_pair<false>, grid, dim3(256), 0, ctx->stream, pair);
+            M8Slices s_da, s_dw;
+            rc = m8_slice(ctx, pair.da, false, !trans_w, true, s_da);
+            if (rc == ZKDL_OK) rc = m8_slice(ctx, pair.dw, true, false, true, s_dw);
+            const uint64_t b_da = l8_ceil(da->rows, 64) * l8_ceil(da->cols, 64) * s_da.count, b_dw = l8_ceil(dw->rows, 64) * l8_ceil(dw->cols, 64) * s_dw.count;
+            if (rc == ZKDL_OK && (b_da >= M8_MAX_TILES || b_da + b_dw >= M8_MAX_TILES)) rc = ZKDL_ETOOBIG;
+            if (rc == ZKDL_OK) {
+                pair.da_blocks = (uint32_t)b_da;
+                const dim3 grid((unsigned)(b_da + b_dw));
+                if (trans_w) hipLaunchKernelGGL(k_m8_pair<true>, grid, dim3(256), 0, ctx->stream, pair);
+                else hipLaunchKernelGGL(k_m8_pair<false>, grid, dim3(256), 0, ctx->stream, pair);
+                m8_join(ctx, s_da);
+                m8_join(ctx, s_dw);
+            }
+            zk_free(ctx, s_da.parts);
+            zk_free(ctx, s_dw.parts);
         }
     }
     for (int i = 0; i < job.packs; ++i) zk_free(ctx, job.pack[i].out);
@@ -722,11 +751,18 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     // Both gradients of a small layer: everything in front of the products in one launch, and the products in another where both take tiles
     // of 64.  Whole calls (us, a launch for each step / like this), rows x in x out: 33 x 100 x 70 14.3 / 7.8, 64 x 1024 x 1024 15.1 / 9.7,
     // 333 x 1000 x 517 22.3 / 9.6, 1024 x 1024 x 1024 21.9 / 15.8, 1000 x 1000 x 1000 30.7 / 18.4.
-    if (da && dw && k && (zk_prepare_fits(dy) || zk_quantize_both_fits(dy))) {
-        const int rc = m8_both_gradients(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw);
-        if (rc != ZKDL_OK) return rc;
-        ZK_HIP(ctx, hipGetLastError());
-        return ZKDL_OK;
+    // Two reads of a larger gradient instead of three, (three / two): 2100 x 256 x 256 21.3 / 19.3, 4000 x 64 x 64 20.0 / 18.7, 3500 x 64 x 8000
+    // 72.6 / 68.2, whose products share a launch; with larger tiles 2500 x 1000 x 1000 50.3 / 53.2, 4096 x 4096 x 4096 157.4 / 155.0,
+    // 8192 x 1024 x 1024 77.7 / 65.8.
+    if (da && dw && k && n && m && st == 1) {
+        // (tiles of 64 for few rows as well: a product of their own kernel costs a launch more)
+        const int c_da = m8_choose(m, k, n, 1, true, false), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false);
+        if (zk_prepare_fits(dy) || (zk_quantize_both_fits(dy) && (m >= 4096 || (c_da <= M8_TILE64 && c_dw <= M8_TILE64)))) {
+            const int rc = m8_both_gradients(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw, c_da, c_dw);
+            if (rc != ZKDL_OK) return rc;
+            ZK_HIP(ctx, hipGetLastError());
+            return ZKDL_OK;
+        }
     }
     // the quantised gradient: rows of whole 16 bytes
     const uint64_t pitch = l8_ceil(n ? n : 1, 16) * 16;

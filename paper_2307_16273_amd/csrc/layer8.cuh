@@ -129,7 +129,8 @@ static __device__ __forceinline__ L8Quant l8_quant(uint32_t top) {
     return r;
 }
 static __device__ __forceinline__ int l8_round(float v, const L8Quant& c) {
-    return c.finite ? (int)rintf(v * c.pre * c.inv) : 0;
+    const float q = rintf(v * c.pre * c.inv);
+    return (int)(c.finite ? q : 0.f);      // (a choice of values, not a branch for each entry)
 }
 
 static __device__ __forceinline__ float l8_wave_sum(float x) {

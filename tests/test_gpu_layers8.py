@@ -705,3 +705,39 @@ def test_matmul_backward_in_between(lib, ctx, shape, trans_w):
     gw = got["dw"].cpu().double()
     assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
     assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
+
+
+@pytest.mark.parametrize("shape", [(2600, 16, 2601), (2700, 70, 2600), (64, 768, 2944), (200, 40, 2100), (2050, 5, 2560), (2200, 16, 7), (2200, 100, 8),
+                                   (2100, 40, 16400), (3000, 271, 100)], ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+def test_matmul_backward_products_in_one_launch(lib, ctx, shape, trans_w):
+    """Long sums on either side, in slices beside the other product, and gradients of every width around eight columns."""
+    m, k, n = shape
+    g = gen(sum(shape) + 5)
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw, dy = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1, normal(g, (m, n), torch.float32, 0.1)
+    q, tq = codes32(dy * sw, 1)
+    p, u = codes32(dy * sa[:, None], 0)
+    da, dw = product64(q, w.t()) * tq, product64(a.t(), p) * u
+    for where in (lambda t: t.cuda(), unaligned):
+        got = lib.matmul_i8_backward(ctx, where(dy), where(a), sa.cuda(), where(stored(w, trans_w)), sw.cuda(), trans_w=trans_w)
+        gw = got["dw"].cpu().double()
+        assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
+        assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
+
+
+@pytest.mark.parametrize("cols", [1, 7, 8, 9, 15, 63, 64, 65, 71, 130])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_quantize_columns_in_chunks(lib, ctx, cols, dtype):
+    """More rows than stay in registers; columns that hold an infinity or a NaN, the last one among them, leave their neighbours alone."""
+    t = TYPES[dtype]
+    x = normal(gen(cols), (2500, cols), t, 2.0)
+    bad = sorted({cols - 1, cols // 2})
+    x[2499, bad[-1]] = float("nan")
+    x[17, bad[0]] = float("-inf")
+    got = lib.quantize_i8(ctx, x.cuda(), axis=-2)
+    q, scale = got["q"].cpu(), got["scale"].cpu()
+    assert torch.all(torch.isnan(scale[bad])) and torch.all(q[:, bad] == 0)
+    rest = [j for j in range(cols) if j not in bad]
+    if rest:
+        check_codes(x[:, rest].float(), -2, q[:, rest], scale[rest], (cols, dtype))
