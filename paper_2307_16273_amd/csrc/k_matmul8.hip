@@ -83,6 +83,36 @@ static __device__ __forceinline__ void m8_store_as(const M8Args& p, uint64_t s, 
         }
     }
     T* o = (T*)p.out + s * p.o_ss + i * p.o_rs + j;
+    if constexpr (sizeof(T) == 2 && FN % 2 == 0) {
+        if (inside) {
+            // Of two fragments side by side every other sixteen lanes' columns change places, so that a lane has eight adjacent ones and
+            // stores 16 bytes (us, 8 / 16 bytes a lane: 8192 x 4096 x 4096 126 / 118, 8192 x 128 x 8192 45 / 35, 4718 x 31 x 4544 25.5 / 21.4).
+            const uint32_t odd = (threadIdx.x >> 4) & 1;
+            T* q = o + (odd ? 12 : 0);
+#pragma unroll
+            for (int x = 0; x < FM; ++x)
+#pragma unroll
+                for (int y = 0; y < FN; y += 2) {
+                    uint32_t v[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        M8Four<T> f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) l8_put((float)acc[x][y + h][e] * sa[x] * sb[y + h][e], f.v[e]);
+                        __builtin_memcpy(v[h], &f, 8);
+                    }
+                    M8Bytes w;
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) {
+                        const auto r = __builtin_amdgcn_permlane16_swap(v[0][d], v[1][d], false, false);
+                        w.v[d] = r[0];
+                        w.v[2 + d] = r[1];
+                    }
+                    *(M8Bytes*)(q + x * 16 * p.o_rs + y * 16) = w;
+                }
+            return;
+        }
+    }
     if (inside) {
 #pragma unroll
         for (int x = 0; x < FM; ++x)
