@@ -83,7 +83,7 @@ typedef enum {
     ZKDL_ENOMEM = -3, /* device or host allocation failed */
     ZKDL_EHIP = -4,   /* a HIP runtime call failed, or a kernel gave up waiting (zkdl_ctx_set_helper_wait) */
     ZKDL_ESMALL = -5, /* an output buffer is too small */
-    ZKDL_ETOOBIG = -6 /* the input exceeds the fixed work memory of an allocation-free entry point */
+    ZKDL_ETOOBIG = -6 /* the input exceeds the fixed work memory of an allocation-free entry point, or a limit an entry point states */
 } zkdl_err;
 
 /* The first three are what field tensors are made of; the others are for the 8-bit layers (zkdl_mat). */
@@ -566,7 +566,8 @@ int zkdl_commit_selfcheck(void);
  * These calls enqueue their kernels on the context's stream and return without waiting; scratch comes from the
  * context.  Under stream capture a call of the same sizes has to have run before, and the context is not trimmed while
  * the graph is in use.  Errors: ZKDL_EINVAL for a null pointer, a wrong type or shape; ZKDL_ETOOBIG for sums that could
- * leave 32 bits; ZKDL_ENOMEM, ZKDL_EHIP. */
+ * leave 32 bits and for what a launch cannot count (2^27 columns and more with axis 0, 2^23 tiles of a product and more);
+ * ZKDL_ENOMEM, ZKDL_EHIP. */
 typedef struct {
     void* data;
     uint64_t stack, rows, cols;

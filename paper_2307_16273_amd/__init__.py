@@ -3,6 +3,8 @@
 A thin ctypes layer over the C ABI of libzkdl.so (include/zkdl.h), with the same
 entry-point names.  It only marshals arguments: every step of a proof runs in
 the library's HIP kernels.  PyTorch is used for device memory and the stream.
+The 8-bit layers (quantisation, RMS norm, integer products and their backward
+passes) take torch tensors through a compiled module, _layers8.so.
 There is no CPU fallback: if the library is missing, importing the binding's
 functions raises.
 """

@@ -207,7 +207,7 @@ struct M8Tile {
     }
 };
 
-// BM x BN entries, WM x WN waves.  256 x 256 with 8 waves of 128 x 64: 8192 x 4096 x 4096 in 111 to 115 us whatever the layouts, 2.4 POP/s;
+// BM x BN entries, WM x WN waves.  256 x 256 with 8 waves of 128 x 64: 8192 x 4096 x 4096 in 117 to 119 us whatever the layouts, 2.3 POP/s;
 // the products alone, nothing loaded or read, take 95 us (85 on zeros: the clock gives way), so what is left is the loads' and LDS' share
 // (a stage is 2048 cycles of products, and 1536 of fragments and 512 of loads in LDS) and a tile's first loads and last stores.
 template <int BM, int BN, int WM, int WN, int STAGES, bool AT, bool BT>
