@@ -530,16 +530,19 @@ static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, int choice)
 //    not with more tiles (8 products of 64 x 1024 x 1024 9.9 / 5.4) or a k that is cut in slices (64 x 8192 x 4096 18 / 12);
 //  - operands that have to be packed first, FEW2 / TILE64 with the packing: 64 x 4001 x 4001 23 / 27, 260 x 515 x 515 13 / 11 (along k),
 //    10 / 12 (one across), 130 x 1001 x 1001 10 / 13, 260 x 1001 x 1001 17 / 13;
+//  - pair: products that may share a launch by tiles of 64, which spares 3: gradients of (rows, in, out, tiles of 128 / the pair) 64 x 768 x 2944
+//    19.5 / 14.9, 256 x 2048 x 2048 19.9 / 17.2, 3000 x 1000 x 700 48.7 / 45.3, but 1000 x 2000 x 2000 37.1 / 38.4;
 //  - tiles of 64, 128, 256 (4096 x 4096 weights, along k): 256 rows 11 / 27 / 52, 512 16 / 28 / 53, 1024 30 / 30 / 55, 2048 58 / 36 / 57,
-//    4096 114 / 66 / 61, 8192 208 / 128 / 114.  That is by how many fit the 256 compute units at once, two of the smaller ones each:
-static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole, bool across) {
+//    4096 114 / 66 / 61, 8192 208 / 128 / 114.  That is by how many fit the 256 compute units at once, two of the smaller ones each.
+static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole, bool across, bool pair = false) {
     const uint64_t few = m < n ? m : n;
     if (few <= 16) return M8_FEW1;
     auto tiles = [&](uint64_t x) { return l8_ceil(m, x) * l8_ceil(n, x) * stack; };
     const uint64_t t64 = tiles(64), t128 = tiles(128), t256 = tiles(256), work = m * n * k * stack;
     if (whole ? few <= 64 && across && k >= 2048 && k <= 4096 && t64 <= 64 : work <= (uint64_t)1 << (few <= 64 ? 30 : 27)) return M8_FEW2;
     const uint64_t c64 = t64 <= 256 ? 11 : 15 * l8_ceil(t64, 512), c128 = t128 <= 256 ? 28 : 34 * l8_ceil(t128, 512), c256 = 54 * l8_ceil(t256, 256);
-    return c64 <= c128 && c64 <= c256 ? M8_TILE64 : c128 <= c256 ? M8_TILE128 : M8_TILE256;
+    const uint64_t spare = pair && work <= (uint64_t)3 << 30 ? 3 : 0;
+    return c64 <= c128 + spare && c64 <= c256 + spare ? M8_TILE64 : c128 <= c256 ? M8_TILE128 : M8_TILE256;
 }
 
 // How many slices of k tiles of 64 are worth, joined by a second launch: few tiles would leave most of the device idle over a long k.
@@ -786,7 +789,7 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     // 8192 x 1024 x 1024 77.7 / 65.8.
     if (da && dw && k && n && m && st == 1) {
         // (tiles of 64 for few rows as well: a product of their own kernel costs a launch more)
-        const int c_da = m8_choose(m, k, n, 1, true, false), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false);
+        const int c_da = m8_choose(m, k, n, 1, true, false, true), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false, true);
         if (zk_prepare_fits(dy) || (zk_quantize_both_fits(dy) && (m >= 4096 || (c_da <= M8_TILE64 && c_dw <= M8_TILE64)))) {
             const int rc = m8_both_gradients(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw, c_da, c_dw);
             if (rc != ZKDL_OK) return rc;
