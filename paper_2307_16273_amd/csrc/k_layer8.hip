@@ -39,6 +39,8 @@ static __device__ __forceinline__ void l8_weights(const L8RowArgs& a, uint64_t s
 
 // threads of a block: four waves, or one group if that is larger
 constexpr int l8_threads(int group) { return group < 256 ? 256 : group; }
+// columns that a group of threads holds with `items` vectors of 8 each; every choice of a kernel below asks this and no number of its own
+constexpr uint64_t l8_covers(int group, int items) { return (uint64_t)group * items * 8; }
 
 // sum and maximum over the G threads of a row
 template <int G>
@@ -236,14 +238,16 @@ static void l8_launch_rows(zkdl_ctx* ctx, const L8RowArgs& a, L8Mat<const T> x, 
 #define L8_ROWS(G, ITEMS)                                                                                                              \
     hipLaunchKernelGGL((k_l8_rows<T, NORM, G, ITEMS>), dim3(l8_grid(l8_ceil(a.rows, l8_threads(G) / G))), dim3(l8_threads(G)), 0, ctx->stream, a, x, \
                        res, q, total, values)
+#define L8_ROWS_TO(G, ITEMS) if (n <= l8_covers(G, ITEMS)) L8_ROWS(G, ITEMS)
     if (n < 8) L8_ROWS(64, 0);
-    else if (n <= 512) L8_ROWS(64, 1);
-    else if (n <= 1024) L8_ROWS(64, 2);
-    else if (n <= 2048) L8_ROWS(256, 1);
-    else if (n <= 4096) L8_ROWS(256, 2);
-    else if (n <= 8192) L8_ROWS(512, 2);
-    else if (n <= 16384) L8_ROWS(1024, 2);
+    else L8_ROWS_TO(64, 1);
+    else L8_ROWS_TO(64, 2);
+    else L8_ROWS_TO(256, 1);
+    else L8_ROWS_TO(256, 2);
+    else L8_ROWS_TO(512, 2);
+    else L8_ROWS_TO(1024, 2);
     else L8_ROWS(1024, 0);
+#undef L8_ROWS_TO
 #undef L8_ROWS
 }
 
@@ -717,16 +721,18 @@ static int l8_both(zkdl_ctx* ctx, const L8Prepare& job) {
     const zkdl_mat* x = job.dy;
     L8BothArgs<T> a = {x->rows, (uint32_t)x->cols, job.a_scale, job.w_scale, job.t, nullptr, l8_mat<const T>(x), l8_mat<int8_t>(job.q)};
     const uint32_t n = a.cols;
-    uint64_t blocks = l8_ceil(a.rows, n <= 1024 ? 4 : 1);
+    uint64_t blocks = l8_ceil(a.rows, n <= l8_covers(64, 2) ? 4 : 1);
     if (blocks > 768) blocks = 768;
     a.part = (uint32_t*)zk_alloc(ctx, blocks * n * 4);
     if (!a.part) return ZKDL_ENOMEM;
-#define L8_BOTH(G, ITEMS) hipLaunchKernelGGL((k_l8_both<T, G, ITEMS>), dim3((unsigned)blocks), dim3(l8_threads(G)), 0, ctx->stream, a)
-    if (n <= 512) L8_BOTH(64, 1);
-    else if (n <= 1024) L8_BOTH(64, 2);
-    else if (n <= 2048) L8_BOTH(256, 1);
-    else if (n <= 4096) L8_BOTH(256, 2);
-    else if (n <= 8192) L8_BOTH(512, 2);
+#define L8_BOTH(G, ITEMS)           \
+    if (n <= l8_covers(G, ITEMS)) \
+    hipLaunchKernelGGL((k_l8_both<T, G, ITEMS>), dim3((unsigned)blocks), dim3(l8_threads(G)), 0, ctx->stream, a)
+    L8_BOTH(64, 1);
+    else L8_BOTH(64, 2);
+    else L8_BOTH(256, 1);
+    else L8_BOTH(256, 2);
+    else L8_BOTH(512, 2);
     else L8_BOTH(1024, 2);
 #undef L8_BOTH
     hipLaunchKernelGGL(k_l8_max_parts, dim3((unsigned)l8_ceil(n, 32)), dim3(1024), 0, ctx->stream, a.part, (uint32_t)blocks, n);
@@ -743,7 +749,7 @@ static int l8_both(zkdl_ctx* ctx, const L8Prepare& job) {
     zk_free(ctx, a.part);
     return ZKDL_OK;
 }
-bool zk_quantize_both_fits(const zkdl_mat* dy) { return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 16384; }
+bool zk_quantize_both_fits(const zkdl_mat* dy) { return dy->stack == 1 && dy->cols >= 8 && dy->cols <= l8_covers(1024, 2); }
 int zk_quantize_both(zkdl_ctx* ctx, const L8Prepare& job) {
     switch (job.dy->dtype) {
         case ZKDL_F32: return l8_both<float>(ctx, job);
@@ -774,8 +780,9 @@ __global__ __launch_bounds__(256) void k_l8_prepare(L8PrepareArgs<T> a) {
     else m8_pack(a.pack[1], b - a.first[2], a.first[3] - a.first[2]);
 }
 
+// false: nothing was launched, no kernel holds so many rows and columns
 template <class T>
-static void l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
+static bool l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
     L8PrepareArgs<T> a = {};
     a.rows.rows = a.rows.per_stack = j.dy->rows;
     a.rows.cols = (uint32_t)j.dy->cols;
@@ -792,37 +799,45 @@ static void l8_prepare(zkdl_ctx* ctx, const L8Prepare& j) {
     a.q = l8_mat<int8_t>(j.q);
     a.p = l8_mat<int8_t>(j.p);
     const uint64_t n = j.dy->cols;
-    a.first[0] = (uint32_t)l8_ceil(j.dy->rows, n <= 1024 ? 4 : 1);
+    a.first[0] = (uint32_t)l8_ceil(j.dy->rows, n <= l8_covers(64, 2) ? 4 : 1);
     a.first[1] = a.first[0] + (uint32_t)l8_ceil(n, 8);
     for (int i = 0; i < 2; ++i) {
         a.pack[i] = j.pack[i];
         const uint64_t pieces = i < j.packs ? j.pack[i].stack * j.pack[i].rows * (j.pack[i].pitch / 16) : 0, blocks = l8_ceil(pieces, 256);
         a.first[2 + i] = a.first[1 + i] + (uint32_t)(blocks < 4096 ? blocks : 4096);
     }
-#define L8_PREPARE(G, ITEMS, COL_ITEMS) hipLaunchKernelGGL((k_l8_prepare<T, G, ITEMS, COL_ITEMS>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a)
-    if (j.dy->rows > 4 * L8_ONCE_R) {       // at most 2046 columns
-        if (n <= 1024) L8_PREPARE(64, 2, 8);
-        else L8_PREPARE(256, 1, 8);
-    } else if (n <= 512) L8_PREPARE(64, 1, 4);
-    else if (n <= 1024) L8_PREPARE(64, 2, 4);
-    else if (n <= 2048) L8_PREPARE(256, 1, 4);
-    else if (n <= 4096) L8_PREPARE(256, 2, 4);
+#define L8_PREPARE(G, ITEMS, COL_ITEMS)                                                            \
+    if (n <= l8_covers(G, ITEMS) && j.dy->rows <= (uint64_t)COL_ITEMS * L8_ONCE_R)                 \
+    hipLaunchKernelGGL((k_l8_prepare<T, G, ITEMS, COL_ITEMS>), dim3(a.first[3]), dim3(256), 0, ctx->stream, a)
+    L8_PREPARE(64, 1, 4);
+    else L8_PREPARE(64, 2, 4);
+    else L8_PREPARE(256, 1, 4);
+    else L8_PREPARE(256, 2, 4);
     else L8_PREPARE(256, 4, 4);
+    else L8_PREPARE(64, 2, 8);
+    else L8_PREPARE(256, 1, 8);
+    else L8_PREPARE(256, 2, 8);     // (1025 to 1279 rows: the entries allow up to 2557 columns)
+    else return false;
 #undef L8_PREPARE
+    return true;
 }
 
 // Rows of one group's registers, columns of a block's, and no more entries than reading the columns eight at a time is worth: whole calls
 // of zkdl_matmul_i8_backward (us, a launch for each step / all in one), rows x in x out: 1024 x 2048 x 2048 34.4 / 34.1, 300 x 500 x 8192
-// 34.7 / 32.7, 512 x 512 x 8192 36 / 40.
+// 34.7 / 32.7, 512 x 512 x 8192 36 / 40; with more than 2048 columns of more than 1024 rows 1025 x 64 x 2557 33.5 / 26.7, 1152 x 1024 x 2112
+// 32.8 / 31.6.
 bool zk_prepare_fits(const zkdl_mat* dy) {
-    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= 8192 && dy->rows >= 1 && dy->rows <= 8 * L8_ONCE_R && dy->rows * dy->cols <= (uint64_t)5 << 19;
+    return dy->stack == 1 && dy->cols >= 8 && dy->cols <= l8_covers(256, 4) && dy->rows >= 1 && dy->rows <= 8 * L8_ONCE_R &&
+           dy->rows * dy->cols <= (uint64_t)5 << 19;
 }
-void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job) {
+int zk_prepare(zkdl_ctx* ctx, const L8Prepare& job) {
+    bool held;
     switch (job.dy->dtype) {
-        case ZKDL_F32: l8_prepare<float>(ctx, job); break;
-        case ZKDL_F16: l8_prepare<__half>(ctx, job); break;
-        default: l8_prepare<bf16_t>(ctx, job);
+        case ZKDL_F32: held = l8_prepare<float>(ctx, job); break;
+        case ZKDL_F16: held = l8_prepare<__half>(ctx, job); break;
+        default: held = l8_prepare<bf16_t>(ctx, job);
     }
+    return held ? ZKDL_OK : ZKDL_ETOOBIG;
 }
 
 // ---------------------------------------------------------------------------
@@ -1054,7 +1069,7 @@ __global__ __launch_bounds__(1024) void k_l8_sum_shares(const float* part, uint3
 template <class T>
 static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const zkdl_mat* h, const zkdl_mat* dt, const zkdl_mat* dx, float* dweight) {
     const uint32_t n = a.cols;
-    const bool wave = n <= 1024, regs = n >= 8 && n <= 16384;
+    const bool wave = n <= l8_covers(64, 2), regs = n >= 8 && n <= l8_covers(1024, 2);
     uint64_t blocks = l8_ceil(a.rows, wave ? 4 : 1);
     if (blocks > 768) blocks = 768;
     const uint64_t col_rows = a.rows < 64 ? a.rows : 64;
@@ -1062,7 +1077,7 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
     // The gradients of few rows are summed by columns in blocks of the same launch, which read them once more, from L2; otherwise the blocks'
     // shares are summed by a second one.  Whole calls (us, second launch / same launch) with 128, 1024, 4096 columns: 64 rows 8.2 / 4.9,
     // 8.6 / 5.0, 8.5 / 5.0; 512 rows 8.4 / 6.8, 8.4 / 7.2, 11.2 / 8.1; 1024 rows 8.6 / 10.6, 8.4 / 11.3, 14.4 / 14.1.
-    const bool together = dweight && regs && n <= 4096 && a.rows <= 512;
+    const bool together = dweight && n >= 8 && n <= l8_covers(256, 2) && a.rows <= 512;
     if (together) {
         a.dweight = dweight;
         blocks += l8_ceil(n, 64);
@@ -1072,16 +1087,17 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
     }
     const L8Mat<const T> mdy = l8_mat<const T>(dy), mh = l8_mat<const T>(h), mdt = l8_mat<const T>(dt);
     const L8Mat<T> mdx = l8_mat<T>(dx);
-#define L8_BACK(G, ITEMS) \
+#define L8_BACK(G, ITEMS)           \
+    if (n <= l8_covers(G, ITEMS)) \
     hipLaunchKernelGGL((k_l8_norm_back<T, G, ITEMS>), dim3((unsigned)blocks), dim3(l8_threads(G)), 0, ctx->stream, a, mdy, mh, mdt, mdx)
     if (!regs) {
         hipLaunchKernelGGL((k_l8_norm_back_long<T>), dim3(l8_grid(a.rows)), dim3(256), 0, ctx->stream, a, mdy, mh, mdt, mdx);
         if (dweight) hipLaunchKernelGGL((k_l8_dweight_long<T>), dim3((unsigned)l8_ceil(n, 2048), (unsigned)col_rows), dim3(256), 0, ctx->stream, a, mdy, mh);
-    } else if (n <= 512) L8_BACK(64, 1);
-    else if (n <= 1024) L8_BACK(64, 2);
-    else if (n <= 2048) L8_BACK(256, 1);
-    else if (n <= 4096) L8_BACK(256, 2);
-    else if (n <= 8192) L8_BACK(512, 2);
+    } else L8_BACK(64, 1);
+    else L8_BACK(64, 2);
+    else L8_BACK(256, 1);
+    else L8_BACK(256, 2);
+    else L8_BACK(512, 2);
     else L8_BACK(1024, 2);
 #undef L8_BACK
     if (a.part)

@@ -732,9 +732,11 @@ static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* 
             if (rc == ZKDL_OK) ++job.packs;
         }
     if (rc == ZKDL_OK) {
-        if (one) zk_prepare(ctx, job);
+        if (one) rc = zk_prepare(ctx, job);
         else
             for (int i = 0; i < job.packs; ++i) m8_launch_pack(ctx, job.pack[i]);
+    }
+    if (rc == ZKDL_OK) {
         M8Pair pair;
         pair.da = m8_args(da, (uint32_t)n, job.t, nullptr);
         m8_operands(pair.da, &q, &pw);

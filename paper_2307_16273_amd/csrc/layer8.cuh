@@ -228,7 +228,7 @@ struct L8Prepare {
     int packs;
 };
 bool zk_prepare_fits(const zkdl_mat* dy);
-void zk_prepare(zkdl_ctx* ctx, const L8Prepare& job);
+int zk_prepare(zkdl_ctx* ctx, const L8Prepare& job);
 // the two quantisations alone, for gradients of many rows
 bool zk_quantize_both_fits(const zkdl_mat* dy);
 int zk_quantize_both(zkdl_ctx* ctx, const L8Prepare& job);

@@ -1,0 +1,56 @@
+"""8-bit layers where one kernel or one way of the work gives way to the next: sizes on both sides of each bound.
+
+u = 2^-24 is the unit roundoff of 32-bit floats."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def codes(g, shape):
+    return torch.randint(-128, 128, shape, generator=g, dtype=torch.int32).to(torch.int8)
+
+
+def codes32(v, axis):
+    """The operator's quantisation in its own 32-bit steps."""
+    top = v.abs().amax(axis, keepdim=True)
+    inv = torch.where(top > 0, torch.full_like(top, 127.0) / top, torch.zeros_like(top))
+    return torch.round(v * inv), top.double() / 127
+
+
+# rows x in x out.  The gradient's preparation: 1024 | 1025 and 2048 | 2049 rows, 512, 1024, 2048, 4096 columns | one more, 8192 | 8193, and
+# 5 * 2^19 entries | more (1025 x 2557 | 2558, 1279 x 2049, 1280 x 2048 | 2049); the two quantisations in one pass: the same widths to 16384 | 16385.
+PREPARED = [(1025, 40, 2557), (1025, 40, 2558), (1088, 64, 2304), (1100, 33, 2300), (1152, 48, 2112), (1279, 33, 2049), (1279, 17, 2050), (1280, 33, 2048),
+            (1281, 40, 2047), (1280, 16, 2049), (1024, 40, 2560), (1024, 40, 2561), (1024, 24, 2049), (1025, 24, 512), (1025, 24, 513), (1024, 24, 1024),
+            (1025, 24, 1025), (2048, 24, 1025), (2048, 24, 1280), (2049, 24, 1281), (640, 24, 4096), (639, 24, 4097), (320, 24, 8192), (319, 24, 8193),
+            (4096, 17, 4097), (4096, 17, 8193), (4096, 16, 16384), (4096, 16, 16385)]
+
+
+@pytest.mark.parametrize("shape", PREPARED, ids=str)
+@pytest.mark.parametrize("trans_w", [False, True])
+def test_gradients_on_both_sides_of_each_bound(lib, ctx, shape, trans_w):
+    """The largest magnitudes of half of the rows stand in the last columns: one that is not looked at changes its row's scale."""
+    m, k, n = shape
+    g = gen(sum(shape))
+    a, w = codes(g, (m, k)), codes(g, (k, n))
+    sa, sw = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) + 0.1
+    dy = torch.randn((m, n), generator=g) * 0.1
+    dy[::2, -1] = 3.0
+    dy[::4, -2] = -5.0
+    q, tq = codes32(dy * sw, 1)
+    p, u = codes32(dy * sa[:, None], 0)
+    da, dw = (q.double() @ w.double().t()) * tq, (a.double().t() @ p.double()) * u
+    dev = dy.cuda(), a.cuda(), sa.cuda(), (w.t().contiguous() if trans_w else w).cuda(), sw.cuda()
+    got = lib.matmul_i8_backward(ctx, *dev, trans_w=trans_w)
+    gw = got["dw"].cpu().double()
+    assert torch.all((got["da"].cpu().double() - da).abs() <= 6 * U * da.abs())
+    assert torch.all(((gw.t() if trans_w else gw) - dw).abs() <= 6 * U * dw.abs())
+    # either gradient alone is made by other kernels, of the same codes
+    assert torch.equal(lib.matmul_i8_backward(ctx, *dev, trans_w=trans_w, need_dw=False)["da"], got["da"])
+    assert torch.equal(lib.matmul_i8_backward(ctx, *dev, trans_w=trans_w, need_da=False)["dw"], got["dw"])
