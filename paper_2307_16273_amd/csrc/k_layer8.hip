@@ -66,9 +66,10 @@ static __device__ __forceinline__ void l8_row_reduce(float& sum, uint32_t& top) 
     }
 }
 
-// the mean square's root when the squares left the range (or an input did): once more, 2^-80 smaller
+// the mean square's root when the squares, or their mean with eps, left the range (or an input did): once more, 2^-80 smaller.  (At that scale
+// the sum is at least 2^-64, so an eps that underflows there is lost beside it in any case.)
 template <class T, int G>
-static __device__ __forceinline__ float l8_rstd_again(const T* x, const T* r, uint32_t cols, uint32_t t) {
+static __device__ __forceinline__ float l8_rstd_again(const T* x, const T* r, uint32_t cols, float eps, uint32_t t) {
     float again = 0.f;
     uint32_t unused = 0;
 #pragma unroll 1
@@ -84,7 +85,7 @@ static __device__ __forceinline__ float l8_rstd_again(const T* x, const T* r, ui
         }
     }
     l8_row_reduce<G>(again, unused);
-    return 0x1p-80f / sqrtf(again / (float)cols);
+    return 0x1p-80f / sqrtf(again / (float)cols + eps * 0x1p-80f * 0x1p-80f);
 }
 
 template <class T, bool NORM, int G, int ITEMS>
@@ -170,7 +171,10 @@ static __device__ __forceinline__ void l8_rows(const L8RowArgs& a, const L8Mat<c
         }
         l8_row_reduce<G>(ss, top);
         float rstd = 1.f;
-        if (NORM) rstd = l8_mag(ss) >= L8_INF ? l8_rstd_again<T, G>(xr, rr, a.cols, t) : 1.f / sqrtf(ss / (float)a.cols + a.eps);
+        if (NORM) {
+            const float ms = ss / (float)a.cols + a.eps;
+            rstd = l8_mag(ms) >= L8_INF ? l8_rstd_again<T, G>(xr, rr, a.cols, a.eps, t) : 1.f / sqrtf(ms);
+        }
         const L8Quant c = l8_quant(top);
         float scale = __uint_as_float(top) / 127.f;
         if (NORM) scale = __uint_as_float(top) * rstd / 127.f;

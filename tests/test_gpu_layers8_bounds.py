@@ -54,3 +54,20 @@ def test_gradients_on_both_sides_of_each_bound(lib, ctx, shape, trans_w):
     # either gradient alone is made by other kernels, of the same codes
     assert torch.equal(lib.matmul_i8_backward(ctx, *dev, trans_w=trans_w, need_dw=False)["da"], got["da"])
     assert torch.equal(lib.matmul_i8_backward(ctx, *dev, trans_w=trans_w, need_da=False)["dw"], got["dw"])
+
+
+@pytest.mark.parametrize("cols", [7, 300, 16400])
+def test_norm_with_a_large_eps(lib, ctx, cols):
+    """eps as large as the mean square of rows whose squares, or whose mean square with eps, leave the range of 32 bits."""
+    g = gen(cols)
+    x = torch.randn((4, cols), generator=g)
+    for size, eps in ((1e19, 3e38), (2.5e19, 1e38), (1.4e19, 2.5e38), (1e19, 1e-6), (1.0, 3e38)):
+        h = x * size
+        got = lib.rmsnorm_i8(ctx, h.cuda(), torch.ones(cols, device="cuda"), eps=eps)
+        eps32 = float(torch.tensor(eps, dtype=torch.float32))
+        rstd = (h.double().square().mean(1) + eps32) ** -0.5
+        top = h.double().abs().amax(1)
+        # a thread adds at most 8 ceil(16400 / 512) = 264 squares, then 12 levels; half of that error is left by the root
+        err = (264 + 20) * U
+        assert torch.all((got["rstd"].cpu().double() - rstd).abs() <= err * rstd), (size, eps)
+        assert torch.all((got["scale"].cpu().double() - top * rstd / 127).abs() <= (err + 4 * U) * top * rstd / 127), (size, eps)
