@@ -566,7 +566,8 @@ int zkdl_commit_selfcheck(void);
  * These calls enqueue their kernels on the context's stream and return without waiting; scratch comes from the
  * context.  Under stream capture a call of the same sizes has to have run before, and the context is not trimmed while
  * the graph is in use.  Errors: ZKDL_EINVAL for a null pointer, a wrong type or shape; ZKDL_ETOOBIG for sums that could
- * leave 32 bits and for what a launch cannot count (2^27 columns and more with axis 0, 2^23 tiles of a product and more);
+ * leave 32 bits and for what a launch cannot count (2^27 columns and more with axis 0; 2^23 tiles of a product and more, of
+ * 16 x 16 entries at least, of 32 x 32 where an operand has 2^23 columns and more that do not run along the sum);
  * ZKDL_ENOMEM, ZKDL_EHIP. */
 typedef struct {
     void* data;

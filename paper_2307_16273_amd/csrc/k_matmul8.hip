@@ -534,9 +534,11 @@ static int m8_launch(zkdl_ctx* ctx, const M8Args& p, uint64_t stack, int choice)
 //    19.5 / 14.9, 256 x 2048 x 2048 19.9 / 17.2, 3000 x 1000 x 700 48.7 / 45.3, but 1000 x 2000 x 2000 37.1 / 38.4;
 //  - tiles of 64, 128, 256 (4096 x 4096 weights, along k): 256 rows 11 / 27 / 52, 512 16 / 28 / 53, 1024 30 / 30 / 55, 2048 58 / 36 / 57,
 //    4096 114 / 66 / 61, 8192 208 / 128 / 114.  That is by how many fit the 256 compute units at once, two of the smaller ones each.
-static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole, bool across, bool pair = false) {
+//  - operands that cannot be packed for the tiles (m8_packs) go to k_m8_few, which takes any strides.
+static int m8_choose(uint64_t m, uint64_t n, uint64_t k, uint64_t stack, bool whole, bool across, bool packs = true, bool pair = false) {
     const uint64_t few = m < n ? m : n;
     if (few <= 16) return M8_FEW1;
+    if (!packs) return M8_FEW2;
     auto tiles = [&](uint64_t x) { return l8_ceil(m, x) * l8_ceil(n, x) * stack; };
     const uint64_t t64 = tiles(64), t128 = tiles(128), t256 = tiles(256), work = m * n * k * stack;
     if (whole ? few <= 64 && across && k >= 2048 && k <= 4096 && t64 <= 64 : work <= (uint64_t)1 << (few <= 64 ? 30 : 27)) return M8_FEW2;
@@ -567,10 +569,12 @@ static bool m8_whole(const zkdl_mat* m, bool padded) {
     return (uintptr_t)m->data % 16 == 0 && m->row_stride % 16 == 0 && (m->stack == 1 || m->stack_stride % 16 == 0) && (padded || m->cols % 16 == 0) &&
            m->row_stride < (uint64_t)1 << 23;
 }
+// Whether a packed copy of so many columns is one that k_m8_tile can fetch.
+static bool m8_packs(uint64_t cols) { return l8_ceil(cols, 16) * 16 < (uint64_t)1 << 23; }
 // Memory for a packed copy of m, which is to be what args say; m becomes the copy.
 static int m8_pack_for(zkdl_ctx* ctx, zkdl_mat* m, M8PackArgs* args) {
+    if (!m8_packs(m->cols)) return ZKDL_ETOOBIG;
     const uint64_t pitch = l8_ceil(m->cols, 16) * 16;
-    if (pitch >= (uint64_t)1 << 23) return ZKDL_ETOOBIG;
     void* out = zk_alloc(ctx, m->stack * m->rows * pitch);
     if (!out) return ZKDL_ENOMEM;
     *args = {(const int8_t*)m->data, m->row_stride, m->stack_stride, m->rows, m->stack, pitch, (uint32_t)m->cols, (int8_t*)out};
@@ -655,7 +659,8 @@ static int m8_product(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int t
     if (out->stack == 0 || out->rows == 0 || out->cols == 0) return ZKDL_OK;
     M8Args p = m8_args(out, (uint32_t)(trans_a ? a->rows : a->cols), sa, sb);
     const bool wa = m8_whole(a, padded == 1), wb = m8_whole(b, padded == 2);
-    const int choice = p.K ? m8_choose(p.M, p.N, p.K, out->stack, wa && wb, trans_a || !trans_b) : M8_FEW1;
+    const bool packs = (wa || m8_packs(a->cols)) && (wb || m8_packs(b->cols));
+    const int choice = p.K ? m8_choose(p.M, p.N, p.K, out->stack, wa && wb, trans_a || !trans_b, packs) : M8_FEW1;
     zkdl_mat pa = *a, pb = *b;
     void* packed[2] = {nullptr, nullptr};
     if (choice >= M8_TILE64) {
@@ -789,9 +794,9 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     // Two reads of a larger gradient instead of three, (three / two): 2100 x 256 x 256 21.3 / 19.3, 4000 x 64 x 64 20.0 / 18.7, 3500 x 64 x 8000
     // 72.6 / 68.2, whose products share a launch; with larger tiles 2500 x 1000 x 1000 50.3 / 53.2, 4096 x 4096 x 4096 157.4 / 155.0,
     // 8192 x 1024 x 1024 77.7 / 65.8.
-    if (da && dw && k && n && m && st == 1) {
+    if (da && dw && k && n && m && st == 1 && m8_packs(k)) {
         // (tiles of 64 for few rows as well: a product of their own kernel costs a launch more)
-        const int c_da = m8_choose(m, k, n, 1, true, false, true), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false, true);
+        const int c_da = m8_choose(m, k, n, 1, true, false, true, true), c_dw = m8_choose(dw->rows, dw->cols, m, 1, true, false, true, true);
         if (zk_prepare_fits(dy) || (zk_quantize_both_fits(dy) && (m >= 4096 || (c_da <= M8_TILE64 && c_dw <= M8_TILE64)))) {
             const int rc = m8_both_gradients(ctx, dy, a, w, trans_w, a_scale, w_scale, da, dw, c_da, c_dw);
             if (rc != ZKDL_OK) return rc;

@@ -71,3 +71,37 @@ def test_norm_with_a_large_eps(lib, ctx, cols):
         err = (264 + 20) * U
         assert torch.all((got["rstd"].cpu().double() - rstd).abs() <= err * rstd), (size, eps)
         assert torch.all((got["scale"].cpu().double() - top * rstd / 127).abs() <= (err + 4 * U) * top * rstd / 127), (size, eps)
+
+
+@pytest.mark.parametrize("n", [3, 17, 64])
+def test_products_of_very_wide_operands(lib, ctx, n):
+    """Operands of 2^23 columns and more that do not run along k and do not start at multiples of 16 bytes: a product, and both gradients.
+    32-bit floats hold these sums exactly (16 products of magnitude 2^14)."""
+    wide, k = 2 ** 23 + 17, 16
+    g = torch.Generator(device="cuda").manual_seed(n)
+
+    def rand(shape):
+        return torch.randint(-128, 128, shape, generator=g, dtype=torch.int8, device="cuda")
+
+    a, b = rand((k, wide)), rand((k, n))
+    got = lib.matmul_i8(ctx, a, b, trans_a=True)
+    for lo in range(0, wide, 1 << 21):
+        part = slice(lo, lo + (1 << 21))
+        assert torch.equal(got[part].float(), a[:, part].float().t().contiguous() @ b.float())
+    del got
+    got = lib.matmul_i8(ctx, b, a, trans_a=True)
+    for lo in range(0, wide, 1 << 21):
+        part = slice(lo, lo + (1 << 21))
+        assert torch.equal(got[:, part].float(), b.float().t().contiguous() @ a[:, part].float())
+    del got
+    # gradients of x [n, wide] by w stored [k, wide]; dy of powers of two whose maxima are 127: the codes are dy itself
+    x, w = rand((n, wide)), a
+    dy = (torch.randint(-60, 61, (n, k), generator=g, device="cuda")).float()
+    dy.fill_diagonal_(127.0)
+    dy[:, 0], dy[0, :] = 127.0, 127.0
+    one = torch.ones(max(n, k), device="cuda")
+    got = lib.matmul_i8_backward(ctx, dy, x, one[:n], w, one[:k], trans_w=True)
+    for lo in range(0, wide, 1 << 21):
+        part = slice(lo, lo + (1 << 21))
+        da, dw = dy @ w[:, part].float(), dy.t().contiguous() @ x[:, part].float()
+        assert torch.equal(got["da"][:, part], da) and torch.equal(got["dw"][:, part], dw)
