@@ -253,7 +253,7 @@ static __device__ __forceinline__ void m8_tile_block(const M8Args& p, int8_t* ld
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) load();
     for (uint32_t k = 0; k < stages; ++k) {
-        // stage k has landed when no more is under way than the stages behind it; then everybody has also left stage k - 1
+        // stage k has landed when no more is under way than the stages behind it
         if (STAGES > 2 && stages - 1 - k >= STAGES - 2) {
             constexpr int V = (STAGES - 2) * LOADS;
             static_assert(V < 64, "counts to 63");
@@ -261,6 +261,10 @@ static __device__ __forceinline__ void m8_tile_block(const M8Args& p, int8_t* ld
         } else {
             __builtin_amdgcn_s_waitcnt(0x0f70);
         }
+        // Behind the barrier everybody has left stage k - 1, which the next loads write over: this wave's reads of it have arrived (lgkmcnt 0;
+        // its products have used them, but the compiler may move products behind the barrier).
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
