@@ -131,7 +131,7 @@ int zkdl_ctx_set_helper_wait(zkdl_ctx* ctx, uint64_t microseconds);
  * and narrow ones otherwise.  Commitments do not depend on it.  Another value: ZKDL_EINVAL. */
 int zkdl_ctx_set_commit_window_bits(zkdl_ctx* ctx, int bits);
 const char* zkdl_strerror(int err);
-/* Frees cached scratch memory (the context keeps freed blocks for reuse). */
+/* Frees cached scratch memory (the context keeps freed blocks for reuse), but for what captured calls work in. */
 int zkdl_ctx_trim(zkdl_ctx* ctx);
 
 /* ---- transcript (host side; format in the header comment of this file) ---
@@ -564,11 +564,13 @@ int zkdl_commit_selfcheck(void);
  * >= (rows - 1) row_stride + cols where stack > 1; no alignment beyond the items'.  Outputs must not overlap inputs or
  * one another.
  * These calls enqueue their kernels on the context's stream and return without waiting; scratch comes from the
- * context.  Under stream capture a call of the same sizes has to have run before, and the context is not trimmed while
- * the graph is in use.  Errors: ZKDL_EINVAL for a null pointer, a wrong type or shape; ZKDL_ETOOBIG for sums that could
- * leave 32 bits and for what a launch cannot count (2^27 columns and more with axis 0; 2^23 tiles of a product and more, of
- * 16 x 16 entries at least, of 32 x 32 where an operand has 2^23 columns and more that do not run along the sum);
- * ZKDL_ENOMEM, ZKDL_EHIP. */
+ * context.  A call can be captured into a graph once a call of the same sizes has run, with nothing of the context's made
+ * in between (ZKDL_ENOMEM if its scratch is not at hand).  The context keeps the scratch of captured calls for its graphs
+ * alone, until it is destroyed: other calls may run beside a replay, replays of graphs of one context may not run beside
+ * one another, and no graph runs once its context is destroyed.
+ * Errors: ZKDL_EINVAL for a null pointer, a wrong type or shape; ZKDL_ETOOBIG for sums that could leave 32 bits and for
+ * what a launch cannot count (2^27 columns and more with axis 0; 2^23 tiles of a product and more, of 16 x 16 entries at
+ * least, of 32 x 32 where an operand has 2^23 columns and more that do not run along the sum); ZKDL_ENOMEM, ZKDL_EHIP. */
 typedef struct {
     void* data;
     uint64_t stack, rows, cols;

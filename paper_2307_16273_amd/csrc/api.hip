@@ -14,29 +14,45 @@
 // context is on one stream, so a block may be handed out again as soon as the
 // host has released it: the kernels that used it are ahead in the stream.
 // ---------------------------------------------------------------------------
+static size_t block_bytes(size_t bytes) { return ((bytes ? bytes : 1) + 255) & ~(size_t)255; }
+
+static void* take_block(zkdl_ctx* ctx, std::multimap<size_t, void*>& blocks, size_t bytes) {
+    auto it = blocks.lower_bound(bytes);
+    if (it == blocks.end() || it->first > bytes * 2) return nullptr;
+    void* p = it->second;
+    ctx->live_blocks[p] = it->first;
+    blocks.erase(it);
+    return p;
+}
+
 void* zk_alloc(zkdl_ctx* ctx, size_t bytes) {
-    if (bytes == 0) bytes = 256;
-    bytes = (bytes + 255) & ~(size_t)255;
-    auto it = ctx->free_blocks.lower_bound(bytes);
-    if (it != ctx->free_blocks.end() && it->first <= bytes * 2) {
-        void* p = it->second;
-        ctx->live_blocks[p] = it->first;
-        ctx->free_blocks.erase(it);
-        return p;
-    }
+    bytes = block_bytes(bytes);
+    if (void* p = take_block(ctx, ctx->free_blocks, bytes)) return p;
     void* p = nullptr;
     hipError_t e = hipMalloc(&p, bytes);
-    if (e != hipSuccess) {
+    if (e == hipErrorOutOfMemory) {
         // give cached memory back and retry once
         zkdl_ctx_trim(ctx);
         e = hipMalloc(&p, bytes);
-        if (e != hipSuccess) {
-            ctx->last_hip = (int)e;
-            (void)hipGetLastError();
-            return nullptr;
-        }
+    }
+    if (e != hipSuccess) {
+        ctx->last_hip = (int)e;
+        (void)hipGetLastError();
+        return nullptr;
     }
     ctx->live_blocks[p] = bytes;
+    return p;
+}
+
+// Memory of captured calls is kept apart: every replay writes there, at any time after the call.  It goes round among the calls of the
+// context's graphs and back to the device with the context.
+void* zk_alloc_scratch(zkdl_ctx* ctx, size_t bytes) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(ctx->stream, &status) != hipSuccess) (void)hipGetLastError();      // (the launches will have the same error)
+    if (status != hipStreamCaptureStatusActive) return zk_alloc(ctx, bytes);
+    void* p = take_block(ctx, ctx->graph_blocks, block_bytes(bytes));
+    if (!p) p = zk_alloc(ctx, bytes);
+    if (p) ctx->graph_owned.insert(p);
     return p;
 }
 
@@ -44,7 +60,7 @@ void zk_free(zkdl_ctx* ctx, void* p) {
     if (!p) return;
     auto it = ctx->live_blocks.find(p);
     if (it == ctx->live_blocks.end()) return;
-    ctx->free_blocks.insert({it->second, p});
+    (ctx->graph_owned.count(p) ? ctx->graph_blocks : ctx->free_blocks).insert({it->second, p});
     ctx->live_blocks.erase(it);
 }
 
@@ -290,6 +306,7 @@ extern "C" int zkdl_ctx_destroy(zkdl_ctx* ctx) {
         (void)hipEventDestroy(sp.e1);
     }
     for (auto& kv : ctx->free_blocks) (void)hipFree(kv.second);
+    for (auto& kv : ctx->graph_blocks) (void)hipFree(kv.second);
     for (auto& kv : ctx->live_blocks) (void)hipFree(kv.first);
     (void)hipFree(ctx->dev);
     (void)hipHostFree(ctx->host_stage);

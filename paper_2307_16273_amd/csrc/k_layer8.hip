@@ -531,7 +531,7 @@ static int l8_quant_cols(zkdl_ctx* ctx, const zkdl_mat* x, const float* mult, co
             hipLaunchKernelGGL((wide ? k_l8_cols<T, 2, true> : k_l8_cols<T, 2, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
             continue;
         }
-        a.part = (uint32_t*)zk_alloc(ctx, ns * a.chunks * x->cols * 4);
+        a.part = (uint32_t*)zk_alloc_scratch(ctx, ns * a.chunks * x->cols * 4);
         if (!a.part) return ZKDL_ENOMEM;
         hipLaunchKernelGGL((wide ? k_l8_cols<T, 0, true> : k_l8_cols<T, 0, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
         hipLaunchKernelGGL((wide ? k_l8_cols<T, 1, true> : k_l8_cols<T, 1, false>), grid, dim3(256), 0, ctx->stream, a, mx, mq, mv);
@@ -727,7 +727,7 @@ static int l8_both(zkdl_ctx* ctx, const L8Prepare& job) {
     const uint32_t n = a.cols;
     uint64_t blocks = l8_ceil(a.rows, n <= l8_covers(64, 2) ? 4 : 1);
     if (blocks > 768) blocks = 768;
-    a.part = (uint32_t*)zk_alloc(ctx, blocks * n * 4);
+    a.part = (uint32_t*)zk_alloc_scratch(ctx, blocks * n * 4);
     if (!a.part) return ZKDL_ENOMEM;
 #define L8_BOTH(G, ITEMS)           \
     if (n <= l8_covers(G, ITEMS)) \
@@ -1086,7 +1086,7 @@ static int l8_norm_back(zkdl_ctx* ctx, L8BackArgs a, const zkdl_mat* dy, const z
         a.dweight = dweight;
         blocks += l8_ceil(n, 64);
     } else if (dweight) {
-        a.part = (float*)zk_alloc(ctx, (regs ? blocks : col_rows) * n * 4);
+        a.part = (float*)zk_alloc_scratch(ctx, (regs ? blocks : col_rows) * n * 4);
         if (!a.part) return ZKDL_ENOMEM;
     }
     const L8Mat<const T> mdy = l8_mat<const T>(dy), mh = l8_mat<const T>(h), mdt = l8_mat<const T>(dt);

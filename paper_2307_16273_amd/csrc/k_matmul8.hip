@@ -579,7 +579,7 @@ static bool m8_packs(uint64_t cols) { return l8_ceil(cols, 16) * 16 < (uint64_t)
 static int m8_pack_for(zkdl_ctx* ctx, zkdl_mat* m, M8PackArgs* args) {
     if (!m8_packs(m->cols)) return ZKDL_ETOOBIG;
     const uint64_t pitch = l8_ceil(m->cols, 16) * 16;
-    void* out = zk_alloc(ctx, m->stack * m->rows * pitch);
+    void* out = zk_alloc_scratch(ctx, m->stack * m->rows * pitch);
     if (!out) return ZKDL_ENOMEM;
     *args = {(const int8_t*)m->data, m->row_stride, m->stack_stride, m->rows, m->stack, pitch, (uint32_t)m->cols, (int8_t*)out};
     m->data = out;
@@ -623,7 +623,7 @@ static int m8_slice(zkdl_ctx* ctx, M8Args& p, bool trans_a, bool trans_b, bool f
     s.count = m8_slices(p.M, p.N, p.K, fresh);
     s.joined = p;
     if (s.count == 1) return ZKDL_OK;
-    s.parts = (int*)zk_alloc(ctx, s.count * p.M * p.N * 4);
+    s.parts = (int*)zk_alloc_scratch(ctx, s.count * p.M * p.N * 4);
     if (!s.parts) return ZKDL_ENOMEM;
     p.all = p.K;
     p.K = (uint32_t)(l8_ceil(l8_ceil(p.K, s.count), 128) * 128);
@@ -713,7 +713,7 @@ extern "C" int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* 
 static int m8_both_gradients(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w, const float* a_scale,
                              const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw, int c_da, int c_dw) {
     const uint64_t m = dy->rows, n = dy->cols, pitch = l8_ceil(n, 16) * 16, codes = l8_ceil(m * pitch, 256) * 256;
-    int8_t* mem = (int8_t*)zk_alloc(ctx, 2 * codes + (m + n) * 4);      // q, p, t, u
+    int8_t* mem = (int8_t*)zk_alloc_scratch(ctx, 2 * codes + (m + n) * 4);      // q, p, t, u
     if (!mem) return ZKDL_ENOMEM;
     const zkdl_mat q = {mem, 1, m, n, pitch, 0, ZKDL_I8, 0}, p = {mem + codes, 1, m, n, pitch, 0, ZKDL_I8, 0};
     L8Prepare job = {};
@@ -810,8 +810,8 @@ extern "C" int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const 
     }
     // the quantised gradient: rows of whole 16 bytes
     const uint64_t pitch = l8_ceil(n ? n : 1, 16) * 16;
-    int8_t* q = (int8_t*)zk_alloc(ctx, st * m * pitch);
-    float* scale = q ? (float*)zk_alloc(ctx, st * (m > n ? m : n) * 4) : nullptr;
+    int8_t* q = (int8_t*)zk_alloc_scratch(ctx, st * m * pitch);
+    float* scale = q ? (float*)zk_alloc_scratch(ctx, st * (m > n ? m : n) * 4) : nullptr;
     int rc = q && scale ? ZKDL_OK : ZKDL_ENOMEM;
     const zkdl_mat mq = {q, st, m, n, pitch, m * pitch, ZKDL_I8, 0};
     if (rc == ZKDL_OK && da) {

@@ -3,6 +3,7 @@
 #include <stdint.h>
 #include <stddef.h>
 #include <map>
+#include <set>
 #include <vector>
 #include <hip/hip_runtime.h>
 
@@ -95,6 +96,9 @@ struct zkdl_ctx {
     void* static_scratch;     // device address, on this context's device, of the library's static work memory
     std::multimap<size_t, void*> free_blocks;
     std::map<void*, size_t> live_blocks;
+    // what captured calls work in: their graph goes on to write there, so nobody else is given it (zk_alloc_scratch)
+    std::multimap<size_t, void*> graph_blocks;
+    std::set<void*> graph_owned;
     // per-call bookkeeping (host mirrors of device cursors)
     int n_chal;
     size_t proof_len;
@@ -147,6 +151,8 @@ void zk_prof_end(zkdl_ctx* ctx);
 // scratch allocator of the context (caches freed blocks)
 void* zk_alloc(zkdl_ctx* ctx, size_t bytes);
 void zk_free(zkdl_ctx* ctx, void* p);
+// zk_alloc for a call that may be captured into a graph
+void* zk_alloc_scratch(zkdl_ctx* ctx, size_t bytes);
 
 static inline FrTab make_tab(void* p, uint64_t ps) {
     FrTab t;

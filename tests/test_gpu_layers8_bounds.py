@@ -1,4 +1,4 @@
-"""8-bit layers where one kernel or one way of the work gives way to the next: sizes on both sides of each bound.
+"""8-bit layers where one kernel or one way of the work gives way to the next: sizes on both sides of each bound, and memory that a graph keeps.
 
 u = 2^-24 is the unit roundoff of 32-bit floats."""
 import pytest
@@ -105,3 +105,46 @@ def test_products_of_very_wide_operands(lib, ctx, n):
         part = slice(lo, lo + (1 << 21))
         da, dw = dy @ w[:, part].float(), dy.t().contiguous() @ x[:, part].float()
         assert torch.equal(got["da"][:, part], da) and torch.equal(got["dw"][:, part], dw)
+
+
+def test_a_graph_keeps_its_scratch(lib):
+    """What a captured call works in is not given to tensors of the context made later, and goes on to work when the context is trimmed."""
+    g = gen(6)
+    side = torch.cuda.Stream()
+    own = lib.Context(0, stream=side.cuda_stream)
+    a, w = codes(g, (70, 500)).cuda(), codes(g, (500, 384)).cuda()
+    sa, sw = torch.rand(70, generator=g).cuda(), torch.rand(384, generator=g).cuda()
+    dy = torch.randn((70, 384), generator=g).cuda()
+
+    def call():
+        got = lib.matmul_i8_backward(own, dy, a, sa, w, sw)
+        return got["da"], got["dw"]
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = call()
+    raws = [bytes(range(1, 9)) * (4 << k) for k in range(8, 13)]          # 32 bytes an entry
+    tabs = [lib.fr_tensor_upload(own, r, (1 << k,)) for k, r in zip(range(8, 13), raws)]
+    before = [t.download() for t in tabs]
+    for k in range(3):
+        torch.cuda.synchronize()
+        dy.copy_(torch.randn((70, 384), generator=g))
+        if k == 1:
+            own.trim()
+            junk = [torch.full((1 << 16,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        assert all(t.download() == b for t, b in zip(tabs, before))
+        with torch.cuda.stream(side):
+            eager = call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, eager))
+    assert all(torch.all(t == 7) for t in junk)
+    del graph, tabs
+    own.close()
