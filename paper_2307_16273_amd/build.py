@@ -23,27 +23,43 @@ def _compile(src):
 MODULE = os.path.join(HERE, "_layers8.so")      # Python's side of the 8-bit layers, against the installed torch
 
 
-def _module():
+def _module_command():
+    """The compiler's command for the module, or why there is none: it needs torch with its headers and g++, which the C library does not."""
+    import shutil
     import sysconfig
-    import torch
-    from torch.utils import cpp_extension
-    inc = [f"-I{d}" for d in cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/opt/rocm/include"]]
+    try:
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError as e:
+        return None, f"torch cannot be imported ({e})"
+    paths = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/opt/rocm/include"]
+    for header in ("torch/csrc/autograd/python_variable.h", "Python.h"):
+        if not any(os.path.exists(os.path.join(d, header)) for d in paths):
+            return None, f"{header} is not installed"
+    if not shutil.which("g++"):
+        return None, "g++ is not installed"
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, os.path.join(CSRC, "layers8_torch.cpp"),
-           "-o", MODULE, f"-L{lib}", f"-Wl,-rpath,{lib}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
-    return subprocess.run(cmd, capture_output=True, text=True)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in paths], os.path.join(CSRC, "layers8_torch.cpp"),
+            "-o", MODULE, f"-L{lib}", f"-Wl,-rpath,{lib}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"], ""
+
+
+def _module():
+    """Compiles the module; returns the compiler's result and, where there was nothing to run, why."""
+    if os.path.exists(MODULE):
+        os.remove(MODULE)       # one that is older than its source would be taken for this one
+    cmd, why = _module_command()
+    return (subprocess.run(cmd, capture_output=True, text=True) if cmd else None), why
 
 
 def build(verbose=True):
+    """Compiles and links libzkdl.so, then tells what became of the module: the prover is there whether or not that could be made, and the
+    8-bit layers raise ImportError without it."""
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as ex:
-        module = ex.submit(_module)
+        pending = ex.submit(_module)
         results = list(ex.map(_compile, SOURCES))
-        r = module.result()
-    if r.returncode != 0:
-        sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("g++ failed on layers8_torch.cpp")
+        module, why = pending.result()
     objs = []
     for src, obj, r in results:
         if r.returncode != 0:
@@ -59,6 +75,11 @@ def build(verbose=True):
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError("link failed")
+    if module is None:
+        sys.stderr.write(f"_layers8.so is not built, the 8-bit layers will be missing from Python: {why}\n")
+    elif module.returncode != 0:
+        sys.stderr.write(module.stdout + module.stderr)
+        raise RuntimeError("g++ failed on layers8_torch.cpp (libzkdl.so is built)")
     return OUT
 
 
