@@ -78,7 +78,16 @@ def prove(torch, zk, ctx, kept, weights):
     return res, ms, int.from_bytes(at.download(), "little") == res["claims"][0]
 
 
+def check(layers, width, batch, steps):
+    for name, n in (("layers", layers), ("width", width), ("batch", batch)):
+        if n < 1 or n & (n - 1):
+            raise ValueError(f"{name}: a power of two is needed for the proof, not {n}")
+    if steps < 1:
+        raise ValueError(f"steps: at least one is needed, whose products are proved, not {steps}")
+
+
 def run(layers=8, width=1024, batch=64, steps=5, lr=None, say=print):
+    check(layers, width, batch, steps)
     import torch
     if lr is None:
         # Steps below 2 / (largest curvature) shrink the loss.  A layer's is about the largest eigenvalue of n^T n / batch, for random
@@ -119,6 +128,10 @@ def main():
     ap.add_argument("--steps", type=int, default=5)
     ap.add_argument("--lr", type=float, default=None)
     args = ap.parse_args()
+    try:
+        check(args.layers, args.width, args.batch, args.steps)
+    except ValueError as e:
+        ap.error(str(e))
     run(args.layers, args.width, args.batch, args.steps, args.lr, lambda s: print(s, flush=True))
 
 
