@@ -593,9 +593,10 @@ int zkdl_quantize_i8(zkdl_ctx* ctx, const zkdl_mat* x, int axis, const float* mu
 /* zkdl_rmsnorm_i8: root-mean-square norm over the columns with the residual's addition in front and an 8-bit output:
  *   h = x + residual (residual may be NULL),  rstd = (mean_j h_j^2 + eps)^(-1/2),  y_j = h_j rstd weight_j,
  * y quantised as by zkdl_quantize_i8 with axis 1.  A row's rstd is one factor of all its y and leaves q as it is: q is
- * quantised from h weight, and scale is a rstd / 127.  weight: cols items of type weight_dtype, ZKDL_F32 or x's.
- * eps: positive, normal, finite.  Stacks of one.  rstd (rows floats), total (h in x's type) and values (q scale in x's
- * type) may be NULL.  h is summed in 32 bits and not rounded before the norm. */
+ * quantised from h weight, and scale is a rstd / 127; a row whose h weight overflows gives q = 0 and scale NaN.
+ * weight: cols items of type weight_dtype, ZKDL_F32 or x's.  eps: positive, normal, finite.  Stacks of one.  rstd (rows
+ * floats), total (h in x's type) and values (q scale in x's type) may be NULL.  h is summed in 32 bits and not rounded
+ * before the norm. */
 int zkdl_rmsnorm_i8(zkdl_ctx* ctx, const zkdl_mat* x, const zkdl_mat* residual, const void* weight, int weight_dtype,
                     float eps, const zkdl_mat* q, float* scale, float* rstd, const zkdl_mat* total, const zkdl_mat* values);
 

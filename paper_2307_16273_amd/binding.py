@@ -683,6 +683,7 @@ def aggregate_verify(ctx, proof, tr):
 # their kernels on the context's stream and return without waiting.  Where the current stream is another one, each of the
 # two waits for the other, so that inputs and outputs are the current stream's as with any torch operator.  Tensors are
 # looked at and made in compiled code (csrc/layers8_torch.cpp): for a single token, Python would take longer than the GPU.
+# They record nothing for autograd: the outputs of tensors that require a gradient do not, and the backward passes are calls of their own.
 
 _L8 = None
 

@@ -1,4 +1,4 @@
-"""Trains a small residual network in 8-bit integers on the GPU, answers with it row by row, and proves the integer products of its last step.
+"""Trains a small residual network in 8-bit integers on the GPU, answers with it row by row, and proves the forward products of its last step.
 
     python -m paper_2307_16273_amd.train_quantized [--layers 8] [--width 1024] [--batch 64] [--steps 5] [--lr X]
 
@@ -7,7 +7,8 @@ each column; its output is added to the stream by the next layer's norm.  Gradie
 output of a network of other weights; the loss is half the mean square of the difference.  After the last step
   - the forward pass runs once more for single rows, as a serving program would, and has to give the batch's rows bit for bit;
   - sumcheck_matmul proves the products of all layers on the stacks of 8-bit activations and weights, and its claim on their result is
-    compared with the multilinear extension of the int32 accumulators that matmul_i8 returns.
+    compared with the multilinear extension of the int32 accumulators that matmul_i8 returns.  (The integers of the gradients stay inside
+    matmul_i8_backward and are not proved.)
 One line of JSON for each step and for what follows.  Layers, width and batch are powers of two, as the proof wants them.
 """
 import argparse
