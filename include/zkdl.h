@@ -626,6 +626,112 @@ int zkdl_matmul_i8(zkdl_ctx* ctx, const zkdl_mat* a, const zkdl_mat* b, int tran
 int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a, const zkdl_mat* w, int trans_w,
                             const float* a_scale, const float* w_scale, const zkdl_mat* da, const zkdl_mat* dw);
 
+/* ---- a training step's two ends: losses of tokens, and the update ------------
+ * What stands in front of a network's first gradient and behind its last one.  logits: a zkdl_mat [T, V] of ZKDL_F32 / F16 /
+ * BF16 (a stack of one, V >= 1), row t the network's output for packed row t; tokens: T integers of tokens_dtype (ZKDL_I32 / ZKDL_I64),
+ * the entry that was taken in each row.  A row whose token is negative counts for nothing: it is not read, its outputs and its
+ * gradient are zero.  A token of V and more gives NaN.  With u = logits / temperature (times 1 / temperature in 32 bits):
+ *   top = max_j u_j,  log_sum = log sum_j exp(u_j - top),  logp = u_token - top - log_sum,  p_j = exp(u_j - top - log_sum).
+ * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.
+ * dlogits: the gradient of the logits, logits' type and shape, dlogits_j = dlogp ([j = token] - p_j) / temperature; a row whose dlogp
+ * is 0 has zeros whatever it holds.  temperature: positive, normal, finite; so is its reciprocal.  Sums in 32 bits and more, in an
+ * order that depends on the sizes alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.
+ * Conventions (stream, scratch, graphs, outputs that overlap nothing) and errors as for the 8-bit layers. */
+
+/* zkdl_token_logprobs: logp, and top and log_sum for the backward pass (both may be NULL). */
+int zkdl_token_logprobs(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, float temperature, float* logp,
+                        float* top, float* log_sum);
+/* zkdl_token_logprobs_backward: dlogits from dlogp, with top and log_sum as returned. */
+int zkdl_token_logprobs_backward(zkdl_ctx* ctx, const float* dlogp, const zkdl_mat* logits, const void* tokens, int tokens_dtype,
+                                 const float* top, const float* log_sum, float temperature, const zkdl_mat* dlogits);
+
+/* zkdl_policy_loss: the clipped policy loss with a divergence term, its sums and its gradient in one pass over the logits.
+ *   r = exp(logp - old_logp),  gain = min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)  (A: advantage; 0 where A = 0),
+ *   d = ref_logp - logp,  k = exp(d) - d - 1  (0 where ref_logp is NULL),
+ *   sums[0] = sum_t w (kl k - gain),  sums[1] = sum_t w k,  sums[2] = sum_t w [clipped]  over the rows that count,
+ *   dlogp = w ((clipped ? 0 : -r A) + kl (1 - exp(d))),
+ * clipped where A > 0 and r > 1 + clip_high or A < 0 and r < 1 - clip_low.  weight: w, or NULL for 1 / T.
+ * 0 <= clip_low <= 1, clip_high >= 0 and finite, kl finite and 0 without ref_logp.  sums: 3 floats.  logp, dlogits may be NULL. */
+typedef struct {
+    const float *old_logp, *advantage, *ref_logp, *weight;
+    float clip_low, clip_high, kl, temperature;
+} zkdl_policy;
+int zkdl_policy_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, const zkdl_policy* terms, float* sums,
+                     float* logp, const zkdl_mat* dlogits);
+
+/* zkdl_preference_loss: pairs of packed sequences, the first of each preferred to the second.  Sequence q is rows offsets[q] ..
+ * offsets[q + 1] - 1, q < 2 pairs; offsets (2 pairs + 1 integers of offsets_dtype) do not fall and stay within 0 .. T.  Rows in front
+ * of the first and behind the last sequence count for nothing.
+ *   h_q = sum over the sequence's rows that count of (logp - ref_logp)  (average: divided by their number; 0 if there are none),
+ *   margin_i = beta (h_2i - h_2i+1),  m = margin_i - target,
+ *   l(m) = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m))  (ZKDL_PREF_LOGISTIC),  max(0, -m)  (ZKDL_PREF_HINGE),
+ *          m^2  (ZKDL_PREF_SQUARE),
+ *   loss = sum_i w_i l(m)  (weight: w, pairs floats, or NULL for 1 / pairs),
+ *   dlogp = +- w_i l'(m) beta  (average: divided by the sequence's number of rows), l'(0) = 0 for the hinge.
+ * beta, target finite; 0 <= smoothing <= 1, 0 but for the logistic form.  Sums over rows in 64 bits.  margin: pairs floats.  ref_logp, margin,
+ * logp, dlogits may be NULL. */
+enum { ZKDL_PREF_LOGISTIC = 0, ZKDL_PREF_HINGE = 1, ZKDL_PREF_SQUARE = 2 };
+typedef struct {
+    const void* offsets;
+    const float *ref_logp, *weight;
+    uint64_t pairs;
+    int32_t offsets_dtype, form, average, reserved; /* reserved: 0 */
+    float beta, target, smoothing, temperature;
+} zkdl_preference;
+int zkdl_preference_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, const zkdl_preference* terms,
+                         float* loss, float* margin, float* logp, const zkdl_mat* dlogits);
+
+/* A tensor of n adjacent entries in device memory; any alignment of its items. */
+typedef struct {
+    const void* data;
+    uint64_t n;
+    int32_t dtype; /* ZKDL_F32 / F16 / BF16 */
+    int32_t reserved; /* 0 */
+} zkdl_vec;
+/* zkdl_gradient_norm: norm = the root of the sum of all entries' squares, over `count` tensors (squares and sums in 64 bits, in an order
+ * that depends on the sizes alone); factor (may be NULL) = limit / norm where norm > limit, else 1, and NaN where the norm is not finite:
+ * zkdl_adamw_step leaves a step out then.  One float each.  limit: positive (infinity: the factor is 1). */
+int zkdl_gradient_norm(zkdl_ctx* ctx, const zkdl_vec* tensors, size_t count, float limit, float* norm, float* factor);
+
+/* zkdl_adamw_step: one step of AdamW over `count` tensors, in place.  With g = factor grad, t = the step's number (from 1 on):
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2   in 64 bits, rounded once to 32,
+ *   param <- param (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)   in 32 bits, rounded once to param's type.
+ * bits 32: m, v are n floats.  bits 8: n codes and one exponent for every 256 adjacent entries (m_scale, v_scale: ceil(n / 256) bytes; all zero
+ * stands for zeros); m, v rounded to 32 bits serve the parameter, and are then rounded to 8:
+ *   a code is a float of 3 mantissa bits: m a sign, 4 exponent bits and the mantissa, v 5 exponent bits and the mantissa.  With E =
+ *   max(40, the block's exponent) and L = 15 (m) or 31 (v), exponent e > 0 and mantissa f stand for (8 + f) 2^(E - 127 - L + e - 3), e = 0 for
+ *   f 2^(E - 127 - L - 2).  E is the (biased) exponent of the block's largest magnitude once that is rounded up to 3 mantissa bits; blocks where it
+ *   is beyond 254, or not a number, have exponent 255 and stand for NaN.
+ *   A magnitude between two codes goes to the upper one with the probability of its place between them: where its place (in 2^-20 of the
+ *   distance for e > 0) plus (b + 1/2) / 2^16 reaches 1, b the upper (m) or lower (v) 16 bits of mix(mix(key ^ block) + 0x9E3779B1 place in the
+ *   block), key = mix(mix(mix(mix(seed's lower word) ^ its upper word) ^ t) ^ the tensor's number in the call), all modulo 2^32,
+ *   mix(x): x ^= x >> 16, x *= 0x9E3779B1, x ^= x >> 15, x *= 0x85A308D3, x ^= x >> 16.  A positive v never goes to 0.
+ *   So the states' expected values are those of 32 bits: with beta2 = 0.999 a step moves v by less than any code's distance.
+ * m_value, v_value (n floats, may be NULL, bits 8 alone): the values that the new states stand for.
+ * t: `step`, or *step_ptr (an int64 in device memory) where that is not NULL, in 1 .. 2^31 - 1; lr: `lr`, or *lr_ptr (a float in device memory).
+ * factor: one float in device memory, or NULL for 1; where it is not finite, or *step_ptr not in its range, nothing changes (m_value and v_value
+ * are written).  0 <= beta1, beta2 < 1; eps positive, normal, finite; lr, decay finite.  params and grads of any of the three types, each its own.
+ * No output may overlap another tensor of the call (ZKDL_EINVAL). */
+typedef struct {
+    void* param;
+    const void* grad;
+    void *m, *v;               /* floats or codes */
+    uint8_t *m_scale, *v_scale; /* bits 8 */
+    float *m_value, *v_value;
+    uint64_t n;
+    int32_t param_dtype, grad_dtype;
+} zkdl_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, decay;
+    uint64_t seed;
+    int64_t step;
+    const int64_t* step_ptr;
+    const float* lr_ptr;
+    const float* factor;
+    int32_t bits, reserved; /* reserved: 0 */
+} zkdl_adamw;
+int zkdl_adamw_step(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const zkdl_adamw* how);
+
 /* ---- per-kernel timing (for callers that measure; paper-independent) -------
  * While enabled, the launches of the kernel classes below are bracketed by HIP
  * events on the context's stream; zkdl_ctx_profile_read returns, per class and

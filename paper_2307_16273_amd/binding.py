@@ -25,6 +25,7 @@ EXPORTED_SYMBOLS = [
     "zkdl_commit_key_create", "zkdl_commit_key_destroy", "zkdl_commit_key_generators", "hyrax_commit", "hyrax_open",
     "zkdl_commit_selfcheck", "aggregate_verify", "zkdl_host_aggregate_verify",
     "zkdl_quantize_i8", "zkdl_rmsnorm_i8", "zkdl_rmsnorm_i8_backward", "zkdl_matmul_i8", "zkdl_matmul_i8_backward",
+    "zkdl_token_logprobs", "zkdl_token_logprobs_backward", "zkdl_policy_loss", "zkdl_preference_loss", "zkdl_gradient_norm", "zkdl_adamw_step",
 ]
 
 PROF_CLASSES = {"sc_round_fused": 0, "sc_round_first": 1, "partial_eval": 2, "zk_bin": 3, "zk_lin": 4,
@@ -48,6 +49,38 @@ class FcnnWitness(C.Structure):
 class Claim(C.Structure):
     _fields_ = [("tensor", C.c_uint32), ("nseg", C.c_uint32), ("seg_off", C.c_uint32 * 4),
                 ("seg_len", C.c_uint32 * 4), ("value", C.c_uint8 * 32)]
+
+
+class Policy(C.Structure):
+    """zkdl_policy."""
+    _fields_ = [("old_logp", C.c_void_p), ("advantage", C.c_void_p), ("ref_logp", C.c_void_p), ("weight", C.c_void_p),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl", C.c_float), ("temperature", C.c_float)]
+
+
+class Preference(C.Structure):
+    """zkdl_preference."""
+    _fields_ = [("offsets", C.c_void_p), ("ref_logp", C.c_void_p), ("weight", C.c_void_p), ("pairs", C.c_uint64),
+                ("offsets_dtype", C.c_int32), ("form", C.c_int32), ("average", C.c_int32), ("reserved", C.c_int32),
+                ("beta", C.c_float), ("target", C.c_float), ("smoothing", C.c_float), ("temperature", C.c_float)]
+
+
+class Vec(C.Structure):
+    """zkdl_vec: a tensor of adjacent entries in device memory."""
+    _fields_ = [("data", C.c_void_p), ("n", C.c_uint64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AdamWTensor(C.Structure):
+    """zkdl_adamw_tensor."""
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("m_value", C.c_void_p), ("v_value", C.c_void_p), ("n", C.c_uint64),
+                ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
+
+
+class AdamW(C.Structure):
+    """zkdl_adamw."""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("decay", C.c_double),
+                ("seed", C.c_uint64), ("step", C.c_int64), ("step_ptr", C.c_void_p), ("lr_ptr", C.c_void_p), ("factor", C.c_void_p),
+                ("bits", C.c_int32), ("reserved", C.c_int32)]
 
 
 class Mat(C.Structure):
@@ -124,6 +157,12 @@ def load_library():
         "zkdl_rmsnorm_i8_backward": [vp, vp, vp, vp, i, vp, vp, vp, vp],
         "zkdl_matmul_i8": [vp, vp, vp, i, i, vp, vp, vp],
         "zkdl_matmul_i8_backward": [vp, vp, vp, vp, i, vp, vp, vp, vp],
+        "zkdl_token_logprobs": [vp, vp, vp, i, C.c_float, vp, vp, vp],
+        "zkdl_token_logprobs_backward": [vp, vp, vp, vp, i, vp, vp, C.c_float, vp],
+        "zkdl_policy_loss": [vp, vp, vp, i, vp, vp, vp, vp],
+        "zkdl_preference_loss": [vp, vp, vp, i, vp, vp, vp, vp, vp],
+        "zkdl_gradient_norm": [vp, vp, sz, C.c_float, vp, vp],
+        "zkdl_adamw_step": [vp, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -703,6 +742,8 @@ def _layers8():
         lib = load_library()
         mod.bind(*(C.cast(fn, C.c_void_p).value for fn in (lib.zkdl_quantize_i8, lib.zkdl_rmsnorm_i8, lib.zkdl_rmsnorm_i8_backward,
                                                            lib.zkdl_matmul_i8, lib.zkdl_matmul_i8_backward)))
+        mod.bind_train(*(C.cast(fn, C.c_void_p).value for fn in (lib.zkdl_token_logprobs, lib.zkdl_token_logprobs_backward, lib.zkdl_policy_loss,
+                                                                 lib.zkdl_preference_loss, lib.zkdl_gradient_norm, lib.zkdl_adamw_step)))
         _L8 = mod
     return _L8
 
@@ -767,5 +808,95 @@ def matmul_i8_backward(ctx, dy, a, a_scale, w, w_scale, trans_w=False, need_da=T
     (zkdl_matmul_i8_backward)"""
     fn = (_L8 or _layers8()).matmul_i8_backward
     args = (dy, a, a_scale, w, w_scale, bool(trans_w), bool(need_da), bool(need_dw))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
+
+
+# ---- a training step's two ends ------------------------------------------------------------------------------------------
+# Losses of the tokens that were taken in each row of a network's logits [T, V] (the rows of all sequences, one behind the other), and the
+# update of its master weights.  Streams, autograd and compiled code as for the 8-bit layers.  tokens [T], int32 or int64: a row whose token is
+# negative counts for nothing, is not read, and has zeros for outputs and gradient.
+
+PREFERENCE_FORMS = {"logistic": 0, "hinge": 1, "square": 2}
+
+
+def token_logprobs(ctx, logits, tokens, temperature=1.0):
+    """Log-probabilities of the tokens under softmax(logits / temperature).  Returns dict(logp, top, log_sum), float32 [T]: top the
+    row's largest logit (/ temperature), log_sum the logarithm of sum exp(logit / temperature - top).  (zkdl_token_logprobs)"""
+    fn = (_L8 or _layers8()).token_logprobs
+    args = (logits, tokens, temperature)
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
+
+
+def token_logprobs_backward(ctx, dlogp, logits, tokens, top, log_sum, temperature=1.0):
+    """Gradient of the logits, in their type, from dlogp, the gradient of token_logprobs' logp (float32 [T]); top and log_sum as
+    returned.  (zkdl_token_logprobs_backward)"""
+    fn = (_L8 or _layers8()).token_logprobs_backward
+    args = (dlogp, logits, tokens, top, log_sum, temperature)
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return _rest(ctx, fn, got, args) if got is None or type(got) is int else got
+
+
+def policy_loss(ctx, logits, tokens, old_logp, advantage, ref_logp=None, weight=None, clip_low=0.2, clip_high=0.2, kl=0.0, temperature=1.0,
+                gradient=True):
+    """sum_t weight (kl k - min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)), r = exp(logp - old_logp), A the advantage,
+    k = exp(d) - d - 1 with d = ref_logp - logp; float32 [T] each, weight 1 / T where there is none.  Returns dict(loss, divergence,
+    clipped, logp, dlogits): the loss, the weighted sums of k and of the clipped rows (numbers on the device), log-probabilities, and the
+    gradient of the logits in their type (None without `gradient`).  (zkdl_policy_loss)"""
+    fn = (_L8 or _layers8()).policy_loss
+    args = (logits, tokens, old_logp, advantage, ref_logp, weight, clip_low, clip_high, kl, temperature, bool(gradient))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
+
+
+def preference_loss(ctx, logits, tokens, offsets, ref_logp=None, weight=None, beta=0.1, target=0.0, smoothing=0.0, form="logistic", average=False,
+                    temperature=1.0, gradient=True):
+    """Sequence q is rows offsets[q] .. offsets[q + 1] - 1 (offsets: int32 or int64 [2 pairs + 1], not falling); the even ones are
+    preferred to the odd ones behind them.  margin = beta (h_2i - h_2i+1), h the sum (average: the mean) over a sequence of logp -
+    ref_logp; loss = sum_i weight l(margin - target), weight float32 [pairs] or 1 / pairs, l(m) by `form`: "logistic"
+    (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m)), "hinge" max(0, -m), "square" m^2.  Returns dict(loss, margin, logp, dlogits):
+    the loss (a number on the device), margins, log-probabilities (zero outside the sequences), and the gradient of the logits in
+    their type (None without `gradient`).  (zkdl_preference_loss)"""
+    if form not in PREFERENCE_FORMS:
+        raise ValueError(f"form: one of {', '.join(PREFERENCE_FORMS)}, not {form}")
+    fn = (_L8 or _layers8()).preference_loss
+    args = (logits, tokens, offsets, ref_logp, weight, beta, target, smoothing, PREFERENCE_FORMS[form], bool(average), temperature, bool(gradient))
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
+
+
+def gradient_norm(ctx, gradients, limit=float("inf")):
+    """The root of the sum of the squares of all entries of a list of contiguous tensors (float32, float16, bfloat16).  Returns dict(norm,
+    factor), numbers on the device: factor = limit / norm where norm is above the limit, else 1; NaN where the norm is not
+    finite, with which adamw_step leaves the step out.  (zkdl_gradient_norm)"""
+    fn = (_L8 or _layers8()).gradient_norm
+    args = (gradients, limit)
+    got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
+    return got if type(got) is dict else _rest(ctx, fn, got, args)
+
+
+def adamw_state(params, bits=32):
+    """The state adamw_step starts from: dict(bits, m, v, m_scale, v_scale), lists with a tensor for each parameter.  bits 32: float32;
+    bits 8: a byte an entry and one exponent (m_scale, v_scale) for every 256 of them."""
+    import torch
+    if bits not in (32, 8):
+        raise ValueError(f"bits: 32 or 8, not {bits}")
+    kind = torch.float32 if bits == 32 else torch.uint8
+    new = lambda: [torch.zeros(p.shape, dtype=kind, device=p.device) for p in params]
+    scales = lambda: [torch.zeros(-(-p.numel() // 256), dtype=torch.uint8, device=p.device) for p in params] if bits == 8 else []
+    return dict(bits=bits, m=new(), v=new(), m_scale=scales(), v_scale=scales())
+
+
+def adamw_step(ctx, params, gradients, state, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.01, factor=None, seed=0, values=False):
+    """One step of AdamW on a list of contiguous parameters (float32, float16, bfloat16), in place, in one launch for up to 40 tensors of the
+    same types; gradients: as many, of any of these types; state: adamw_state's.  step: the step's number from 1 on, or an int64 number on
+    the device; lr: a number, or a float32 number on the device (a captured call reads both at every replay).  factor: a float32 number on
+    the device that the gradients are multiplied by (gradient_norm's); where it is not finite the step is left out.  8-bit states are
+    rounded up or down at random, by seed, step, the tensor's place in the list and the entry's in the tensor.  values: the lists m, v
+    of the values that the new 8-bit states stand for.  Returns dict(m, v), None without values.  (zkdl_adamw_step)"""
+    fn = (_L8 or _layers8()).adamw_step
+    args = (params, gradients, state["m"], state["v"], state["m_scale"], state["v_scale"], step, lr, beta1, beta2, eps, decay, factor, seed,
+            state["bits"], bool(values))
     got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
     return got if type(got) is dict else _rest(ctx, fn, got, args)

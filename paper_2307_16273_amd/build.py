@@ -1,4 +1,4 @@
-"""Builds libzkdl.so (the C-ABI HIP library) for gfx950 with hipcc, and _layers8.so (Python's side of its 8-bit layers), in-tree."""
+"""Builds libzkdl.so (the C-ABI HIP library) for gfx950 with hipcc, and _layers8.so (Python's side of its 8-bit layers, losses and update), in-tree."""
 import os
 import subprocess
 import sys
@@ -7,7 +7,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libzkdl.so")
-SOURCES = ["api.hip", "k_basic.hip", "k_sumcheck.hip", "k_scpair.hip", "k_schelp.hip", "k_zkrelu.hip", "k_zkprefix.hip", "k_zkshort.hip", "k_zkhelp.hip", "k_zktail.hip", "k_reindex.hip", "k_selfbench.hip", "k_commit.hip", "k_verify.hip", "k_general.hip", "k_layer8.hip", "k_matmul8.hip"]
+SOURCES = ["api.hip", "k_basic.hip", "k_sumcheck.hip", "k_scpair.hip", "k_schelp.hip", "k_zkrelu.hip", "k_zkprefix.hip", "k_zkshort.hip", "k_zkhelp.hip", "k_zktail.hip", "k_reindex.hip", "k_selfbench.hip", "k_commit.hip", "k_verify.hip", "k_general.hip", "k_layer8.hip", "k_matmul8.hip", "k_loss.hip", "k_update.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-unknown-attributes"]
@@ -20,7 +20,7 @@ def _compile(src):
     return src, obj, r
 
 
-MODULE = os.path.join(HERE, "_layers8.so")      # Python's side of the 8-bit layers, against the installed torch
+MODULE = os.path.join(HERE, "_layers8.so")      # Python's side of the 8-bit layers, the losses and the update, against the installed torch
 
 
 def _module_command():
@@ -40,7 +40,7 @@ def _module_command():
         return None, "g++ is not installed"
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in paths], os.path.join(CSRC, "layers8_torch.cpp"),
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in paths], *[os.path.join(CSRC, src) for src in ("layers8_torch.cpp", "train_torch.cpp")],
             "-o", MODULE, f"-L{lib}", f"-Wl,-rpath,{lib}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"], ""
 
 
@@ -54,7 +54,7 @@ def _module():
 
 def build(verbose=True):
     """Compiles and links libzkdl.so, then tells what became of the module: the prover is there whether or not that could be made, and the
-    8-bit layers raise ImportError without it."""
+    8-bit layers, the losses and the update raise ImportError without it."""
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=8) as ex:
         pending = ex.submit(_module)
@@ -76,10 +76,10 @@ def build(verbose=True):
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError("link failed")
     if module is None:
-        sys.stderr.write(f"_layers8.so is not built, the 8-bit layers will be missing from Python: {why}\n")
+        sys.stderr.write(f"_layers8.so is not built, the 8-bit layers, the losses and the update will be missing from Python: {why}\n")
     elif module.returncode != 0:
         sys.stderr.write(module.stdout + module.stderr)
-        raise RuntimeError("g++ failed on layers8_torch.cpp (libzkdl.so is built)")
+        raise RuntimeError("g++ failed on layers8_torch.cpp or train_torch.cpp (libzkdl.so is built)")
     return OUT
 
 

@@ -1,0 +1,655 @@
+// Losses of tokens and their gradients (zkdl_token_logprobs, zkdl_token_logprobs_backward, zkdl_policy_loss, zkdl_preference_loss).
+//
+// A row of logits x gives, with u = x / temperature and c = max_j x_j, the sum S = sum_j exp(u_j - u_c) and with it the token's
+// log-probability and every p_j = exp(u_j - u_c) / S.  All of it is bound by memory: 2 or 4 bytes an entry read (and written) against about
+// 12 vector operations, of which the exponential takes four.  So a row is read once, all its loads under way before the first is looked at, and
+// stays in registers (128 kB of 16-bit entries at most: a block of 1024 threads with 16 vectors of eight each) until its gradient
+// leaves; only rows that are longer, few or wanted for several sequences at once (the preference's sums need all of them first) are read twice.
+#include <cfloat>
+#include <cmath>
+
+#include "layer8.cuh"
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float INF = __builtin_huge_valf(), NAN32 = __builtin_nanf("");
+
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }    // 1 ulp; 0 below 2^-126, where nothing is left of a probability
+
+// Integers of 32 or 64 bits.
+struct Ints {
+    const void* p;
+    int wide;
+    __device__ __forceinline__ int64_t at(uint64_t i) const { return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i]; }
+};
+
+struct LossArgs {
+    uint64_t rows;
+    uint32_t cols;
+    float inv_tau, k;            // 1 / temperature; log2(e) / temperature
+    Ints tokens;
+    Ints offsets;                // preference: rows outside [offsets[0], offsets[last]) count for nothing
+    uint64_t last;
+    float *logp, *top, *log_sum; // may be null
+    float* dlogp;                // preference: zeros, for the pairs to fill in
+    // policy
+    const float *old_logp, *advantage, *ref_logp, *weight;
+    float every, low, high, kl;  // the weight where there are none; 1 - clip_low, 1 + clip_high
+    float* terms;                // [3][rows]: weighted loss, divergence, clipped
+};
+
+// The row's token, or -1 where the row counts for nothing.
+__device__ __forceinline__ int64_t token_of(const LossArgs& a, uint64_t r) {
+    int64_t y = a.tokens.at(r);
+    if (a.offsets.p) {
+        const int64_t lo = a.offsets.at(0), hi = a.offsets.at(a.last);
+        if ((int64_t)r < lo || (int64_t)r >= hi) y = -1;
+    }
+    return y;
+}
+
+// Terms are exp2((x - c) k): the difference first, so that rows of the type's lowest value (masks) and of its largest stay in the range.
+__device__ __forceinline__ float term_of(float x, float c, float k) { return exp2_raw((x - c) * k); }
+
+struct RowStats {
+    float top, log_sum, logp;
+};
+__device__ __forceinline__ RowStats row_stats(const LossArgs& a, float c, float sum, int64_t y, float xy) {
+    RowStats s;
+    s.log_sum = __log2f(sum) * LN2;
+    s.top = c * a.inv_tau;
+    if (!(sum < INF)) s.top = s.log_sum = NAN32;          // a NaN, +infinity, or nothing but -infinity
+    s.logp = y >= (int64_t)a.cols ? NAN32 : (xy - c) * a.inv_tau - s.log_sum;
+    return s;
+}
+
+// exp(d) - 1 - d without what cancels: the series where d is small
+__device__ __forceinline__ float divergence_of(float d, float em) {
+    const float p = fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), .5f);
+    return fabsf(d) < .25f ? d * d * p : em - d;
+}
+
+// One row's share of the policy loss; returns dlogp.
+__device__ __forceinline__ float policy_row(const LossArgs& a, uint64_t r, float logp, float (&term)[3]) {
+    const float w = a.weight ? a.weight[r] : a.every, adv = a.advantage[r];
+    const float ratio = expf(logp - a.old_logp[r]);
+    const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
+    const float gain = adv == 0 ? 0.f : (up ? a.high : down ? a.low : ratio) * adv;
+    float slope = clipped || adv == 0 ? 0.f : -adv * ratio, div = 0.f;
+    if (a.ref_logp) {
+        const float d = a.ref_logp[r] - logp, em = expm1f(d);
+        div = divergence_of(d, em);
+        slope = fmaf(-a.kl, em, slope);
+    }
+    term[0] = w * fmaf(a.kl, div, -gain);
+    term[1] = w * div;
+    term[2] = clipped ? w : 0.f;
+    return w * slope;
+}
+__device__ __forceinline__ void put_terms(const LossArgs& a, uint64_t r, const float (&term)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) a.terms[i * a.rows + r] = term[i];
+}
+
+// c ([j = token] - p_j) of eight entries from j on, p_j = e_j inv: e comes in, the gradient goes out.
+__device__ __forceinline__ void slope8(float (&e)[8], float c, float c_inv, uint64_t j, int64_t y) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] *= -c_inv;
+    const uint64_t at = (uint64_t)y - j;
+    if (at < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] += at == i ? c : 0.f;
+    }
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+// over the G threads of a row, a block's waves with one store each
+template <int G, bool MAX>
+__device__ __forceinline__ float row_reduce(float x, float* s) {
+    x = MAX ? wave_max(x) : l8_wave_sum(x);
+    if constexpr (G > 64) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = s[0];
+#pragma unroll
+        for (int i = 1; i < G / 64; ++i) x = MAX ? fmaxf(x, s[i]) : x + s[i];
+    }
+    return x;
+}
+
+enum { ROWS_LOGP, ROWS_POLICY };
+
+// ---------------------------------------------------------------------------
+// Rows that stay in registers: G threads a row (a wave: four rows a block), ITEMS vectors of eight a thread.  8 <= cols <= 8 G ITEMS.
+// ---------------------------------------------------------------------------
+constexpr int loss_threads(int G) { return G < 256 ? 256 : G; }
+template <class T, int MODE, int G, int ITEMS>
+__global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat<const T> x, L8Mat<T> out) {
+    constexpr int GROUPS = loss_threads(G) / G;
+    __shared__ float s_max[G / 64], s_sum[G / 64];
+    const uint32_t t = threadIdx.x % G;
+    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
+    for (uint64_t r = (uint64_t)blockIdx.x * GROUPS + threadIdx.x / G; r < a.rows; r += step) {
+        const int64_t y = token_of(a, r);
+        const bool leader = t == 0;
+        if (y < 0) {
+            if (leader) {
+                if (a.logp) a.logp[r] = 0.f;
+                if (a.top) a.top[r] = 0.f;
+                if (a.log_sum) a.log_sum[r] = 0.f;
+                if (a.dlogp) a.dlogp[r] = 0.f;
+                const float none[3] = {0.f, 0.f, 0.f};
+                if (MODE == ROWS_POLICY) put_terms(a, r, none);
+            }
+            if (MODE == ROWS_POLICY && out.p) {
+                const float zero[8] = {};
+#pragma unroll
+                for (int k = 0; k < ITEMS; ++k) {
+                    const L8At at = l8_at((k * G + t) * 8, a.cols);
+                    if (at.live) l8_store(out.p + r * out.rs + at.start, 8, zero);
+                }
+            }
+            continue;
+        }
+        const T* row = x.p + r * x.rs;
+        L8Vec<T> v[ITEMS];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) v[k] = l8_raw(row + l8_at((k * G + t) * 8, a.cols).start);
+        const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
+        float c = -INF;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            float f[8];
+            l8_floats(v[k], f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c = fmaxf(c, f[i]);
+        }
+        c = row_reduce<G, true>(c, s_max);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            float f[8];
+            l8_floats(v[k], f);
+            if ((uint32_t)(k + 1) * G * 8 <= a.cols) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += term_of(f[i], c, a.k);
+            } else {            // the row's end: what another thread has, or nobody, stays out
+                const L8At at = l8_at((k * G + t) * 8, a.cols);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += at.live && (uint32_t)i >= at.dup ? term_of(f[i], c, a.k) : 0.f;
+            }
+        }
+        sum = row_reduce<G, false>(sum, s_sum);
+        const RowStats st = row_stats(a, c, sum, y, xy);
+        float term[3], dlogp = 0.f;
+        if (MODE == ROWS_POLICY) dlogp = policy_row(a, r, st.logp, term);
+        if (leader) {
+            if (a.logp) a.logp[r] = st.logp;
+            if (a.top) a.top[r] = st.top;
+            if (a.log_sum) a.log_sum[r] = st.log_sum;
+            if (a.dlogp) a.dlogp[r] = 0.f;
+            if (MODE == ROWS_POLICY) put_terms(a, r, term);
+        }
+        if (MODE == ROWS_POLICY && out.p) {
+            const float co = dlogp * a.inv_tau, co_inv = co / sum;
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const L8At at = l8_at((k * G + t) * 8, a.cols);
+                float f[8];
+                l8_floats(v[k], f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = term_of(f[i], c, a.k);
+                slope8(f, co, co_inv, at.start, y);
+                if (dlogp == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+                }
+                if (at.live) l8_store(out.p + r * out.rs + at.start, 8, f);
+            }
+        }
+        if (G > 64) __syncthreads();        // s_max and s_sum are the next row's
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rows in parts: few long rows on many blocks, rows longer than the registers, rows of less than eight.
+// A block has 2048 ITEMS entries of a row: their largest, and the sum of exp2((x - largest) k).
+// ---------------------------------------------------------------------------
+struct Part {
+    float top, sum;
+};
+template <class T, int ITEMS>
+__global__ __launch_bounds__(256) void k_loss_part(LossArgs a, L8Mat<const T> x, Part* part, uint32_t parts) {
+    __shared__ float s_max[4], s_sum[4];
+    for (uint64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+        if (token_of(a, r) < 0) continue;
+        const T* row = x.p + r * x.rs;
+        for (uint32_t q = blockIdx.x; q < parts; q += gridDim.x) {
+            float f[ITEMS][8], c = -INF, sum = 0.f;
+            int n[ITEMS];
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const uint64_t j = ((uint64_t)(q * ITEMS + k) * 256 + threadIdx.x) * 8;
+                n[k] = j < a.cols ? (int)min((uint64_t)8, a.cols - j) : 0;
+                l8_load(row + (n[k] ? j : 0), n[k], f[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) c = fmaxf(c, i < n[k] ? f[k][i] : -INF);
+            c = row_reduce<256, true>(c, s_max);
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += i < n[k] ? term_of(f[k][i], c, a.k) : 0.f;
+            sum = row_reduce<256, false>(sum, s_sum);
+            if (threadIdx.x == 0) part[r * parts + q] = {c, c == -INF ? 0.f : sum};      // a part of nothing but -infinity adds nothing
+            __syncthreads();
+        }
+    }
+}
+
+// A row's parts together, a block a row; of the policy loss the row's terms and dlogp as well.
+template <class T, int MODE>
+__global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x, const Part* part, uint32_t parts) {
+    __shared__ float s_max[4], s_sum[4];
+    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const int64_t y = token_of(a, r);
+        RowStats st = {0.f, 0.f, 0.f};
+        float term[3] = {0.f, 0.f, 0.f}, dlogp = 0.f;
+        if (y >= 0) {
+            const float xy = l8_f32(x.p[r * x.rs + (y < (int64_t)a.cols ? y : 0)]);
+            float c = -INF, sum = 0.f;
+            for (uint32_t q = threadIdx.x; q < parts; q += 256) c = fmaxf(c, part[r * parts + q].top);
+            c = row_reduce<256, true>(c, s_max);
+            for (uint32_t q = threadIdx.x; q < parts; q += 256) {
+                const Part p = part[r * parts + q];
+                sum = fmaf(p.sum, term_of(p.top, c, a.k), sum);
+            }
+            sum = row_reduce<256, false>(sum, s_sum);
+            st = row_stats(a, c, sum, y, xy);
+            if (MODE == ROWS_POLICY) dlogp = policy_row(a, r, st.logp, term);
+        }
+        if (threadIdx.x == 0) {
+            if (a.logp) a.logp[r] = st.logp;
+            if (a.top) a.top[r] = st.top;
+            if (a.log_sum) a.log_sum[r] = st.log_sum;
+            if (a.dlogp) a.dlogp[r] = dlogp;
+            if (MODE == ROWS_POLICY) put_terms(a, r, term);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The gradient of the logits from dlogp, top and log_sum: a wave has 2048 entries of a row.
+// ---------------------------------------------------------------------------
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
+                                                    uint32_t segs, uint32_t waves) {
+    // waves: of a row in one block, 1, 2 or 4
+    const uint32_t per = 4 / waves, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (uint64_t r = (uint64_t)blockIdx.y * per + wave / waves; r < a.rows; r += (uint64_t)gridDim.y * per) {
+        const int64_t y = token_of(a, r);
+        const float co = dlogp[r] * a.inv_tau, top_r = top[r], norm = log_sum[r] * LOG2E;
+        const bool none = y < 0 || dlogp[r] == 0, bad = y >= (int64_t)a.cols;
+        for (uint32_t q = blockIdx.x * waves + wave % waves; q < segs; q += gridDim.x * waves) {
+            float f[4][8];
+            int n[4];
+            uint64_t j[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                j[k] = (uint64_t)q * 2048 + (k * 64 + lane) * 8;
+                n[k] = j[k] < a.cols ? (int)min((uint64_t)8, a.cols - j[k]) : 0;
+                if (none) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
+                } else {
+                    l8_load(x.p + r * x.rs + (n[k] ? j[k] : 0), n[k], f[k]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (!none) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[k][i] = exp2_raw(fmaf(fmaf(f[k][i], a.inv_tau, -top_r), LOG2E, -norm));
+                    slope8(f[k], co, bad ? NAN32 : co, j[k], y);
+                }
+                l8_store(out.p + r * out.rs + (n[k] ? j[k] : 0), n[k], f[k]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums over rows, in 64 bits and always in the same order
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double block_sum64(double x, double* s) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0;
+    for (uint32_t i = 0; i < blockDim.x / 64; ++i) x += s[i];
+    return x;
+}
+// out[b] = the sum of in[b][0 .. n), a block each
+template <class IN, class OUT>
+__global__ __launch_bounds__(1024) void k_loss_sum(const IN* in, uint64_t n, uint64_t per, OUT* out) {
+    __shared__ double s[16];
+    const uint64_t lo = blockIdx.x * per, hi = min(n, lo + per);
+    double x = 0;
+    for (uint64_t i = lo + threadIdx.x; i < hi; i += 1024) x += (double)in[blockIdx.y * n + i];
+    x = block_sum64(x, s);
+    if (threadIdx.x == 0) out[(uint64_t)blockIdx.y * gridDim.x + blockIdx.x] = (OUT)x;
+}
+
+// ---------------------------------------------------------------------------
+// A pair of sequences: its margin, its share of the loss, and dlogp of its rows
+// ---------------------------------------------------------------------------
+struct PairArgs {
+    uint64_t rows, pairs;
+    Ints tokens, offsets;
+    const float *logp, *ref_logp, *weight;
+    int form, average;
+    float every, beta, target, smoothing;
+    float *margin, *losses, *dlogp;
+};
+__global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
+    __shared__ double s[4];
+    for (uint64_t i = blockIdx.x; i < a.pairs; i += gridDim.x) {
+        uint64_t at[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int64_t o = a.offsets.at(2 * i + k);
+            at[k] = o < 0 ? 0 : min((uint64_t)o, a.rows);
+        }
+        double h[2], share[2];
+        for (int q = 0; q < 2; ++q) {
+            double x = 0, n = 0;
+            for (uint64_t r = at[q] + threadIdx.x; r < at[q + 1]; r += 256)
+                if (a.tokens.at(r) >= 0) {
+                    x += (double)a.logp[r] - (a.ref_logp ? (double)a.ref_logp[r] : 0.);
+                    n += 1;
+                }
+            x = block_sum64(x, s);
+            share[q] = 1;
+            if (a.average) {
+                n = block_sum64(n, s);
+                share[q] = 1 / fmax(n, 1.);
+            }
+            h[q] = x * share[q];
+        }
+        const double margin = a.beta * (h[0] - h[1]), m = margin - a.target, w = a.weight ? (double)a.weight[i] : (double)a.every;
+        double each, slope;
+        if (a.form == ZKDL_PREF_LOGISTIC) {
+            const double small = log1p(exp(-fabs(m)));          // log(1 + exp(-|m|))
+            each = (1 - a.smoothing) * (fmax(-m, 0.) + small) + a.smoothing * (fmax(m, 0.) + small);
+            slope = a.smoothing - 1 / (1 + exp(m));
+        } else if (a.form == ZKDL_PREF_HINGE) {
+            each = m >= 0 ? 0 : -m;
+            slope = m >= 0 ? 0 : m < 0 ? -1 : m;
+        } else {
+            each = m * m;
+            slope = 2 * m;
+        }
+        if (m != m) each = slope = m;
+        if (threadIdx.x == 0) {
+            if (a.margin) a.margin[i] = (float)margin;
+            a.losses[i] = (float)(w * each);
+        }
+        if (a.dlogp)
+            for (int q = 0; q < 2; ++q) {
+                const float d = (float)((q ? -w : w) * slope * a.beta * share[q]);
+                for (uint64_t r = at[q] + threadIdx.x; r < at[q + 1]; r += 256) a.dlogp[r] = a.tokens.at(r) >= 0 ? d : 0.f;
+            }
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------
+// Columns that a group of G threads with ITEMS vectors has in registers.
+constexpr uint32_t loss_covers(int G, int ITEMS) { return (uint32_t)G * ITEMS * 8; }
+template <class T>
+constexpr uint32_t loss_longest() { return sizeof(T) == 4 ? loss_covers(1024, 8) : loss_covers(1024, 16); }
+
+template <class T, int MODE>
+void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
+    const uint32_t n = a.cols;
+#define LOSS_ROWS(G, ITEMS)                                                                                     \
+    if (n <= loss_covers(G, ITEMS)) {                                                                           \
+        const uint64_t blocks = l8_ceil(a.rows, loss_threads(G) / G);                                           \
+        hipLaunchKernelGGL((k_loss_rows<T, MODE, G, ITEMS>), dim3((unsigned)(blocks < (1u << 20) ? blocks : 1u << 20)), \
+                           dim3(loss_threads(G)), 0, ctx->stream, a, x, out);                                   \
+    }
+    LOSS_ROWS(64, 1)
+    else LOSS_ROWS(64, 2)
+    else LOSS_ROWS(64, 4)
+    else LOSS_ROWS(256, 2)
+    else LOSS_ROWS(256, 4)
+    else LOSS_ROWS(512, 4)
+    else LOSS_ROWS(1024, 4)
+    else LOSS_ROWS(1024, 8)
+    else if constexpr (sizeof(T) == 2) LOSS_ROWS(1024, 16)
+#undef LOSS_ROWS
+}
+
+template <class T>
+void launch_slope(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out) {
+    const uint32_t segs = (uint32_t)l8_ceil(a.cols, 2048), waves = segs >= 4 ? 4 : segs >= 2 ? 2 : 1;
+    const uint64_t gx = l8_ceil(segs, waves), gy = l8_ceil(a.rows, 4 / waves);
+    hipLaunchKernelGGL((k_loss_slope<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(gy < 4096 ? gy : 4096)), dim3(256), 0, ctx->stream, a, dlogp, top,
+                       log_sum, x, out, segs, waves);
+}
+
+// `sets` sums over n values each, one behind the other
+int launch_sum(zkdl_ctx* ctx, const float* in, uint64_t n, unsigned sets, float* out) {
+    constexpr uint64_t per = 1 << 14;
+    const uint64_t blocks = l8_ceil(n, per) < 4096 ? l8_ceil(n, per) : 4096;
+    if (blocks <= 1) {
+        hipLaunchKernelGGL((k_loss_sum<float, float>), dim3(1, sets), dim3(1024), 0, ctx->stream, in, n, n, out);
+        return ZKDL_OK;
+    }
+    double* mid = (double*)zk_alloc_scratch(ctx, blocks * sets * 8);
+    if (!mid) return ZKDL_ENOMEM;
+    hipLaunchKernelGGL((k_loss_sum<float, double>), dim3((unsigned)blocks, sets), dim3(1024), 0, ctx->stream, in, n, l8_ceil(n, blocks), mid);
+    hipLaunchKernelGGL((k_loss_sum<double, float>), dim3(1, sets), dim3(1024), 0, ctx->stream, mid, blocks, blocks, out);
+    zk_free(ctx, mid);
+    return ZKDL_OK;
+}
+
+// Whether rows stay in registers, or go in parts.
+template <class T>
+bool rows_fit(const LossArgs& a) { return a.cols >= 8 && a.cols <= loss_longest<T>() && (a.rows >= 64 || a.cols <= loss_covers(256, 4)); }
+
+template <class T, int MODE>
+int launch_parts(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x) {
+    const uint32_t parts = (uint32_t)l8_ceil(a.cols, 2048 * 4);
+    Part* part = (Part*)zk_alloc_scratch(ctx, a.rows * parts * sizeof(Part));
+    if (!part) return ZKDL_ENOMEM;
+    const dim3 grid(parts < 65535 ? parts : 65535, (unsigned)(a.rows < 256 ? a.rows : 256));
+    hipLaunchKernelGGL((k_loss_part<T, 4>), grid, dim3(256), 0, ctx->stream, a, x, part, parts);
+    hipLaunchKernelGGL((k_loss_join<T, MODE>), dim3((unsigned)(a.rows < 65536 ? a.rows : 65536)), dim3(256), 0, ctx->stream, a, x, part, parts);
+    zk_free(ctx, part);
+    return ZKDL_OK;
+}
+
+bool ints_ok(int dtype) { return dtype == ZKDL_I32 || dtype == ZKDL_I64; }
+bool good_tau(float tau) { return tau >= FLT_MIN && tau <= FLT_MAX && 1.f / tau >= FLT_MIN && 1.f / tau <= FLT_MAX; }
+bool rows_ok(const zkdl_mat* m) { return l8_mat_ok(m, false) && l8_is_float(m->dtype) && m->stack == 1 && (m->rows == 0 || m->cols > 0); }
+bool slope_ok(const zkdl_mat* d, const zkdl_mat* x) { return !d || (l8_mat_ok(d, true) && d->dtype == x->dtype && l8_same_shape(d, x)); }
+
+LossArgs loss_args(const zkdl_mat* x, const void* tokens, int tokens_dtype, float tau) {
+    LossArgs a = {};
+    a.rows = x->rows;
+    a.cols = (uint32_t)x->cols;
+    a.inv_tau = 1.f / tau;
+    a.k = (float)(1.4426950408889634 / tau);
+    a.tokens = {tokens, tokens_dtype == ZKDL_I64};
+    return a;
+}
+
+template <class F>
+int by_type(int dtype, F&& go) {
+    switch (dtype) {
+        case ZKDL_F32: return go(float{});
+        case ZKDL_F16: return go(__half{});
+        default: return go(bf16_t{});
+    }
+}
+
+// Scratch that goes back to the context whatever happens.
+struct Scratch {
+    zkdl_ctx* ctx;
+    float* p;
+    Scratch(zkdl_ctx* c, size_t floats) : ctx(c), p((float*)zk_alloc_scratch(c, floats * 4)) {}
+    ~Scratch() { zk_free(ctx, p); }
+    Scratch(const Scratch&) = delete;
+};
+
+template <class T>
+int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const zkdl_mat* dlogits) {
+    const bool fit = rows_fit<T>(a);
+    Scratch s(ctx, a.rows * (fit || !dlogits ? 3 : 6));
+    if (!s.p) return ZKDL_ENOMEM;
+    a.terms = s.p;
+    if (fit) {
+        launch_rows<T, ROWS_POLICY>(ctx, a, l8_mat<const T>(logits), l8_mat<T>(dlogits));
+    } else {
+        if (dlogits) {
+            a.dlogp = s.p + 3 * a.rows;
+            a.top = s.p + 4 * a.rows;
+            a.log_sum = s.p + 5 * a.rows;
+        }
+        const int rc = launch_parts<T, ROWS_POLICY>(ctx, a, l8_mat<const T>(logits));
+        if (rc != ZKDL_OK) return rc;
+        if (dlogits) launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits));
+    }
+    return launch_sum(ctx, a.terms, a.rows, 3, sums);
+}
+
+template <class T>
+int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_preference* p, float* loss, float* margin, float* logp, const zkdl_mat* dlogits) {
+    Scratch s(ctx, (a.rows ? a.rows : 1) * 4 + p->pairs);
+    if (!s.p) return ZKDL_ENOMEM;
+    a.logp = logp ? logp : s.p;
+    a.dlogp = s.p + a.rows;
+    a.top = s.p + 2 * a.rows;
+    a.log_sum = s.p + 3 * a.rows;
+    a.offsets = {p->offsets, p->offsets_dtype == ZKDL_I64};
+    a.last = 2 * p->pairs;
+    float* losses = s.p + 4 * a.rows;
+    if (a.rows) {
+        if (rows_fit<T>(a)) {
+            launch_rows<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits), L8Mat<T>{nullptr, 0, 0});
+        } else {
+            const int rc = launch_parts<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits));
+            if (rc != ZKDL_OK) return rc;
+        }
+    }
+    PairArgs q = {a.rows, p->pairs, a.tokens, a.offsets, a.logp, p->ref_logp, p->weight, p->form, p->average, 1.f / (float)p->pairs, p->beta, p->target,
+                  p->smoothing, margin, losses, dlogits ? a.dlogp : nullptr};
+    if (p->pairs) hipLaunchKernelGGL(k_loss_pair, dim3((unsigned)(p->pairs < 65536 ? p->pairs : 65536)), dim3(256), 0, ctx->stream, q);
+    if (dlogits && a.rows) launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits));
+    return launch_sum(ctx, losses, p->pairs, 1, loss);
+}
+
+}  // namespace
+
+extern "C" int zkdl_token_logprobs(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, float temperature, float* logp, float* top,
+                                   float* log_sum) try {
+    if (!ctx || !rows_ok(logits) || !ints_ok(tokens_dtype) || !good_tau(temperature)) return ZKDL_EINVAL;
+    if (logits->rows == 0) return ZKDL_OK;
+    if (!tokens || !logp) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    LossArgs a = loss_args(logits, tokens, tokens_dtype, temperature);
+    a.logp = logp;
+    a.top = top;
+    a.log_sum = log_sum;
+    const int rc = by_type(logits->dtype, [&](auto t) {
+        using T = decltype(t);
+        if (!rows_fit<T>(a)) return launch_parts<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits));
+        launch_rows<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits), L8Mat<T>{nullptr, 0, 0});
+        return (int)ZKDL_OK;
+    });
+    if (rc != ZKDL_OK) return rc;
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+extern "C" int zkdl_token_logprobs_backward(zkdl_ctx* ctx, const float* dlogp, const zkdl_mat* logits, const void* tokens, int tokens_dtype, const float* top,
+                                            const float* log_sum, float temperature, const zkdl_mat* dlogits) try {
+    if (!ctx || !rows_ok(logits) || !ints_ok(tokens_dtype) || !good_tau(temperature) || !dlogits || !slope_ok(dlogits, logits)) return ZKDL_EINVAL;
+    if (logits->rows == 0) return ZKDL_OK;
+    if (!dlogp || !tokens || !top || !log_sum) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    const LossArgs a = loss_args(logits, tokens, tokens_dtype, temperature);
+    by_type(logits->dtype, [&](auto t) {
+        using T = decltype(t);
+        launch_slope<T>(ctx, a, dlogp, top, log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits));
+        return 0;
+    });
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+extern "C" int zkdl_policy_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, const zkdl_policy* terms, float* sums, float* logp,
+                                const zkdl_mat* dlogits) try {
+    if (!ctx || !rows_ok(logits) || !ints_ok(tokens_dtype) || !terms || !good_tau(terms->temperature) || !slope_ok(dlogits, logits) || !sums) return ZKDL_EINVAL;
+    if (!(terms->clip_low >= 0 && terms->clip_low <= 1) || !(terms->clip_high >= 0 && terms->clip_high <= FLT_MAX) || !std::isfinite(terms->kl) ||
+        (terms->kl != 0 && logits->rows && !terms->ref_logp))
+        return ZKDL_EINVAL;
+    if (logits->rows && (!tokens || !terms->old_logp || !terms->advantage)) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    LossArgs a = loss_args(logits, tokens, tokens_dtype, terms->temperature);
+    a.logp = logp;
+    a.old_logp = terms->old_logp;
+    a.advantage = terms->advantage;
+    a.ref_logp = terms->ref_logp;
+    a.weight = terms->weight;
+    a.every = 1.f / (float)logits->rows;
+    a.low = 1.f - terms->clip_low;
+    a.high = 1.f + terms->clip_high;
+    a.kl = terms->kl;
+    const int rc = logits->rows == 0 ? launch_sum(ctx, nullptr, 0, 3, sums)
+                                     : by_type(logits->dtype, [&](auto t) { return policy<decltype(t)>(ctx, a, logits, sums, dlogits); });
+    if (rc != ZKDL_OK) return rc;
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+extern "C" int zkdl_preference_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, const zkdl_preference* terms, float* loss,
+                                    float* margin, float* logp, const zkdl_mat* dlogits) try {
+    if (!ctx || !rows_ok(logits) || !ints_ok(tokens_dtype) || !terms || !good_tau(terms->temperature) || !slope_ok(dlogits, logits) || !loss) return ZKDL_EINVAL;
+    if (!ints_ok(terms->offsets_dtype) || terms->reserved != 0 || terms->form < ZKDL_PREF_LOGISTIC || terms->form > ZKDL_PREF_SQUARE || !terms->offsets ||
+        !std::isfinite(terms->beta) || !std::isfinite(terms->target) || !(terms->smoothing >= 0 && terms->smoothing <= 1) ||
+        (terms->smoothing != 0 && terms->form != ZKDL_PREF_LOGISTIC))
+        return ZKDL_EINVAL;
+    if (terms->pairs >= (uint64_t)1 << 31 || (logits->rows && !tokens)) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    const LossArgs a = loss_args(logits, tokens, tokens_dtype, terms->temperature);
+    const int rc = by_type(logits->dtype, [&](auto t) {
+        using T = decltype(t);
+        return preference<T>(ctx, a, logits, terms, loss, margin, logp, dlogits);
+    });
+    if (rc != ZKDL_OK) return rc;
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}

@@ -1,0 +1,477 @@
+// The end of a training step: the norm of all gradients (zkdl_gradient_norm) and AdamW over many tensors (zkdl_adamw_step).
+//
+// Both are bound by memory: an entry of a step in 32 bits is 28 bytes moved for about 40 vector operations, with 8-bit states 14 bytes
+// for about 90.  A launch takes many tensors: their addresses stand in its arguments (4 kB at most, so nothing is copied to the device
+// and nothing is kept of a call), and a block finds its tensor by the number of its chunk.
+#include <cfloat>
+#include <cmath>
+#include <algorithm>
+
+#include "layer8.cuh"
+
+namespace {
+
+// The tensor that chunk c is of: first[] rises, first[0] = 0 <= c < first[count].
+template <int N>
+__device__ __forceinline__ uint32_t tensor_of(const uint32_t (&first)[N], uint32_t count, uint32_t c) {
+    uint32_t lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (first[mid] <= c) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// ---------------------------------------------------------------------------
+// Norm: squares in 64 bits, so that no gradient in the range of 32 bits leaves it
+// ---------------------------------------------------------------------------
+constexpr uint32_t NORM_TENSORS = 160, NORM_ITEMS = 4, NORM_CHUNK = 256 * 8 * NORM_ITEMS, NORM_BLOCKS = 2048;
+struct NormArgs {
+    const void* p[NORM_TENSORS];
+    uint64_t n[NORM_TENSORS];
+    uint32_t first[NORM_TENSORS + 1];
+    uint8_t dtype[NORM_TENSORS];
+    uint32_t count;
+    double* part;       // a sum for each block
+};
+static_assert(sizeof(NormArgs) <= 4096 - 256, "a launch's arguments");
+
+__device__ __forceinline__ double block_sum(double x, double* s) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0;
+    for (uint32_t i = 0; i < blockDim.x / 64; ++i) x += s[i];
+    return x;
+}
+
+template <class T>
+__device__ __forceinline__ void add_squares(const T* p, uint64_t n, uint64_t at, double (&sum)[2]) {
+    float f[NORM_ITEMS][8];
+    if (at + NORM_CHUNK <= n) {
+        L8Vec<T> v[NORM_ITEMS];
+#pragma unroll
+        for (int k = 0; k < (int)NORM_ITEMS; ++k) v[k] = l8_raw(p + at + (k * 256 + threadIdx.x) * 8);
+#pragma unroll
+        for (int k = 0; k < (int)NORM_ITEMS; ++k) l8_floats(v[k], f[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < (int)NORM_ITEMS; ++k) {
+            const uint64_t j = at + (k * 256 + threadIdx.x) * 8;
+            const int left = j < n ? (int)min((uint64_t)8, n - j) : 0;
+            l8_load(p + (left ? j : 0), left, f[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < (int)NORM_ITEMS; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double g = f[k][i];
+            sum[i & 1] = fma(g, g, sum[i & 1]);
+        }
+}
+__global__ __launch_bounds__(256) void k_norm_part(NormArgs a) {
+    __shared__ double s[4];
+    double sum[2] = {0, 0};
+    for (uint32_t c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
+        const uint32_t i = tensor_of(a.first, a.count, c);
+        const uint64_t at = (uint64_t)(c - a.first[i]) * NORM_CHUNK;
+        switch (a.dtype[i]) {
+            case L8_F32: add_squares((const float*)a.p[i], a.n[i], at, sum); break;
+            case L8_F16: add_squares((const __half*)a.p[i], a.n[i], at, sum); break;
+            default: add_squares((const bf16_t*)a.p[i], a.n[i], at, sum);
+        }
+    }
+    const double x = block_sum(sum[0] + sum[1], s);
+    if (threadIdx.x == 0) a.part[blockIdx.x] = x;
+}
+__global__ __launch_bounds__(1024) void k_norm_join(const double* part, uint64_t n, float limit, float* norm, float* factor) {
+    __shared__ double s[16];
+    double x = 0;
+    for (uint64_t i = threadIdx.x; i < n; i += 1024) x += part[i];
+    x = sqrt(block_sum(x, s));
+    if (threadIdx.x == 0) {
+        const float f = (float)x;
+        *norm = f;
+        if (factor) *factor = !(f < __builtin_huge_valf()) ? __builtin_nanf("") : x > (double)limit ? (float)((double)limit / x) : 1.f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+constexpr uint32_t ADAM_TENSORS = 40, ADAM_ITEMS = 2, ADAM_CHUNK = 256 * 8 * ADAM_ITEMS, ADAM_BLOCK8 = 256;
+struct AdamTensor {
+    void* param;
+    const void* grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    float *m_value, *v_value;
+    uint64_t n;
+    uint32_t number;        // of the tensor in the call: its random bits
+};
+struct AdamArgs {
+    AdamTensor t[ADAM_TENSORS];
+    uint32_t first[ADAM_TENSORS + 1];
+    uint32_t count, seed_lo, seed_hi, step;
+    double lr, decay, beta1, beta2;
+    const int64_t* step_ptr;
+    const float *lr_ptr, *factor;
+    float eps;
+    float rate, root, keep;     // lr / (1 - beta1^t), (1 - beta2^t)^(-1/2), 1 - lr decay
+};
+static_assert(sizeof(AdamArgs) <= 4096 - 256, "a launch's arguments");
+
+// What the step's number and the learning rate give: on the host, or, where they are read from device memory, in every block.
+struct AdamRates {
+    float rate, root, keep;
+};
+static __host__ __device__ inline double power_of(double b, uint32_t t) {       // by squaring: the same on either side
+    double r = 1;
+    for (; t; t >>= 1) {
+        if (t & 1) r = r * b;
+        b = b * b;
+    }
+    return r;
+}
+static __host__ __device__ inline AdamRates adam_rates(double lr, double decay, double beta1, double beta2, uint32_t t) {
+    AdamRates r;
+    r.rate = (float)(lr / (1 - power_of(beta1, t)));
+    r.root = (float)(1 / sqrt(1 - power_of(beta2, t)));
+    r.keep = (float)(1 - lr * decay);
+    return r;
+}
+
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0x9E3779B1u;
+    x ^= x >> 15;
+    x *= 0x85A308D3u;
+    return x ^ x >> 16;
+}
+
+// 8-bit floats: 3 mantissa bits and LOG exponent bits, the largest of which is the binade of scale byte e.
+template <int LOG>
+struct Float8 {
+    static constexpr uint32_t LAST = (1u << LOG) - 1;
+    // of a block whose largest magnitude is `top` (the bits of a float)
+    static __device__ __forceinline__ uint32_t scale(uint32_t top) {
+        const uint32_t e = max(40u, (top + 0xFFFFFu) >> 23);
+        return e > 254 ? 255u : e;
+    }
+    // value of a code without its sign
+    static __device__ __forceinline__ float value(uint32_t code, uint32_t e) {
+        const float whole = __uint_as_float((code << 20) + ((e - LAST) << 23)), part = (float)code * __uint_as_float((e - LAST - 2) << 23);
+        return code >= 8 ? whole : part;
+    }
+    // code of the magnitude with the bits u; r: 16 random bits
+    static __device__ __forceinline__ uint32_t code(uint32_t u, uint32_t e, uint32_t r) {
+        const uint32_t base = (e - LAST) << 23;
+        const uint32_t whole = (u - base + (r << 4 | 8)) >> 20;
+        const float place = __uint_as_float(u) * __uint_as_float((254 - (e - LAST - 2)) << 23);
+        const uint32_t part = (uint32_t)(int)(place + ((float)r + .5f) * 0x1p-16f);
+        return u >= base + (1u << 23) ? whole : part;
+    }
+};
+typedef Float8<4> M8;
+typedef Float8<5> V8;
+
+struct __attribute__((packed, aligned(1))) Codes8 {
+    uint32_t w[2];
+};
+__device__ __forceinline__ Codes8 load_codes(const uint8_t* p, int n) {
+    Codes8 c = {{0, 0}};
+    if (n >= 8) return *(const Codes8*)p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) c.w[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+    return c;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, const Codes8& c) {
+    if (n >= 8) {
+        *(Codes8*)p = c;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = (uint8_t)(c.w[i / 4] >> (8 * (i % 4)));
+}
+// over the 32 lanes that share a block of 256 entries
+__device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d, 64));
+    return x;
+}
+
+// BITS: of the states.  Thread t has eight adjacent entries of every 2048; 32 threads have a block of an 8-bit state.
+template <class P, class G, int BITS>
+__global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
+    __shared__ AdamRates s_rates;
+    const uint32_t i = tensor_of(a.first, a.count, blockIdx.x);
+    const AdamTensor& t = a.t[i];
+    uint32_t step = a.step;
+    AdamRates rates = {a.rate, a.root, a.keep};
+    bool go = true;
+    if (a.step_ptr) {
+        const int64_t v = *a.step_ptr;
+        go = v >= 1 && v < (int64_t)1 << 31;
+        step = go ? (uint32_t)v : 1;
+    }
+    if (a.step_ptr || a.lr_ptr) {
+        if (threadIdx.x == 0) s_rates = adam_rates(a.lr_ptr ? (double)*a.lr_ptr : a.lr, a.decay, a.beta1, a.beta2, step);
+        __syncthreads();
+        rates = s_rates;
+    }
+    double factor = 1;
+    if (a.factor) {
+        const float f = *a.factor;
+        go = go && fabsf(f) < __builtin_huge_valf();
+        factor = f;
+    }
+    if (BITS == 32 && !go) return;
+    const double b1 = a.beta1, c1 = 1 - b1, b2 = a.beta2, c2 = 1 - b2;
+    const uint32_t key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
+    const uint64_t at = (uint64_t)(blockIdx.x - a.first[i]) * ADAM_CHUNK + threadIdx.x * 8;
+    P* const param = (P*)t.param;
+    const G* const grad = (const G*)t.grad;
+    float p[ADAM_ITEMS][8], g[ADAM_ITEMS][8], m[ADAM_ITEMS][8], v[ADAM_ITEMS][8];
+    int n[ADAM_ITEMS];
+    uint64_t j[ADAM_ITEMS];
+#pragma unroll
+    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
+        j[k] = at + k * 2048;
+        n[k] = j[k] < t.n ? (int)min((uint64_t)8, t.n - j[k]) : 0;
+        if (!n[k]) j[k] = 0;
+        l8_load(param + j[k], n[k], p[k]);
+        l8_load(grad + j[k], n[k], g[k]);
+        if constexpr (BITS == 32) {
+            l8_load((const float*)t.m + j[k], n[k], m[k]);
+            l8_load((const float*)t.v + j[k], n[k], v[k]);
+        } else {
+            const Codes8 cm = load_codes((const uint8_t*)t.m + j[k], n[k]), cv = load_codes((const uint8_t*)t.v + j[k], n[k]);
+            const uint32_t em = n[k] ? max(40u, (uint32_t)t.m_scale[j[k] / ADAM_BLOCK8]) : 40u, ev = n[k] ? max(40u, (uint32_t)t.v_scale[j[k] / ADAM_BLOCK8]) : 40u;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t x = cm.w[q / 4] >> (8 * (q % 4)) & 255u, y = cv.w[q / 4] >> (8 * (q % 4)) & 255u;
+                m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x & 127, em)) | (x & 128) << 24);
+                v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
+        if (go) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const double d = (double)g[k][q] * factor;
+                m[k][q] = (float)fma(b1, (double)m[k][q], c1 * d);
+                v[k][q] = (float)fma(b2, (double)v[k][q], c2 * (d * d));
+                const float below = fmaf(__builtin_amdgcn_sqrtf(v[k][q]), rates.root, a.eps);
+                p[k][q] = fmaf(-rates.rate * m[k][q], __builtin_amdgcn_rcpf(below), p[k][q] * rates.keep);
+            }
+            l8_store(param + j[k], n[k], p[k]);
+        }
+        if constexpr (BITS == 32) {
+            l8_store((float*)t.m + j[k], n[k], m[k]);
+            l8_store((float*)t.v + j[k], n[k], v[k]);
+        } else {
+            if (go) {
+                uint32_t tm = 0, tv = 0;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    if (q < n[k]) {
+                        tm = max(tm, l8_mag(m[k][q]));
+                        tv = max(tv, l8_mag(v[k][q]));
+                    }
+                }
+                const uint32_t em = M8::scale(half_wave_max(tm)), ev = V8::scale(half_wave_max(tv));
+                const uint64_t block = j[k] / ADAM_BLOCK8;
+                const uint32_t kb = mix(key ^ (uint32_t)block), place = (uint32_t)(j[k] % ADAM_BLOCK8);
+                Codes8 cm = {{0, 0}}, cv = {{0, 0}};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t r = mix(kb + (place + q) * 0x9E3779B1u);
+                    const uint32_t um = __float_as_uint(m[k][q]), uv = l8_mag(v[k][q]);
+                    uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16), y = V8::code(uv, ev, r & 0xFFFFu);
+                    y = uv ? max(y, 1u) : y;
+                    x = em == 255 ? 0 : x;
+                    y = ev == 255 ? 0 : y;
+                    m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x, em)) | (um & 0x80000000u));
+                    v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
+                    x |= em == 255 ? 0 : um >> 24 & 128u;
+                    cm.w[q / 4] |= x << (8 * (q % 4));
+                    cv.w[q / 4] |= y << (8 * (q % 4));
+                }
+                store_codes((uint8_t*)t.m + j[k], n[k], cm);
+                store_codes((uint8_t*)t.v + j[k], n[k], cv);
+                if ((threadIdx.x & 31) == 0 && n[k]) {
+                    t.m_scale[block] = (uint8_t)em;
+                    t.v_scale[block] = (uint8_t)ev;
+                }
+            }
+            if (t.m_value) l8_store(t.m_value + j[k], n[k], m[k]);
+            if (t.v_value) l8_store(t.v_value + j[k], n[k], v[k]);
+        }
+    }
+}
+
+template <class P, class G>
+void launch_adamw(zkdl_ctx* ctx, const AdamArgs& a, int bits) {
+    const dim3 grid(a.first[a.count]);
+    if (bits == 32) hipLaunchKernelGGL((k_adamw<P, G, 32>), grid, dim3(256), 0, ctx->stream, a);
+    else hipLaunchKernelGGL((k_adamw<P, G, 8>), grid, dim3(256), 0, ctx->stream, a);
+}
+template <class F>
+void by_type(int dtype, F&& go) {
+    switch (dtype) {
+        case ZKDL_F32: go(float{}); break;
+        case ZKDL_F16: go(__half{}); break;
+        default: go(bf16_t{});
+    }
+}
+uint64_t item_bytes(int dtype) { return dtype == ZKDL_F32 ? 4 : 2; }
+
+// Memory that a call reads or writes: nothing that is written may overlap anything else.
+struct Span {
+    uint64_t lo, hi;
+    bool out;
+};
+bool spans_apart(std::vector<Span>& s) {
+    const auto less = [](const Span& a, const Span& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(s.begin(), s.end(), less)) std::sort(s.begin(), s.end(), less);
+    uint64_t any = 0, outs = 0;      // where what came before ends
+    for (const Span& x : s) {
+        if (x.lo < (x.out ? any : outs)) return false;
+        any = std::max(any, x.hi);
+        if (x.out) outs = std::max(outs, x.hi);
+    }
+    return true;
+}
+
+}  // namespace
+
+extern "C" int zkdl_gradient_norm(zkdl_ctx* ctx, const zkdl_vec* tensors, size_t count, float limit, float* norm, float* factor) try {
+    if (!ctx || (count && !tensors) || !norm || !(limit > 0)) return ZKDL_EINVAL;
+    uint64_t total = 0;
+    for (size_t i = 0; i < count; ++i) {
+        const zkdl_vec& t = tensors[i];
+        if (!l8_is_float(t.dtype) || t.reserved != 0 || (t.n && !t.data) || t.n >= (uint64_t)1 << 40) return ZKDL_EINVAL;
+        if (l8_ceil(t.n, NORM_CHUNK) >= (uint64_t)1 << 31) return ZKDL_ETOOBIG;
+        total += l8_ceil(t.n, NORM_CHUNK);
+    }
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    // blocks of all launches: each has NORM_BLOCKS at most
+    const uint64_t most = (l8_ceil(count, NORM_TENSORS) + 2 * l8_ceil(total, (uint64_t)1 << 31) + 1) * NORM_BLOCKS;
+    double* part = (double*)zk_alloc_scratch(ctx, std::min(most, total + 1) * 8);
+    if (!part) return ZKDL_ENOMEM;
+    NormArgs a;
+    a.count = 0;
+    a.first[0] = 0;
+    uint64_t blocks = 0;
+    const auto flush = [&] {
+        if (!a.count) return;
+        const uint32_t grid = std::min(a.first[a.count], NORM_BLOCKS);
+        a.part = part + blocks;
+        hipLaunchKernelGGL(k_norm_part, dim3(grid), dim3(256), 0, ctx->stream, a);
+        blocks += grid;
+        a.count = 0;
+    };
+    for (size_t i = 0; i < count; ++i) {
+        const zkdl_vec& t = tensors[i];
+        if (!t.n) continue;
+        const uint64_t chunks = l8_ceil(t.n, NORM_CHUNK);
+        if (a.count == NORM_TENSORS || (a.count && a.first[a.count] + chunks >= (uint64_t)1 << 31)) flush();
+        a.p[a.count] = t.data;
+        a.n[a.count] = t.n;
+        a.dtype[a.count] = t.dtype == ZKDL_F32 ? L8_F32 : t.dtype == ZKDL_F16 ? L8_F16 : L8_BF16;
+        a.first[a.count + 1] = a.first[a.count] + (uint32_t)chunks;
+        ++a.count;
+    }
+    flush();
+    hipLaunchKernelGGL(k_norm_join, dim3(1), dim3(1024), 0, ctx->stream, part, blocks, limit, norm, factor);
+    zk_free(ctx, part);
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}
+
+extern "C" int zkdl_adamw_step(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const zkdl_adamw* how) try {
+    if (!ctx || (count && !tensors) || !how || how->reserved != 0 || (how->bits != 32 && how->bits != 8)) return ZKDL_EINVAL;
+    if (!(how->beta1 >= 0 && how->beta1 < 1) || !(how->beta2 >= 0 && how->beta2 < 1) || !((float)how->eps >= FLT_MIN && (float)how->eps <= FLT_MAX) ||
+        !std::isfinite(how->decay) || (!how->lr_ptr && !std::isfinite(how->lr)) || (!how->step_ptr && (how->step < 1 || how->step >= (int64_t)1 << 31)))
+        return ZKDL_EINVAL;
+    if (count >= (size_t)1 << 31) return ZKDL_EINVAL;
+    std::vector<Span> spans;
+    spans.reserve(8 * count);
+    const auto span = [&](const void* p, uint64_t bytes, bool out) {
+        if (bytes && p) spans.push_back({(uint64_t)p, (uint64_t)p + bytes, out});
+    };
+    for (size_t i = 0; i < count; ++i) {
+        const zkdl_adamw_tensor& t = tensors[i];
+        if (!l8_is_float(t.param_dtype) || !l8_is_float(t.grad_dtype) || t.n >= (uint64_t)1 << 40) return ZKDL_EINVAL;
+        if (how->bits == 32 && (t.m_value || t.v_value)) return ZKDL_EINVAL;
+        if (!t.n) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || (how->bits == 8 && (!t.m_scale || !t.v_scale))) return ZKDL_EINVAL;
+        if (l8_ceil(t.n, ADAM_CHUNK) >= (uint64_t)1 << 23) return ZKDL_ETOOBIG;      // a launch's threads are counted in 32 bits
+        span(t.param, t.n * item_bytes(t.param_dtype), true);
+        span(t.grad, t.n * item_bytes(t.grad_dtype), false);
+        const uint64_t state = how->bits == 32 ? 4 : 1;
+        span(t.m, t.n * state, true);
+        span(t.v, t.n * state, true);
+        if (how->bits == 8) {
+            span(t.m_scale, l8_ceil(t.n, ADAM_BLOCK8), true);
+            span(t.v_scale, l8_ceil(t.n, ADAM_BLOCK8), true);
+            span(t.m_value, t.n * 4, true);
+            span(t.v_value, t.n * 4, true);
+        }
+    }
+    span(how->step_ptr, 8, false);
+    span(how->lr_ptr, 4, false);
+    span(how->factor, 4, false);
+    if (!spans_apart(spans)) return ZKDL_EINVAL;
+    L8Device dev(ctx);
+    ZK_HIP(ctx, dev.err);
+    AdamArgs a = {};
+    a.seed_lo = (uint32_t)how->seed;
+    a.seed_hi = (uint32_t)(how->seed >> 32);
+    a.step = how->step_ptr ? 1 : (uint32_t)how->step;
+    a.lr = how->lr_ptr ? 0 : how->lr;
+    a.decay = how->decay;
+    a.beta1 = how->beta1;
+    a.beta2 = how->beta2;
+    a.step_ptr = how->step_ptr;
+    a.lr_ptr = how->lr_ptr;
+    a.factor = how->factor;
+    a.eps = (float)how->eps;
+    const AdamRates rates = adam_rates(a.lr, a.decay, a.beta1, a.beta2, a.step);
+    a.rate = rates.rate;
+    a.root = rates.root;
+    a.keep = rates.keep;
+    // tensors of the same types share launches
+    for (int pt : {ZKDL_F32, ZKDL_F16, ZKDL_BF16})
+        for (int gt : {ZKDL_F32, ZKDL_F16, ZKDL_BF16}) {
+            const auto flush = [&] {
+                if (!a.count) return;
+                by_type(pt, [&](auto p) { by_type(gt, [&](auto g) { launch_adamw<decltype(p), decltype(g)>(ctx, a, how->bits); }); });
+                a.count = 0;
+            };
+            for (size_t i = 0; i < count; ++i) {
+                const zkdl_adamw_tensor& t = tensors[i];
+                if (t.param_dtype != pt || t.grad_dtype != gt || !t.n) continue;
+                const uint64_t chunks = l8_ceil(t.n, ADAM_CHUNK);
+                if (a.count == ADAM_TENSORS || (a.count && a.first[a.count] + chunks >= (uint64_t)1 << 23)) flush();
+                a.t[a.count] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.m_value, t.v_value, t.n, (uint32_t)i};
+                a.first[a.count + 1] = a.first[a.count] + (uint32_t)chunks;
+                ++a.count;
+            }
+            flush();
+        }
+    ZK_HIP(ctx, hipGetLastError());
+    return ZKDL_OK;
+} catch (...) {
+    return ZKDL_ENOMEM;
+}

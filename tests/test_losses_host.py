@@ -1,0 +1,39 @@
+"""Losses and update without a GPU: null pointers are refused before anything else is looked at, descriptors have the header's layout."""
+import ctypes as C
+
+import pytest
+
+import paper_2307_16273_amd as zk
+from paper_2307_16273_amd.binding import AdamW, AdamWTensor, Mat, Policy, Preference, Vec
+
+
+def test_null_contexts_are_refused():
+    lib = zk.load_library()
+    m, p, q, v, t, h = Mat(None, 1, 2, 2, 2, 0, 4, 0), Policy(), Preference(), Vec(), AdamWTensor(), AdamW()
+    ref = C.byref
+    assert lib.zkdl_token_logprobs(None, ref(m), None, 0, 1.0, None, None, None) == -1
+    assert lib.zkdl_token_logprobs_backward(None, None, ref(m), None, 0, None, None, 1.0, ref(m)) == -1
+    assert lib.zkdl_policy_loss(None, ref(m), None, 0, ref(p), None, None, None) == -1
+    assert lib.zkdl_preference_loss(None, ref(m), None, 0, ref(q), None, None, None, None) == -1
+    assert lib.zkdl_gradient_norm(None, ref(v), 1, 1.0, None, None) == -1
+    assert lib.zkdl_adamw_step(None, ref(t), 1, ref(h)) == -1
+
+
+def test_descriptors_are_the_headers_layout():
+    assert C.sizeof(Policy) == 48 and Policy.temperature.offset == 44
+    assert C.sizeof(Preference) == 64 and Preference.pairs.offset == 24 and Preference.beta.offset == 48
+    assert C.sizeof(Vec) == 24 and Vec.dtype.offset == 16
+    assert C.sizeof(AdamWTensor) == 80 and AdamWTensor.n.offset == 64 and AdamWTensor.grad_dtype.offset == 76
+    assert C.sizeof(AdamW) == 88 and AdamW.seed.offset == 40 and AdamW.factor.offset == 72 and AdamW.bits.offset == 80
+
+
+def test_forms_and_bits_by_name():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError, match="form"):
+        zk.preference_loss(None, None, None, None, form="sigmoid")
+    with pytest.raises(ValueError, match="bits"):
+        zk.adamw_state([torch.zeros(3)], bits=16)
+    s = zk.adamw_state([torch.zeros(300, 2), torch.zeros(0)], bits=8)
+    assert [x.shape for x in s["m"]] == [(300, 2), (0,)] and [x.shape for x in s["v_scale"]] == [(3,), (0,)] and s["m"][0].dtype == torch.uint8
+    s = zk.adamw_state([torch.zeros(5, dtype=torch.bfloat16)])
+    assert s["m"][0].dtype == torch.float32 and s["m_scale"] == []
