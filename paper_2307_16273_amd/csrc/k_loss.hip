@@ -92,17 +92,6 @@ __device__ __forceinline__ void put_terms(const LossArgs& a, uint64_t r, const f
     for (int i = 0; i < 3; ++i) a.terms[i * a.rows + r] = term[i];
 }
 
-// c ([j = token] - p_j) of eight entries from j on, p_j = e_j inv: e comes in, the gradient goes out.
-__device__ __forceinline__ void slope8(float (&e)[8], float c, float c_inv, uint64_t j, int64_t y) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] *= -c_inv;
-    const uint64_t at = (uint64_t)y - j;
-    if (at < 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] += at == i ? c : 0.f;
-    }
-}
-
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
@@ -122,95 +111,168 @@ __device__ __forceinline__ float row_reduce(float x, float* s) {
     return x;
 }
 
+// Eight adjacent items as they lie in memory, two of 16 bits to a register, and as floats.
+template <class T>
+struct __attribute__((packed, aligned(1))) Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+template <class T>
+__device__ __forceinline__ Raw8<T> load8(const T* p) { return *(const Raw8<T>*)p; }
+__device__ __forceinline__ void floats8(const Raw8<float>& v, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v.w[i]);
+}
+__device__ __forceinline__ void floats8(const Raw8<bf16_t>& v, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(v.w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(v.w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void floats8(const Raw8<__half>& v, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = __half22float2(__builtin_bit_cast(__half2, v.w[i]));
+        f[2 * i] = x.x;
+        f[2 * i + 1] = x.y;
+    }
+}
+// What follows takes the floats of v from its registers again: without this they would stay in registers of their own, twice as many.
+template <class T>
+__device__ __forceinline__ void keep_packed(Raw8<T>& v) {
+#pragma unroll
+    for (uint32_t& w : v.w) asm("" : "+v"(w));
+}
+template <class T>
+__device__ __forceinline__ float max8(float c, const Raw8<T>& v) {
+    float f[8];
+    floats8(v, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = fmaxf(c, f[i]);
+    return c;
+}
+// -co p_j of eight entries; the token's own entry is put over it by the same thread afterwards.
+template <class T>
+__device__ __forceinline__ void slope8(const Raw8<T>& v, float c, float k, float co_inv, float (&f)[8]) {
+    floats8(v, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = term_of(f[i], c, k) * -co_inv;
+}
+template <class T>
+__device__ __forceinline__ void put_one(T* to, float x) {
+    T o;
+    l8_put(x, o);
+    *to = o;
+}
+// The part of a vector at the row's end that no other thread has.
+template <class T>
+__device__ __forceinline__ void put_end(T* row, const L8At& end, const float (&f)[8]) {
+    if (!end.live) return;
+    if (end.dup == 0) {
+        l8_store(row + end.start, 8, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 1; i < 8; ++i)
+        if ((uint32_t)i >= end.dup) put_one(row + end.start + i, f[i]);
+}
+
+// p + n as an address of the whole wave's: a load or store then adds the lane's own offset by itself, without an address of 64 bits for each vector.
+template <class T>
+__device__ __forceinline__ T* at_uniform(T* p, uint32_t n) {
+    p += n;
+    asm("" : "+s"(p));
+    return p;
+}
+template <class T, int G, int WHOLE>
+__device__ __forceinline__ void put_zeros(T* to, uint32_t t, bool ends, const L8At& end) {
+    const float zero[8] = {};
+#pragma unroll 1
+    for (int k = 0; k < WHOLE; ++k) l8_store(to + k * 8 * G + t * 8, 8, zero);
+    if (ends) put_end(to, end, zero);
+}
+
 enum { ROWS_LOGP, ROWS_POLICY };
 
 // ---------------------------------------------------------------------------
-// Rows that stay in registers: G threads a row (a wave: four rows a block), ITEMS vectors of eight a thread.  8 <= cols <= 8 G ITEMS.
+// Rows that stay in registers: G threads a row (a wave: four rows a block) with WHOLE vectors of eight each, and one at the row's end:
+// 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols >= 8.  (As many instances as there are lengths: with a count that the kernel learns when it
+// runs, the vectors' registers were copied and spilled.)
 // ---------------------------------------------------------------------------
 constexpr int loss_threads(int G) { return G < 256 ? 256 : G; }
-template <class T, int MODE, int G, int ITEMS>
+template <class T, int MODE, int G, int WHOLE>
 __global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat<const T> x, L8Mat<T> out) {
     constexpr int GROUPS = loss_threads(G) / G;
+    constexpr uint32_t EACH = 8 * G;
     __shared__ float s_max[G / 64], s_sum[G / 64];
     const uint32_t t = threadIdx.x % G;
-    const uint64_t step = (uint64_t)gridDim.x * GROUPS;
-    for (uint64_t r = (uint64_t)blockIdx.x * GROUPS + threadIdx.x / G; r < a.rows; r += step) {
+    const uint32_t group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
+    const bool leader = t == 0, ends = WHOLE * EACH < a.cols;
+    const L8At end = l8_at(WHOLE * EACH + t * 8, a.cols);
+    for (uint64_t r = (uint64_t)blockIdx.x * GROUPS + group; r < a.rows; r += (uint64_t)gridDim.x * GROUPS) {
         const int64_t y = token_of(a, r);
-        const bool leader = t == 0;
-        if (y < 0) {
-            if (leader) {
-                if (a.logp) a.logp[r] = 0.f;
-                if (a.top) a.top[r] = 0.f;
-                if (a.log_sum) a.log_sum[r] = 0.f;
-                if (a.dlogp) a.dlogp[r] = 0.f;
-                const float none[3] = {0.f, 0.f, 0.f};
-                if (MODE == ROWS_POLICY) put_terms(a, r, none);
-            }
-            if (MODE == ROWS_POLICY && out.p) {
-                const float zero[8] = {};
+        T* const to = out.p + r * out.rs;
+        float term[3] = {0.f, 0.f, 0.f};
+        RowStats st = {0.f, 0.f, 0.f};
+        if (y >= 0) {
+            const T* const row = x.p + r * x.rs;
+            Raw8<T> v[WHOLE + 1];
 #pragma unroll
-                for (int k = 0; k < ITEMS; ++k) {
-                    const L8At at = l8_at((k * G + t) * 8, a.cols);
-                    if (at.live) l8_store(out.p + r * out.rs + at.start, 8, zero);
-                }
-            }
-            continue;
-        }
-        const T* row = x.p + r * x.rs;
-        L8Vec<T> v[ITEMS];
+            for (int k = 0; k < WHOLE; ++k) v[k] = load8(at_uniform(row, k * EACH) + t * 8);
+            if (ends) v[WHOLE] = load8(row + end.start);
+            const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
+            float c = -INF, sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) v[k] = l8_raw(row + l8_at((k * G + t) * 8, a.cols).start);
-        const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
-        float c = -INF;
+            for (int k = 0; k < WHOLE; ++k) c = max8(c, v[k]);
+            if (ends) c = max8(c, v[WHOLE]);
+            c = row_reduce<G, true>(c, s_max);
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            float f[8];
-            l8_floats(v[k], f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) c = fmaxf(c, f[i]);
-        }
-        c = row_reduce<G, true>(c, s_max);
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            float f[8];
-            l8_floats(v[k], f);
-            if ((uint32_t)(k + 1) * G * 8 <= a.cols) {
+            for (int k = 0; k < WHOLE; ++k) {
+                float f[8];
+                keep_packed(v[k]);
+                floats8(v[k], f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += term_of(f[i], c, a.k);
-            } else {            // the row's end: what another thread has, or nobody, stays out
-                const L8At at = l8_at((k * G + t) * 8, a.cols);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += at.live && (uint32_t)i >= at.dup ? term_of(f[i], c, a.k) : 0.f;
             }
+            if (ends) {         // what another thread has, or nobody, stays out
+                float f[8];
+                keep_packed(v[WHOLE]);
+                floats8(v[WHOLE], f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += end.live && (uint32_t)i >= end.dup ? term_of(f[i], c, a.k) : 0.f;
+            }
+            sum = row_reduce<G, false>(sum, s_sum);
+            st = row_stats(a, c, sum, y, xy);
+            if (MODE == ROWS_POLICY) {
+                const float dlogp = policy_row(a, r, st.logp, term);
+                const float co = dlogp * a.inv_tau, co_inv = co / sum;
+                if (out.p && dlogp != 0) {
+                    float f[8];
+#pragma unroll
+                    for (int k = 0; k < WHOLE; ++k) {
+                        keep_packed(v[k]);
+                        slope8(v[k], c, a.k, co_inv, f);
+                        l8_store(at_uniform(to, k * EACH) + t * 8, 8, f);
+                    }
+                    if (ends) {
+                        keep_packed(v[WHOLE]);
+                        slope8(v[WHOLE], c, a.k, co_inv, f);
+                        put_end(to, end, f);
+                    }
+                    if (y < (int64_t)a.cols && t == (uint32_t)y / 8 % G) put_one(to + y, fmaf(-co_inv, term_of(xy, c, a.k), co));
+                } else if (out.p) {
+                    put_zeros<T, G, WHOLE>(to, t, ends, end);
+                }
+            }
+        } else if (MODE == ROWS_POLICY && out.p) {
+            put_zeros<T, G, WHOLE>(to, t, ends, end);
         }
-        sum = row_reduce<G, false>(sum, s_sum);
-        const RowStats st = row_stats(a, c, sum, y, xy);
-        float term[3], dlogp = 0.f;
-        if (MODE == ROWS_POLICY) dlogp = policy_row(a, r, st.logp, term);
         if (leader) {
             if (a.logp) a.logp[r] = st.logp;
             if (a.top) a.top[r] = st.top;
             if (a.log_sum) a.log_sum[r] = st.log_sum;
             if (a.dlogp) a.dlogp[r] = 0.f;
             if (MODE == ROWS_POLICY) put_terms(a, r, term);
-        }
-        if (MODE == ROWS_POLICY && out.p) {
-            const float co = dlogp * a.inv_tau, co_inv = co / sum;
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                const L8At at = l8_at((k * G + t) * 8, a.cols);
-                float f[8];
-                l8_floats(v[k], f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = term_of(f[i], c, a.k);
-                slope8(f, co, co_inv, at.start, y);
-                if (dlogp == 0) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = 0.f;
-                }
-                if (at.live) l8_store(out.p + r * out.rs + at.start, 8, f);
-            }
         }
         if (G > 64) __syncthreads();        // s_max and s_sum are the next row's
     }
@@ -317,8 +379,12 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
             for (int k = 0; k < 4; ++k) {
                 if (!none) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[k][i] = exp2_raw(fmaf(fmaf(f[k][i], a.inv_tau, -top_r), LOG2E, -norm));
-                    slope8(f[k], co, bad ? NAN32 : co, j[k], y);
+                    for (int i = 0; i < 8; ++i) f[k][i] = exp2_raw(fmaf(fmaf(f[k][i], a.inv_tau, -top_r), LOG2E, -norm)) * (bad ? NAN32 : -co);
+                    // the token's own entry
+                    if ((uint64_t)y - j[k] < 8 && !bad) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)y - j[k] == i ? co : 0.f;
+                    }
                 }
                 l8_store(out.p + r * out.rs + (n[k] ? j[k] : 0), n[k], f[k]);
             }
@@ -413,30 +479,26 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
 }
 
 // ---- launches ----------------------------------------------------------------------
-// Columns that a group of G threads with ITEMS vectors has in registers.
-constexpr uint32_t loss_covers(int G, int ITEMS) { return (uint32_t)G * ITEMS * 8; }
+// The longest row that stays in a block's registers: 16 vectors a thread of 16-bit entries, less than 8 of 32-bit ones.
 template <class T>
-constexpr uint32_t loss_longest() { return sizeof(T) == 4 ? loss_covers(1024, 8) : loss_covers(1024, 16); }
+constexpr uint32_t loss_longest() { return sizeof(T) == 2 ? 1024 * 8 * 16 : 1024 * 8 * 8 - 1; }
 
+template <class T, int MODE, int G, int WHOLE>
+void launch_rows_of(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
+    const uint64_t blocks = l8_ceil(a.rows, loss_threads(G) / G);
+    hipLaunchKernelGGL((k_loss_rows<T, MODE, G, WHOLE>), dim3((unsigned)(blocks < (1u << 20) ? blocks : 1u << 20)), dim3(loss_threads(G)), 0, ctx->stream, a, x, out);
+}
+template <class T, int MODE, int G, int WHOLE, int LAST>
+void launch_rows_from(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
+    if (a.cols / (8 * G) == WHOLE) launch_rows_of<T, MODE, G, WHOLE>(ctx, a, x, out);
+    else if constexpr (WHOLE < LAST) launch_rows_from<T, MODE, G, WHOLE + 1, LAST>(ctx, a, x, out);
+}
+// a wave a row up to 2047 entries, a block of four up to 8191, of sixteen above
 template <class T, int MODE>
 void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
-    const uint32_t n = a.cols;
-#define LOSS_ROWS(G, ITEMS)                                                                                     \
-    if (n <= loss_covers(G, ITEMS)) {                                                                           \
-        const uint64_t blocks = l8_ceil(a.rows, loss_threads(G) / G);                                           \
-        hipLaunchKernelGGL((k_loss_rows<T, MODE, G, ITEMS>), dim3((unsigned)(blocks < (1u << 20) ? blocks : 1u << 20)), \
-                           dim3(loss_threads(G)), 0, ctx->stream, a, x, out);                                   \
-    }
-    LOSS_ROWS(64, 1)
-    else LOSS_ROWS(64, 2)
-    else LOSS_ROWS(64, 4)
-    else LOSS_ROWS(256, 2)
-    else LOSS_ROWS(256, 4)
-    else LOSS_ROWS(512, 4)
-    else LOSS_ROWS(1024, 4)
-    else LOSS_ROWS(1024, 8)
-    else if constexpr (sizeof(T) == 2) LOSS_ROWS(1024, 16)
-#undef LOSS_ROWS
+    if (a.cols < 2048) launch_rows_from<T, MODE, 64, 0, 3>(ctx, a, x, out);
+    else if (a.cols < 8192) launch_rows_from<T, MODE, 256, 1, 3>(ctx, a, x, out);
+    else launch_rows_from<T, MODE, 1024, 1, sizeof(T) == 2 ? 16 : 7>(ctx, a, x, out);
 }
 
 template <class T>
@@ -465,7 +527,7 @@ int launch_sum(zkdl_ctx* ctx, const float* in, uint64_t n, unsigned sets, float*
 
 // Whether rows stay in registers, or go in parts.
 template <class T>
-bool rows_fit(const LossArgs& a) { return a.cols >= 8 && a.cols <= loss_longest<T>() && (a.rows >= 64 || a.cols <= loss_covers(256, 4)); }
+bool rows_fit(const LossArgs& a) { return a.cols >= 8 && a.cols <= loss_longest<T>() && (a.rows >= 64 || a.cols < 8192); }
 
 template <class T, int MODE>
 int launch_parts(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x) {
