@@ -177,12 +177,41 @@ __device__ __forceinline__ void put_end(T* row, const L8At& end, const float (&f
         if ((uint32_t)i >= end.dup) put_one(row + end.start + i, f[i]);
 }
 
-// p + n as an address of the whole wave's: a load or store then adds the lane's own offset by itself, without an address of 64 bits for each vector.
+// Eight items at p + n + lane, p and n being the whole wave's: the instruction adds the lane's own offset, and no vector has an address of 64
+// bits of its own.
+typedef uint32_t Quad __attribute__((ext_vector_type(4), aligned(1)));
 template <class T>
-__device__ __forceinline__ T* at_uniform(T* p, uint32_t n) {
-    p += n;
-    asm("" : "+s"(p));
-    return p;
+__device__ __forceinline__ Raw8<T> load8_at(const T* p, uint32_t n, uint32_t lane) {
+    uint64_t at = (uint64_t)(p + n);
+    asm("" : "+s"(at));
+    const auto* q = (const __attribute__((address_space(1))) Quad*)(at + lane * (uint32_t)sizeof(T));
+    Raw8<T> v;
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const Quad x = q[h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[4 * h + i] = x[i];
+    }
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void store8_at(T* p, uint32_t n, uint32_t lane, const float (&f)[8]) {
+    uint64_t at = (uint64_t)(p + n);
+    asm("" : "+s"(at));
+    auto* q = (__attribute__((address_space(1))) Quad*)(at + lane * (uint32_t)sizeof(T));
+    struct {
+        T v[8];
+    } o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l8_put(f[i], o.v[i]);
+    const Raw8<T> w = __builtin_bit_cast(Raw8<T>, o);
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        Quad x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = w.w[4 * h + i];
+        q[h] = x;
+    }
 }
 template <class T, int G, int WHOLE>
 __device__ __forceinline__ void put_zeros(T* to, uint32_t t, bool ends, const L8At& end) {
@@ -218,7 +247,7 @@ __global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat
             const T* const row = x.p + r * x.rs;
             Raw8<T> v[WHOLE + 1];
 #pragma unroll
-            for (int k = 0; k < WHOLE; ++k) v[k] = load8(at_uniform(row, k * EACH) + t * 8);
+            for (int k = 0; k < WHOLE; ++k) v[k] = load8_at(row, k * EACH, t * 8);
             if (ends) v[WHOLE] = load8(row + end.start);
             const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
             float c = -INF, sum = 0.f;
@@ -252,7 +281,7 @@ __global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat
                     for (int k = 0; k < WHOLE; ++k) {
                         keep_packed(v[k]);
                         slope8(v[k], c, a.k, co_inv, f);
-                        l8_store(at_uniform(to, k * EACH) + t * 8, 8, f);
+                        store8_at(to, k * EACH, t * 8, f);
                     }
                     if (ends) {
                         keep_packed(v[WHOLE]);
@@ -285,6 +314,41 @@ __global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat
 struct Part {
     float top, sum;
 };
+// FULL: the row does not end in it, so that no load waits for a branch.
+template <class T, int ITEMS, bool FULL>
+__device__ __forceinline__ void part_of(const LossArgs& a, const T* row, uint32_t q, float& c, float& sum, float* s_max, float* s_sum) {
+    float f[ITEMS][8];
+    int n[ITEMS];
+    if constexpr (FULL) {
+        Raw8<T> v[ITEMS];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) v[k] = load8_at(row + (uint64_t)q * (ITEMS * 2048), k * 2048, threadIdx.x * 8);
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            n[k] = 8;
+            floats8(v[k], f[k]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const uint64_t j = ((uint64_t)(q * ITEMS + k) * 256 + threadIdx.x) * 8;
+            n[k] = j < a.cols ? (int)min((uint64_t)8, a.cols - j) : 0;
+            l8_load(row + (n[k] ? j : 0), n[k], f[k]);
+        }
+    }
+    c = -INF;
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c = fmaxf(c, FULL || i < n[k] ? f[k][i] : -INF);
+    c = row_reduce<256, true>(c, s_max);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += FULL || i < n[k] ? term_of(f[k][i], c, a.k) : 0.f;
+    sum = row_reduce<256, false>(sum, s_sum);
+}
 template <class T, int ITEMS>
 __global__ __launch_bounds__(256) void k_loss_part(LossArgs a, L8Mat<const T> x, Part* part, uint32_t parts) {
     __shared__ float s_max[4], s_sum[4];
@@ -292,24 +356,9 @@ __global__ __launch_bounds__(256) void k_loss_part(LossArgs a, L8Mat<const T> x,
         if (token_of(a, r) < 0) continue;
         const T* row = x.p + r * x.rs;
         for (uint32_t q = blockIdx.x; q < parts; q += gridDim.x) {
-            float f[ITEMS][8], c = -INF, sum = 0.f;
-            int n[ITEMS];
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                const uint64_t j = ((uint64_t)(q * ITEMS + k) * 256 + threadIdx.x) * 8;
-                n[k] = j < a.cols ? (int)min((uint64_t)8, a.cols - j) : 0;
-                l8_load(row + (n[k] ? j : 0), n[k], f[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) c = fmaxf(c, i < n[k] ? f[k][i] : -INF);
-            c = row_reduce<256, true>(c, s_max);
-#pragma unroll
-            for (int k = 0; k < ITEMS; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += i < n[k] ? term_of(f[k][i], c, a.k) : 0.f;
-            sum = row_reduce<256, false>(sum, s_sum);
+            float c, sum;
+            if ((uint64_t)(q + 1) * ITEMS * 2048 <= a.cols) part_of<T, ITEMS, true>(a, row, q, c, sum, s_max, s_sum);
+            else part_of<T, ITEMS, false>(a, row, q, c, sum, s_max, s_sum);
             if (threadIdx.x == 0) part[r * parts + q] = {c, c == -INF ? 0.f : sum};      // a part of nothing but -infinity adds nothing
             __syncthreads();
         }
@@ -351,43 +400,62 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
 // ---------------------------------------------------------------------------
 // The gradient of the logits from dlogp, top and log_sum: a wave has 2048 entries of a row.
 // ---------------------------------------------------------------------------
+struct SlopeRow {
+    float co, inv_tau, top, norm;       // p_j = exp2((x_j inv_tau - top) log2(e) - norm)
+    int64_t y;
+    bool none, bad;                     // zeros, NaN
+};
+template <class T, bool FULL>
+__device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to, uint32_t cols, uint32_t at, uint32_t lane) {
+    float f[4][8];
+    int n[4];
+    if constexpr (FULL) {
+        if (!s.none) {
+            Raw8<T> v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = load8(row + at + (k * 64 + lane) * 8);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) floats8(v[k], f[k]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t j = (uint64_t)at + (k * 64 + lane) * 8;
+            n[k] = j < cols ? (int)min((uint64_t)8, cols - j) : 0;
+            if (!s.none) l8_load(row + (n[k] ? j : 0), n[k], f[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t j = (uint64_t)at + (k * 64 + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[k][i] = s.none ? 0.f : exp2_raw(fmaf(fmaf(f[k][i], s.inv_tau, -s.top), LOG2E, -s.norm)) * (s.bad ? NAN32 : -s.co);
+        if ((uint64_t)s.y - j < 8 && !s.bad && !s.none) {       // the token's own entry
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)s.y - j == i ? s.co : 0.f;
+        }
+        if (FULL) l8_store(to + j, 8, f[k]);
+        else l8_store(to + (n[k] ? j : 0), n[k], f[k]);
+    }
+}
 template <class T>
 __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
                                                     uint32_t segs, uint32_t waves) {
     // waves: of a row in one block, 1, 2 or 4
-    const uint32_t per = 4 / waves, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t per = 4 / waves, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (uint64_t r = (uint64_t)blockIdx.y * per + wave / waves; r < a.rows; r += (uint64_t)gridDim.y * per) {
-        const int64_t y = token_of(a, r);
-        const float co = dlogp[r] * a.inv_tau, top_r = top[r], norm = log_sum[r] * LOG2E;
-        const bool none = y < 0 || dlogp[r] == 0, bad = y >= (int64_t)a.cols;
+        SlopeRow s;
+        s.y = token_of(a, r);
+        s.co = dlogp[r] * a.inv_tau;
+        s.none = s.y < 0 || dlogp[r] == 0;
+        s.bad = s.y >= (int64_t)a.cols;
+        s.inv_tau = a.inv_tau;
+        s.top = top[r];
+        s.norm = log_sum[r] * LOG2E;
         for (uint32_t q = blockIdx.x * waves + wave % waves; q < segs; q += gridDim.x * waves) {
-            float f[4][8];
-            int n[4];
-            uint64_t j[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                j[k] = (uint64_t)q * 2048 + (k * 64 + lane) * 8;
-                n[k] = j[k] < a.cols ? (int)min((uint64_t)8, a.cols - j[k]) : 0;
-                if (none) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
-                } else {
-                    l8_load(x.p + r * x.rs + (n[k] ? j[k] : 0), n[k], f[k]);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (!none) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[k][i] = exp2_raw(fmaf(fmaf(f[k][i], a.inv_tau, -top_r), LOG2E, -norm)) * (bad ? NAN32 : -co);
-                    // the token's own entry
-                    if ((uint64_t)y - j[k] < 8 && !bad) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)y - j[k] == i ? co : 0.f;
-                    }
-                }
-                l8_store(out.p + r * out.rs + (n[k] ? j[k] : 0), n[k], f[k]);
-            }
+            if ((uint64_t)(q + 1) * 2048 <= a.cols) slope_of<T, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
+            else slope_of<T, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
         }
     }
 }
@@ -493,12 +561,15 @@ void launch_rows_from(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<
     if (a.cols / (8 * G) == WHOLE) launch_rows_of<T, MODE, G, WHOLE>(ctx, a, x, out);
     else if constexpr (WHOLE < LAST) launch_rows_from<T, MODE, G, WHOLE + 1, LAST>(ctx, a, x, out);
 }
-// a wave a row up to 2047 entries, a block of four up to 8191, of sixteen above
+// Few threads a row, with many vectors each, where there are rows enough to fill the device: more rows are under way at once, and fewer
+// threads wait for one another.
 template <class T, int MODE>
 void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
-    if (a.cols < 2048) launch_rows_from<T, MODE, 64, 0, 3>(ctx, a, x, out);
-    else if (a.cols < 8192) launch_rows_from<T, MODE, 256, 1, 3>(ctx, a, x, out);
-    else launch_rows_from<T, MODE, 1024, 1, sizeof(T) == 2 ? 16 : 7>(ctx, a, x, out);
+    constexpr int MOST = sizeof(T) == 2 ? 16 : 7;       // vectors that leave room for what else a thread holds
+    const bool many = a.rows >= 1024;
+    if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
+    else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST + 1))) launch_rows_from<T, MODE, 256, 1, MOST>(ctx, a, x, out);
+    else launch_rows_from<T, MODE, 1024, 1, MOST>(ctx, a, x, out);
 }
 
 template <class T>

@@ -205,7 +205,105 @@ __device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
     return x;
 }
 
-// BITS: of the states.  Thread t has eight adjacent entries of every 2048; 32 threads have a block of an 8-bit state.
+// BITS: of the states.  A thread has eight adjacent entries of every 2048; 32 threads have a block of an 8-bit state.  FULL: the tensor does not end in
+// the chunk, so that no load waits for a branch.
+struct AdamJob {
+    double factor, b1, c1, b2, c2;
+    AdamRates rates;
+    float eps;
+    uint32_t key;
+    bool go;
+};
+template <bool FULL, class T>
+__device__ __forceinline__ void load_entries(const T* p, int n, float (&f)[8]) {
+    if constexpr (FULL) l8_floats(l8_raw(p), f);
+    else l8_load(p, n, f);
+}
+template <class P, class G, int BITS, bool FULL>
+__device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t, uint64_t at) {
+    P* const param = (P*)t.param;
+    const G* const grad = (const G*)t.grad;
+    float p[ADAM_ITEMS][8], g[ADAM_ITEMS][8], m[ADAM_ITEMS][8], v[ADAM_ITEMS][8];
+    int n[ADAM_ITEMS];
+    uint64_t j[ADAM_ITEMS];
+#pragma unroll
+    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
+        j[k] = at + k * 2048;
+        n[k] = FULL ? 8 : j[k] < t.n ? (int)min((uint64_t)8, t.n - j[k]) : 0;
+        if (!n[k]) j[k] = 0;
+        load_entries<FULL>(param + j[k], n[k], p[k]);
+        load_entries<FULL>(grad + j[k], n[k], g[k]);
+        if constexpr (BITS == 32) {
+            load_entries<FULL>((const float*)t.m + j[k], n[k], m[k]);
+            load_entries<FULL>((const float*)t.v + j[k], n[k], v[k]);
+        } else {
+            const Codes8 cm = load_codes((const uint8_t*)t.m + j[k], n[k]), cv = load_codes((const uint8_t*)t.v + j[k], n[k]);
+            const uint32_t em = n[k] ? max(40u, (uint32_t)t.m_scale[j[k] / ADAM_BLOCK8]) : 40u, ev = n[k] ? max(40u, (uint32_t)t.v_scale[j[k] / ADAM_BLOCK8]) : 40u;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t x = cm.w[q / 4] >> (8 * (q % 4)) & 255u, y = cv.w[q / 4] >> (8 * (q % 4)) & 255u;
+                m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x & 127, em)) | (x & 128) << 24);
+                v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
+        if (a.go) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const double d = (double)g[k][q] * a.factor;
+                m[k][q] = (float)fma(a.b1, (double)m[k][q], a.c1 * d);
+                v[k][q] = (float)fma(a.b2, (double)v[k][q], a.c2 * (d * d));
+                const float below = fmaf(__builtin_amdgcn_sqrtf(v[k][q]), a.rates.root, a.eps);
+                p[k][q] = fmaf(-a.rates.rate * m[k][q], __builtin_amdgcn_rcpf(below), p[k][q] * a.rates.keep);
+            }
+            l8_store(param + j[k], n[k], p[k]);
+        }
+        if constexpr (BITS == 32) {
+            l8_store((float*)t.m + j[k], n[k], m[k]);
+            l8_store((float*)t.v + j[k], n[k], v[k]);
+        } else {
+            if (a.go) {
+                uint32_t tm = 0, tv = 0;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    if (FULL || q < n[k]) {
+                        tm = max(tm, l8_mag(m[k][q]));
+                        tv = max(tv, l8_mag(v[k][q]));
+                    }
+                }
+                const uint32_t em = M8::scale(half_wave_max(tm)), ev = V8::scale(half_wave_max(tv));
+                const uint64_t block = j[k] / ADAM_BLOCK8;
+                const uint32_t kb = mix(a.key ^ (uint32_t)block), place = (uint32_t)(j[k] % ADAM_BLOCK8);
+                Codes8 cm = {{0, 0}}, cv = {{0, 0}};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t r = mix(kb + (place + q) * 0x9E3779B1u);
+                    const uint32_t um = __float_as_uint(m[k][q]), uv = l8_mag(v[k][q]);
+                    uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16), y = V8::code(uv, ev, r & 0xFFFFu);
+                    y = uv ? max(y, 1u) : y;
+                    x = em == 255 ? 0 : x;
+                    y = ev == 255 ? 0 : y;
+                    m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x, em)) | (um & 0x80000000u));
+                    v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
+                    x |= em == 255 ? 0 : um >> 24 & 128u;
+                    cm.w[q / 4] |= x << (8 * (q % 4));
+                    cv.w[q / 4] |= y << (8 * (q % 4));
+                }
+                store_codes((uint8_t*)t.m + j[k], n[k], cm);
+                store_codes((uint8_t*)t.v + j[k], n[k], cv);
+                if ((threadIdx.x & 31) == 0 && n[k]) {
+                    t.m_scale[block] = (uint8_t)em;
+                    t.v_scale[block] = (uint8_t)ev;
+                }
+            }
+            if (t.m_value) l8_store(t.m_value + j[k], n[k], m[k]);
+            if (t.v_value) l8_store(t.v_value + j[k], n[k], v[k]);
+        }
+    }
+}
+
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
     __shared__ AdamRates s_rates;
@@ -234,87 +332,9 @@ __global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
     const double b1 = a.beta1, c1 = 1 - b1, b2 = a.beta2, c2 = 1 - b2;
     const uint32_t key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
     const uint64_t at = (uint64_t)(blockIdx.x - a.first[i]) * ADAM_CHUNK + threadIdx.x * 8;
-    P* const param = (P*)t.param;
-    const G* const grad = (const G*)t.grad;
-    float p[ADAM_ITEMS][8], g[ADAM_ITEMS][8], m[ADAM_ITEMS][8], v[ADAM_ITEMS][8];
-    int n[ADAM_ITEMS];
-    uint64_t j[ADAM_ITEMS];
-#pragma unroll
-    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
-        j[k] = at + k * 2048;
-        n[k] = j[k] < t.n ? (int)min((uint64_t)8, t.n - j[k]) : 0;
-        if (!n[k]) j[k] = 0;
-        l8_load(param + j[k], n[k], p[k]);
-        l8_load(grad + j[k], n[k], g[k]);
-        if constexpr (BITS == 32) {
-            l8_load((const float*)t.m + j[k], n[k], m[k]);
-            l8_load((const float*)t.v + j[k], n[k], v[k]);
-        } else {
-            const Codes8 cm = load_codes((const uint8_t*)t.m + j[k], n[k]), cv = load_codes((const uint8_t*)t.v + j[k], n[k]);
-            const uint32_t em = n[k] ? max(40u, (uint32_t)t.m_scale[j[k] / ADAM_BLOCK8]) : 40u, ev = n[k] ? max(40u, (uint32_t)t.v_scale[j[k] / ADAM_BLOCK8]) : 40u;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const uint32_t x = cm.w[q / 4] >> (8 * (q % 4)) & 255u, y = cv.w[q / 4] >> (8 * (q % 4)) & 255u;
-                m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x & 127, em)) | (x & 128) << 24);
-                v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
-            }
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
-        if (go) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const double d = (double)g[k][q] * factor;
-                m[k][q] = (float)fma(b1, (double)m[k][q], c1 * d);
-                v[k][q] = (float)fma(b2, (double)v[k][q], c2 * (d * d));
-                const float below = fmaf(__builtin_amdgcn_sqrtf(v[k][q]), rates.root, a.eps);
-                p[k][q] = fmaf(-rates.rate * m[k][q], __builtin_amdgcn_rcpf(below), p[k][q] * rates.keep);
-            }
-            l8_store(param + j[k], n[k], p[k]);
-        }
-        if constexpr (BITS == 32) {
-            l8_store((float*)t.m + j[k], n[k], m[k]);
-            l8_store((float*)t.v + j[k], n[k], v[k]);
-        } else {
-            if (go) {
-                uint32_t tm = 0, tv = 0;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (q < n[k]) {
-                        tm = max(tm, l8_mag(m[k][q]));
-                        tv = max(tv, l8_mag(v[k][q]));
-                    }
-                }
-                const uint32_t em = M8::scale(half_wave_max(tm)), ev = V8::scale(half_wave_max(tv));
-                const uint64_t block = j[k] / ADAM_BLOCK8;
-                const uint32_t kb = mix(key ^ (uint32_t)block), place = (uint32_t)(j[k] % ADAM_BLOCK8);
-                Codes8 cm = {{0, 0}}, cv = {{0, 0}};
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const uint32_t r = mix(kb + (place + q) * 0x9E3779B1u);
-                    const uint32_t um = __float_as_uint(m[k][q]), uv = l8_mag(v[k][q]);
-                    uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16), y = V8::code(uv, ev, r & 0xFFFFu);
-                    y = uv ? max(y, 1u) : y;
-                    x = em == 255 ? 0 : x;
-                    y = ev == 255 ? 0 : y;
-                    m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x, em)) | (um & 0x80000000u));
-                    v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
-                    x |= em == 255 ? 0 : um >> 24 & 128u;
-                    cm.w[q / 4] |= x << (8 * (q % 4));
-                    cv.w[q / 4] |= y << (8 * (q % 4));
-                }
-                store_codes((uint8_t*)t.m + j[k], n[k], cm);
-                store_codes((uint8_t*)t.v + j[k], n[k], cv);
-                if ((threadIdx.x & 31) == 0 && n[k]) {
-                    t.m_scale[block] = (uint8_t)em;
-                    t.v_scale[block] = (uint8_t)ev;
-                }
-            }
-            if (t.m_value) l8_store(t.m_value + j[k], n[k], m[k]);
-            if (t.v_value) l8_store(t.v_value + j[k], n[k], v[k]);
-        }
-    }
+    AdamJob job = {factor, b1, c1, b2, c2, rates, a.eps, key, go};
+    if ((uint64_t)(blockIdx.x - a.first[i] + 1) * ADAM_CHUNK <= t.n) adam_chunk<P, G, BITS, true>(job, t, at);
+    else adam_chunk<P, G, BITS, false>(job, t, at);
 }
 
 template <class P, class G>
