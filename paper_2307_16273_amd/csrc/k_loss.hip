@@ -92,6 +92,8 @@ __device__ __forceinline__ void put_terms(const LossArgs& a, uint64_t r, const f
     for (int i = 0; i < 3; ++i) a.terms[i * a.rows + r] = term[i];
 }
 
+// A number that all lanes of the wave have, in a scalar register.
+__device__ __forceinline__ float of_wave(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
@@ -112,36 +114,74 @@ __device__ __forceinline__ float row_reduce(float x, float* s) {
 }
 
 // Eight adjacent items as they lie in memory, two of 16 bits to a register, and as floats.
+typedef uint32_t Quad __attribute__((ext_vector_type(4)));
+typedef uint32_t QuadAnywhere __attribute__((ext_vector_type(4), aligned(1)));
 template <class T>
-struct __attribute__((packed, aligned(1))) Raw8 {
-    uint32_t w[2 * sizeof(T)];
+struct Raw8 {
+    Quad q[sizeof(T) / 2];
+    __device__ __forceinline__ uint32_t operator[](int i) const { return q[i / 4][i % 4]; }
 };
 template <class T>
-__device__ __forceinline__ Raw8<T> load8(const T* p) { return *(const Raw8<T>*)p; }
+__device__ __forceinline__ Raw8<T> load8(const T* p) {
+    Raw8<T> v;
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.q[h] = ((const QuadAnywhere*)p)[h];
+    return v;
+}
 __device__ __forceinline__ void floats8(const Raw8<float>& v, float (&f)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v.w[i]);
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]);
 }
 __device__ __forceinline__ void floats8(const Raw8<bf16_t>& v, float (&f)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(v.w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(v.w[i] & 0xFFFF0000u);
+        f[2 * i] = __uint_as_float(v[i] << 16);
+        f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
     }
 }
 __device__ __forceinline__ void floats8(const Raw8<__half>& v, float (&f)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 x = __half22float2(__builtin_bit_cast(__half2, v.w[i]));
+        const float2 x = __half22float2(__builtin_bit_cast(__half2, v[i]));
         f[2 * i] = x.x;
         f[2 * i + 1] = x.y;
     }
+}
+// Eight floats as they leave for memory, two of 16 bits rounded by one instruction.
+__device__ __forceinline__ void pack8(const float (&f)[8], Raw8<float>& v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.q[i / 4][i % 4] = __float_as_uint(f[i]);
+}
+__device__ __forceinline__ void pack8(const float (&f)[8], Raw8<bf16_t>& v) {
+    typedef float F2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const F2 x = {f[2 * i], f[2 * i + 1]};
+        v.q[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, B2));
+    }
+}
+__device__ __forceinline__ void pack8(const float (&f)[8], Raw8<__half>& v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __half lo, hi;
+        l8_put(f[2 * i], lo);
+        l8_put(f[2 * i + 1], hi);
+        v.q[0][i] = (uint32_t)__half_as_ushort(lo) | (uint32_t)__half_as_ushort(hi) << 16;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+    Raw8<T> w;
+    pack8(f, w);
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) ((QuadAnywhere*)p)[h] = w.q[h];
 }
 // What follows takes the floats of v from its registers again: without this they would stay in registers of their own, twice as many.
 template <class T>
 __device__ __forceinline__ void keep_packed(Raw8<T>& v) {
 #pragma unroll
-    for (uint32_t& w : v.w) asm("" : "+v"(w));
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) asm("" : "+v"(v.q[h]));
 }
 template <class T>
 __device__ __forceinline__ float max8(float c, const Raw8<T>& v) {
@@ -177,41 +217,47 @@ __device__ __forceinline__ void put_end(T* row, const L8At& end, const float (&f
         if ((uint32_t)i >= end.dup) put_one(row + end.start + i, f[i]);
 }
 
-// Eight items at p + n + lane, p and n being the whole wave's: the instruction adds the lane's own offset, and no vector has an address of 64
-// bits of its own.
-typedef uint32_t Quad __attribute__((ext_vector_type(4), aligned(1)));
+// Eight items, `lane` bytes behind p + n, p and n being the whole wave's: the instruction adds the lane's own offset, and no vector has an address
+// of 64 bits of its own.
+// In bytes.  (Opaque, so that it stays the 32-bit offset that the instruction takes.)
+template <class T>
+__device__ __forceinline__ uint32_t own_offset(uint32_t t) {
+    uint32_t o = t * 8 * (uint32_t)sizeof(T);
+    asm("" : "+v"(o));
+    return o;
+}
 template <class T>
 __device__ __forceinline__ Raw8<T> load8_at(const T* p, uint32_t n, uint32_t lane) {
     uint64_t at = (uint64_t)(p + n);
     asm("" : "+s"(at));
-    const auto* q = (const __attribute__((address_space(1))) Quad*)(at + lane * (uint32_t)sizeof(T));
+    const auto* q = (const __attribute__((address_space(1))) QuadAnywhere*)(at + lane);
     Raw8<T> v;
 #pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-        const Quad x = q[h];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v.w[4 * h + i] = x[i];
-    }
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.q[h] = q[h];
     return v;
 }
 template <class T>
 __device__ __forceinline__ void store8_at(T* p, uint32_t n, uint32_t lane, const float (&f)[8]) {
     uint64_t at = (uint64_t)(p + n);
     asm("" : "+s"(at));
-    auto* q = (__attribute__((address_space(1))) Quad*)(at + lane * (uint32_t)sizeof(T));
-    struct {
-        T v[8];
-    } o;
+    auto* q = (__attribute__((address_space(1))) QuadAnywhere*)(at + lane);
+    Raw8<T> w;
+    pack8(f, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) l8_put(f[i], o.v[i]);
-    const Raw8<T> w = __builtin_bit_cast(Raw8<T>, o);
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) q[h] = w.q[h];
+}
+// A thread's vector in LDS, 16 bytes of it next to the other threads'.
+template <class T, int N>
+__device__ __forceinline__ void put_lds(Quad (*to)[N], uint32_t t, const Raw8<T>& v) {
 #pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-        Quad x;
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) to[h][t] = v.q[h];
+}
+template <class T, int N>
+__device__ __forceinline__ Raw8<T> get_lds(Quad (*from)[N], uint32_t t) {
+    Raw8<T> v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = w.w[4 * h + i];
-        q[h] = x;
-    }
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.q[h] = from[h][t];
+    return v;
 }
 template <class T, int G, int WHOLE>
 __device__ __forceinline__ void put_zeros(T* to, uint32_t t, bool ends, const L8At& end) {
@@ -224,86 +270,115 @@ __device__ __forceinline__ void put_zeros(T* to, uint32_t t, bool ends, const L8
 enum { ROWS_LOGP, ROWS_POLICY };
 
 // ---------------------------------------------------------------------------
-// Rows that stay in registers: G threads a row (a wave: four rows a block) with WHOLE vectors of eight each, and one at the row's end:
-// 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols >= 8.  (As many instances as there are lengths: with a count that the kernel learns when it
-// runs, the vectors' registers were copied and spilled.)
+// Rows that stay on the chip: G threads a row (a wave: four rows a block) with WHOLE vectors of eight each, and one at the row's end:
+// 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols >= 8.  The vectors are in registers, but for the last of the longest rows, which lie in LDS: so two
+// blocks of 512 threads with 128 registers each, and half of the LDS, have room in a compute unit up to rows of 256 kB, and one of them has
+// memory at work while the other computes.  (As many instances as there are lengths: with a count that the kernel learns when it runs, the
+// vectors' registers were copied and spilled.)
 // ---------------------------------------------------------------------------
 constexpr int loss_threads(int G) { return G < 256 ? 256 : G; }
+// vectors in registers, by what else a thread holds, and in LDS, of which a compute unit has 160 kB
+template <class T>
+constexpr int loss_regs(int whole) { return whole <= 32 / (int)sizeof(T) ? whole : whole <= 50 / (int)sizeof(T) ? 32 / (int)sizeof(T) : whole - 18 / (int)sizeof(T); }
 template <class T, int MODE, int G, int WHOLE>
-__global__ __launch_bounds__(loss_threads(G)) void k_loss_rows(LossArgs a, L8Mat<const T> x, L8Mat<T> out) {
-    constexpr int GROUPS = loss_threads(G) / G;
+__global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows(LossArgs a, L8Mat<const T> x, L8Mat<T> out) {
+    constexpr int GROUPS = loss_threads(G) / G, REGS = loss_regs<T>(WHOLE), STORED = WHOLE - REGS;
     constexpr uint32_t EACH = 8 * G;
     __shared__ float s_max[G / 64], s_sum[G / 64];
-    const uint32_t t = threadIdx.x % G;
+    __shared__ Quad s_v[STORED ? STORED * (sizeof(T) / 2) : 1][STORED ? G : 1];
+    const uint32_t t = threadIdx.x % G, mine = own_offset<T>(t);
     const uint32_t group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
-    const bool leader = t == 0, ends = WHOLE * EACH < a.cols;
+    const bool ends = WHOLE * EACH < a.cols;
     const L8At end = l8_at(WHOLE * EACH + t * 8, a.cols);
-    for (uint64_t r = (uint64_t)blockIdx.x * GROUPS + group; r < a.rows; r += (uint64_t)gridDim.x * GROUPS) {
-        const int64_t y = token_of(a, r);
-        T* const to = out.p + r * out.rs;
-        float term[3] = {0.f, 0.f, 0.f};
-        RowStats st = {0.f, 0.f, 0.f};
-        if (y >= 0) {
-            const T* const row = x.p + r * x.rs;
-            Raw8<T> v[WHOLE + 1];
+    const uint64_t r = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + group;       // (a loop over rows would keep its constants in registers)
+    if (r >= a.rows) return;
+    const int64_t y = token_of(a, r);
+    T* const to = out.p + r * out.rs;
+    float term[3] = {0.f, 0.f, 0.f};
+    RowStats st = {0.f, 0.f, 0.f};
+    if (y >= 0) {
+        const T* const row = x.p + r * x.rs;
+        Raw8<T> v[REGS ? REGS : 1], last;
+        float c = -INF, sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < WHOLE; ++k) v[k] = load8_at(row, k * EACH, t * 8);
-            if (ends) v[WHOLE] = load8(row + end.start);
-            const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
-            float c = -INF, sum = 0.f;
+        for (int k = 0; k < STORED; ++k) v[k] = load8_at(row, (REGS + k) * EACH, mine);
 #pragma unroll
-            for (int k = 0; k < WHOLE; ++k) c = max8(c, v[k]);
-            if (ends) c = max8(c, v[WHOLE]);
-            c = row_reduce<G, true>(c, s_max);
+        for (int k = STORED; k < REGS; ++k) v[k] = load8_at(row, k * EACH, mine);
 #pragma unroll
-            for (int k = 0; k < WHOLE; ++k) {
-                float f[8];
-                keep_packed(v[k]);
-                floats8(v[k], f);
+        for (int k = 0; k < STORED; ++k) {
+            c = max8(c, v[k]);
+            put_lds<T>(&s_v[k * (sizeof(T) / 2)], t, v[k]);
+            v[k] = load8_at(row, k * EACH, mine);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ends) last = load8(row + end.start);
+        const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += term_of(f[i], c, a.k);
+        for (int k = 0; k < REGS; ++k) {
+            c = max8(c, v[(k + STORED) % (REGS ? REGS : 1)]);       // in the order in which they were asked for
+            if (STORED) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ends) c = max8(c, last);
+        c = of_wave(row_reduce<G, true>(c, s_max));
+#pragma unroll
+        for (int k = 0; k < WHOLE; ++k) {
+            float f[8];
+            if (k < REGS) {
+                keep_packed(v[k < REGS ? k : 0]);
+                floats8(v[k < REGS ? k : 0], f);
+            } else {
+                floats8(get_lds<T>(&s_v[(k < REGS ? 0 : k - REGS) * (sizeof(T) / 2)], t), f);
             }
-            if (ends) {         // what another thread has, or nobody, stays out
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += term_of(f[i], c, a.k);
+            if (STORED) __builtin_amdgcn_sched_barrier(0);      // one vector's floats at a time: no registers are left for more
+        }
+        if (ends) {         // what another thread has, or nobody, stays out
+            float f[8];
+            if (STORED) last = load8(row + end.start);          // (read again: the registers are the others')
+            else keep_packed(last);
+            floats8(last, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += end.live && (uint32_t)i >= end.dup ? term_of(f[i], c, a.k) : 0.f;
+        }
+        sum = of_wave(row_reduce<G, false>(sum, s_sum));
+        st = row_stats(a, c, sum, y, xy);
+        if (MODE == ROWS_POLICY) {
+            const float dlogp = policy_row(a, r, st.logp, term);
+            const float co = dlogp * a.inv_tau, co_inv = of_wave(co / sum);
+            if (out.p && dlogp != 0) {
                 float f[8];
-                keep_packed(v[WHOLE]);
-                floats8(v[WHOLE], f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += end.live && (uint32_t)i >= end.dup ? term_of(f[i], c, a.k) : 0.f;
-            }
-            sum = row_reduce<G, false>(sum, s_sum);
-            st = row_stats(a, c, sum, y, xy);
-            if (MODE == ROWS_POLICY) {
-                const float dlogp = policy_row(a, r, st.logp, term);
-                const float co = dlogp * a.inv_tau, co_inv = co / sum;
-                if (out.p && dlogp != 0) {
-                    float f[8];
-#pragma unroll
-                    for (int k = 0; k < WHOLE; ++k) {
-                        keep_packed(v[k]);
-                        slope8(v[k], c, a.k, co_inv, f);
-                        store8_at(to, k * EACH, t * 8, f);
+                for (int k = 0; k < WHOLE; ++k) {
+                    if (k < REGS) {
+                        keep_packed(v[k < REGS ? k : 0]);
+                        slope8(v[k < REGS ? k : 0], c, a.k, co_inv, f);
+                    } else {
+                        slope8(get_lds<T>(&s_v[(k < REGS ? 0 : k - REGS) * (sizeof(T) / 2)], t), c, a.k, co_inv, f);
                     }
-                    if (ends) {
-                        keep_packed(v[WHOLE]);
-                        slope8(v[WHOLE], c, a.k, co_inv, f);
-                        put_end(to, end, f);
-                    }
-                    if (y < (int64_t)a.cols && t == (uint32_t)y / 8 % G) put_one(to + y, fmaf(-co_inv, term_of(xy, c, a.k), co));
-                } else if (out.p) {
-                    put_zeros<T, G, WHOLE>(to, t, ends, end);
+                    store8_at(to, k * EACH, mine, f);
+                    if (STORED) __builtin_amdgcn_sched_barrier(0);
                 }
+                if (ends) {
+                    if (STORED) last = load8(row + end.start);
+                    else keep_packed(last);
+                    slope8(last, c, a.k, co_inv, f);
+                    put_end(to, end, f);
+                }
+                if (y < (int64_t)a.cols && t == (uint32_t)y / 8 % G) put_one(to + y, fmaf(-co_inv, term_of(xy, c, a.k), co));
+            } else if (out.p) {
+                put_zeros<T, G, WHOLE>(to, t, ends, end);
             }
-        } else if (MODE == ROWS_POLICY && out.p) {
-            put_zeros<T, G, WHOLE>(to, t, ends, end);
         }
-        if (leader) {
-            if (a.logp) a.logp[r] = st.logp;
-            if (a.top) a.top[r] = st.top;
-            if (a.log_sum) a.log_sum[r] = st.log_sum;
-            if (a.dlogp) a.dlogp[r] = 0.f;
-            if (MODE == ROWS_POLICY) put_terms(a, r, term);
-        }
-        if (G > 64) __syncthreads();        // s_max and s_sum are the next row's
+    } else if (MODE == ROWS_POLICY && out.p) {
+        put_zeros<T, G, WHOLE>(to, t, ends, end);
+    }
+    if (t == 0) {
+        if (a.logp) a.logp[r] = st.logp;
+        if (a.top) a.top[r] = st.top;
+        if (a.log_sum) a.log_sum[r] = st.log_sum;
+        if (a.dlogp) a.dlogp[r] = 0.f;
+        if (MODE == ROWS_POLICY) put_terms(a, r, term);
     }
 }
 
@@ -322,7 +397,7 @@ __device__ __forceinline__ void part_of(const LossArgs& a, const T* row, uint32_
     if constexpr (FULL) {
         Raw8<T> v[ITEMS];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) v[k] = load8_at(row + (uint64_t)q * (ITEMS * 2048), k * 2048, threadIdx.x * 8);
+        for (int k = 0; k < ITEMS; ++k) v[k] = load8_at(row + (uint64_t)q * (ITEMS * 2048), k * 2048, own_offset<T>(threadIdx.x));
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             n[k] = 8;
@@ -435,7 +510,7 @@ __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to,
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)s.y - j == i ? s.co : 0.f;
         }
-        if (FULL) l8_store(to + j, 8, f[k]);
+        if (FULL) store8(to + j, f[k]);
         else l8_store(to + (n[k] ? j : 0), n[k], f[k]);
     }
 }
@@ -547,14 +622,14 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
 }
 
 // ---- launches ----------------------------------------------------------------------
-// The longest row that stays in a block's registers: 16 vectors a thread of 16-bit entries, less than 8 of 32-bit ones.
+// The longest row that stays on the chip: 256 kB.
 template <class T>
-constexpr uint32_t loss_longest() { return sizeof(T) == 2 ? 1024 * 8 * 16 : 1024 * 8 * 8 - 1; }
+constexpr uint32_t loss_longest() { return 262144 / sizeof(T); }
 
 template <class T, int MODE, int G, int WHOLE>
 void launch_rows_of(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
-    const uint64_t blocks = l8_ceil(a.rows, loss_threads(G) / G);
-    hipLaunchKernelGGL((k_loss_rows<T, MODE, G, WHOLE>), dim3((unsigned)(blocks < (1u << 20) ? blocks : 1u << 20)), dim3(loss_threads(G)), 0, ctx->stream, a, x, out);
+    const uint64_t blocks = l8_ceil(a.rows, loss_threads(G) / G), wide = blocks < (1u << 20) ? blocks : 1u << 20;
+    hipLaunchKernelGGL((k_loss_rows<T, MODE, G, WHOLE>), dim3((unsigned)wide, (unsigned)l8_ceil(blocks, wide)), dim3(loss_threads(G)), 0, ctx->stream, a, x, out);
 }
 template <class T, int MODE, int G, int WHOLE, int LAST>
 void launch_rows_from(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
@@ -565,11 +640,11 @@ void launch_rows_from(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<
 // threads wait for one another.
 template <class T, int MODE>
 void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
-    constexpr int MOST = sizeof(T) == 2 ? 16 : 7;       // vectors that leave room for what else a thread holds
+    constexpr int MOST = 32 / sizeof(T);        // vectors in registers
     const bool many = a.rows >= 1024;
     if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
     else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST + 1))) launch_rows_from<T, MODE, 256, 1, MOST>(ctx, a, x, out);
-    else launch_rows_from<T, MODE, 1024, 1, MOST>(ctx, a, x, out);
+    else launch_rows_from<T, MODE, 512, 2, 2 * MOST>(ctx, a, x, out);
 }
 
 template <class T>
