@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "layer8.cuh"
+#include "vec8.cuh"
 
 namespace {
 
@@ -116,7 +117,7 @@ struct AdamArgs {
     AdamTensor t[ADAM_TENSORS];
     uint32_t first[ADAM_TENSORS + 1];
     uint32_t count, seed_lo, seed_hi, step;
-    double lr, decay, beta1, beta2;
+    double lr, decay, beta1, beta2, root2;      // root2: (1 - beta2)^(1/2)
     const int64_t* step_ptr;
     const float *lr_ptr, *factor;
     float eps;
@@ -161,22 +162,29 @@ struct Float8 {
         const uint32_t e = max(40u, (top + 0xFFFFFu) >> 23);
         return e > 254 ? 255u : e;
     }
-    // value of a code without its sign
-    static __device__ __forceinline__ float value(uint32_t code, uint32_t e) {
-        const float whole = __uint_as_float((code << 20) + ((e - LAST) << 23)), part = (float)code * __uint_as_float((e - LAST - 2) << 23);
-        return code >= 8 ? whole : part;
+    // A code's bits are those of a float's exponent and mantissa: that float (subnormal where the code's exponent is 0) times 2^(e - LAST) is its value.
+    // NaN where the block holds none.
+    static __device__ __forceinline__ double unit(uint32_t e) {
+        const double u = __hiloint2double((int)((1023 - LAST + e) << 20), 0);
+        return e == 255 ? (double)__builtin_nanf("") : u;
     }
     // code of the magnitude with the bits u; r: 16 random bits
     static __device__ __forceinline__ uint32_t code(uint32_t u, uint32_t e, uint32_t r) {
         const uint32_t base = (e - LAST) << 23;
         const uint32_t whole = (u - base + (r << 4 | 8)) >> 20;
         const float place = __uint_as_float(u) * __uint_as_float((254 - (e - LAST - 2)) << 23);
-        const uint32_t part = (uint32_t)(int)(place + ((float)r + .5f) * 0x1p-16f);
+        const uint32_t part = (uint32_t)(int)(place + fmaf((float)r, 0x1p-16f, 0x1p-17f));
         return u >= base + (1u << 23) ? whole : part;
     }
 };
 typedef Float8<4> M8;
 typedef Float8<5> V8;
+// Entry q of eight codes as the float that a code's bits are
+__device__ __forceinline__ float m_float(const uint32_t (&w)[2], int q) {
+    const uint32_t c = w[q / 4] >> (8 * (q % 4));
+    return __uint_as_float((c & 0x7Fu) << 20 | (c & 0x80u) << 24);
+}
+__device__ __forceinline__ float v_float(const uint32_t (&w)[2], int q) { return __uint_as_float((w[q / 4] >> (8 * (q % 4)) & 0xFFu) << 20); }
 
 struct __attribute__((packed, aligned(1))) Codes8 {
     uint32_t w[2];
@@ -208,22 +216,35 @@ __device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
 // BITS: of the states.  A thread has eight adjacent entries of every 2048; 32 threads have a block of an 8-bit state.  FULL: the tensor does not end in
 // the chunk, so that no load waits for a branch.
 struct AdamJob {
-    double factor, b1, c1, b2, c2;
+    double b1, b2, c1, c2;      // m <- b1 m + c1 grad, v <- b2 v + (c2 grad)^2: the gradients' factor is in c1 and c2
     AdamRates rates;
     float eps;
     uint32_t key;
     bool go;
 };
 template <bool FULL, class T>
-__device__ __forceinline__ void load_entries(const T* p, int n, float (&f)[8]) {
-    if constexpr (FULL) l8_floats(l8_raw(p), f);
-    else l8_load(p, n, f);
+__device__ __forceinline__ Raw8<T> load_raw(const T* p, int n) {
+    if constexpr (FULL) return load8(p);
+    float f[8];
+    Raw8<T> v;
+    l8_load(p, n, f);
+    pack8(f, v);        // (exactly: they came from T)
+    return v;
+}
+template <bool FULL, class T>
+__device__ __forceinline__ void store_entries(T* p, int n, const float (&f)[8]) {
+    if constexpr (FULL) store8(p, f);
+    else l8_store(p, n, f);
 }
 template <class P, class G, int BITS, bool FULL>
 __device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t, uint64_t at) {
     P* const param = (P*)t.param;
     const G* const grad = (const G*)t.grad;
-    float p[ADAM_ITEMS][8], g[ADAM_ITEMS][8], m[ADAM_ITEMS][8], v[ADAM_ITEMS][8];
+    Raw8<P> praw[ADAM_ITEMS];
+    Raw8<G> graw[ADAM_ITEMS];
+    Raw8<float> mraw[BITS == 32 ? ADAM_ITEMS : 1], vraw[BITS == 32 ? ADAM_ITEMS : 1];
+    Codes8 mcode[ADAM_ITEMS], vcode[ADAM_ITEMS];
+    uint32_t mscale[ADAM_ITEMS], vscale[ADAM_ITEMS];
     int n[ADAM_ITEMS];
     uint64_t j[ADAM_ITEMS];
 #pragma unroll
@@ -231,79 +252,103 @@ __device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t
         j[k] = at + k * 2048;
         n[k] = FULL ? 8 : j[k] < t.n ? (int)min((uint64_t)8, t.n - j[k]) : 0;
         if (!n[k]) j[k] = 0;
-        load_entries<FULL>(param + j[k], n[k], p[k]);
-        load_entries<FULL>(grad + j[k], n[k], g[k]);
         if constexpr (BITS == 32) {
-            load_entries<FULL>((const float*)t.m + j[k], n[k], m[k]);
-            load_entries<FULL>((const float*)t.v + j[k], n[k], v[k]);
+            mraw[k] = load_raw<FULL>((const float*)t.m + j[k], n[k]);
+            vraw[k] = load_raw<FULL>((const float*)t.v + j[k], n[k]);
         } else {
-            const Codes8 cm = load_codes((const uint8_t*)t.m + j[k], n[k]), cv = load_codes((const uint8_t*)t.v + j[k], n[k]);
-            const uint32_t em = n[k] ? max(40u, (uint32_t)t.m_scale[j[k] / ADAM_BLOCK8]) : 40u, ev = n[k] ? max(40u, (uint32_t)t.v_scale[j[k] / ADAM_BLOCK8]) : 40u;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const uint32_t x = cm.w[q / 4] >> (8 * (q % 4)) & 255u, y = cv.w[q / 4] >> (8 * (q % 4)) & 255u;
-                m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x & 127, em)) | (x & 128) << 24);
-                v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
-            }
+            mscale[k] = n[k] ? t.m_scale[j[k] / ADAM_BLOCK8] : 0;
+            vscale[k] = n[k] ? t.v_scale[j[k] / ADAM_BLOCK8] : 0;
+            mcode[k] = load_codes((const uint8_t*)t.m + j[k], n[k]);
+            vcode[k] = load_codes((const uint8_t*)t.v + j[k], n[k]);
         }
+        praw[k] = load_raw<FULL>(param + j[k], n[k]);
+        graw[k] = load_raw<FULL>(grad + j[k], n[k]);
     }
 #pragma unroll
     for (int k = 0; k < (int)ADAM_ITEMS; ++k) {
-        if (a.go) {
+        float p[8], g[8], m[8], v[8];
+        double b1 = a.b1, b2 = a.b2;
+        uint32_t em = 0, ev = 0;
+        if constexpr (BITS == 32) {
+            floats8(mraw[k], m);
+            floats8(vraw[k], v);
+        } else {
+            em = max(40u, mscale[k]);
+            ev = max(40u, vscale[k]);
+            b1 *= M8::unit(em);
+            b2 *= V8::unit(ev);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const double d = (double)g[k][q] * a.factor;
-                m[k][q] = (float)fma(a.b1, (double)m[k][q], a.c1 * d);
-                v[k][q] = (float)fma(a.b2, (double)v[k][q], a.c2 * (d * d));
-                const float below = fmaf(__builtin_amdgcn_sqrtf(v[k][q]), a.rates.root, a.eps);
-                p[k][q] = fmaf(-a.rates.rate * m[k][q], __builtin_amdgcn_rcpf(below), p[k][q] * a.rates.keep);
+                m[q] = m_float(mcode[k].w, q);
+                v[q] = v_float(vcode[k].w, q);
             }
-            l8_store(param + j[k], n[k], p[k]);
         }
-        if constexpr (BITS == 32) {
-            l8_store((float*)t.m + j[k], n[k], m[k]);
-            l8_store((float*)t.v + j[k], n[k], v[k]);
-        } else {
-            if (a.go) {
-                uint32_t tm = 0, tv = 0;
+        if (a.go) {
+            floats8(praw[k], p);
+            floats8(graw[k], g);
+            uint32_t tm = 0, tv = 0;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (FULL || q < n[k]) {
-                        tm = max(tm, l8_mag(m[k][q]));
-                        tv = max(tv, l8_mag(v[k][q]));
-                    }
+            for (int q = 0; q < 8; ++q) {
+                const double d = (double)g[q], d2 = a.c2 * d;
+                m[q] = (float)fma(a.c1, d, b1 * (double)m[q]);
+                v[q] = (float)fma(d2, d2, b2 * (double)v[q]);
+                const float below = fmaf(__builtin_amdgcn_sqrtf(v[q]), a.rates.root, a.eps);
+                p[q] = fmaf(-a.rates.rate * m[q], __builtin_amdgcn_rcpf(below), p[q] * a.rates.keep);
+                if (BITS == 8 && (FULL || q < n[k])) {
+                    tm = max(tm, l8_mag(m[q]));
+                    tv = max(tv, l8_mag(v[q]));
                 }
-                const uint32_t em = M8::scale(half_wave_max(tm)), ev = V8::scale(half_wave_max(tv));
+            }
+            store_entries<FULL>(param + j[k], n[k], p);
+            if constexpr (BITS == 32) {
+                store_entries<FULL>((float*)t.m + j[k], n[k], m);
+                store_entries<FULL>((float*)t.v + j[k], n[k], v);
+            } else {
+                em = M8::scale(half_wave_max(tm));
+                ev = V8::scale(half_wave_max(tv));
                 const uint64_t block = j[k] / ADAM_BLOCK8;
-                const uint32_t kb = mix(a.key ^ (uint32_t)block), place = (uint32_t)(j[k] % ADAM_BLOCK8);
-                Codes8 cm = {{0, 0}}, cv = {{0, 0}};
+                const uint32_t first = mix(a.key ^ (uint32_t)block) + (uint32_t)(j[k] % ADAM_BLOCK8) * 0x9E3779B1u;
+                mcode[k] = vcode[k] = {{0, 0}};
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const uint32_t r = mix(kb + (place + q) * 0x9E3779B1u);
-                    const uint32_t um = __float_as_uint(m[k][q]), uv = l8_mag(v[k][q]);
-                    uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16), y = V8::code(uv, ev, r & 0xFFFFu);
-                    y = uv ? max(y, 1u) : y;
-                    x = em == 255 ? 0 : x;
-                    y = ev == 255 ? 0 : y;
-                    m[k][q] = em == 255 ? __builtin_nanf("") : __uint_as_float(__float_as_uint(M8::value(x, em)) | (um & 0x80000000u));
-                    v[k][q] = ev == 255 ? __builtin_nanf("") : V8::value(y, ev);
-                    x |= em == 255 ? 0 : um >> 24 & 128u;
-                    cm.w[q / 4] |= x << (8 * (q % 4));
-                    cv.w[q / 4] |= y << (8 * (q % 4));
+                    const uint32_t r = mix(first + (uint32_t)q * 0x9E3779B1u);
+                    const uint32_t um = __float_as_uint(m[q]), uv = l8_mag(v[q]);
+                    const uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16) | (um >> 24 & 128u);
+                    const uint32_t y = max(V8::code(uv, ev, r & 0xFFFFu), min(uv, 1u));       // a second moment that is there does not vanish
+                    mcode[k].w[q / 4] |= x << (8 * (q % 4));
+                    vcode[k].w[q / 4] |= y << (8 * (q % 4));
                 }
-                store_codes((uint8_t*)t.m + j[k], n[k], cm);
-                store_codes((uint8_t*)t.v + j[k], n[k], cv);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    mcode[k].w[h] = em == 255 ? 0 : mcode[k].w[h];
+                    vcode[k].w[h] = ev == 255 ? 0 : vcode[k].w[h];
+                }
+                store_codes((uint8_t*)t.m + j[k], n[k], mcode[k]);
+                store_codes((uint8_t*)t.v + j[k], n[k], vcode[k]);
                 if ((threadIdx.x & 31) == 0 && n[k]) {
                     t.m_scale[block] = (uint8_t)em;
                     t.v_scale[block] = (uint8_t)ev;
                 }
             }
-            if (t.m_value) l8_store(t.m_value + j[k], n[k], m[k]);
-            if (t.v_value) l8_store(t.v_value + j[k], n[k], v[k]);
+        }
+        if constexpr (BITS == 8) {
+            if (t.m_value) {
+                const double u = M8::unit(em);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) m[q] = (float)(u * (double)m_float(mcode[k].w, q));
+                store_entries<FULL>(t.m_value + j[k], n[k], m);
+            }
+            if (t.v_value) {
+                const double u = V8::unit(ev);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = (float)(u * (double)v_float(vcode[k].w, q));
+                store_entries<FULL>(t.v_value + j[k], n[k], v);
+            }
         }
     }
 }
 
+// BITS: of the states
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
     __shared__ AdamRates s_rates;
@@ -329,10 +374,9 @@ __global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
         factor = f;
     }
     if (BITS == 32 && !go) return;
-    const double b1 = a.beta1, c1 = 1 - b1, b2 = a.beta2, c2 = 1 - b2;
     const uint32_t key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
     const uint64_t at = (uint64_t)(blockIdx.x - a.first[i]) * ADAM_CHUNK + threadIdx.x * 8;
-    AdamJob job = {factor, b1, c1, b2, c2, rates, a.eps, key, go};
+    const AdamJob job = {a.beta1, a.beta2, (1 - a.beta1) * factor, a.root2 * factor, rates, a.eps, key, go};
     if ((uint64_t)(blockIdx.x - a.first[i] + 1) * ADAM_CHUNK <= t.n) adam_chunk<P, G, BITS, true>(job, t, at);
     else adam_chunk<P, G, BITS, false>(job, t, at);
 }
@@ -463,6 +507,7 @@ extern "C" int zkdl_adamw_step(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, 
     a.decay = how->decay;
     a.beta1 = how->beta1;
     a.beta2 = how->beta2;
+    a.root2 = std::sqrt(1 - how->beta2);
     a.step_ptr = how->step_ptr;
     a.lr_ptr = how->lr_ptr;
     a.factor = how->factor;
