@@ -168,23 +168,29 @@ struct Float8 {
         const double u = __hiloint2double((int)((1023 - LAST + e) << 20), 0);
         return e == 255 ? (double)__builtin_nanf("") : u;
     }
-    // code of the magnitude with the bits u; r: 16 random bits
+    // code of the magnitude with the bits u; r: 16 random bits; WHOLE: where the code's exponent is known not to be 0
+    static __device__ __forceinline__ uint32_t smallest(uint32_t e) { return (e - LAST + 1) << 23; }
+    template <bool WHOLE>
     static __device__ __forceinline__ uint32_t code(uint32_t u, uint32_t e, uint32_t r) {
         const uint32_t base = (e - LAST) << 23;
         const uint32_t whole = (u - base + (r << 4 | 8)) >> 20;
+        if (WHOLE) return whole;
         const float place = __uint_as_float(u) * __uint_as_float((254 - (e - LAST - 2)) << 23);
         const uint32_t part = (uint32_t)(int)(place + fmaf((float)r, 0x1p-16f, 0x1p-17f));
-        return u >= base + (1u << 23) ? whole : part;
+        return u >= smallest(e) ? whole : part;
     }
 };
 typedef Float8<4> M8;
 typedef Float8<5> V8;
-// Entry q of eight codes as the float that a code's bits are
+// Entry q of eight codes as the float that a code's bits are: moved to the sign, the exponent's last bits and the mantissa's first
 __device__ __forceinline__ float m_float(const uint32_t (&w)[2], int q) {
-    const uint32_t c = w[q / 4] >> (8 * (q % 4));
-    return __uint_as_float((c & 0x7Fu) << 20 | (c & 0x80u) << 24);
+    const uint32_t high = w[q / 4] << (24 - 8 * (q % 4));
+    return __uint_as_float((uint32_t)((int32_t)high >> 4) & 0x87F00000u);
 }
-__device__ __forceinline__ float v_float(const uint32_t (&w)[2], int q) { return __uint_as_float((w[q / 4] >> (8 * (q % 4)) & 0xFFu) << 20); }
+__device__ __forceinline__ float v_float(const uint32_t (&w)[2], int q) {
+    const uint32_t x = q % 4 == 3 ? w[q / 4] >> 4 : w[q / 4] << (20 - 8 * (q % 4) & 31);
+    return __uint_as_float(x & 0x0FF00000u);
+}
 
 struct __attribute__((packed, aligned(1))) Codes8 {
     uint32_t w[2];
@@ -205,6 +211,19 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int n, const Codes8& c) 
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) p[i] = (uint8_t)(c.w[i / 4] >> (8 * (i % 4)));
+}
+// Codes of eight entries, with their random bits: the upper 16 of m, the lower ones of v.
+template <class F, bool WHOLE>
+__device__ __forceinline__ void put_codes(const float (&x)[8], uint32_t e, const uint32_t (&r)[8], Codes8& to) {
+    to = {{0, 0}};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const uint32_t u = l8_mag(x[q]);
+        uint32_t c;
+        if constexpr (F::LAST == M8::LAST) c = F::template code<WHOLE>(u, e, r[q] >> 16) | (__float_as_uint(x[q]) >> 24 & 128u);
+        else c = WHOLE ? F::template code<WHOLE>(u, e, r[q] & 0xFFFFu) : max(F::template code<WHOLE>(u, e, r[q] & 0xFFFFu), min(u, 1u));       // a second moment that is there does not vanish
+        to.w[q / 4] |= c << (8 * (q % 4));
+    }
 }
 // over the 32 lanes that share a block of 256 entries
 __device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
@@ -308,16 +327,18 @@ __device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t
                 ev = V8::scale(half_wave_max(tv));
                 const uint64_t block = j[k] / ADAM_BLOCK8;
                 const uint32_t first = mix(a.key ^ (uint32_t)block) + (uint32_t)(j[k] % ADAM_BLOCK8) * 0x9E3779B1u;
-                mcode[k] = vcode[k] = {{0, 0}};
+                uint32_t lm = ~0u, lv = ~0u, r[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const uint32_t r = mix(first + (uint32_t)q * 0x9E3779B1u);
-                    const uint32_t um = __float_as_uint(m[q]), uv = l8_mag(v[q]);
-                    const uint32_t x = M8::code(um & 0x7FFFFFFFu, em, r >> 16) | (um >> 24 & 128u);
-                    const uint32_t y = max(V8::code(uv, ev, r & 0xFFFFu), min(uv, 1u));       // a second moment that is there does not vanish
-                    mcode[k].w[q / 4] |= x << (8 * (q % 4));
-                    vcode[k].w[q / 4] |= y << (8 * (q % 4));
+                    r[q] = mix(first + (uint32_t)q * 0x9E3779B1u);
+                    lm = min(lm, l8_mag(m[q]));
+                    lv = min(lv, l8_mag(v[q]));
                 }
+                // codes with exponent 0 cost half as much again and are rare (below 2^-14 or 2^-30 of the block's largest): a wave without any goes without
+                if (__any(lm < M8::smallest(em))) put_codes<M8, false>(m, em, r, mcode[k]);
+                else put_codes<M8, true>(m, em, r, mcode[k]);
+                if (__any(lv < V8::smallest(ev))) put_codes<V8, false>(v, ev, r, vcode[k]);
+                else put_codes<V8, true>(v, ev, r, vcode[k]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     mcode[k].w[h] = em == 255 ? 0 : mcode[k].w[h];
