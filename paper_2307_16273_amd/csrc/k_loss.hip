@@ -404,6 +404,41 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
 }
 
 // ---------------------------------------------------------------------------
+// Sums over rows, in 64 bits and always in the same order
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double wave_sum64(double x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+// N sums over a block of WAVES waves; s: N times as many numbers
+template <int N, int WAVES>
+__device__ __forceinline__ void block_sums64(double (&x)[N], double (*s)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = wave_sum64(x[i]);
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6][i] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) x[i] += s[w][i];
+    }
+}
+// out[b] = the sum of in[b][0 .. n), a block each
+template <class IN, class OUT>
+__global__ __launch_bounds__(1024) void k_loss_sum(const IN* in, uint64_t n, uint64_t per, OUT* out) {
+    __shared__ double s[16][1];
+    const uint64_t lo = blockIdx.x * per, hi = min(n, lo + per);
+    double x[1] = {0};
+    for (uint64_t i = lo + threadIdx.x; i < hi; i += 1024) x[0] += (double)in[blockIdx.y * n + i];
+    block_sums64<1, 16>(x, s);
+    if (threadIdx.x == 0) out[(uint64_t)blockIdx.y * gridDim.x + blockIdx.x] = (OUT)x[0];
+}
+
+// ---------------------------------------------------------------------------
 // The gradient of the logits from dlogp, top and log_sum: a wave has 2048 entries of a row.
 // ---------------------------------------------------------------------------
 struct SlopeRow {
@@ -447,7 +482,14 @@ __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to,
 }
 template <class T>
 __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
-                                                    uint32_t segs, uint32_t waves) {
+                                                    uint32_t segs, uint32_t waves, const float* losses, uint64_t pairs, float* loss) {
+    if (losses && blockIdx.x == 0 && blockIdx.y == 0) {         // the preference's loss, beside the gradient
+        __shared__ double s_loss[4][1];
+        double sum[1] = {0};
+        for (uint64_t i = threadIdx.x; i < pairs; i += 256) sum[0] += (double)losses[i];
+        block_sums64<1, 4>(sum, s_loss);
+        if (threadIdx.x == 0) *loss = (float)sum[0];
+    }
     // waves: of a row in one block, 1, 2 or 4
     const uint32_t per = 4 / waves, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (uint64_t r = (uint64_t)blockIdx.y * per + wave / waves; r < a.rows; r += (uint64_t)gridDim.y * per) {
@@ -467,30 +509,6 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
 }
 
 // ---------------------------------------------------------------------------
-// Sums over rows, in 64 bits and always in the same order
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ double block_sum64(double x, double* s) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0;
-    for (uint32_t i = 0; i < blockDim.x / 64; ++i) x += s[i];
-    return x;
-}
-// out[b] = the sum of in[b][0 .. n), a block each
-template <class IN, class OUT>
-__global__ __launch_bounds__(1024) void k_loss_sum(const IN* in, uint64_t n, uint64_t per, OUT* out) {
-    __shared__ double s[16];
-    const uint64_t lo = blockIdx.x * per, hi = min(n, lo + per);
-    double x = 0;
-    for (uint64_t i = lo + threadIdx.x; i < hi; i += 1024) x += (double)in[blockIdx.y * n + i];
-    x = block_sum64(x, s);
-    if (threadIdx.x == 0) out[(uint64_t)blockIdx.y * gridDim.x + blockIdx.x] = (OUT)x;
-}
-
-// ---------------------------------------------------------------------------
 // A pair of sequences: its margin, its share of the loss, and dlogp of its rows
 // ---------------------------------------------------------------------------
 struct PairArgs {
@@ -502,7 +520,7 @@ struct PairArgs {
     float *margin, *losses, *dlogp;
 };
 __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
-    __shared__ double s[4];
+    __shared__ double s[4][4];
     for (uint64_t i = blockIdx.x; i < a.pairs; i += gridDim.x) {
         uint64_t at[3];
 #pragma unroll
@@ -510,22 +528,17 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
             const int64_t o = a.offsets.at(2 * i + k);
             at[k] = o < 0 ? 0 : min((uint64_t)o, a.rows);
         }
-        double h[2], share[2];
-        for (int q = 0; q < 2; ++q) {
-            double x = 0, n = 0;
-            for (uint64_t r = at[q] + threadIdx.x; r < at[q + 1]; r += 256)
-                if (a.tokens.at(r) >= 0) {
-                    x += (double)a.logp[r] - (a.ref_logp ? (double)a.ref_logp[r] : 0.);
-                    n += 1;
-                }
-            x = block_sum64(x, s);
-            share[q] = 1;
-            if (a.average) {
-                n = block_sum64(n, s);
-                share[q] = 1 / fmax(n, 1.);
+        at[1] = max(at[1], at[0]);
+        double x[4] = {0, 0, 0, 0};         // of either sequence the sum, and the rows that count
+        for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += 256)
+            if (a.tokens.at(r) >= 0) {
+                const double d = (double)a.logp[r] - (a.ref_logp ? (double)a.ref_logp[r] : 0.);
+                const bool second = r >= at[1];
+                x[second] += d;
+                x[2 + second] += 1;
             }
-            h[q] = x * share[q];
-        }
+        block_sums64<4, 4>(x, s);
+        const double share[2] = {a.average ? 1 / fmax(x[2], 1.) : 1., a.average ? 1 / fmax(x[3], 1.) : 1.}, h[2] = {x[0] * share[0], x[1] * share[1]};
         const double margin = a.beta * (h[0] - h[1]), m = margin - a.target, w = a.weight ? (double)a.weight[i] : (double)a.every;
         double each, slope;
         if (a.form == ZKDL_PREF_LOGISTIC) {
@@ -544,11 +557,11 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
             if (a.margin) a.margin[i] = (float)margin;
             a.losses[i] = (float)(w * each);
         }
-        if (a.dlogp)
-            for (int q = 0; q < 2; ++q) {
-                const float d = (float)((q ? -w : w) * slope * a.beta * share[q]);
-                for (uint64_t r = at[q] + threadIdx.x; r < at[q + 1]; r += 256) a.dlogp[r] = a.tokens.at(r) >= 0 ? d : 0.f;
-            }
+        if (a.dlogp) {
+            const float d0 = (float)(w * slope * a.beta * share[0]), d1 = (float)(-w * slope * a.beta * share[1]);
+            for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += 256) a.dlogp[r] = a.tokens.at(r) < 0 ? 0.f : r >= at[1] ? d1 : d0;
+        }
+        __syncthreads();        // s is the next pair's
     }
 }
 
@@ -579,11 +592,12 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
 }
 
 template <class T>
-void launch_slope(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out) {
+void launch_slope(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
+                  const float* losses = nullptr, uint64_t pairs = 0, float* loss = nullptr) {
     const uint32_t segs = (uint32_t)l8_ceil(a.cols, 2048), waves = segs >= 4 ? 4 : segs >= 2 ? 2 : 1;
     const uint64_t gx = l8_ceil(segs, waves), gy = l8_ceil(a.rows, 4 / waves);
     hipLaunchKernelGGL((k_loss_slope<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(gy < 4096 ? gy : 4096)), dim3(256), 0, ctx->stream, a, dlogp, top,
-                       log_sum, x, out, segs, waves);
+                       log_sum, x, out, segs, waves, losses, pairs, loss);
 }
 
 // `sets` sums over n values each, one behind the other
@@ -694,8 +708,10 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
     PairArgs q = {a.rows, p->pairs, a.tokens, a.offsets, a.logp, p->ref_logp, p->weight, p->form, p->average, 1.f / (float)p->pairs, p->beta, p->target,
                   p->smoothing, margin, losses, dlogits ? a.dlogp : nullptr};
     if (p->pairs) hipLaunchKernelGGL(k_loss_pair, dim3((unsigned)(p->pairs < 65536 ? p->pairs : 65536)), dim3(256), 0, ctx->stream, q);
-    if (dlogits && a.rows) launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits));
-    return launch_sum(ctx, losses, p->pairs, 1, loss);
+    const bool few = dlogits && a.rows && p->pairs <= 4096;         // pairs whose losses one block adds up while others are at the gradient
+    if (dlogits && a.rows)
+        launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits), few ? losses : nullptr, p->pairs, loss);
+    return few ? (int)ZKDL_OK : launch_sum(ctx, losses, p->pairs, 1, loss);
 }
 
 }  // namespace
