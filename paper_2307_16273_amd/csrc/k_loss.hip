@@ -566,9 +566,15 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
 }
 
 // ---- launches ----------------------------------------------------------------------
-// The longest row that stays on the chip: 256 kB.
+// Whether rows stay on the chip, or go in parts: in registers rows below 136 kB are faster there however few they are (one row of 32768 16-bit entries
+// 5.3 us against 8.2, 1024 of them 15 / 17.5; with the policy's gradient 8.6 / 14.3 and 25 / 43).  With a part of the row in LDS, up to
+// 256 kB, only where a second read is saved, which a gradient needs, and rows enough to fill the device (policy, 131072 16-bit entries, in
+// LDS / in parts: 128 rows 29.5 / 24.8, 256 rows 37.9 / 41.6, 1024 rows 130 / 155; log-probabilities of 1024 rows 73 / 52).
 template <class T>
-constexpr uint32_t loss_longest() { return 262144 / sizeof(T); }
+bool rows_fit(const LossArgs& a, bool slope) {
+    constexpr uint32_t most = 32 / sizeof(T);       // vectors in registers
+    return a.cols >= 8 && (a.cols < 4096 * (most + 1) || (slope && a.rows >= 192 && a.cols <= 4096 * 2 * most));
+}
 
 template <class T, int MODE, int G, int WHOLE>
 void launch_rows_of(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
@@ -588,7 +594,7 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
     const bool many = a.rows >= 1024;
     if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
     else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST + 1))) launch_rows_from<T, MODE, 256, 1, MOST>(ctx, a, x, out);
-    else launch_rows_from<T, MODE, 512, 2, 2 * MOST>(ctx, a, x, out);
+    else launch_rows_from<T, MODE, 512, 2, MODE == ROWS_LOGP ? MOST : 2 * MOST>(ctx, a, x, out);
 }
 
 template <class T>
@@ -615,10 +621,6 @@ int launch_sum(zkdl_ctx* ctx, const float* in, uint64_t n, unsigned sets, float*
     zk_free(ctx, mid);
     return ZKDL_OK;
 }
-
-// Whether rows stay in registers, or go in parts.
-template <class T>
-bool rows_fit(const LossArgs& a) { return a.cols >= 8 && a.cols <= loss_longest<T>() && (a.rows >= 64 || a.cols < 8192); }
 
 template <class T, int MODE>
 int launch_parts(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x) {
@@ -667,7 +669,7 @@ struct Scratch {
 
 template <class T>
 int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const zkdl_mat* dlogits) {
-    const bool fit = rows_fit<T>(a);
+    const bool fit = rows_fit<T>(a, dlogits);
     Scratch s(ctx, a.rows * (fit || !dlogits ? 3 : 6));
     if (!s.p) return ZKDL_ENOMEM;
     a.terms = s.p;
@@ -698,7 +700,7 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
     a.last = 2 * p->pairs;
     float* losses = s.p + 4 * a.rows;
     if (a.rows) {
-        if (rows_fit<T>(a)) {
+        if (rows_fit<T>(a, false)) {
             launch_rows<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits), L8Mat<T>{nullptr, 0, 0});
         } else {
             const int rc = launch_parts<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits));
@@ -729,7 +731,7 @@ extern "C" int zkdl_token_logprobs(zkdl_ctx* ctx, const zkdl_mat* logits, const 
     a.log_sum = log_sum;
     const int rc = by_type(logits->dtype, [&](auto t) {
         using T = decltype(t);
-        if (!rows_fit<T>(a)) return launch_parts<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits));
+        if (!rows_fit<T>(a, false)) return launch_parts<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits));
         launch_rows<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits), L8Mat<T>{nullptr, 0, 0});
         return (int)ZKDL_OK;
     });

@@ -204,6 +204,32 @@ def test_policy_loss(lib, ctx, shape, dtype):
         assert alone["dlogits"] is None and all(torch.equal(alone[k], got[k]) for k in ("loss", "divergence", "clipped", "logp"))
 
 
+# a length for each number of whole vectors a thread has, for a wave, a block of 256 and one of 512 threads a row (from 1024 rows on fewer threads
+# have a row), and for rows of which a part lies in LDS (from 192 rows on)
+LENGTHS = ([(5, 512 * w + 77) for w in range(4)] + [(1030, 512 * w + 509) for w in range(8)] + [(9, 2048 * w + 3) for w in range(1, 4)] +
+           [(1024, 2048 * w + 1021) for w in range(2, 17)] + [(11, 4096 * w + 4089) for w in range(2, 17)])
+LONG = [(192, 4096 * w + 1365) for w in range(9, 32)] + [(192, 131072), (193, 65536), (200, 131071), (191, 131072)]
+
+
+@pytest.mark.parametrize("shape", LENGTHS + LONG, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_every_length(lib, ctx, shape, dtype):
+    """Log-probabilities and the policy's gradient; inputs made on the device."""
+    T, V = shape
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (torch.randn((T, V), generator=g, device="cuda") * 2).to(TYPES[dtype])
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[0], y[1], y[2] = V - 1, V // 8 * 8 - 1, -1
+    row = Row64(x, y, 1.0)
+    row.check(lib.token_logprobs(ctx, x, y))
+    old, adv, ref, w = policy_inputs(gen(V), row, T)
+    got = lib.policy_loss(ctx, x, y, old.cuda(), adv.cuda(), ref_logp=ref.cuda(), weight=w.cuda(), clip_low=0.2, clip_high=0.3, kl=0.125)
+    sums, errs, dlogp, derr = policy64(row, old, adv, ref, w, 0.2, 0.3, 0.125)
+    for k, s, e in zip(("loss", "divergence", "clipped"), sums, errs):
+        assert abs(got[k].item() - s.item()) <= e.item(), k
+    row.check_slope(got["dlogits"], dlogp, derr, TYPES[dtype])
+
+
 def preference64(row, off, ref, w, beta, target, smoothing, form, average):
     P, T = len(off) // 2, len(row.y)
     alive, logp, logp_err = row.live.cpu(), row.logp.cpu(), row.logp_err.cpu()
