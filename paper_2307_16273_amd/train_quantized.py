@@ -1,10 +1,17 @@
 """Trains a small residual network in 8-bit integers on the GPU, answers with it row by row, and proves the forward products of its last step.
 
     python -m paper_2307_16273_amd.train_quantized [--layers 8] [--width 1024] [--batch 64] [--steps 5] [--lr X]
+        [--loss squares|policy|preference] [--optimizer sgd|adamw] [--state-bits 32|8] [--limit X]
 
 Layer l normalises the residual stream, in 8 bits with a scale for each row, and multiplies it by its weights, in 8 bits with a scale for
-each column; its output is added to the stream by the next layer's norm.  Gradients go back through the same integers.  The target is the
-output of a network of other weights; the loss is half the mean square of the difference.  After the last step
+each column; its output is added to the stream by the next layer's norm.  Gradients go back through the same integers.  A network of other
+weights is the teacher.  By --loss the network learns
+  squares     the teacher's output: half the mean square of the difference;
+  policy      to choose: its output is the logits of a choice of one entry for each row, choices are drawn from it at every other step, and an
+              entry's reward is its log-probability under the teacher's output; policy_loss, with the network of before as the reference;
+  preference  the teacher's preferences: rows 2 i and 2 i + 1 ask the same, each answered by an entry drawn from the network of before, and
+              the answer that the teacher finds likelier is preferred; preference_loss, with the network of before as the reference.
+adamw updates all tensors with one call, its states in 32 or 8 bits; --limit scales gradients whose norm is above it.  After the last step
   - the forward pass runs once more for single rows, as a serving program would, and has to give the batch's rows bit for bit;
   - sumcheck_matmul proves the products of all layers on the stacks of 8-bit activations and weights, and its claim on their result is
     compared with the multilinear extension of the int32 accumulators that matmul_i8 returns.  (The integers of the gradients stay inside
@@ -45,20 +52,84 @@ def network(torch, zk, ctx, layers, width, seed):
     return net
 
 
-def step(zk, ctx, x, target, net, lr):
-    """One step of gradient descent; returns the loss in front of it (a tensor) and the step's kept activations."""
+def squares(zk, ctx, target):
+    """An objective: from the network's output its loss (a tensor) and the gradient of the output."""
+    def of(out):
+        diff = out - target
+        return 0.5 * diff.square().mean(), diff / out.shape[0]       # the mean over the rows; over the columns it is the learning rate's
+    return of
+
+
+def draw(torch, logits, seed):
+    return torch.multinomial(torch.softmax(logits, 1), 1, generator=torch.Generator(device="cuda").manual_seed(seed))[:, 0]
+
+
+def policy(torch, zk, ctx, teacher, before):
+    """teacher, before: outputs for the batch of the teacher and of the network before the first step."""
+    held, steps = {}, 0
+
+    def of(out):
+        nonlocal steps
+        if steps % 2 == 0:
+            tokens = draw(torch, out, 100 + steps)
+            reward = zk.token_logprobs(ctx, teacher, tokens)["logp"]
+            held.update(tokens=tokens, old=zk.token_logprobs(ctx, out, tokens)["logp"], ref=zk.token_logprobs(ctx, before, tokens)["logp"],
+                        advantage=(reward - reward.mean()) / (reward.std(correction=0) + 1e-6))
+        steps += 1
+        got = zk.policy_loss(ctx, out, held["tokens"], held["old"], held["advantage"], ref_logp=held["ref"], kl=0.01)
+        return got["loss"], got["dlogits"]
+    return of
+
+
+def preference(torch, zk, ctx, teacher, before):
+    tokens = draw(torch, before, 100)
+    likely = zk.token_logprobs(ctx, teacher, tokens)["logp"].view(-1, 2)
+    tokens = torch.where((likely[:, :1] >= likely[:, 1:]), tokens.view(-1, 2), tokens.view(-1, 2).flip(1)).reshape(-1)
+    ref = zk.token_logprobs(ctx, before, tokens)["logp"]
+    offsets = torch.arange(before.shape[0] + 1, device="cuda")      # sequences of one row each
+
+    def of(out):
+        got = zk.preference_loss(ctx, out, tokens, offsets, ref_logp=ref, beta=0.5)
+        return got["loss"], got["dlogits"]
+    return of
+
+
+def sgd(zk, ctx, net, lr, limit):
+    def update(dw, dgain):
+        factor = zk.gradient_norm(ctx, dw + dgain, limit)["factor"] if limit else None
+        for l in range(len(dw)):
+            net["w"][l].sub_(dw[l] if factor is None else dw[l] * factor, alpha=lr)
+            net["gain"][l].sub_(dgain[l] if factor is None else dgain[l] * factor, alpha=lr)
+    return update
+
+
+def adamw(zk, ctx, net, lr, limit, bits):
+    params = list(net["w"]) + net["gain"]
+    state, steps = zk.adamw_state(params, bits), 0
+
+    def update(dw, dgain):
+        nonlocal steps
+        steps += 1
+        factor = zk.gradient_norm(ctx, dw + dgain, limit)["factor"] if limit else None
+        zk.adamw_step(ctx, params, dw + dgain, state, steps, lr, factor=factor)
+    return update
+
+
+def step(zk, ctx, x, objective, net, update):
+    """One step; returns the loss in front of it (a tensor) and the step's kept activations."""
     out, kept = forward(zk, ctx, x, net)
-    diff = out - target
-    loss = 0.5 * diff.square().mean()
-    d = (diff / x.shape[0]).to(x.dtype)         # the mean over the rows; over the columns it is the learning rate's
+    loss, d = objective(out)
+    d = d.to(x.dtype)
     used = net["stack"]
+    dw, dgain = [], []
     for l in reversed(range(len(kept))):
         n, stream = kept[l]
         back = zk.matmul_i8_backward(ctx, d, n["q"], n["scale"], net["q"][l], net["s"][l])
         norm = zk.rmsnorm_i8_backward(ctx, back["da"], stream, net["gain"][l], n["rstd"], dtotal=d)
-        net["w"][l].sub_(back["dw"], alpha=lr)
-        net["gain"][l].sub_(norm["dweight"], alpha=lr)
+        dw.insert(0, back["dw"])
+        dgain.insert(0, norm["dweight"])
         d = norm["dx"]
+    update(dw, dgain)
     quantise_weights(zk, ctx, net)
     return loss, kept, used
 
@@ -79,7 +150,17 @@ def prove(torch, zk, ctx, kept, weights):
     return res, ms, int.from_bytes(at.download(), "little") == res["claims"][0]
 
 
-def check(layers, width, batch, steps):
+LOSSES, OPTIMIZERS, BITS = ("squares", "policy", "preference"), ("sgd", "adamw"), (32, 8)
+
+
+def check(layers, width, batch, steps, loss="squares", optimizer="sgd", state_bits=32, limit=None):
+    for name, x, known in (("loss", loss, LOSSES), ("optimizer", optimizer, OPTIMIZERS), ("state_bits", state_bits, BITS)):
+        if x not in known:
+            raise ValueError(f"{name}: one of {', '.join(map(str, known))}, not {x}")
+    if loss == "preference" and batch == 1:
+        raise ValueError("batch: two rows at least are needed, answers come in pairs")
+    if limit is not None and not limit > 0:
+        raise ValueError(f"limit: a positive norm, not {limit}")
     for name, n in (("layers", layers), ("width", width), ("batch", batch)):
         if n < 1 or n & (n - 1):
             raise ValueError(f"{name}: a power of two is needed for the proof, not {n}")
@@ -87,9 +168,13 @@ def check(layers, width, batch, steps):
         raise ValueError(f"steps: at least one is needed, whose products are proved, not {steps}")
 
 
-def run(layers=8, width=1024, batch=64, steps=5, lr=None, say=print):
-    check(layers, width, batch, steps)
+def run(layers=8, width=1024, batch=64, steps=5, lr=None, say=print, loss="squares", optimizer="sgd", state_bits=32, limit=None):
+    check(layers, width, batch, steps, loss, optimizer, state_bits, limit)
     import torch
+    if lr is None and optimizer == "adamw":
+        # The first steps move every weight by about lr, all in the direction that counts: a row of normalised activations answers by lr times
+        # the sum of their magnitudes, up to `width`, in each layer.  All layers together move an output by about a quarter.
+        lr = 0.25 / (layers * width)
     if lr is None:
         # Steps below 2 / (largest curvature) shrink the loss.  A layer's is about the largest eigenvalue of n^T n / batch, for random
         # rows (1 + sqrt(width / batch))^2, and the layers add up along the stream.
@@ -98,14 +183,21 @@ def run(layers=8, width=1024, batch=64, steps=5, lr=None, say=print):
     ctx = zk.Context(0)
     g = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(batch, width, generator=g, device="cuda").to(torch.bfloat16)
+    if loss == "preference":
+        x = x[::2].repeat_interleave(2, 0)
     target, _ = forward(zk, ctx, x, network(torch, zk, ctx, layers, width, 2))
     net = network(torch, zk, ctx, layers, width, 3)
+    if loss == "squares":
+        objective = squares(zk, ctx, target)
+    else:
+        objective = (policy if loss == "policy" else preference)(torch, zk, ctx, target, forward(zk, ctx, x, net)[0])
+    update = sgd(zk, ctx, net, lr, limit) if optimizer == "sgd" else adamw(zk, ctx, net, lr, limit, state_bits)
     losses, kept, used = [], None, None
     for k in range(steps):
         torch.cuda.synchronize()
         t0 = time.perf_counter()
-        loss, kept, used = step(zk, ctx, x, target, net, lr)
-        losses.append(float(loss))
+        value, kept, used = step(zk, ctx, x, objective, net, update)
+        losses.append(float(value))
         say(json.dumps({"step": k, "loss": losses[-1], "step_ms": 1e3 * (time.perf_counter() - t0)}))
     whole, _ = forward(zk, ctx, x, net)
     rows_equal = all(torch.equal(forward(zk, ctx, x[i:i + 1], net)[0], whole[i:i + 1]) for i in range(min(batch, 4)))
@@ -128,12 +220,17 @@ def main():
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--steps", type=int, default=5)
     ap.add_argument("--lr", type=float, default=None)
+    ap.add_argument("--loss", default="squares")
+    ap.add_argument("--optimizer", default="sgd")
+    ap.add_argument("--state-bits", type=int, default=32)
+    ap.add_argument("--limit", type=float, default=None)
     args = ap.parse_args()
+    how = dict(loss=args.loss, optimizer=args.optimizer, state_bits=args.state_bits, limit=args.limit)
     try:
-        check(args.layers, args.width, args.batch, args.steps)
+        check(args.layers, args.width, args.batch, args.steps, **how)
     except ValueError as e:
         ap.error(str(e))
-    run(args.layers, args.width, args.batch, args.steps, args.lr, lambda s: print(s, flush=True))
+    run(args.layers, args.width, args.batch, args.steps, args.lr, lambda s: print(s, flush=True), **how)
 
 
 if __name__ == "__main__":
