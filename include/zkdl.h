@@ -632,7 +632,8 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
  * the entry that was taken in each row.  A row whose token is negative counts for nothing: it is not read, its outputs and its
  * gradient are zero.  A token of V and more gives NaN.  With u = logits / temperature (times 1 / temperature in 32 bits):
  *   top = max_j u_j,  log_sum = log sum_j exp(u_j - top),  logp = u_token - top - log_sum,  p_j = exp(u_j - top - log_sum).
- * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.
+ * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.  u has to
+ * stay in the range of 32 bits.
  * dlogits: the gradient of the logits, logits' type and shape, dlogits_j = dlogp ([j = token] - p_j) / temperature; a row whose dlogp
  * is 0 has zeros whatever it holds.  temperature: positive, normal, finite; so is its reciprocal.  Sums in 32 bits and more, in an
  * order that depends on the sizes alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.
@@ -650,7 +651,8 @@ int zkdl_token_logprobs_backward(zkdl_ctx* ctx, const float* dlogp, const zkdl_m
  *   d = ref_logp - logp,  k = exp(d) - d - 1  (0 where ref_logp is NULL),
  *   sums[0] = sum_t w (kl k - gain),  sums[1] = sum_t w k,  sums[2] = sum_t w [clipped]  over the rows that count,
  *   dlogp = w ((clipped ? 0 : -r A) + kl (1 - exp(d))),
- * clipped where A > 0 and r > 1 + clip_high or A < 0 and r < 1 - clip_low.  weight: w, or NULL for 1 / T.
+ * clipped where A > 0 and r > 1 + clip_high or A < 0 and r < 1 - clip_low.  weight: w, or NULL for 1 / T; a row of weight 0 adds nothing and has
+ * no gradient whatever else is given for it.
  * 0 <= clip_low <= 1, clip_high >= 0 and finite, kl finite and 0 without ref_logp.  sums: 3 floats.  logp, dlogits may be NULL. */
 typedef struct {
     const float *old_logp, *advantage, *ref_logp, *weight;
@@ -666,7 +668,7 @@ int zkdl_policy_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, 
  *   margin_i = beta (h_2i - h_2i+1),  m = margin_i - target,
  *   l(m) = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m))  (ZKDL_PREF_LOGISTIC),  max(0, -m)  (ZKDL_PREF_HINGE),
  *          m^2  (ZKDL_PREF_SQUARE),
- *   loss = sum_i w_i l(m)  (weight: w, pairs floats, or NULL for 1 / pairs),
+ *   loss = sum_i w_i l(m)  (weight: w, pairs floats, or NULL for 1 / pairs; a pair of weight 0 adds nothing and has no gradient),
  *   dlogp = +- w_i l'(m) beta  (average: divided by the sequence's number of rows), l'(0) = 0 for the hinge.
  * beta, target finite; 0 <= smoothing <= 1, 0 but for the logistic form.  Sums over rows in 64 bits.  margin: pairs floats.  ref_logp, margin,
  * logp, dlogits may be NULL. */

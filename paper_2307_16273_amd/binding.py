@@ -817,6 +817,11 @@ def matmul_i8_backward(ctx, dy, a, a_scale, w, w_scale, trans_w=False, need_da=T
 # update of its master weights.  Streams, autograd and compiled code as for the 8-bit layers.  tokens [T], int32 or int64: a row whose token is
 # negative counts for nothing, is not read, and has zeros for outputs and gradient.
 
+def _listed(tensors):
+    """What can be gone through twice: a call on another stream than the context's is made a second time."""
+    return tensors if isinstance(tensors, (list, tuple)) or not hasattr(tensors, "__next__") else list(tensors)
+
+
 PREFERENCE_FORMS = {"logistic": 0, "hinge": 1, "square": 2}
 
 
@@ -871,7 +876,7 @@ def gradient_norm(ctx, gradients, limit=float("inf")):
     factor), numbers on the device: factor = limit / norm where norm is above the limit, else 1; NaN where the norm is not
     finite, with which adamw_step leaves the step out.  (zkdl_gradient_norm)"""
     fn = (_L8 or _layers8()).gradient_norm
-    args = (gradients, limit)
+    args = (_listed(gradients), limit)
     got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
     return got if type(got) is dict else _rest(ctx, fn, got, args)
 
@@ -896,7 +901,7 @@ def adamw_step(ctx, params, gradients, state, step, lr, beta1=0.9, beta2=0.999, 
     rounded up or down at random, by seed, step, the tensor's place in the list and the entry's in the tensor.  values: the lists m, v
     of the values that the new 8-bit states stand for.  Returns dict(m, v), None without values.  (zkdl_adamw_step)"""
     fn = (_L8 or _layers8()).adamw_step
-    args = (params, gradients, state["m"], state["v"], state["m_scale"], state["v_scale"], step, lr, beta1, beta2, eps, decay, factor, seed,
+    args = (_listed(params), _listed(gradients), state["m"], state["v"], state["m_scale"], state["v_scale"], step, lr, beta1, beta2, eps, decay, factor, seed,
             state["bits"], bool(values))
     got = fn(ctx.address, ctx.device, ctx.stream, False, *args)
     return got if type(got) is dict else _rest(ctx, fn, got, args)

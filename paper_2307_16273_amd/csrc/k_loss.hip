@@ -74,6 +74,10 @@ __device__ __forceinline__ float divergence_of(float d, float em) {
 // One row's share of the policy loss; returns dlogp.
 __device__ __forceinline__ float policy_row(const LossArgs& a, uint64_t r, float logp, float (&term)[3]) {
     const float w = a.weight ? a.weight[r] : a.every, adv = a.advantage[r];
+    if (w == 0) {           // whatever the rest is
+        term[0] = term[1] = term[2] = 0.f;
+        return 0.f;
+    }
     const float ratio = expf(logp - a.old_logp[r]);
     const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
     const float gain = adv == 0 ? 0.f : (up ? a.high : down ? a.low : ratio) * adv;
@@ -81,9 +85,9 @@ __device__ __forceinline__ float policy_row(const LossArgs& a, uint64_t r, float
     if (a.ref_logp) {
         const float d = a.ref_logp[r] - logp, em = expm1f(d);
         div = divergence_of(d, em);
-        slope = fmaf(-a.kl, em, slope);
+        if (a.kl != 0) slope = fmaf(-a.kl, em, slope);
     }
-    term[0] = w * fmaf(a.kl, div, -gain);
+    term[0] = w * (a.kl != 0 ? fmaf(a.kl, div, -gain) : -gain);     // (a divergence beyond 32 bits that nobody asked for stays out)
     term[1] = w * div;
     term[2] = clipped ? w : 0.f;
     return w * slope;
@@ -348,11 +352,18 @@ __device__ __forceinline__ void part_of(const LossArgs& a, const T* row, uint32_
     for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) c = fmaxf(c, FULL || i < n[k] ? f[k][i] : -INF);
-    c = row_reduce<256, true>(c, s_max);
+    c = of_wave(row_reduce<256, true>(c, s_max));
+    if (c == -INF) {        // nothing but -infinity, which adds nothing, or NaN
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k)
+        for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += FULL || i < n[k] ? term_of(f[k][i], c, a.k) : 0.f;
+            for (int i = 0; i < 8; ++i) sum += (FULL || i < n[k]) && f[k][i] != f[k][i] ? NAN32 : 0.f;
+    } else {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += FULL || i < n[k] ? term_of(f[k][i], c, a.k) : 0.f;
+    }
     sum = row_reduce<256, false>(sum, s_sum);
 }
 template <class T, int ITEMS>
@@ -365,7 +376,7 @@ __global__ __launch_bounds__(256) void k_loss_part(LossArgs a, L8Mat<const T> x,
             float c, sum;
             if ((uint64_t)(q + 1) * ITEMS * 2048 <= a.cols) part_of<T, ITEMS, true>(a, row, q, c, sum, s_max, s_sum);
             else part_of<T, ITEMS, false>(a, row, q, c, sum, s_max, s_sum);
-            if (threadIdx.x == 0) part[r * parts + q] = {c, c == -INF ? 0.f : sum};      // a part of nothing but -infinity adds nothing
+            if (threadIdx.x == 0) part[r * parts + q] = {c, sum};
             __syncthreads();
         }
     }
@@ -553,6 +564,7 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
             slope = 2 * m;
         }
         if (m != m) each = slope = m;
+        if (w == 0) each = slope = 0;       // whatever the sequences hold
         if (threadIdx.x == 0) {
             if (a.margin) a.margin[i] = (float)margin;
             a.losses[i] = (float)(w * each);

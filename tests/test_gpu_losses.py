@@ -333,6 +333,38 @@ def test_rows_of_infinities_and_nan(lib, ctx, shape):
         assert got["loss"].item() == 0
 
 
+@pytest.mark.parametrize("V", [40, 3000, 40000])
+def test_a_nan_among_masked_entries(lib, ctx, V):
+    """A NaN whose whole neighbourhood is -infinity is not lost, in rows of any number of parts."""
+    x, y = inputs(gen(V), 5, V, "f32", ignore=False)
+    x[:, V // 2:] = float("-inf")
+    y %= V // 2
+    x[1:3, V - 3] = float("nan")
+    got = lib.token_logprobs(ctx, x.cuda(), y.cuda())
+    assert torch.isnan(got["logp"]).tolist() == [False, True, True, False, False]
+    x = x.repeat(1, 1 if V < 40000 else 4)      # a row in parts
+    got = lib.token_logprobs(ctx, x.cuda(), y.cuda())
+    assert torch.isnan(got["logp"]).tolist() == [False, True, True, False, False]
+    assert torch.isnan(got["top"]).tolist() == torch.isnan(got["log_sum"]).tolist() == [False, True, True, False, False]
+
+
+@pytest.mark.parametrize("shape", [(70, 300), (5, 90000)], ids=str)
+def test_rows_of_weight_0(lib, ctx, shape):
+    """Nothing that such a row holds reaches the loss, nor a divergence that has no part in it."""
+    T, V = shape
+    x, y = inputs(gen(6), T, V, "f32", ignore=False)
+    old, adv, ref, w = torch.full((T,), -3.0), torch.ones(T), torch.full((T,), -3.0), torch.full((T,), 1.0 / T)
+    w[1] = w[3] = 0
+    clean = lib.policy_loss(ctx, x.cuda(), y.cuda(), old.cuda(), adv.cuda(), weight=w.cuda(), clip_high=1e30)
+    old[1], adv[1], ref[1], x[3] = -math.inf, -math.nan, math.nan, math.nan
+    ref[0] = 1e30
+    got = lib.policy_loss(ctx, x.cuda(), y.cuda(), old.cuda(), adv.cuda(), ref_logp=ref.cuda(), weight=w.cuda(), clip_high=1e30)
+    assert torch.equal(got["loss"], clean["loss"]) and torch.equal(got["dlogits"], clean["dlogits"]) and not got["dlogits"][[1, 3]].any()
+    off = torch.tensor([0, 1, 2, 4, 5]).cuda()
+    pref = lib.preference_loss(ctx, x.cuda(), y.cuda(), off, weight=torch.tensor([1.0, 0.0]).cuda())
+    assert torch.isfinite(pref["loss"]) and torch.isnan(pref["margin"][1]) and not pref["dlogits"][2:].any() and pref["dlogits"][0].any()
+
+
 def test_logits_of_any_size(lib, ctx):
     """Logits far from zero and far apart, and the largest of their type."""
     x = torch.tensor([[1e4, 1e4 - 1, 0.0], [-1e30, -1e30, -1e30], [3e38, -3e38, 3e38], [88.0, 0.0, -88.0], [0.0, -200.0, -1e9]])

@@ -409,6 +409,21 @@ def test_autograd_is_told_of_the_update(lib, ctx):
         y.backward()
 
 
+def test_lists_of_any_kind(lib, ctx):
+    """Tuples, generators and a stack of parameters, on the context's stream and on another."""
+    stack, d = torch.zeros(3, 50, device="cuda"), torch.ones(3, 50, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for k, on in enumerate((torch.cuda.default_stream(), side)):
+        with torch.cuda.stream(on):
+            assert abs(lib.gradient_norm(ctx, (x for x in d))["norm"].item() - math.sqrt(150)) <= 1e-6
+            state = lib.adamw_state(stack)
+            lib.adamw_step(ctx, stack, (x for x in d), state, 1, 0.5, decay=0.0)
+            lib.adamw_step(ctx, (x for x in stack), tuple(d), state, 2, 0.5, decay=0.0)
+            assert torch.all(stack < -0.9 * (k + 1)) and torch.all(stack > -1.1 * (k + 1))
+        torch.cuda.synchronize()
+
+
 def test_refusals(lib, ctx):
     p, d = [torch.zeros(10, device="cuda")], [torch.ones(10, device="cuda")]
     s, s8 = lib.adamw_state(p), lib.adamw_state(p, bits=8)
