@@ -194,11 +194,18 @@ __device__ __forceinline__ Raw8<T> get_lds(Quad (*from)[N], uint32_t t) {
     for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.q[h] = from[h][t];
     return v;
 }
+// Where vector k of a row lies: rows begin with different ones.  Blocks run side by side, and rows of a power of two of bytes would have all of them
+// ask the same memory channels at once.
+template <int G, int WHOLE>
+__device__ __forceinline__ uint32_t place_of(int k, uint32_t turn) {
+    const uint32_t i = k + turn;
+    return (i < (uint32_t)WHOLE ? i : i - WHOLE) * (8 * G);
+}
 template <class T, int G, int WHOLE>
-__device__ __forceinline__ void put_zeros(T* to, uint32_t t, bool ends, const L8At& end) {
+__device__ __forceinline__ void put_zeros(T* to, uint32_t mine, uint32_t turn, bool ends, const L8At& end) {
     const float zero[8] = {};
-#pragma unroll 1
-    for (int k = 0; k < WHOLE; ++k) l8_store(to + k * 8 * G + t * 8, 8, zero);
+#pragma unroll 4
+    for (int k = 0; k < WHOLE; ++k) store8_at(to, place_of<G, WHOLE>(k, turn), mine, zero);
     if (ends) put_end(to, end, zero);
 }
 
@@ -227,6 +234,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
     const L8At end = l8_at(WHOLE * EACH + t * 8, a.cols);
     const uint64_t r = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + group;       // (a loop over rows would keep its constants in registers)
     if (r >= a.rows) return;
+    const uint32_t turn = G > 64 && WHOLE > 1 ? (uint32_t)r % (WHOLE ? WHOLE : 1) : 0;
     const int64_t y = token_of(a, r);
     T* const to = out.p + r * out.rs;
     float term[3] = {0.f, 0.f, 0.f};
@@ -236,14 +244,14 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         Raw8<T> v[REGS ? REGS : 1], last;
         float c = -INF, sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < STORED; ++k) v[k] = load8_at(row, (REGS + k) * EACH, mine);
+        for (int k = 0; k < STORED; ++k) v[k] = load8_at(row, place_of<G, WHOLE>(REGS + k, turn), mine);
 #pragma unroll
-        for (int k = STORED; k < REGS; ++k) v[k] = load8_at(row, k * EACH, mine);
+        for (int k = STORED; k < REGS; ++k) v[k] = load8_at(row, place_of<G, WHOLE>(k, turn), mine);
 #pragma unroll
         for (int k = 0; k < STORED; ++k) {
             c = max8(c, v[k]);
             put_lds<T>(&s_v[k * (sizeof(T) / 2)], t, v[k]);
-            v[k] = load8_at(row, k * EACH, mine);
+            v[k] = load8_at(row, place_of<G, WHOLE>(k, turn), mine);
             __builtin_amdgcn_sched_barrier(0);
         }
         if (ends) last = load8(row + end.start);
@@ -291,7 +299,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
                     } else {
                         slope8(get_lds<T>(&s_v[(k < REGS ? 0 : k - REGS) * (sizeof(T) / 2)], t), c, a.k, co_inv, f);
                     }
-                    store8_at(to, k * EACH, mine, f);
+                    store8_at(to, place_of<G, WHOLE>(k, turn), mine, f);
                     if (STORED) __builtin_amdgcn_sched_barrier(0);
                 }
                 if (ends) {
@@ -302,11 +310,11 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
                 }
                 if (y < (int64_t)a.cols && t == (uint32_t)y / 8 % G) put_one(to + y, fmaf(-co_inv, term_of(xy, c, a.k), co));
             } else if (out.p) {
-                put_zeros<T, G, WHOLE>(to, t, ends, end);
+                put_zeros<T, G, WHOLE>(to, mine, turn, ends, end);
             }
         }
     } else if (MODE == ROWS_POLICY && out.p) {
-        put_zeros<T, G, WHOLE>(to, t, ends, end);
+        put_zeros<T, G, WHOLE>(to, mine, turn, ends, end);
     }
     if (t == 0) {
         if (a.logp) a.logp[r] = st.logp;
