@@ -613,7 +613,7 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
     constexpr int MOST = 32 / sizeof(T);        // vectors in registers
     const bool many = a.rows >= 1024;
     if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
-    else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST + 1))) launch_rows_from<T, MODE, 256, 1, MOST>(ctx, a, x, out);
+    else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST / 2 + 1))) launch_rows_from<T, MODE, 256, 1, MOST / 2>(ctx, a, x, out);
     else launch_rows_from<T, MODE, 512, 2, MODE == ROWS_LOGP ? MOST : 2 * MOST>(ctx, a, x, out);
 }
 
