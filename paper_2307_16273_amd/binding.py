@@ -894,8 +894,8 @@ def adamw_state(params, bits=32):
 
 
 def adamw_step(ctx, params, gradients, state, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.01, factor=None, seed=0, values=False):
-    """One step of AdamW on a list of contiguous parameters (float32, float16, bfloat16), in place, in one launch for up to 40 tensors of the
-    same types; gradients: as many, of any of these types; state: adamw_state's.  step: the step's number from 1 on, or an int64 number on
+    """One step of AdamW on a list of contiguous parameters (float32, float16, bfloat16), in place, in one launch for up to 80 tensors of the
+    same types (8-bit states: 40); gradients: as many, of any of these types; state: adamw_state's.  step: the step's number from 1 on, or an int64 number on
     the device; lr: a number, or a float32 number on the device (a captured call reads both at every replay).  factor: a float32 number on
     the device that the gradients are multiplied by (gradient_norm's); where it is not finite the step is left out.  8-bit states are
     rounded up or down at random, by seed, step, the tensor's place in the list and the entry's in the tensor.  values: the lists m, v

@@ -7,6 +7,7 @@
 // leaves; only rows that are longer, few or wanted for several sequences at once (the preference's sums need all of them first) are read twice.
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "layer8.cuh"
 #include "vec8.cuh"
@@ -209,11 +210,11 @@ __device__ __forceinline__ void put_zeros(T* to, uint32_t mine, uint32_t turn, b
     if (ends) put_end(to, end, zero);
 }
 
-enum { ROWS_LOGP, ROWS_POLICY };
+enum { ROWS_LOGP, ROWS_POLICY, ROWS_SLOPE };
 
 // ---------------------------------------------------------------------------
 // Rows that stay on the chip: G threads a row (a wave: four rows a block) with WHOLE vectors of eight each, and one at the row's end:
-// 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols >= 8.  The vectors are in registers, but for the last of the longest rows, which lie in LDS: so two
+// 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols > 256.  The vectors are in registers, but for the last of the longest rows, which lie in LDS: so two
 // blocks of 512 threads with 128 registers each, and half of the LDS, have room in a compute unit up to rows of 256 kB, and one of them has
 // memory at work while the other computes.  (As many instances as there are lengths: with a count that the kernel learns when it runs, the
 // vectors' registers were copied and spilled.)
@@ -322,6 +323,76 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         if (a.log_sum) a.log_sum[r] = st.log_sum;
         if (a.dlogp) a.dlogp[r] = 0.f;
         if (MODE == ROWS_POLICY) put_terms(a, r, term);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rows of up to 8 G entries for G = 8, 16 or 32 lanes: as many rows in a wave as fit, a vector of eight (or what there is) a lane.
+// ROWS_SLOPE: the gradient from dlogp, top and log_sum alone.
+// ---------------------------------------------------------------------------
+template <int G, bool MAX>
+__device__ __forceinline__ float lanes_reduce(float x) {
+#pragma unroll
+    for (int d = G / 2; d; d >>= 1) {
+        const float y = __shfl_xor(x, d, 64);
+        x = MAX ? fmaxf(x, y) : x + y;
+    }
+    return x;
+}
+template <class T, int MODE, int G>
+__global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlogp_in, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out) {
+    const uint32_t t = threadIdx.x % G, j = t * 8;
+    const uint64_t r = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / G) + threadIdx.x / G;
+    if (r >= a.rows) return;
+    const int n = j < a.cols ? (int)min(8u, a.cols - j) : 0;
+    const int64_t y = token_of(a, r);
+    float f[8], term[3] = {0.f, 0.f, 0.f}, dlogp = 0.f, co_inv = 0.f;
+    RowStats st = {0.f, 0.f, 0.f};
+    if (MODE == ROWS_SLOPE) dlogp = y < 0 ? 0.f : dlogp_in[r];
+    const bool bad = y >= (int64_t)a.cols, live = MODE == ROWS_SLOPE ? dlogp != 0 : y >= 0;
+    if (live) {
+        const T* const row = x.p + r * x.rs;
+        l8_load(row + (n ? j : 0), n, f);
+        if (MODE == ROWS_SLOPE) {
+            const float norm = log_sum[r] * LOG2E, top_r = top[r];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = exp2_raw(fmaf(fmaf(f[i], a.inv_tau, -top_r), LOG2E, -norm));
+            if (bad) dlogp = NAN32;
+            co_inv = dlogp * a.inv_tau;
+        } else {
+            const float xy = l8_f32(row[bad ? 0 : y]);
+            float c = -INF, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c = fmaxf(c, i < n ? f[i] : -INF);
+            c = lanes_reduce<G, true>(c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                f[i] = term_of(f[i], c, a.k);
+                sum += i < n ? f[i] : 0.f;
+            }
+            sum = lanes_reduce<G, false>(sum);
+            st = row_stats(a, c, sum, y, xy);
+            if (MODE == ROWS_POLICY) {
+                dlogp = policy_row(a, r, st.logp, term);
+                co_inv = dlogp * a.inv_tau / sum;
+            }
+        }
+    }
+    if (MODE != ROWS_SLOPE && t == 0) {
+        if (a.logp) a.logp[r] = st.logp;
+        if (a.top) a.top[r] = st.top;
+        if (a.log_sum) a.log_sum[r] = st.log_sum;
+        if (a.dlogp) a.dlogp[r] = 0.f;
+        if (MODE == ROWS_POLICY) put_terms(a, r, term);
+    }
+    if (MODE != ROWS_LOGP && out.p && n) {
+        const float co = dlogp * a.inv_tau;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = dlogp == 0 ? 0.f : f[i] * -co_inv;
+            f[i] += dlogp != 0 && (uint64_t)y == j + i ? co : 0.f;
+        }
+        l8_store(out.p + r * out.rs + j, n, f);
     }
 }
 
@@ -538,8 +609,9 @@ struct PairArgs {
     float every, beta, target, smoothing;
     float *margin, *losses, *dlogp;
 };
-__global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
-    __shared__ double s[4][4];
+template <int N>
+__global__ __launch_bounds__(N) void k_loss_pair(PairArgs a) {
+    __shared__ double s[N / 64][4];
     for (uint64_t i = blockIdx.x; i < a.pairs; i += gridDim.x) {
         uint64_t at[3];
 #pragma unroll
@@ -549,14 +621,19 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
         }
         at[1] = max(at[1], at[0]);
         double x[4] = {0, 0, 0, 0};         // of either sequence the sum, and the rows that count
-        for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += 256)
-            if (a.tokens.at(r) >= 0) {
-                const double d = (double)a.logp[r] - (a.ref_logp ? (double)a.ref_logp[r] : 0.);
-                const bool second = r >= at[1];
-                x[second] += d;
-                x[2 + second] += 1;
-            }
-        block_sums64<4, 4>(x, s);
+#pragma unroll 4
+        for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += N)
+        {
+            const int64_t y = a.tokens.at(r);
+            const float p = a.logp[r], q = a.ref_logp ? a.ref_logp[r] : 0.f;        // (no load waits for the token)
+            const double d = y >= 0 ? (double)p - (double)q : 0., one = y >= 0 ? 1. : 0.;
+            const bool second = r >= at[1];
+            x[0] += second ? 0. : d;
+            x[1] += second ? d : 0.;
+            x[2] += second ? 0. : one;
+            x[3] += second ? one : 0.;
+        }
+        block_sums64<4, N / 64>(x, s);
         const double share[2] = {a.average ? 1 / fmax(x[2], 1.) : 1., a.average ? 1 / fmax(x[3], 1.) : 1.}, h[2] = {x[0] * share[0], x[1] * share[1]};
         const double margin = a.beta * (h[0] - h[1]), m = margin - a.target, w = a.weight ? (double)a.weight[i] : (double)a.every;
         double each, slope;
@@ -579,7 +656,8 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
         }
         if (a.dlogp) {
             const float d0 = (float)(w * slope * a.beta * share[0]), d1 = (float)(-w * slope * a.beta * share[1]);
-            for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += 256) a.dlogp[r] = a.tokens.at(r) < 0 ? 0.f : r >= at[1] ? d1 : d0;
+#pragma unroll 4
+            for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += N) a.dlogp[r] = a.tokens.at(r) < 0 ? 0.f : r >= at[1] ? d1 : d0;
         }
         __syncthreads();        // s is the next pair's
     }
@@ -593,7 +671,7 @@ __global__ __launch_bounds__(256) void k_loss_pair(PairArgs a) {
 template <class T>
 bool rows_fit(const LossArgs& a, bool slope) {
     constexpr uint32_t most = 32 / sizeof(T);       // vectors in registers
-    return a.cols >= 8 && (a.cols < 4096 * (most + 1) || (slope && a.rows >= 192 && a.cols <= 4096 * 2 * most));
+    return a.cols < 4096 * (most + 1) || (slope && a.rows >= 192 && a.cols <= 4096 * 2 * most);
 }
 
 template <class T, int MODE, int G, int WHOLE>
@@ -606,13 +684,28 @@ void launch_rows_from(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<
     if (a.cols / (8 * G) == WHOLE) launch_rows_of<T, MODE, G, WHOLE>(ctx, a, x, out);
     else if constexpr (WHOLE < LAST) launch_rows_from<T, MODE, G, WHOLE + 1, LAST>(ctx, a, x, out);
 }
+// Rows of 256 entries and less; 2^20 rows of 32 took 242 us with a wave each, 4 * 2^20 rows of 7 in parts 44 ms.
+constexpr uint32_t LOSS_SMALL = 256;
+template <class T, int MODE>
+void launch_small(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out) {
+    const auto go = [&](auto g) {
+        constexpr int G = decltype(g)::value;
+        const uint64_t blocks = l8_ceil(a.rows, 256 / G), wide = blocks < (1u << 20) ? blocks : 1u << 20;
+        hipLaunchKernelGGL((k_loss_small<T, MODE, G>), dim3((unsigned)wide, (unsigned)l8_ceil(blocks, wide)), dim3(256), 0, ctx->stream, a, dlogp, top, log_sum, x, out);
+    };
+    if (a.cols <= 64) go(std::integral_constant<int, 8>());
+    else if (a.cols <= 128) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 32>());
+}
+
 // Few threads a row, with many vectors each, where there are rows enough to fill the device: more rows are under way at once, and fewer
 // threads wait for one another.
 template <class T, int MODE>
 void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> out) {
     constexpr int MOST = 32 / sizeof(T);        // vectors in registers
     const bool many = a.rows >= 1024;
-    if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
+    if (a.cols <= LOSS_SMALL) launch_small<T, MODE>(ctx, a, nullptr, nullptr, nullptr, x, out);
+    else if (a.cols < 2048 || (many && a.cols < 4096)) launch_rows_from<T, MODE, 64, 0, 7>(ctx, a, x, out);
     else if (a.cols < 8192 || (many && a.cols < 2048 * (MOST / 2 + 1))) launch_rows_from<T, MODE, 256, 1, MOST / 2>(ctx, a, x, out);
     else launch_rows_from<T, MODE, 512, 2, MODE == ROWS_LOGP ? MOST : 2 * MOST>(ctx, a, x, out);
 }
@@ -620,6 +713,7 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
 template <class T>
 void launch_slope(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
                   const float* losses = nullptr, uint64_t pairs = 0, float* loss = nullptr) {
+    if (a.cols <= LOSS_SMALL && !losses) return launch_small<T, ROWS_SLOPE>(ctx, a, dlogp, top, log_sum, x, out);
     const uint32_t segs = (uint32_t)l8_ceil(a.cols, 2048), waves = segs >= 4 ? 4 : segs >= 2 ? 2 : 1;
     const uint64_t gx = l8_ceil(segs, waves), gy = l8_ceil(a.rows, 4 / waves);
     hipLaunchKernelGGL((k_loss_slope<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(gy < 4096 ? gy : 4096)), dim3(256), 0, ctx->stream, a, dlogp, top,
@@ -729,8 +823,13 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
     }
     PairArgs q = {a.rows, p->pairs, a.tokens, a.offsets, a.logp, p->ref_logp, p->weight, p->form, p->average, 1.f / (float)p->pairs, p->beta, p->target,
                   p->smoothing, margin, losses, dlogits ? a.dlogp : nullptr};
-    if (p->pairs) hipLaunchKernelGGL(k_loss_pair, dim3((unsigned)(p->pairs < 65536 ? p->pairs : 65536)), dim3(256), 0, ctx->stream, q);
-    const bool few = dlogits && a.rows && p->pairs <= 4096;         // pairs whose losses one block adds up while others are at the gradient
+    if (p->pairs) {
+        // threads by the rows of a pair (8192 of them 37 us with 256 threads)
+        const dim3 grid((unsigned)(p->pairs < 65536 ? p->pairs : 65536));
+        if (a.rows / p->pairs < 1024) hipLaunchKernelGGL((k_loss_pair<256>), grid, dim3(256), 0, ctx->stream, q);
+        else hipLaunchKernelGGL((k_loss_pair<1024>), grid, dim3(1024), 0, ctx->stream, q);
+    }
+    const bool few = dlogits && a.rows && p->pairs <= 4096 && a.cols > LOSS_SMALL;         // pairs whose losses one block adds up while others are at the gradient
     if (dlogits && a.rows)
         launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits), few ? losses : nullptr, p->pairs, loss);
     return few ? (int)ZKDL_OK : launch_sum(ctx, losses, p->pairs, 1, loss);

@@ -6,6 +6,7 @@
 #include <cfloat>
 #include <cmath>
 #include <algorithm>
+#include <type_traits>
 
 #include "layer8.cuh"
 #include "vec8.cuh"
@@ -103,19 +104,25 @@ __global__ __launch_bounds__(1024) void k_norm_join(const double* part, uint64_t
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
-constexpr uint32_t ADAM_TENSORS = 40, ADAM_ITEMS = 2, ADAM_CHUNK = 256 * 8 * ADAM_ITEMS, ADAM_BLOCK8 = 256;
+constexpr uint32_t ADAM_ITEMS = 2, ADAM_CHUNK = 256 * 8 * ADAM_ITEMS, ADAM_BLOCK8 = 256;
 struct AdamTensor {
     void* param;
     const void* grad;
     void *m, *v;
+    uint64_t n;
+};
+struct AdamTensor8 : AdamTensor {
     uint8_t *m_scale, *v_scale;
     float *m_value, *v_value;
-    uint64_t n;
     uint32_t number;        // of the tensor in the call: its random bits
 };
+// BITS: of the states
+template <int BITS>
 struct AdamArgs {
-    AdamTensor t[ADAM_TENSORS];
-    uint32_t first[ADAM_TENSORS + 1];
+    typedef std::conditional_t<BITS == 32, AdamTensor, AdamTensor8> Tensor;
+    static constexpr uint32_t TENSORS = BITS == 32 ? 80 : 40;
+    Tensor t[TENSORS];
+    uint32_t first[TENSORS + 1];
     uint32_t count, seed_lo, seed_hi, step;
     double lr, decay, beta1, beta2, root2;      // root2: (1 - beta2)^(1/2)
     const int64_t* step_ptr;
@@ -123,7 +130,7 @@ struct AdamArgs {
     float eps;
     float rate, root, keep;     // lr / (1 - beta1^t), (1 - beta2^t)^(-1/2), 1 - lr decay
 };
-static_assert(sizeof(AdamArgs) <= 4096 - 256, "a launch's arguments");
+static_assert(sizeof(AdamArgs<32>) <= 4096 - 256 && sizeof(AdamArgs<8>) <= 4096 - 256, "a launch's arguments");
 
 // What the step's number and the learning rate give: on the host, or, where they are read from device memory, in every block.
 struct AdamRates {
@@ -256,7 +263,7 @@ __device__ __forceinline__ void store_entries(T* p, int n, const float (&f)[8]) 
     else l8_store(p, n, f);
 }
 template <class P, class G, int BITS, bool FULL>
-__device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t, uint64_t at) {
+__device__ __forceinline__ void adam_chunk(const AdamJob& a, const typename AdamArgs<BITS>::Tensor& t, uint64_t at) {
     P* const param = (P*)t.param;
     const G* const grad = (const G*)t.grad;
     Raw8<P> praw[ADAM_ITEMS];
@@ -371,10 +378,10 @@ __device__ __forceinline__ void adam_chunk(const AdamJob& a, const AdamTensor& t
 
 // BITS: of the states
 template <class P, class G, int BITS>
-__global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
+__global__ __launch_bounds__(256) void k_adamw(AdamArgs<BITS> a) {
     __shared__ AdamRates s_rates;
     const uint32_t i = tensor_of(a.first, a.count, blockIdx.x);
-    const AdamTensor& t = a.t[i];
+    const auto& t = a.t[i];
     uint32_t step = a.step;
     AdamRates rates = {a.rate, a.root, a.keep};
     bool go = true;
@@ -395,19 +402,14 @@ __global__ __launch_bounds__(256) void k_adamw(AdamArgs a) {
         factor = f;
     }
     if (BITS == 32 && !go) return;
-    const uint32_t key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
+    uint32_t key = 0;
+    if constexpr (BITS == 8) key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
     const uint64_t at = (uint64_t)(blockIdx.x - a.first[i]) * ADAM_CHUNK + threadIdx.x * 8;
     const AdamJob job = {a.beta1, a.beta2, (1 - a.beta1) * factor, a.root2 * factor, rates, a.eps, key, go};
     if ((uint64_t)(blockIdx.x - a.first[i] + 1) * ADAM_CHUNK <= t.n) adam_chunk<P, G, BITS, true>(job, t, at);
     else adam_chunk<P, G, BITS, false>(job, t, at);
 }
 
-template <class P, class G>
-void launch_adamw(zkdl_ctx* ctx, const AdamArgs& a, int bits) {
-    const dim3 grid(a.first[a.count]);
-    if (bits == 32) hipLaunchKernelGGL((k_adamw<P, G, 32>), grid, dim3(256), 0, ctx->stream, a);
-    else hipLaunchKernelGGL((k_adamw<P, G, 8>), grid, dim3(256), 0, ctx->stream, a);
-}
 template <class F>
 void by_type(int dtype, F&& go) {
     switch (dtype) {
@@ -422,10 +424,22 @@ uint64_t item_bytes(int dtype) { return dtype == ZKDL_F32 ? 4 : 2; }
 struct Span {
     uint64_t lo, hi;
     bool out;
+    bool operator<(const Span& o) const { return lo < o.lo; }
 };
-bool spans_apart(std::vector<Span>& s) {
-    const auto less = [](const Span& a, const Span& b) { return a.lo < b.lo; };
-    if (!std::is_sorted(s.begin(), s.end(), less)) std::sort(s.begin(), s.end(), less);
+// runs: where the spans of one kind begin, and their end.  Tensors of a kind mostly lie in the order in which they were made, so the runs are
+// merged: 8000 spans of 1000 tensors would take longer to sort than their update.
+bool spans_apart(std::vector<Span>& s, std::vector<size_t> runs) {
+    for (size_t i = 0; i + 1 < runs.size(); ++i)
+        if (!std::is_sorted(s.begin() + runs[i], s.begin() + runs[i + 1])) std::sort(s.begin() + runs[i], s.begin() + runs[i + 1]);
+    while (runs.size() > 2) {
+        std::vector<size_t> left;
+        for (size_t i = 0; i + 1 < runs.size(); i += 2) {
+            left.push_back(runs[i]);
+            if (i + 2 < runs.size()) std::inplace_merge(s.begin() + runs[i], s.begin() + runs[i + 1], s.begin() + runs[i + 2]);
+        }
+        left.push_back(runs.back());
+        runs.swap(left);
+    }
     uint64_t any = 0, outs = 0;      // where what came before ends
     for (const Span& x : s) {
         if (x.lo < (x.out ? any : outs)) return false;
@@ -433,6 +447,69 @@ bool spans_apart(std::vector<Span>& s) {
         if (x.out) outs = std::max(outs, x.hi);
     }
     return true;
+}
+
+template <int BITS>
+void adamw(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const zkdl_adamw* how) {
+    AdamArgs<BITS> a = {};
+    a.seed_lo = (uint32_t)how->seed;
+    a.seed_hi = (uint32_t)(how->seed >> 32);
+    a.step = how->step_ptr ? 1 : (uint32_t)how->step;
+    a.lr = how->lr_ptr ? 0 : how->lr;
+    a.decay = how->decay;
+    a.beta1 = how->beta1;
+    a.beta2 = how->beta2;
+    a.root2 = std::sqrt(1 - how->beta2);
+    a.step_ptr = how->step_ptr;
+    a.lr_ptr = how->lr_ptr;
+    a.factor = how->factor;
+    a.eps = (float)how->eps;
+    const AdamRates rates = adam_rates(a.lr, a.decay, a.beta1, a.beta2, a.step);
+    a.rate = rates.rate;
+    a.root = rates.root;
+    a.keep = rates.keep;
+    // tensors of the same types share launches
+    const int types[3] = {ZKDL_F32, ZKDL_F16, ZKDL_BF16};
+    uint32_t there = 0;
+    const auto kind = [&](const zkdl_adamw_tensor& t) {
+        const auto at = [&](int dtype) { return dtype == ZKDL_F32 ? 0 : dtype == ZKDL_F16 ? 1 : 2; };
+        return 3 * at(t.param_dtype) + at(t.grad_dtype);
+    };
+    for (size_t i = 0; i < count; ++i) there |= 1u << kind(tensors[i]);
+    for (int k = 0; k < 9; ++k) {
+        if (!(there >> k & 1)) continue;
+        const auto flush = [&] {
+            if (!a.count) return;
+            by_type(types[k / 3], [&](auto p) {
+                by_type(types[k % 3], [&](auto g) {
+                    hipLaunchKernelGGL((k_adamw<decltype(p), decltype(g), BITS>), dim3(a.first[a.count]), dim3(256), 0, ctx->stream, a);
+                });
+            });
+            a.count = 0;
+        };
+        for (size_t i = 0; i < count; ++i) {
+            const zkdl_adamw_tensor& t = tensors[i];
+            if (kind(t) != k || !t.n) continue;
+            const uint64_t chunks = l8_ceil(t.n, ADAM_CHUNK);
+            if (a.count == a.TENSORS || (a.count && a.first[a.count] + chunks >= (uint64_t)1 << 23)) flush();
+            auto& to = a.t[a.count];
+            to.param = t.param;
+            to.grad = t.grad;
+            to.m = t.m;
+            to.v = t.v;
+            to.n = t.n;
+            if constexpr (BITS == 8) {
+                to.m_scale = t.m_scale;
+                to.v_scale = t.v_scale;
+                to.m_value = t.m_value;
+                to.v_value = t.v_value;
+                to.number = (uint32_t)i;
+            }
+            a.first[a.count + 1] = a.first[a.count] + (uint32_t)chunks;
+            ++a.count;
+        }
+        flush();
+    }
 }
 
 }  // namespace
@@ -490,11 +567,6 @@ extern "C" int zkdl_adamw_step(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, 
         !std::isfinite(how->decay) || (!how->lr_ptr && !std::isfinite(how->lr)) || (!how->step_ptr && (how->step < 1 || how->step >= (int64_t)1 << 31)))
         return ZKDL_EINVAL;
     if (count >= (size_t)1 << 31) return ZKDL_EINVAL;
-    std::vector<Span> spans;
-    spans.reserve(8 * count);
-    const auto span = [&](const void* p, uint64_t bytes, bool out) {
-        if (bytes && p) spans.push_back({(uint64_t)p, (uint64_t)p + bytes, out});
-    };
     for (size_t i = 0; i < count; ++i) {
         const zkdl_adamw_tensor& t = tensors[i];
         if (!l8_is_float(t.param_dtype) || !l8_is_float(t.grad_dtype) || t.n >= (uint64_t)1 << 40) return ZKDL_EINVAL;
@@ -502,60 +574,39 @@ extern "C" int zkdl_adamw_step(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, 
         if (!t.n) continue;
         if (!t.param || !t.grad || !t.m || !t.v || (how->bits == 8 && (!t.m_scale || !t.v_scale))) return ZKDL_EINVAL;
         if (l8_ceil(t.n, ADAM_CHUNK) >= (uint64_t)1 << 23) return ZKDL_ETOOBIG;      // a launch's threads are counted in 32 bits
-        span(t.param, t.n * item_bytes(t.param_dtype), true);
-        span(t.grad, t.n * item_bytes(t.grad_dtype), false);
-        const uint64_t state = how->bits == 32 ? 4 : 1;
-        span(t.m, t.n * state, true);
-        span(t.v, t.n * state, true);
-        if (how->bits == 8) {
-            span(t.m_scale, l8_ceil(t.n, ADAM_BLOCK8), true);
-            span(t.v_scale, l8_ceil(t.n, ADAM_BLOCK8), true);
-            span(t.m_value, t.n * 4, true);
-            span(t.v_value, t.n * 4, true);
-        }
     }
+    std::vector<Span> spans;
+    std::vector<size_t> runs;
+    spans.reserve((how->bits == 8 ? 8 : 4) * count + 3);
+    const auto span = [&](const void* p, uint64_t bytes, bool out) {
+        if (bytes && p) spans.push_back({(uint64_t)p, (uint64_t)p + bytes, out});
+    };
+    const auto run = [&](auto of) {
+        runs.push_back(spans.size());
+        for (size_t i = 0; i < count; ++i) of(tensors[i]);
+    };
+    typedef const zkdl_adamw_tensor& Tensor;
+    const uint64_t state = how->bits == 32 ? 4 : 1;
+    run([&](Tensor t) { span(t.param, t.n * item_bytes(t.param_dtype), true); });
+    run([&](Tensor t) { span(t.grad, t.n * item_bytes(t.grad_dtype), false); });
+    run([&](Tensor t) { span(t.m, t.n * state, true); });
+    run([&](Tensor t) { span(t.v, t.n * state, true); });
+    if (how->bits == 8) {
+        run([&](Tensor t) { span(t.m_scale, l8_ceil(t.n, ADAM_BLOCK8), true); });
+        run([&](Tensor t) { span(t.v_scale, l8_ceil(t.n, ADAM_BLOCK8), true); });
+        run([&](Tensor t) { span(t.m_value, t.n * 4, true); });
+        run([&](Tensor t) { span(t.v_value, t.n * 4, true); });
+    }
+    runs.push_back(spans.size());
     span(how->step_ptr, 8, false);
     span(how->lr_ptr, 4, false);
     span(how->factor, 4, false);
-    if (!spans_apart(spans)) return ZKDL_EINVAL;
+    runs.push_back(spans.size());
+    if (!spans_apart(spans, std::move(runs))) return ZKDL_EINVAL;
     L8Device dev(ctx);
     ZK_HIP(ctx, dev.err);
-    AdamArgs a = {};
-    a.seed_lo = (uint32_t)how->seed;
-    a.seed_hi = (uint32_t)(how->seed >> 32);
-    a.step = how->step_ptr ? 1 : (uint32_t)how->step;
-    a.lr = how->lr_ptr ? 0 : how->lr;
-    a.decay = how->decay;
-    a.beta1 = how->beta1;
-    a.beta2 = how->beta2;
-    a.root2 = std::sqrt(1 - how->beta2);
-    a.step_ptr = how->step_ptr;
-    a.lr_ptr = how->lr_ptr;
-    a.factor = how->factor;
-    a.eps = (float)how->eps;
-    const AdamRates rates = adam_rates(a.lr, a.decay, a.beta1, a.beta2, a.step);
-    a.rate = rates.rate;
-    a.root = rates.root;
-    a.keep = rates.keep;
-    // tensors of the same types share launches
-    for (int pt : {ZKDL_F32, ZKDL_F16, ZKDL_BF16})
-        for (int gt : {ZKDL_F32, ZKDL_F16, ZKDL_BF16}) {
-            const auto flush = [&] {
-                if (!a.count) return;
-                by_type(pt, [&](auto p) { by_type(gt, [&](auto g) { launch_adamw<decltype(p), decltype(g)>(ctx, a, how->bits); }); });
-                a.count = 0;
-            };
-            for (size_t i = 0; i < count; ++i) {
-                const zkdl_adamw_tensor& t = tensors[i];
-                if (t.param_dtype != pt || t.grad_dtype != gt || !t.n) continue;
-                const uint64_t chunks = l8_ceil(t.n, ADAM_CHUNK);
-                if (a.count == ADAM_TENSORS || (a.count && a.first[a.count] + chunks >= (uint64_t)1 << 23)) flush();
-                a.t[a.count] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.m_value, t.v_value, t.n, (uint32_t)i};
-                a.first[a.count + 1] = a.first[a.count] + (uint32_t)chunks;
-                ++a.count;
-            }
-            flush();
-        }
+    if (how->bits == 32) adamw<32>(ctx, tensors, count, how);
+    else adamw<8>(ctx, tensors, count, how);
     ZK_HIP(ctx, hipGetLastError());
     return ZKDL_OK;
 } catch (...) {

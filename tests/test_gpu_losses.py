@@ -87,7 +87,7 @@ class Row64:
 # both sides of every bound between kernels
 SHAPES = [(1, 1), (3, 1), (2, 7), (5, 8), (70, 7), (70, 8), (70, 9), (4, 71), (65, 511), (65, 512), (65, 513), (70, 1024), (70, 1025), (66, 2047),
           (66, 2048), (66, 2049), (1, 4096), (64, 4097), (3, 8192), (64, 8193), (63, 8200), (64, 16384), (65, 16385), (2, 16385), (64, 32768), (64, 32769),
-          (64, 65536), (64, 65537), (1, 131072), (64, 131072), (64, 131073), (1, 200001), (300, 33)]
+          (64, 65536), (64, 65537), (1, 131072), (64, 131072), (64, 131073), (1, 200001), (300, 33), (1000, 7), (40, 63), (41, 64), (39, 65), (20, 127), (17, 128), (19, 129), (9, 255), (7, 256), (11, 257)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
@@ -269,7 +269,7 @@ def preference64(row, off, ref, w, beta, target, smoothing, form, average):
 
 @pytest.mark.parametrize("shape,off", [((12, 5), [0, 3, 6, 6, 9]), ((70, 700), [2, 20, 33, 50, 65]), ((64, 3000), [0, 1, 2, 32, 64]), ((3, 40000), [0, 1, 3]),
                                        ((90, 8200), [5, 5, 5, 40, 40, 41, 88]), ((2, 1), [0, 1, 2]), ((5, 9), [5, 5, 5]), ((600, 100), [0, 299, 600]),
-                                       ((4, 16), [4]), ((64, 70000), [0, 10, 20, 21, 60])], ids=str)
+                                       ((4, 16), [4]), ((64, 70000), [0, 10, 20, 21, 60]), ((5000, 12), [0, 2100, 5000]), ((2500, 300), [3, 7, 2499])], ids=str)
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("form", ["logistic", "hinge", "square"])
 def test_preference_loss(lib, ctx, shape, off, dtype, form):

@@ -84,7 +84,7 @@ def check_params(got, want, move, before):
     assert torch.all((got.cpu().double() - want).abs() <= err), ((got.cpu().double() - want).abs() / err).max()
 
 
-SHAPES = [[(1,)], [(7,), (8,), (9,)], [(256,), (255,), (257,)], [(4095,), (4096,), (4097,)], [(3, 0), (130, 70), ()], [(33,)] * 41, [(1000, 1003), (5,)]]
+SHAPES = [[(1,)], [(7,), (8,), (9,)], [(256,), (255,), (257,)], [(4095,), (4096,), (4097,)], [(3, 0), (130, 70), ()], [(33,)] * 41, [(33,)] * 81, [(1000, 1003), (5,)]]
 HOW = dict(lr=0.01, beta1=0.9, beta2=0.99, eps=1e-6, decay=0.1)
 
 
