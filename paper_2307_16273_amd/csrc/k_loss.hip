@@ -39,6 +39,7 @@ struct LossArgs {
     const float *old_logp, *advantage, *ref_logp, *weight;
     float every, low, high, kl;  // the weight where there are none; 1 - clip_low, 1 + clip_high
     float* terms;                // [3][rows]: weighted loss, divergence, clipped
+    int past;                    // the gradient goes past the caches (where a kernel has that)
 };
 
 // The row's token, or -1 where the row counts for nothing.
@@ -172,7 +173,7 @@ __device__ __forceinline__ Raw8<T> load8_at(const T* p, uint32_t n, uint32_t lan
     for (int h = 0; h < (int)sizeof(T) / 2; ++h) v.q[h] = q[h];
     return v;
 }
-template <class T>
+template <bool PAST = false, class T>
 __device__ __forceinline__ void store8_at(T* p, uint32_t n, uint32_t lane, const float (&f)[8]) {
     uint64_t at = (uint64_t)(p + n);
     asm("" : "+s"(at));
@@ -180,7 +181,10 @@ __device__ __forceinline__ void store8_at(T* p, uint32_t n, uint32_t lane, const
     Raw8<T> w;
     pack8(f, w);
 #pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) q[h] = w.q[h];
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        if (PAST) __builtin_nontemporal_store(w.q[h], q + h);
+        else q[h] = w.q[h];
+    }
 }
 // A thread's vector in LDS, 16 bytes of it next to the other threads'.
 template <class T, int N>
@@ -292,17 +296,21 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
             const float co = dlogp * a.inv_tau, co_inv = of_wave(co / sum);
             if (out.p && dlogp != 0) {
                 float f[8];
+                const auto put_all = [&](auto past) {
 #pragma unroll
-                for (int k = 0; k < WHOLE; ++k) {
-                    if (k < REGS) {
-                        keep_packed(v[k < REGS ? k : 0]);
-                        slope8(v[k < REGS ? k : 0], c, a.k, co_inv, f);
-                    } else {
-                        slope8(get_lds<T>(&s_v[(k < REGS ? 0 : k - REGS) * (sizeof(T) / 2)], t), c, a.k, co_inv, f);
+                    for (int k = 0; k < WHOLE; ++k) {
+                        if (k < REGS) {
+                            keep_packed(v[k < REGS ? k : 0]);
+                            slope8(v[k < REGS ? k : 0], c, a.k, co_inv, f);
+                        } else {
+                            slope8(get_lds<T>(&s_v[(k < REGS ? 0 : k - REGS) * (sizeof(T) / 2)], t), c, a.k, co_inv, f);
+                        }
+                        store8_at<decltype(past)::value>(to, place_of<G, WHOLE>(k, turn), mine, f);
+                        if (STORED) __builtin_amdgcn_sched_barrier(0);
                     }
-                    store8_at(to, place_of<G, WHOLE>(k, turn), mine, f);
-                    if (STORED) __builtin_amdgcn_sched_barrier(0);
-                }
+                };
+                if (STORED && a.past) put_all(std::true_type());
+                else put_all(std::false_type());
                 if (ends) {
                     if (STORED) last = load8(row + end.start);
                     else keep_packed(last);
@@ -536,7 +544,7 @@ struct SlopeRow {
     int64_t y;
     bool none, bad;                     // zeros, NaN
 };
-template <class T, bool FULL>
+template <class T, bool FULL, bool PAST>
 __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to, uint32_t cols, uint32_t at, uint32_t lane) {
     float f[4][8];
     int n[4];
@@ -566,7 +574,7 @@ __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to,
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)s.y - j == i ? s.co : 0.f;
         }
-        if (FULL) store8(to + j, f[k]);
+        if (FULL) store8<PAST>(to + j, f[k]);
         else l8_store(to + (n[k] ? j : 0), n[k], f[k]);
     }
 }
@@ -592,8 +600,10 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
         s.top = top[r];
         s.norm = log_sum[r] * LOG2E;
         for (uint32_t q = blockIdx.x * waves + wave % waves; q < segs; q += gridDim.x * waves) {
-            if ((uint64_t)(q + 1) * 2048 <= a.cols) slope_of<T, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
-            else slope_of<T, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
+            if ((uint64_t)(q + 1) * 2048 <= a.cols) {
+                if (a.past) slope_of<T, true, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
+                else slope_of<T, true, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
+            } else slope_of<T, false, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
         }
     }
 }
@@ -710,10 +720,19 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
     else launch_rows_from<T, MODE, 512, 2, MODE == ROWS_LOGP ? MOST : 2 * MOST>(ctx, a, x, out);
 }
 
+// Logits that the last-level cache (256 MiB) holds, but not beside their gradient, are still there for the second read if the gradient goes past
+// it: preference loss of 4096 x 32768 16-bit entries 131 us / 106 past it, with the gradient read once behind it 285 / 275.  Below 128 MiB
+// the gradient's reader finds it in the cache (64 MiB 71 / 75), far above 256 it makes no difference.
 template <class T>
-void launch_slope(zkdl_ctx* ctx, const LossArgs& a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
+bool slope_past(const LossArgs& a) {
+    const uint64_t bytes = a.rows * a.cols * sizeof(T);
+    return bytes > (uint64_t)128 << 20 && bytes <= (uint64_t)288 << 20;
+}
+template <class T>
+void launch_slope(zkdl_ctx* ctx, LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
                   const float* losses = nullptr, uint64_t pairs = 0, float* loss = nullptr) {
     if (a.cols <= LOSS_SMALL && !losses) return launch_small<T, ROWS_SLOPE>(ctx, a, dlogp, top, log_sum, x, out);
+    a.past = slope_past<T>(a);
     const uint32_t segs = (uint32_t)l8_ceil(a.cols, 2048), waves = segs >= 4 ? 4 : segs >= 2 ? 2 : 1;
     const uint64_t gx = l8_ceil(segs, waves), gy = l8_ceil(a.rows, 4 / waves);
     hipLaunchKernelGGL((k_loss_slope<T>), dim3((unsigned)(gx < 1024 ? gx : 1024), (unsigned)(gy < 4096 ? gy : 4096)), dim3(256), 0, ctx->stream, a, dlogp, top,
@@ -787,6 +806,9 @@ int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const
     Scratch s(ctx, a.rows * (fit || !dlogits ? 3 : 6));
     if (!s.p) return ZKDL_ENOMEM;
     a.terms = s.p;
+    // rows in LDS (launch_rows): 1024 x 131072 16-bit entries 134 us / 126 past the cache, with the gradient read once behind it 249 / 242; 256 x
+    // 131072, which stay in the cache for that, 64 / 68
+    a.past = a.rows * a.cols * sizeof(T) > (uint64_t)128 << 20;
     if (fit) {
         launch_rows<T, ROWS_POLICY>(ctx, a, l8_mat<const T>(logits), l8_mat<T>(dlogits));
     } else {

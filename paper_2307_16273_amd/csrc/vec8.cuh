@@ -59,12 +59,16 @@ static __device__ __forceinline__ void pack8(const float (&f)[8], Raw8<__half>& 
         v.q[0][i] = (uint32_t)__half_as_ushort(lo) | (uint32_t)__half_as_ushort(hi) << 16;
     }
 }
-template <class T>
+// PAST: past the caches, whose lines go on holding what was there.
+template <bool PAST = false, class T>
 static __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
     Raw8<T> w;
     pack8(f, w);
 #pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) ((QuadAnywhere*)p)[h] = w.q[h];
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        if (PAST) __builtin_nontemporal_store(w.q[h], (QuadAnywhere*)p + h);
+        else ((QuadAnywhere*)p)[h] = w.q[h];
+    }
 }
 // What follows takes the floats of v from its registers again: without this they would stay in registers of their own, twice as many.
 template <class T>
