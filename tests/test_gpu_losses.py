@@ -444,6 +444,35 @@ def test_offsets_beyond_32_bits(lib, ctx):
     assert not back[1:-3].any() and back[-3:].any() and back[0, 5] > 0.99
 
 
+@pytest.mark.parametrize("shape", [(1100, 65541), (600, 120001), (520, 131072)], ids=str)
+def test_large_gradients(lib, ctx, shape):
+    """Gradients of more than 128 MiB go past the cache; a few of their rows against the definition, rows that count for nothing among them."""
+    T, V = shape
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (torch.randn((T, V), generator=g, device="cuda") * 2).to(torch.bfloat16)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[1::50] = -1
+    rows = torch.tensor([0, 1, 2, 63, T // 2, T - 2, T - 1], device="cuda")
+    row = Row64(x[rows], y[rows], 1.0)
+    lp = lib.token_logprobs(ctx, x, y)
+    row.check({k: v[rows] for k, v in lp.items()})
+    adv = torch.randn(T, generator=g, device="cuda")
+    got = lib.policy_loss(ctx, x, y, lp["logp"], adv, weight=torch.ones(T, device="cuda"), clip_low=1.0, clip_high=1e30)
+    dlogp = -adv[rows].double() * row.live
+    row.check_slope(got["dlogits"][rows], dlogp, dlogp.abs() * (2 * row.logp_err + 8 * U), torch.bfloat16)
+    back = lib.token_logprobs_backward(ctx, adv, x, y, lp["top"], lp["log_sum"])
+    sum_err = row.sum_err
+    row.sum_err = (3 * 40 + 3 * 20 + 200) * U + 2 * sum_err        # |logits| below 40, log_sum below 20, both statistics as they came out of the forward pass
+    row.check_slope(back[rows], adv[rows].double() * row.live, torch.zeros(len(rows)).double(), torch.bfloat16)
+    off = torch.tensor([0, T // 3, T], device="cuda")
+    pref = lib.preference_loss(ctx, x, y, off, beta=0.01)
+    m = pref["margin"].double().item()
+    sign = torch.where(rows < T // 3, 1.0, -1.0).double()
+    dlogp = sign * 0.01 * (1 / (1 + math.exp(-m)) - 1) * row.live
+    # the margin is a sum over all rows and comes back rounded to 32 bits: |m| below 300 (T rows of at most 30 each), slope 1/4
+    row.check_slope(pref["dlogits"][rows], dlogp, 0.01 * 0.25 * 300 * U + 4 * U * dlogp.abs(), torch.bfloat16)
+
+
 def calls(lib, c, x, y, old, adv, off):
     lp = lib.token_logprobs(c, x, y)
     back = lib.token_logprobs_backward(c, adv, x, y, lp["top"], lp["log_sum"])
