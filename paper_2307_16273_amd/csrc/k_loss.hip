@@ -256,8 +256,9 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         for (int k = 0; k < STORED; ++k) {
             c = max8(c, v[k]);
             put_lds<T>(&s_v[k * (sizeof(T) / 2)], t, v[k]);
-            v[k] = load8_at(row, place_of<G, WHOLE>(k, turn), mine);
-            __builtin_amdgcn_sched_barrier(0);
+            const T* rest = row;
+            asm volatile("" : "+s"(rest), "+v"(c));        // the next load waits for this vector's maximum: its registers are that load's
+            v[k] = load8_at(rest, place_of<G, WHOLE>(k, turn), mine);
         }
         if (ends) last = load8(row + end.start);
         const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
                         if (STORED) __builtin_amdgcn_sched_barrier(0);
                     }
                 };
-                if (STORED && a.past) put_all(std::true_type());
+                if (STORED && sizeof(T) == 2 && a.past) put_all(std::true_type());
                 else put_all(std::false_type());
                 if (ends) {
                     if (STORED) last = load8(row + end.start);
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
         s.norm = log_sum[r] * LOG2E;
         for (uint32_t q = blockIdx.x * waves + wave % waves; q < segs; q += gridDim.x * waves) {
             if ((uint64_t)(q + 1) * 2048 <= a.cols) {
-                if (a.past) slope_of<T, true, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
+                if (sizeof(T) == 2 && a.past) slope_of<T, true, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
                 else slope_of<T, true, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
             } else slope_of<T, false, false>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);
         }
@@ -722,11 +723,12 @@ void launch_rows(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x, L8Mat<T> ou
 
 // Logits that the last-level cache (256 MiB) holds, but not beside their gradient, are still there for the second read if the gradient goes past
 // it: preference loss of 4096 x 32768 16-bit entries 131 us / 106 past it, with the gradient read once behind it 285 / 275.  Below 128 MiB
-// the gradient's reader finds it in the cache (64 MiB 71 / 75), far above 256 it makes no difference.
+// the gradient's reader finds it in the cache (64 MiB 71 / 75), far above 256 it makes no difference.  32-bit entries leave a thread as two pieces of
+// 16 bytes, half of what lies between its neighbours' each: past the cache such halves cost a third more (below).
 template <class T>
 bool slope_past(const LossArgs& a) {
     const uint64_t bytes = a.rows * a.cols * sizeof(T);
-    return bytes > (uint64_t)128 << 20 && bytes <= (uint64_t)288 << 20;
+    return sizeof(T) == 2 && bytes > (uint64_t)128 << 20 && bytes <= (uint64_t)288 << 20;
 }
 template <class T>
 void launch_slope(zkdl_ctx* ctx, LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
@@ -807,8 +809,8 @@ int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const
     if (!s.p) return ZKDL_ENOMEM;
     a.terms = s.p;
     // rows in LDS (launch_rows): 1024 x 131072 16-bit entries 134 us / 126 past the cache, with the gradient read once behind it 249 / 242; 256 x
-    // 131072, which stay in the cache for that, 64 / 68
-    a.past = a.rows * a.cols * sizeof(T) > (uint64_t)128 << 20;
+    // 131072, which stay in the cache for that, 64 / 68; 4096 x 49152 32-bit entries 320 / 425
+    a.past = sizeof(T) == 2 && a.rows * a.cols * sizeof(T) > (uint64_t)128 << 20;
     if (fit) {
         launch_rows<T, ROWS_POLICY>(ctx, a, l8_mat<const T>(logits), l8_mat<T>(dlogits));
     } else {
