@@ -1,7 +1,7 @@
 // The end of a training step: the norm of all gradients (zkdl_gradient_norm) and AdamW over many tensors (zkdl_adamw_step).
 //
 // Both are bound by memory: an entry of a step in 32 bits is 28 bytes moved for about 40 vector operations, with 8-bit states 14 bytes
-// for about 90.  A launch takes many tensors: their addresses stand in its arguments (4 kB at most, so nothing is copied to the device
+// (16-bit gradients) for about 80, ten of them in 64 bits.  A launch takes many tensors: their addresses stand in its arguments (4 kB at most, so nothing is copied to the device
 // and nothing is kept of a call), and a block finds its tensor by the number of its chunk.
 #include <cfloat>
 #include <cmath>
@@ -26,7 +26,8 @@ __device__ __forceinline__ uint32_t tensor_of(const uint32_t (&first)[N], uint32
 }
 
 // ---------------------------------------------------------------------------
-// Norm: squares in 64 bits, so that no gradient in the range of 32 bits leaves it
+// Norm: squares in 64 bits, so that no gradient in the range of 32 bits leaves it.  0.8 GB of 16-bit gradients 136 us (5.9 TB/s) and 5 for the
+// join; 34 MB in 32 bits 5.9 us and 2.3.
 // ---------------------------------------------------------------------------
 constexpr uint32_t NORM_TENSORS = 160, NORM_ITEMS = 4, NORM_CHUNK = 256 * 8 * NORM_ITEMS, NORM_BLOCKS = 2048;
 struct NormArgs {
@@ -102,7 +103,9 @@ __global__ __launch_bounds__(1024) void k_norm_join(const double* part, uint64_t
 }
 
 // ---------------------------------------------------------------------------
-// AdamW
+// AdamW.  2^28 entries (MI355X, a copy moves 5.2 TB/s): all in 32 bits 1375 us (5.5 TB/s); 8-bit states with 32-bit gradients 775 us (5.5), with 16-bit
+// gradients 685 us (5.5), all parameters and gradients in 16 bits 540 us (5.0: here the vector operations show).  The moments are taken
+// in 64 bits because the codes' rounding has to come out the same for whoever computes the step.
 // ---------------------------------------------------------------------------
 constexpr uint32_t ADAM_ITEMS = 2, ADAM_CHUNK = 256 * 8 * ADAM_ITEMS, ADAM_BLOCK8 = 256;
 struct AdamTensor {
