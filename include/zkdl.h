@@ -636,7 +636,7 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
  * stay in the range of 32 bits.
  * dlogits: the gradient of the logits, logits' type and shape, dlogits_j = dlogp ([j = token] - p_j) / temperature; a row whose dlogp
  * is 0 has zeros whatever it holds.  temperature: positive, normal, finite; so is its reciprocal.  Sums in 32 bits and more, in an
- * order that depends on the sizes alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.
+ * order that depends on the sizes and the row's place alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.
  * Conventions (stream, scratch, graphs, outputs that overlap nothing) and errors as for the 8-bit layers. */
 
 /* zkdl_token_logprobs: logp, and top and log_sum for the backward pass (both may be NULL). */

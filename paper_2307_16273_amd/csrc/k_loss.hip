@@ -155,15 +155,15 @@ __device__ __forceinline__ void put_end(T* row, const L8At& end, const float (&f
         if ((uint32_t)i >= end.dup) put_one(row + end.start + i, f[i]);
 }
 
-// Eight items, `lane` bytes behind p + n, p and n being the whole wave's: the instruction adds the lane's own offset, and no vector has an address
-// of 64 bits of its own.
-// In bytes.  (Opaque, so that it stays the 32-bit offset that the instruction takes.)
+// A thread's offset in bytes, opaque, so that it stays the 32-bit offset that the instructions below take.
 template <class T>
 __device__ __forceinline__ uint32_t own_offset(uint32_t t) {
     uint32_t o = t * 8 * (uint32_t)sizeof(T);
     asm("" : "+v"(o));
     return o;
 }
+// Eight items, `lane` bytes behind p + n, p and n being the whole wave's: the instruction adds the lane's own offset, and no vector has an address
+// of 64 bits of its own.
 template <class T>
 __device__ __forceinline__ Raw8<T> load8_at(const T* p, uint32_t n, uint32_t lane) {
     uint64_t at = (uint64_t)(p + n);
@@ -640,8 +640,7 @@ __global__ __launch_bounds__(N) void k_loss_pair(PairArgs a) {
         at[1] = max(at[1], at[0]);
         double x[4] = {0, 0, 0, 0};         // of either sequence the sum, and the rows that count
 #pragma unroll 4
-        for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += N)
-        {
+        for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += N) {
             const int64_t y = a.tokens.at(r);
             const float p = a.logp[r], q = a.ref_logp ? a.ref_logp[r] : 0.f;        // (no load waits for the token)
             const double d = y >= 0 ? (double)p - (double)q : 0., one = y >= 0 ? 1. : 0.;
@@ -657,7 +656,9 @@ __global__ __launch_bounds__(N) void k_loss_pair(PairArgs a) {
         double each, slope;
         if (a.form == ZKDL_PREF_LOGISTIC) {
             const double small = log1p(exp(-fabs(m)));          // log(1 + exp(-|m|))
-            each = (1 - a.smoothing) * (fmax(-m, 0.) + small) + a.smoothing * (fmax(m, 0.) + small);
+            const double toward = fmax(-m, 0.) + small, away = fmax(m, 0.) + small;
+            // (margins may be infinite: a sequence that cannot be)
+            each = (a.smoothing < 1 ? (1 - a.smoothing) * toward : 0.) + (a.smoothing > 0 ? a.smoothing * away : 0.);
             slope = a.smoothing - 1 / (1 + exp(m));
         } else if (a.form == ZKDL_PREF_HINGE) {
             each = m >= 0 ? 0 : -m;

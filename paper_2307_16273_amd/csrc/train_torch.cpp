@@ -268,11 +268,11 @@ PyObject* adamw_step(const Call& c, PyObject* const* a) {
                 (k ? t[i].v_value : t[i].m_value) = floats(outs.back());
             }
     }
-    const int rc = f_adamw(c.ctx, t.data(), t.size(), &how);
-    if (rc) return PyLong_FromLong(rc);
-    // what autograd keeps of these tensors is not theirs any more
+    // what autograd keeps of these tensors will not be theirs any more (tensors of inference mode outside of it are refused here, before anything is written)
     for (Py_ssize_t i = 0; i < n; ++i)
         for (const List* l : {&params, &ms, &vs}) l->at(c, i).unsafeGetTensorImpl()->bump_version();
+    const int rc = f_adamw(c.ctx, t.data(), t.size(), &how);
+    if (rc) return PyLong_FromLong(rc);
     PyObject* d = PyDict_New();
     for (int k = 0; k < 2; ++k) {
         PyObject* o = values ? PyList_New(n) : Py_NewRef(Py_None);

@@ -365,6 +365,19 @@ def test_rows_of_weight_0(lib, ctx, shape):
     assert torch.isfinite(pref["loss"]) and torch.isnan(pref["margin"][1]) and not pref["dlogits"][2:].any() and pref["dlogits"][0].any()
 
 
+def test_margins_without_end(lib, ctx):
+    """A pair whose other answer holds an entry that cannot be: nothing is lost by it and nothing to be learnt; the other way round the loss has no end."""
+    x = torch.zeros(2, 10)
+    x[1, 3] = -math.inf
+    y, off = torch.tensor([3, 3]).cuda(), torch.tensor([0, 1, 2]).cuda()
+    for form in ("logistic", "hinge"):
+        got = lib.preference_loss(ctx, x.cuda(), y, off, form=form)
+        assert got["margin"].item() == math.inf and got["loss"].item() == 0 and not got["dlogits"].any()
+        got = lib.preference_loss(ctx, x.flip(0).cuda(), y, off, form=form)
+        assert got["margin"].item() == -math.inf and got["loss"].item() == math.inf
+    assert lib.preference_loss(ctx, x.cuda(), y, off, smoothing=1.0)["loss"].item() == math.inf
+
+
 def test_logits_of_any_size(lib, ctx):
     """Logits far from zero and far apart, and the largest of their type."""
     x = torch.tensor([[1e4, 1e4 - 1, 0.0], [-1e30, -1e30, -1e30], [3e38, -3e38, 3e38], [88.0, 0.0, -88.0], [0.0, -200.0, -1e9]])

@@ -409,6 +409,19 @@ def test_autograd_is_told_of_the_update(lib, ctx):
         y.backward()
 
 
+def test_tensors_of_inference_mode(lib, ctx):
+    """Updated inside of it; refused outside, with nothing written."""
+    with torch.inference_mode():
+        w = [torch.ones(300, device="cuda")]
+        d, state = [torch.ones(300, device="cuda")], lib.adamw_state(w)
+        lib.adamw_step(ctx, w, d, state, 1, 0.25, decay=0.0)
+    kept = w[0].cpu()
+    assert torch.all((kept - 0.75).abs() < 1e-6)
+    with pytest.raises(RuntimeError, match="nference"):
+        lib.adamw_step(ctx, w, d, state, 2, 0.25)
+    assert torch.equal(w[0].cpu(), kept)
+
+
 def test_lists_of_any_kind(lib, ctx):
     """Tuples, generators and a stack of parameters, on the context's stream and on another."""
     stack, d = torch.zeros(3, 50, device="cuda"), torch.ones(3, 50, device="cuda")
