@@ -20,11 +20,15 @@ constexpr float INF = __builtin_huge_valf(), NAN32 = __builtin_nanf("");
 
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }    // 1 ulp; 0 below 2^-126, where nothing is left of a probability
 
-// Integers of 32 or 64 bits.
+// Integers of 32 or 64 bits, without a branch: loads of several are under way at once.
 struct Ints {
     const void* p;
-    int wide;
-    __device__ __forceinline__ int64_t at(uint64_t i) const { return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i]; }
+    int wide;       // 0 or 1
+    __device__ __forceinline__ int64_t at(uint64_t i) const {
+        const uint32_t* q = (const uint32_t*)p + (i << wide);
+        const uint32_t low = q[0], high = q[wide];
+        return (int64_t)((uint64_t)(wide ? high : (uint32_t)((int32_t)low >> 31)) << 32 | low);
+    }
 };
 
 struct LossArgs {
@@ -43,14 +47,14 @@ struct LossArgs {
     int past;                    // the gradient goes past the caches (where a kernel has that)
 };
 
+enum { ROWS_LOGP, ROWS_POLICY, ROWS_SLOPE };
+
 // The row's token, or -1 where the row counts for nothing.
 __device__ __forceinline__ int64_t token_of(const LossArgs& a, uint64_t r) {
-    int64_t y = a.tokens.at(r);
-    if (a.offsets.p) {
-        const int64_t lo = a.offsets.at(0), hi = a.offsets.at(a.last);
-        if ((int64_t)r < lo || (int64_t)r >= hi) y = -1;
-    }
-    return y;
+    const int64_t y = a.tokens.at(r);
+    if (!a.offsets.p) return y;
+    const int64_t lo = a.offsets.at(0), hi = a.offsets.at(a.last);
+    return (int64_t)r < lo || (int64_t)r >= hi ? -1 : y;
 }
 
 // Terms are exp2((x - c) k): the difference first, so that rows of the type's lowest value (masks) and of its largest stay in the range.
@@ -74,19 +78,28 @@ __device__ __forceinline__ float divergence_of(float d, float em) {
     return fabsf(d) < .25f ? d * d * p : em - d;
 }
 
+// What the policy loss has of a row beside its logits, asked for before they are looked at.
+struct PolicyRow {
+    float w, adv, old, ref;
+};
+template <int MODE>
+__device__ __forceinline__ PolicyRow policy_of(const LossArgs& a, uint64_t r) {
+    if constexpr (MODE != ROWS_POLICY) return {0.f, 0.f, 0.f, 0.f};
+    return {a.weight ? a.weight[r] : a.every, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
+}
 // One row's share of the policy loss; returns dlogp.
-__device__ __forceinline__ float policy_row(const LossArgs& a, uint64_t r, float logp, float (&term)[3]) {
-    const float w = a.weight ? a.weight[r] : a.every, adv = a.advantage[r];
+__device__ __forceinline__ float policy_row(const LossArgs& a, const PolicyRow& row, float logp, float (&term)[3]) {
+    const float w = row.w, adv = row.adv;
     if (w == 0) {           // whatever the rest is
         term[0] = term[1] = term[2] = 0.f;
         return 0.f;
     }
-    const float ratio = expf(logp - a.old_logp[r]);
+    const float ratio = expf(logp - row.old);
     const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
     const float gain = adv == 0 ? 0.f : (up ? a.high : down ? a.low : ratio) * adv;
     float slope = clipped || adv == 0 ? 0.f : -adv * ratio, div = 0.f;
     if (a.ref_logp) {
-        const float d = a.ref_logp[r] - logp, em = expm1f(d);
+        const float d = row.ref - logp, em = expm1f(d);
         div = divergence_of(d, em);
         if (a.kl != 0) slope = fmaf(-a.kl, em, slope);
     }
@@ -215,8 +228,6 @@ __device__ __forceinline__ void put_zeros(T* to, uint32_t mine, uint32_t turn, b
     if (ends) put_end(to, end, zero);
 }
 
-enum { ROWS_LOGP, ROWS_POLICY, ROWS_SLOPE };
-
 // ---------------------------------------------------------------------------
 // Rows that stay on the chip: G threads a row (a wave: four rows a block) with WHOLE vectors of eight each, and one at the row's end:
 // 8 G WHOLE <= cols < 8 G (WHOLE + 1), cols > 256.  The vectors are in registers, but for the last of the longest rows, which lie in LDS: so two
@@ -264,6 +275,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         }
         if (ends) last = load8(row + end.start);
         const float xy = l8_f32(row[y < (int64_t)a.cols ? y : 0]);
+        const PolicyRow given = policy_of<MODE>(a, r);
 #pragma unroll
         for (int k = 0; k < REGS; ++k) {
             c = max8(c, v[(k + STORED) % (REGS ? REGS : 1)]);       // in the order in which they were asked for
@@ -295,7 +307,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         sum = of_wave(row_reduce<G, false>(sum, s_sum));
         st = row_stats(a, c, sum, y, xy);
         if (MODE == ROWS_POLICY) {
-            const float dlogp = policy_row(a, r, st.logp, term);
+            const float dlogp = policy_row(a, given, st.logp, term);
             const float co = dlogp * a.inv_tau, co_inv = of_wave(co / sum);
             if (out.p && dlogp != 0) {
                 float f[8];
@@ -373,6 +385,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
             co_inv = dlogp * a.inv_tau;
         } else {
             const float xy = l8_f32(row[bad ? 0 : y]);
+            const PolicyRow given = policy_of<MODE>(a, r);
             float c = -INF, sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) c = fmaxf(c, i < n ? f[i] : -INF);
@@ -385,7 +398,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
             sum = lanes_reduce<G, false>(sum);
             st = row_stats(a, c, sum, y, xy);
             if (MODE == ROWS_POLICY) {
-                dlogp = policy_row(a, r, st.logp, term);
+                dlogp = policy_row(a, given, st.logp, term);
                 co_inv = dlogp * a.inv_tau / sum;
             }
         }
@@ -484,6 +497,7 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
         float term[3] = {0.f, 0.f, 0.f}, dlogp = 0.f;
         if (y >= 0) {
             const float xy = l8_f32(x.p[r * x.rs + (y < (int64_t)a.cols ? y : 0)]);
+            const PolicyRow given = policy_of<MODE>(a, r);
             float c = -INF, sum = 0.f;
             for (uint32_t q = threadIdx.x; q < parts; q += 256) c = fmaxf(c, part[r * parts + q].top);
             c = row_reduce<256, true>(c, s_max);
@@ -493,7 +507,7 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
             }
             sum = row_reduce<256, false>(sum, s_sum);
             st = row_stats(a, c, sum, y, xy);
-            if (MODE == ROWS_POLICY) dlogp = policy_row(a, r, st.logp, term);
+            if (MODE == ROWS_POLICY) dlogp = policy_row(a, given, st.logp, term);
         }
         if (threadIdx.x == 0) {
             if (a.logp) a.logp[r] = st.logp;
@@ -599,9 +613,10 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
     const uint32_t per = 4 / waves, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (uint64_t r = (uint64_t)blockIdx.y * per + wave / waves; r < a.rows; r += (uint64_t)gridDim.y * per) {
         SlopeRow s;
+        const float d = dlogp[r];
         s.y = token_of(a, r);
-        s.co = dlogp[r] * a.inv_tau;
-        s.none = s.y < 0 || dlogp[r] == 0;
+        s.co = d * a.inv_tau;
+        s.none = s.y < 0 || d == 0;
         s.bad = s.y >= (int64_t)a.cols;
         s.inv_tau = a.inv_tau;
         s.top = top[r];
@@ -862,6 +877,7 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
         else hipLaunchKernelGGL((k_loss_pair<1024>), grid, dim3(1024), 0, ctx->stream, q);
     }
     const bool few = dlogits && a.rows && p->pairs <= 4096 && a.cols > LOSS_SMALL;         // pairs whose losses one block adds up while others are at the gradient
+    a.offsets.p = nullptr;          // dlogp is 0 where rows are in no sequence
     if (dlogits && a.rows)
         launch_slope<T>(ctx, a, a.dlogp, a.top, a.log_sum, l8_mat<const T>(logits), l8_mat<T>(dlogits), few ? losses : nullptr, p->pairs, loss);
     return few ? (int)ZKDL_OK : launch_sum(ctx, losses, p->pairs, 1, loss);
