@@ -632,8 +632,8 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
  * the entry that was taken in each row.  A row whose token is negative counts for nothing: it is not read, its outputs and its
  * gradient are zero.  A token of V and more gives NaN.  With u = logits / temperature (times 1 / temperature in 32 bits):
  *   top = max_j u_j,  log_sum = log sum_j exp(u_j - top),  logp = u_token - top - log_sum,  p_j = exp(u_j - top - log_sum).
- * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.  u has to
- * stay in the range of 32 bits.
+ * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.  Where u is beyond
+ * the range of 32 bits (masks of the lowest value at a temperature below 1) top is infinite; the rest holds.
  * dlogits: the gradient of the logits, logits' type and shape, dlogits_j = dlogp ([j = token] - p_j) / temperature; a row whose dlogp
  * is 0 has zeros whatever it holds.  temperature: positive, normal, finite; so is its reciprocal.  Sums in 32 bits and more, in an
  * order that depends on the sizes and the row's place alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.

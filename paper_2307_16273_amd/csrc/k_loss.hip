@@ -378,9 +378,18 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
         const T* const row = x.p + r * x.rs;
         l8_load(row + (n ? j : 0), n, f);
         if (MODE == ROWS_SLOPE) {
-            const float norm = log_sum[r] * LOG2E, top_r = top[r];
+            const float norm = log_sum[r] * LOG2E;
+            float c = top[r], times = a.inv_tau, k = LOG2E;
+            if (fabsf(c) == INF) {          // as in slope_far
+                c = -INF;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = exp2_raw(fmaf(fmaf(f[i], a.inv_tau, -top_r), LOG2E, -norm));
+                for (int i = 0; i < 8; ++i) c = fmaxf(c, i < n ? f[i] : -INF);
+                c = lanes_reduce<G, true>(c);
+                times = 1.f;
+                k = a.k;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = exp2_raw(fmaf(fmaf(f[i], times, -c), k, -norm));
             if (bad) dlogp = NAN32;
             co_inv = dlogp * a.inv_tau;
         } else {
@@ -569,11 +578,12 @@ template <class T, bool FULL, bool PAST>
 __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to, uint32_t cols, uint32_t at, uint32_t lane) {
     float f[4][8];
     int n[4];
+    const uint32_t mine = own_offset<T>(lane);
     if constexpr (FULL) {
         if (!s.none) {
             Raw8<T> v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = load8(row + at + (k * 64 + lane) * 8);
+            for (int k = 0; k < 4; ++k) v[k] = load8_at(row + at, k * 512, mine);
 #pragma unroll
             for (int k = 0; k < 4; ++k) floats8(v[k], f[k]);
         }
@@ -595,9 +605,28 @@ __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to,
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)s.y - j == i ? s.co : 0.f;
         }
-        if (FULL) store8<PAST>(to + j, f[k]);
+        if (FULL) store8_at<PAST>(to + at, k * 512, mine, f[k]);
         else l8_store(to + (n[k] ? j : 0), n[k], f[k]);
     }
+}
+// The same where logits / temperature, and with it top, are beyond 32 bits: from the row's largest logit c, p_j = exp2((x_j - c) k - norm).  Rare (rows of
+// nothing but a mask of the lowest value), and apart from the rest, whose registers it would take.
+template <class T>
+__device__ __forceinline__ void slope_far(const SlopeRow& s, float k, const T* row, T* to, uint32_t cols, uint32_t first, uint32_t step, uint32_t lane) {
+    asm volatile("" : "+v"(lane));
+    float c = -INF;
+#pragma unroll 1
+    for (uint32_t j = lane; j < cols; j += 64) c = fmaxf(c, l8_f32(row[j]));
+#pragma unroll 1
+    for (int d = 32; d; d >>= 1) c = fmaxf(c, __int_as_float(__builtin_amdgcn_ds_bpermute((int)((lane ^ d) * 4), __float_as_int(c))));
+    c = of_wave(c);
+#pragma unroll 1
+    for (uint64_t at = first; at < cols; at += step)
+#pragma unroll 1
+        for (uint64_t j = at + lane; j < min(at + 2048, (uint64_t)cols); j += 64) {
+            const float p = exp2_raw(fmaf(l8_f32(row[j]) - c, k, -s.norm));
+            put_one(to + j, s.bad ? NAN32 : (uint64_t)s.y == j ? fmaf(-p, s.co, s.co) : -p * s.co);
+        }
 }
 template <class T>
 __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlogp, const float* top, const float* log_sum, L8Mat<const T> x, L8Mat<T> out,
@@ -621,6 +650,10 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
         s.inv_tau = a.inv_tau;
         s.top = top[r];
         s.norm = log_sum[r] * LOG2E;
+        if (!s.none && fabsf(s.top) == INF) {
+            slope_far(s, a.k, x.p + r * x.rs, out.p + r * out.rs, a.cols, (blockIdx.x * waves + wave % waves) * 2048, gridDim.x * waves * 2048, lane);
+            continue;
+        }
         for (uint32_t q = blockIdx.x * waves + wave % waves; q < segs; q += gridDim.x * waves) {
             if ((uint64_t)(q + 1) * 2048 <= a.cols) {
                 if (sizeof(T) == 2 && a.past) slope_of<T, true, true>(s, x.p + r * x.rs, out.p + r * out.rs, a.cols, q * 2048, lane);

@@ -136,6 +136,43 @@ def test_a_mask_of_the_lowest_value(lib, ctx):
             want.check_slope(back, torch.ones(T).double(), torch.zeros(T).double(), t)
 
 
+@pytest.mark.parametrize("shape", [(66, 40), (5, 250), (70, 9000), (3, 20000), (4, 140001)], ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_mask_of_the_lowest_value_below_temperature_1(lib, ctx, shape, dtype):
+    """logits / temperature leave the range of 32 bits where nothing but the mask, or nothing but the largest value, is left: a row of equals all the same."""
+    T, V = shape
+    x, y = inputs(gen(V + 1), T, V, dtype, ignore=False)
+    t = TYPES[dtype]
+    x[:, 2::5] = torch.finfo(t).min
+    y = torch.where(y % 5 == 2, y - 1, y)
+    x[0], x[1] = torch.finfo(t).min, torch.finfo(t).max
+    row = Row64(x, y, 0.5)
+    # log-probabilities are (logit - the largest) / temperature - log_sum: of the largest itself they have no rounding
+    row.logp_err = 3 * U * (row.logp + row.log_sum).abs() + row.log_sum_err + 2 * U * row.logp.abs()
+    x, y = x.cuda(), y.cuda()
+    got = lib.token_logprobs(ctx, x, y, temperature=0.5)
+    row.check({k: got[k] for k in ("logp", "log_sum")})
+    if dtype != "f16":
+        assert got["top"][0] == -math.inf and got["top"][1] == math.inf
+    ones, none = torch.ones(T), torch.zeros(T).double()
+    old, ref, w = row.logp.float().cpu(), row.logp.float().cpu() - 0.25, torch.full((T,), 1 / T)
+    policy = lib.policy_loss(ctx, x, y, old.cuda(), ones.cuda(), ref_logp=ref.cuda(), weight=w.cuda(), clip_low=0.2, clip_high=0.3, kl=0.125, temperature=0.5)
+    off = [0, 1, 2, T // 2 + 1, T] if T > 4 else [0, 1, T]
+    pairs = torch.full((len(off) // 2,), 0.5)
+    preference = lib.preference_loss(ctx, x, y, torch.tensor(off).cuda(), weight=pairs.cuda(), beta=0.25, temperature=0.5)
+    back = lib.token_logprobs_backward(ctx, ones.cuda(), x, y, got["top"], got["log_sum"], temperature=0.5)
+    sums, errs, dlogp, derr = policy64(row, old, ones, ref, w, 0.2, 0.3, 0.125)
+    for k, s, e in zip(("loss", "divergence", "clipped"), sums, errs):
+        assert abs(policy[k].item() - s.item()) <= e.item(), k
+    margins, merr, loss, lerr, dpref, dpref_err, seen = preference64(row, off, None, pairs, 0.25, 0.0, 0.0, "logistic", False)
+    assert seen.all() and torch.all((preference["margin"].cpu().double() - margins).abs() <= merr) and abs(preference["loss"].item() - loss) <= lerr
+    # what comes from top and log_sum has their roundings, as in the test of that pass
+    row.sum_err += (3 * row.u[2:].amax().item() + 3 * row.log_sum.amax().item() + 3 * row.top[2:].abs().amax().item() + 10) * U
+    row.check_slope(policy["dlogits"], dlogp, derr, t)
+    row.check_slope(preference["dlogits"], dpref, dpref_err, t)
+    row.check_slope(back, ones.double(), none, t)
+
+
 def policy64(row, old, adv, ref, w, lo, hi, kl):
     """Loss, divergence, clipped, dlogp and by how much they may differ."""
     E = row.logp_err
