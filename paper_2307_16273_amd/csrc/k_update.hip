@@ -151,7 +151,7 @@ static __host__ __device__ inline AdamRates adam_rates(double lr, double decay, 
     AdamRates r;
     r.rate = (float)(lr / (1 - power_of(beta1, t)));
     r.root = (float)(1 / sqrt(1 - power_of(beta2, t)));
-    r.keep = (float)(1 - lr * decay);
+    r.keep = (float)fma(-lr, decay, 1.0);       // (rounded once, on either side)
     return r;
 }
 
