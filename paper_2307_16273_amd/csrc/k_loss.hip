@@ -234,7 +234,7 @@ __device__ __forceinline__ void put_zeros(T* to, uint32_t mine, uint32_t turn, b
 // blocks of 512 threads with 128 registers each, and half of the LDS, have room in a compute unit up to rows of 256 kB, and one of them has
 // memory at work while the other computes.  (As many instances as there are lengths: with a count that the kernel learns when it runs, the
 // vectors' registers were copied and spilled.)  Bound by memory: log-probabilities of 4096 x 32768 16-bit entries, a quarter of the rows
-// not read, 39 us (5.1 TB/s); the policy's gradient of 4096 x 131072, a quarter zeros, 356 us (5.3 TB/s), of 4096 x 16384 50 us (5.4 TB/s).
+// not read, 38.3 us (5.2 TB/s); the policy's gradient of 4096 x 131072, a quarter zeros, 356 us (5.3 TB/s), of 4096 x 16384 50 us (5.4 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int loss_threads(int G) { return G < 256 ? 256 : G; }
 // vectors in registers, by what else a thread holds, and in LDS, of which a compute unit has 160 kB
