@@ -630,7 +630,7 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
  * What stands in front of a network's first gradient and behind its last one.  logits: a zkdl_mat [T, V] of ZKDL_F32 / F16 /
  * BF16 (a stack of one, V >= 1), row t the network's output for packed row t; tokens: T integers of tokens_dtype (ZKDL_I32 / ZKDL_I64),
  * the entry that was taken in each row.  A row whose token is negative counts for nothing: it is not read, its outputs and its
- * gradient are zero.  A token of V and more gives NaN.  With u = logits / temperature (times 1 / temperature in 32 bits):
+ * gradient are zero.  A token of V and more gives NaN.  With u = logits / temperature:
  *   top = max_j u_j,  log_sum = log sum_j exp(u_j - top),  logp = u_token - top - log_sum,  p_j = exp(u_j - top - log_sum).
  * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.  Where u is beyond
  * the range of 32 bits (masks of the lowest value at a temperature below 1) top is infinite; the rest holds.

@@ -15,7 +15,7 @@
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float INF = __builtin_huge_valf(), NAN32 = __builtin_nanf("");
 
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }    // 1 ulp; 0 below 2^-126, where nothing is left of a probability
@@ -35,6 +35,7 @@ struct LossArgs {
     uint64_t rows;
     uint32_t cols;
     float inv_tau, k;            // 1 / temperature; log2(e) / temperature
+    double inv_tau64;
     Ints tokens;
     Ints offsets;                // preference: rows outside [offsets[0], offsets[last]) count for nothing
     uint64_t last;
@@ -60,15 +61,22 @@ __device__ __forceinline__ int64_t token_of(const LossArgs& a, uint64_t r) {
 // Terms are exp2((x - c) k): the difference first, so that rows of the type's lowest value (masks) and of its largest stay in the range.
 __device__ __forceinline__ float term_of(float x, float c, float k) { return exp2_raw((x - c) * k); }
 
+// log_sum and logp in 64 bits: in 32 their last places are a millionth at 10, which a loss has in every ratio and, of sums that cancel, in its first
+// places.  The logarithm is the exponent and that of a number next to 1, which 32 bits hold to 2^-25.
 struct RowStats {
-    float top, log_sum, logp;
+    float top, log_sum;
+    double logp;
 };
 __device__ __forceinline__ RowStats row_stats(const LossArgs& a, float c, float sum, int64_t y, float xy) {
+    const float m = __builtin_amdgcn_frexp_mantf(sum);          // 1/2 <= m < 1
+    const bool low = m < .70710678f;
+    const double log_sum = ((double)(__builtin_amdgcn_frexp_expf(sum) - low) + (double)__builtin_amdgcn_logf(low ? 2 * m : m)) * 0.69314718055994530942;
     RowStats s;
-    s.log_sum = __log2f(sum) * LN2;
+    s.log_sum = (float)log_sum;
     s.top = c * a.inv_tau;
+    s.logp = ((double)xy - (double)c) * a.inv_tau64 - log_sum;
     if (!(sum < INF)) s.top = s.log_sum = NAN32;          // a NaN, +infinity, or nothing but -infinity
-    s.logp = y >= (int64_t)a.cols ? NAN32 : (xy - c) * a.inv_tau - s.log_sum;
+    if (!(sum < INF) || y >= (int64_t)a.cols) s.logp = NAN32;
     return s;
 }
 
@@ -88,18 +96,18 @@ __device__ __forceinline__ PolicyRow policy_of(const LossArgs& a, uint64_t r) {
     return {a.weight ? a.weight[r] : a.every, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
 }
 // One row's share of the policy loss; returns dlogp.
-__device__ __forceinline__ float policy_row(const LossArgs& a, const PolicyRow& row, float logp, float (&term)[3]) {
+__device__ __forceinline__ float policy_row(const LossArgs& a, const PolicyRow& row, double logp, float (&term)[3]) {
     const float w = row.w, adv = row.adv;
     if (w == 0) {           // whatever the rest is
         term[0] = term[1] = term[2] = 0.f;
         return 0.f;
     }
-    const float ratio = expf(logp - row.old);
+    const float ratio = expf((float)(logp - row.old));
     const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
     const float gain = adv == 0 ? 0.f : (up ? a.high : down ? a.low : ratio) * adv;
     float slope = clipped || adv == 0 ? 0.f : -adv * ratio, div = 0.f;
     if (a.ref_logp) {
-        const float d = row.ref - logp, em = expm1f(d);
+        const float d = (float)(row.ref - logp), em = expm1f(d);
         div = divergence_of(d, em);
         if (a.kl != 0) slope = fmaf(-a.kl, em, slope);
     }
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
     const int64_t y = token_of(a, r);
     T* const to = out.p + r * out.rs;
     float term[3] = {0.f, 0.f, 0.f};
-    RowStats st = {0.f, 0.f, 0.f};
+    RowStats st = {0.f, 0.f, 0.};
     if (y >= 0) {
         const T* const row = x.p + r * x.rs;
         Raw8<T> v[REGS ? REGS : 1], last;
@@ -341,7 +349,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
         put_zeros<T, G, WHOLE>(to, mine, turn, ends, end);
     }
     if (t == 0) {
-        if (a.logp) a.logp[r] = st.logp;
+        if (a.logp) a.logp[r] = (float)st.logp;
         if (a.top) a.top[r] = st.top;
         if (a.log_sum) a.log_sum[r] = st.log_sum;
         if (a.dlogp) a.dlogp[r] = 0.f;
@@ -371,7 +379,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
     const int n = j < a.cols ? (int)min(8u, a.cols - j) : 0;
     const int64_t y = token_of(a, r);
     float f[8], term[3] = {0.f, 0.f, 0.f}, dlogp = 0.f, co_inv = 0.f;
-    RowStats st = {0.f, 0.f, 0.f};
+    RowStats st = {0.f, 0.f, 0.};
     if (MODE == ROWS_SLOPE) dlogp = y < 0 ? 0.f : dlogp_in[r];
     const bool bad = y >= (int64_t)a.cols, live = MODE == ROWS_SLOPE ? dlogp != 0 : y >= 0;
     if (live) {
@@ -413,7 +421,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
         }
     }
     if (MODE != ROWS_SLOPE && t == 0) {
-        if (a.logp) a.logp[r] = st.logp;
+        if (a.logp) a.logp[r] = (float)st.logp;
         if (a.top) a.top[r] = st.top;
         if (a.log_sum) a.log_sum[r] = st.log_sum;
         if (a.dlogp) a.dlogp[r] = 0.f;
@@ -502,7 +510,7 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
     __shared__ float s_max[4], s_sum[4];
     for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t y = token_of(a, r);
-        RowStats st = {0.f, 0.f, 0.f};
+        RowStats st = {0.f, 0.f, 0.};
         float term[3] = {0.f, 0.f, 0.f}, dlogp = 0.f;
         if (y >= 0) {
             const float xy = l8_f32(x.p[r * x.rs + (y < (int64_t)a.cols ? y : 0)]);
@@ -519,7 +527,7 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
             if (MODE == ROWS_POLICY) dlogp = policy_row(a, given, st.logp, term);
         }
         if (threadIdx.x == 0) {
-            if (a.logp) a.logp[r] = st.logp;
+            if (a.logp) a.logp[r] = (float)st.logp;
             if (a.top) a.top[r] = st.top;
             if (a.log_sum) a.log_sum[r] = st.log_sum;
             if (a.dlogp) a.dlogp[r] = dlogp;
@@ -835,6 +843,7 @@ LossArgs loss_args(const zkdl_mat* x, const void* tokens, int tokens_dtype, floa
     a.rows = x->rows;
     a.cols = (uint32_t)x->cols;
     a.inv_tau = 1.f / tau;
+    a.inv_tau64 = 1 / (double)tau;
     a.k = (float)(1.4426950408889634 / tau);
     a.tokens = {tokens, tokens_dtype == ZKDL_I64};
     return a;

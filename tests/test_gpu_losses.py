@@ -173,6 +173,18 @@ def test_a_mask_of_the_lowest_value_below_temperature_1(lib, ctx, shape, dtype):
     row.check_slope(back, ones.double(), none, t)
 
 
+@pytest.mark.parametrize("n", range(18))
+def test_rows_of_equals_are_rounded_once(lib, ctx, n):
+    """Terms are 1 and their sums exact: log_sum and logp are n log 2 rounded to 32 bits, whatever the temperature."""
+    want = torch.tensor(n * math.log(2), dtype=torch.float64).float().cuda()
+    for T in (3, 70):
+        for t in TYPES.values():
+            x, y = torch.full((T, 2 ** n), 1.5, dtype=t).cuda(), torch.arange(T).cuda() % 2 ** n
+            for tau in (1.0, 0.7):
+                got = lib.token_logprobs(ctx, x, y, temperature=tau)
+                assert torch.all(got["log_sum"] == want) and torch.all(got["logp"] == -want)
+
+
 def policy64(row, old, adv, ref, w, lo, hi, kl):
     """Loss, divergence, clipped, dlogp and by how much they may differ."""
     E = row.logp_err
