@@ -43,7 +43,7 @@ struct LossArgs {
     float* dlogp;                // preference: zeros, for the pairs to fill in
     // policy
     const float *old_logp, *advantage, *ref_logp, *weight;
-    float every, low, high, kl;  // the weight where there are none; 1 - clip_low, 1 + clip_high
+    double every, low, high, kl; // the weight where there are none; 1 - clip_low, 1 + clip_high
     float* terms;                // [3][rows]: weighted loss, divergence, clipped
     int past;                    // the gradient goes past the caches (where a kernel has that)
 };
@@ -81,41 +81,48 @@ __device__ __forceinline__ RowStats row_stats(const LossArgs& a, float c, float 
     return s;
 }
 
-// exp(d) - 1 - d without what cancels: the series where d is small
-__device__ __forceinline__ float divergence_of(float d, float em) {
-    const float p = fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), .5f);
-    return fabsf(d) < .25f ? d * d * p : em - d;
+// em = exp(d) - 1 and exp(d) - 1 - d: where d is small by the series, which is off by d^3 / 60 < 2^-35 of it; the difference in 64 bits by 2^-52 of 1,
+// 2^-31 of it at most.
+__device__ __forceinline__ double divergence_of(double d, double& em) {
+    const double small = d * d * fma(d, fma(d, 1. / 24, 1. / 6), .5);
+    const bool near = fabs(d) < 0x1p-10;
+    em = near ? small + d : exp(d) - 1;
+    return near ? small : em < INF ? em - d : em;       // (d may be infinite: a token that cannot be)
 }
 
 // What the policy loss has of a row beside its logits, asked for before they are looked at.
 struct PolicyRow {
-    float w, adv, old, ref;
+    double w;
+    float adv, old, ref;
 };
 template <int MODE>
 __device__ __forceinline__ PolicyRow policy_of(const LossArgs& a, uint64_t r) {
-    if constexpr (MODE != ROWS_POLICY) return {0.f, 0.f, 0.f, 0.f};
-    return {a.weight ? a.weight[r] : a.every, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
+    if constexpr (MODE != ROWS_POLICY) return {0., 0.f, 0.f, 0.f};
+    return {a.weight ? (double)a.weight[r] : a.every, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
 }
-// One row's share of the policy loss; returns dlogp.
+// One row's share of the policy loss; returns dlogp.  In 64 bits up to the three terms and dlogp, which are rounded once, with the weight in them: a
+// ratio or a divergence beyond 2^128 may have a weight that brings it back, and the terms' sum may be much smaller than they are (the
+// loss of 4096 x 131072 16-bit entries, terms of 0.6 and a sum of 0.01: off by 1.2e-9, with shares in 32 bits by 1.4e-9).  Short rows pay for it: 2^20
+// rows of 32 with a reference 102 us, in 32 bits 89; rows of 16384 51 and 50.
 __device__ __forceinline__ float policy_row(const LossArgs& a, const PolicyRow& row, double logp, float (&term)[3]) {
-    const float w = row.w, adv = row.adv;
+    const double w = row.w, adv = row.adv;
     if (w == 0) {           // whatever the rest is
         term[0] = term[1] = term[2] = 0.f;
         return 0.f;
     }
-    const float ratio = expf((float)(logp - row.old));
+    const double ratio = exp(logp - (double)row.old);
     const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
-    const float gain = adv == 0 ? 0.f : (up ? a.high : down ? a.low : ratio) * adv;
-    float slope = clipped || adv == 0 ? 0.f : -adv * ratio, div = 0.f;
+    const double gain = adv == 0 ? 0. : (up ? a.high : down ? a.low : ratio) * adv;
+    double slope = clipped || adv == 0 ? 0. : -adv * ratio, div = 0.;
     if (a.ref_logp) {
-        const float d = (float)(row.ref - logp), em = expm1f(d);
-        div = divergence_of(d, em);
-        if (a.kl != 0) slope = fmaf(-a.kl, em, slope);
+        double em;
+        div = divergence_of((double)row.ref - logp, em);
+        if (a.kl != 0) slope = fma(-a.kl, em, slope);
     }
-    term[0] = w * (a.kl != 0 ? fmaf(a.kl, div, -gain) : -gain);     // (a divergence beyond 32 bits that nobody asked for stays out)
-    term[1] = w * div;
-    term[2] = clipped ? w : 0.f;
-    return w * slope;
+    term[0] = (float)(w * (a.kl != 0 ? fma(a.kl, div, -gain) : -gain));     // (a divergence without end that nobody asked for stays out)
+    term[1] = (float)(w * div);
+    term[2] = clipped ? (float)w : 0.f;
+    return (float)(w * slope);
 }
 __device__ __forceinline__ void put_terms(const LossArgs& a, uint64_t r, const float (&term)[3]) {
 #pragma unroll
@@ -361,7 +368,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
 // ---------------------------------------------------------------------------
 // Rows of up to 8 G entries for G = 8, 16 or 32 lanes: as many rows in a wave as fit, a vector of eight (or what there is) a lane.
 // ROWS_SLOPE: the gradient from dlogp, top and log_sum alone.  2^20 rows of 128 32-bit entries: log-probabilities 112 us (4.8 TB/s), gradient
-// 191 us (5.6 TB/s), policy 219 us.
+// 191 us (5.6 TB/s), policy 225 us.
 // ---------------------------------------------------------------------------
 template <int G, bool MAX>
 __device__ __forceinline__ float lanes_reduce(float x) {
@@ -986,9 +993,9 @@ extern "C" int zkdl_policy_loss(zkdl_ctx* ctx, const zkdl_mat* logits, const voi
     a.advantage = terms->advantage;
     a.ref_logp = terms->ref_logp;
     a.weight = terms->weight;
-    a.every = 1.f / (float)logits->rows;
-    a.low = 1.f - terms->clip_low;
-    a.high = 1.f + terms->clip_high;
+    a.every = 1 / (double)logits->rows;
+    a.low = 1 - (double)terms->clip_low;
+    a.high = 1 + (double)terms->clip_high;
     a.kl = terms->kl;
     const int rc = logits->rows == 0 ? launch_sum(ctx, nullptr, 0, 3, sums)
                                      : by_type(logits->dtype, [&](auto t) { return policy<decltype(t)>(ctx, a, logits, sums, dlogits); });
