@@ -35,6 +35,8 @@ struct LossArgs {
     uint64_t rows;
     uint32_t cols;
     float inv_tau, k;            // 1 / temperature; log2(e) / temperature
+    float times, step;           // top is the largest logit times `times`, and p_j = exp2((x_j times - top) step - log_sum log2(e)):
+                                 // 1 / temperature and log2(e) where the caller has top, 1 and log2(e) / temperature where it stays here
     double inv_tau64;
     Ints tokens;
     Ints offsets;                // preference: rows outside [offsets[0], offsets[last]) count for nothing
@@ -61,6 +63,14 @@ __device__ __forceinline__ int64_t token_of(const LossArgs& a, uint64_t r) {
 // Terms are exp2((x - c) k): the difference first, so that rows of the type's lowest value (masks) and of its largest stay in the range.
 __device__ __forceinline__ float term_of(float x, float c, float k) { return exp2_raw((x - c) * k); }
 
+// x times - top, the product rounded by itself as top was: of the row's largest nothing is left.  (With what a fused product has beyond 32 bits all p_j
+// of a row would be off by a factor, up to exp(2^-24 |top|).)
+__device__ __forceinline__ float below_top(float x, float times, float top) {
+#pragma clang fp contract(off)
+    const float u = x * times;
+    return u - top;
+}
+
 // log_sum and logp in 64 bits: in 32 their last places are a millionth at 10, which a loss has in every ratio and, of sums that cancel, in its first
 // places (policy, 2000 x 4001 16-bit entries, a loss of 0.03: off by 2.9e-9, from log-probabilities in 32 bits by 7.8e-9).  The logarithm is the
 // exponent and that of a number next to 1, which 32 bits hold to 2^-25.
@@ -74,7 +84,7 @@ __device__ __forceinline__ RowStats row_stats(const LossArgs& a, float c, float 
     const double log_sum = ((double)(__builtin_amdgcn_frexp_expf(sum) - low) + (double)__builtin_amdgcn_logf(low ? 2 * m : m)) * 0.69314718055994530942;
     RowStats s;
     s.log_sum = (float)log_sum;
-    s.top = c * a.inv_tau;
+    s.top = c * a.times;
     s.logp = ((double)xy - (double)c) * a.inv_tau64 - log_sum;
     if (!(sum < INF)) s.top = s.log_sum = NAN32;          // a NaN, +infinity, or nothing but -infinity
     if (!(sum < INF) || y >= (int64_t)a.cols) s.logp = NAN32;
@@ -395,7 +405,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
         l8_load(row + (n ? j : 0), n, f);
         if (MODE == ROWS_SLOPE) {
             const float norm = log_sum[r] * LOG2E;
-            float c = top[r], times = a.inv_tau, k = LOG2E;
+            float c = top[r], times = a.times, k = a.step;
             if (fabsf(c) == INF) {          // as in slope_far
                 c = -INF;
 #pragma unroll
@@ -405,7 +415,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
                 k = a.k;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = exp2_raw(fmaf(fmaf(f[i], times, -c), k, -norm));
+            for (int i = 0; i < 8; ++i) f[i] = exp2_raw(fmaf(below_top(f[i], times, c), k, -norm));
             if (bad) dlogp = NAN32;
             co_inv = dlogp * a.inv_tau;
         } else {
@@ -586,7 +596,7 @@ __global__ __launch_bounds__(1024) void k_loss_sum(const IN* in, uint64_t n, uin
 // last-level cache).
 // ---------------------------------------------------------------------------
 struct SlopeRow {
-    float co, inv_tau, top, norm;       // p_j = exp2((x_j inv_tau - top) log2(e) - norm)
+    float co, times, step, top, norm;   // p_j = exp2((x_j times - top) step - norm)
     int64_t y;
     bool none, bad;                     // zeros, NaN
 };
@@ -616,7 +626,7 @@ __device__ __forceinline__ void slope_of(const SlopeRow& s, const T* row, T* to,
         const uint64_t j = (uint64_t)at + (k * 64 + lane) * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            f[k][i] = s.none ? 0.f : exp2_raw(fmaf(fmaf(f[k][i], s.inv_tau, -s.top), LOG2E, -s.norm)) * (s.bad ? NAN32 : -s.co);
+            f[k][i] = s.none ? 0.f : exp2_raw(fmaf(below_top(f[k][i], s.times, s.top), s.step, -s.norm)) * (s.bad ? NAN32 : -s.co);
         if ((uint64_t)s.y - j < 8 && !s.bad && !s.none) {       // the token's own entry
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[k][i] += (uint64_t)s.y - j == i ? s.co : 0.f;
@@ -663,7 +673,8 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
         s.co = d * a.inv_tau;
         s.none = s.y < 0 || d == 0;
         s.bad = s.y >= (int64_t)a.cols;
-        s.inv_tau = a.inv_tau;
+        s.times = a.times;
+        s.step = a.step;
         s.top = top[r];
         s.norm = log_sum[r] * LOG2E;
         if (!s.none && fabsf(s.top) == INF) {
@@ -853,6 +864,8 @@ LossArgs loss_args(const zkdl_mat* x, const void* tokens, int tokens_dtype, floa
     a.inv_tau = 1.f / tau;
     a.inv_tau64 = 1 / (double)tau;
     a.k = (float)(1.4426950408889634 / tau);
+    a.times = a.inv_tau;
+    a.step = LOG2E;
     a.tokens = {tokens, tokens_dtype == ZKDL_I64};
     return a;
 }
@@ -891,6 +904,8 @@ int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const
             a.dlogp = s.p + 3 * a.rows;
             a.top = s.p + 4 * a.rows;
             a.log_sum = s.p + 5 * a.rows;
+            a.times = 1;
+            a.step = a.k;
         }
         const int rc = launch_parts<T, ROWS_POLICY>(ctx, a, l8_mat<const T>(logits));
         if (rc != ZKDL_OK) return rc;
@@ -907,6 +922,8 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
     a.dlogp = s.p + a.rows;
     a.top = s.p + 2 * a.rows;
     a.log_sum = s.p + 3 * a.rows;
+    a.times = 1;
+    a.step = a.k;
     a.offsets = {p->offsets, p->offsets_dtype == ZKDL_I64};
     a.last = 2 * p->pairs;
     float* losses = s.p + 4 * a.rows;

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_losses import Row64, TYPES, U, gen, inputs, policy64
+from test_gpu_losses import Row64, TYPES, U, gen, inputs, policy64, preference64
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,68 @@ def test_a_divergence_without_end(lib, ctx, shape):
     got = lib.policy_loss(ctx, x, y, f, f, ref_logp=f)
     alone = lib.policy_loss(ctx, x, y, f, f)
     assert got["divergence"].item() == math.inf and torch.equal(got["loss"], alone["loss"]) and torch.isfinite(got["loss"])
+
+
+LARGE = {"f32": (-1e4, -65504.0, -1e9, torch.finfo(torch.float32).min, 3e37), "f16": (-1e4, -65504.0, 6e4), "bf16": (-1e4, -1e9, torch.finfo(torch.bfloat16).min, 3e37)}
+
+
+@pytest.mark.parametrize("shape", PATHS, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_of_equals_of_any_size_away_from_temperature_1(lib, ctx, shape, dtype):
+    """Every row holds one value, far from zero: p is 1 / V whatever the value is.  The sum is exact; log_sum and its product with log2(e) are rounded, 3 U log V
+    in p with the exponential's ulp, a ratio has the rounding of logp, U log V, and the rest is products: 8 U."""
+    T, V = shape
+    t = TYPES[dtype]
+    value = torch.tensor(LARGE[dtype]).repeat(T)[:T]
+    x, y = value[:, None].expand(T, V).to(t).cuda(), torch.arange(T).cuda() % V
+    g = gen(V)
+    dlogp, off = torch.randn(T, generator=g), [0, 1, 3, T // 2, T] if T > 6 else [0, 2, T]
+    hot = torch.nn.functional.one_hot(y, V).double()
+    for tau in (0.7, 1.3):
+        tau32 = torch.tensor(tau).item()
+        lp = lib.token_logprobs(ctx, x, y, temperature=tau)
+        assert torch.all((lp["logp"] + math.log(V)).abs() <= 2 * U * math.log(V))
+
+        def check(got, d):
+            c = d.double().cuda()[:, None] / tau32
+            want = c * (hot - 1 / V)
+            err = c.abs() * ((math.log(V) + 8) * U * hot + (4 * math.log(V) + 8) * U / V + 2.0 ** -126)
+            half = torch.finfo(t).eps / 2
+            assert torch.all((got.double() - want).abs() <= err + half * (want.abs() + err) + torch.finfo(t).smallest_normal * half)
+
+        check(lib.token_logprobs_backward(ctx, dlogp.cuda(), x, y, lp["top"], lp["log_sum"], temperature=tau), dlogp)
+        # ratios of 1, but for the rounding of logp: dlogp is -weight advantage
+        got = lib.policy_loss(ctx, x, y, lp["logp"], dlogp.cuda(), weight=torch.ones(T).cuda(), clip_low=1.0, clip_high=1e30, temperature=tau)
+        check(got["dlogits"], -dlogp)
+        # margins of whole multiples of log V
+        got = lib.preference_loss(ctx, x, y, torch.tensor(off).cuda(), beta=0.125, form="square", temperature=tau, ref_logp=torch.zeros(T).cuda())
+        d = torch.zeros(T, dtype=torch.float64)
+        for i in range(len(off) // 2):
+            a, b, c = off[2 * i:2 * i + 3]
+            m = -0.125 * math.log(V) * ((b - a) - (c - b))
+            d[a:b], d[b:c] = 2 * m * 0.125 / (len(off) // 2), -2 * m * 0.125 / (len(off) // 2)
+        check(got["dlogits"], d)
+
+
+@pytest.mark.parametrize("shape", PATHS, ids=str)
+def test_gradients_of_logits_far_from_zero(lib, ctx, shape):
+    """Logits around 4000 at a temperature of 0.7, where one step of 32 bits is 2^-12: what stays in the library has no rounding of that size.  A
+    thread adds at most 8 (32 + 1) terms of its own."""
+    T, V = shape
+    x, y = inputs(gen(T * V), T, V, "f32", ignore=False, scale=1.0)
+    x = x + 4000
+    row = Row64(x, y, torch.tensor(0.7).item())
+    row.sum_err = (2 * math.log(V) + 22 + 264 + 3 * math.log(V)) * U
+    row.log_sum_err = row.sum_err + 4 * U * row.log_sum.abs()
+    row.logp_err = 3 * U * (row.logp + row.log_sum).abs() + row.log_sum_err + 2 * U * row.logp.abs()
+    old, adv, w = row.logp.float().cpu() - 0.125, torch.randn(T, generator=gen(1)), torch.full((T,), 1 / T)
+    x, y = x.cuda(), y.cuda()
+    got = lib.policy_loss(ctx, x, y, old.cuda(), adv.cuda(), weight=w.cuda(), clip_low=0.2, clip_high=0.3, temperature=0.7)
+    _, _, dlogp, derr = policy64(row, old, adv, None, w, 0.2, 0.3, 0.0)
+    row.check_slope(got["dlogits"], dlogp, derr, torch.float32)
+    off = [0, 1, 3, T // 2, T] if T > 6 else [0, 2, T]
+    pairs = torch.full((len(off) // 2,), 0.5)
+    got = lib.preference_loss(ctx, x, y, torch.tensor(off).cuda(), weight=pairs.cuda(), beta=0.03125, temperature=0.7)
+    margins, merr, _, _, dlogp, derr, _ = preference64(row, off, None, pairs, 0.03125, 0.0, 0.0, "logistic", False)
+    assert torch.all((got["margin"].cpu().double() - margins).abs() <= merr)
+    row.check_slope(got["dlogits"], dlogp, derr, torch.float32)
