@@ -11,7 +11,8 @@ weights is the teacher.  By --loss the network learns
               entry's reward is its log-probability under the teacher's output; policy_loss, with the network of before as the reference;
   preference  the teacher's preferences: rows 2 i and 2 i + 1 ask the same, each answered by an entry drawn from the network of before, and
               the answer that the teacher finds likelier is preferred; preference_loss, with the network of before as the reference.
-adamw updates all tensors with one call, its states in 32 or 8 bits; --limit scales gradients whose norm is above it.  After the last step
+adamw updates all tensors with one call, its states in 32 or 8 bits; --limit scales gradients whose norm is above it, and leaves a step out whose
+norm is not finite.  After the last step
   - the forward pass runs once more for single rows, as a serving program would, and has to give the batch's rows bit for bit;
   - sumcheck_matmul proves the products of all layers on the stacks of 8-bit activations and weights, and its claim on their result is
     compared with the multilinear extension of the int32 accumulators that matmul_i8 returns.  (The integers of the gradients stay inside
@@ -94,12 +95,15 @@ def preference(torch, zk, ctx, teacher, before):
     return of
 
 
-def sgd(zk, ctx, net, lr, limit):
+def sgd(torch, zk, ctx, net, lr, limit):
     def update(dw, dgain):
-        factor = zk.gradient_norm(ctx, dw + dgain, limit)["factor"] if limit else None
+        if limit:       # a norm that is not finite leaves the step out: its factor would turn every weight to NaN
+            factor = zk.gradient_norm(ctx, dw + dgain, limit)["factor"]
+            whole, none = torch.isfinite(factor), torch.zeros((), device="cuda")
+            dw, dgain = ([torch.where(whole, d * factor, none) for d in l] for l in (dw, dgain))
         for l in range(len(dw)):
-            net["w"][l].sub_(dw[l] if factor is None else dw[l] * factor, alpha=lr)
-            net["gain"][l].sub_(dgain[l] if factor is None else dgain[l] * factor, alpha=lr)
+            net["w"][l].sub_(dw[l], alpha=lr)
+            net["gain"][l].sub_(dgain[l], alpha=lr)
     return update
 
 
@@ -191,7 +195,7 @@ def run(layers=8, width=1024, batch=64, steps=5, lr=None, say=print, loss="squar
         objective = squares(zk, ctx, target)
     else:
         objective = (policy if loss == "policy" else preference)(torch, zk, ctx, target, forward(zk, ctx, x, net)[0])
-    update = sgd(zk, ctx, net, lr, limit) if optimizer == "sgd" else adamw(zk, ctx, net, lr, limit, state_bits)
+    update = sgd(torch, zk, ctx, net, lr, limit) if optimizer == "sgd" else adamw(zk, ctx, net, lr, limit, state_bits)
     losses, kept, used = [], None, None
     for k in range(steps):
         torch.cuda.synchronize()
