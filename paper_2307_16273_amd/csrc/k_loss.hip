@@ -42,6 +42,7 @@ struct LossArgs {
     Ints offsets;                // preference: rows outside [offsets[0], offsets[last]) count for nothing
     uint64_t last;
     float *logp, *top, *log_sum; // may be null
+    double* logp64;              // preference: for the pairs' sums
     float* dlogp;                // preference: zeros, for the pairs to fill in
     // policy
     const float *old_logp, *advantage, *ref_logp, *weight;
@@ -368,6 +369,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
     }
     if (t == 0) {
         if (a.logp) a.logp[r] = (float)st.logp;
+        if (a.logp64) a.logp64[r] = st.logp;
         if (a.top) a.top[r] = st.top;
         if (a.log_sum) a.log_sum[r] = st.log_sum;
         if (a.dlogp) a.dlogp[r] = 0.f;
@@ -440,6 +442,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
     }
     if (MODE != ROWS_SLOPE && t == 0) {
         if (a.logp) a.logp[r] = (float)st.logp;
+        if (a.logp64) a.logp64[r] = st.logp;
         if (a.top) a.top[r] = st.top;
         if (a.log_sum) a.log_sum[r] = st.log_sum;
         if (a.dlogp) a.dlogp[r] = 0.f;
@@ -546,6 +549,7 @@ __global__ __launch_bounds__(256) void k_loss_join(LossArgs a, L8Mat<const T> x,
         }
         if (threadIdx.x == 0) {
             if (a.logp) a.logp[r] = (float)st.logp;
+            if (a.logp64) a.logp64[r] = st.logp;
             if (a.top) a.top[r] = st.top;
             if (a.log_sum) a.log_sum[r] = st.log_sum;
             if (a.dlogp) a.dlogp[r] = dlogp;
@@ -697,7 +701,8 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
 struct PairArgs {
     uint64_t rows, pairs;
     Ints tokens, offsets;
-    const float *logp, *ref_logp, *weight;
+    const double* logp;
+    const float *ref_logp, *weight;
     int form, average;
     float every, beta, target, smoothing;
     float *margin, *losses, *dlogp;
@@ -717,8 +722,9 @@ __global__ __launch_bounds__(N) void k_loss_pair(PairArgs a) {
 #pragma unroll 4
         for (uint64_t r = at[0] + threadIdx.x; r < at[2]; r += N) {
             const int64_t y = a.tokens.at(r);
-            const float p = a.logp[r], q = a.ref_logp ? a.ref_logp[r] : 0.f;        // (no load waits for the token)
-            const double d = y >= 0 ? (double)p - (double)q : 0., one = y >= 0 ? 1. : 0.;
+            const double p = a.logp[r];        // (no load waits for the token)
+            const float q = a.ref_logp ? a.ref_logp[r] : 0.f;
+            const double d = y >= 0 ? p - (double)q : 0., one = y >= 0 ? 1. : 0.;
             const bool second = r >= at[1];
             x[0] += second ? 0. : d;
             x[1] += second ? d : 0.;
@@ -916,17 +922,18 @@ int policy(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, float* sums, const
 
 template <class T>
 int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_preference* p, float* loss, float* margin, float* logp, const zkdl_mat* dlogits) {
-    Scratch s(ctx, (a.rows ? a.rows : 1) * 4 + p->pairs);
+    Scratch s(ctx, (a.rows ? a.rows : 1) * 5 + p->pairs);
     if (!s.p) return ZKDL_ENOMEM;
-    a.logp = logp ? logp : s.p;
-    a.dlogp = s.p + a.rows;
-    a.top = s.p + 2 * a.rows;
-    a.log_sum = s.p + 3 * a.rows;
+    a.logp = logp;
+    a.logp64 = (double*)s.p;
+    a.dlogp = s.p + 2 * a.rows;
+    a.top = s.p + 3 * a.rows;
+    a.log_sum = s.p + 4 * a.rows;
     a.times = 1;
     a.step = a.k;
     a.offsets = {p->offsets, p->offsets_dtype == ZKDL_I64};
     a.last = 2 * p->pairs;
-    float* losses = s.p + 4 * a.rows;
+    float* losses = s.p + 5 * a.rows;
     if (a.rows) {
         if (rows_fit<T>(a, false)) {
             launch_rows<T, ROWS_LOGP>(ctx, a, l8_mat<const T>(logits), L8Mat<T>{nullptr, 0, 0});
@@ -935,7 +942,7 @@ int preference(zkdl_ctx* ctx, LossArgs a, const zkdl_mat* logits, const zkdl_pre
             if (rc != ZKDL_OK) return rc;
         }
     }
-    PairArgs q = {a.rows, p->pairs, a.tokens, a.offsets, a.logp, p->ref_logp, p->weight, p->form, p->average, 1.f / (float)p->pairs, p->beta, p->target,
+    PairArgs q = {a.rows, p->pairs, a.tokens, a.offsets, a.logp64, p->ref_logp, p->weight, p->form, p->average, 1.f / (float)p->pairs, p->beta, p->target,
                   p->smoothing, margin, losses, dlogits ? a.dlogp : nullptr};
     if (p->pairs) {
         // threads by the rows of a pair (8192 of them 37 us with 256 threads)

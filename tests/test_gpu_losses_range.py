@@ -136,3 +136,23 @@ def test_gradients_of_logits_far_from_zero(lib, ctx, shape):
     margins, merr, _, _, dlogp, derr, _ = preference64(row, off, None, pairs, 0.03125, 0.0, 0.0, "logistic", False)
     assert torch.all((got["margin"].cpu().double() - margins).abs() <= merr)
     row.check_slope(got["dlogits"], dlogp, derr, torch.float32)
+
+
+@pytest.mark.parametrize("T,n", [(64, 5), (70, 10), (70, 13), (5, 17)])
+def test_a_margin_is_rounded_once(lib, ctx, T, n):
+    """Rows of 2^n equals, whose logp is -n log 2 in 64 bits, against a reference of the same rounded to 32: what is left of a sequence is that rounding times its
+    rows.  The margin is one rounding off, and 2^-50 of what cancels."""
+    ref = torch.tensor(-n * math.log(2), dtype=torch.float32)
+    delta = -n * math.log(2) - ref.double().item()
+    assert abs(delta) > 1e-9
+    x, y = torch.ones(T, 2 ** n, device="cuda"), torch.arange(T, device="cuda") % 2 ** n
+    y[-1] = -1
+    first = T - 2
+    off = torch.tensor([0, first, T], device="cuda")        # one row that counts in the second sequence
+    for average in (False, True):
+        got = lib.preference_loss(ctx, x, y, off, ref_logp=ref.cuda().expand(T).contiguous(), beta=2.0 ** 20, form="square", average=average)
+        want = 2.0 ** 20 * (delta * (1 if average else first) - delta)
+        noise = 2.0 ** 20 * T * n * 2.0 ** -50
+        assert abs(got["margin"].item() - want) <= 1.01 * U * abs(want) + noise
+        assert abs(got["loss"].item() - want ** 2) <= 1.01 * 2 * U * want ** 2 + (2 * abs(want) + noise) * noise
+        assert torch.all(got["logp"][:-1] == ref.item()) and got["logp"][-1] == 0
