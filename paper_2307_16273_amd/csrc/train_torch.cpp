@@ -268,10 +268,17 @@ PyObject* adamw_step(const Call& c, PyObject* const* a) {
                 (k ? t[i].v_value : t[i].m_value) = floats(outs.back());
             }
     }
-    // what autograd keeps of these tensors will not be theirs any more (tensors of inference mode outside of it are refused here, before anything is written)
-    for (Py_ssize_t i = 0; i < n; ++i)
-        for (const List* l : {&params, &ms, &vs}) l->at(c, i).unsafeGetTensorImpl()->bump_version();
+    const auto written = [&](auto of) {
+        for (Py_ssize_t i = 0; i < n; ++i)
+            for (const List* l : {&params, &ms, &vs, &m_scales, &v_scales})
+                if (eight || (l != &m_scales && l != &v_scales)) of(l->at(c, i));
+    };
+    written([](const at::Tensor& x) {
+        TORCH_CHECK(!x.is_inference() || c10::InferenceMode::is_enabled(), "adamw_step: tensors of inference mode cannot be updated outside of it");
+    });
     const int rc = f_adamw(c.ctx, t.data(), t.size(), &how);
+    // what autograd keeps of these tensors is not theirs any more, unless the call was refused
+    if (rc != ZKDL_EINVAL && rc != ZKDL_ETOOBIG) written([](const at::Tensor& x) { x.unsafeGetTensorImpl()->bump_version(); });
     if (rc) return PyLong_FromLong(rc);
     PyObject* d = PyDict_New();
     for (int k = 0; k < 2; ++k) {

@@ -409,6 +409,25 @@ def test_autograd_is_told_of_the_update(lib, ctx):
         y.backward()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_refused_update_leaves_autograd_alone(lib, ctx, bits):
+    """Tensors that overlap, a rate that is no number: nothing is written, and what autograd keeps of the tensors is still theirs."""
+    w = torch.randn(4, 4, device="cuda", requires_grad=True)
+    x = torch.randn(4, 4, device="cuda", requires_grad=True)
+    y = (w * x).sum()
+    d, state = torch.ones(4, 4, device="cuda"), lib.adamw_state([w], bits)
+    tensors = [w, *state["m"], *state["v"], *state["m_scale"], *state["v_scale"]]
+    versions = [t._version for t in tensors]
+    for grads, kw in (([w], {}), ([d], dict(lr=math.nan)), ([d], dict(beta1=1.0)), ([d], dict(eps=0.0)), ([d], dict(step=0))):
+        with pytest.raises(lib.ZkdlError):
+            lib.adamw_step(ctx, [w], grads, state, **{**dict(step=1, lr=0.1), **kw})
+    assert [t._version for t in tensors] == versions
+    y.backward()
+    assert torch.equal(x.grad, w.detach())
+    lib.adamw_step(ctx, [w], [d], state, 1, 0.1)
+    assert all(t._version > v for t, v in zip(tensors, versions))
+
+
 def test_tensors_of_inference_mode(lib, ctx):
     """Updated inside of it; refused outside, with nothing written."""
     with torch.inference_mode():
