@@ -887,6 +887,7 @@ def adamw_state(params, bits=32):
     import torch
     if bits not in (32, 8):
         raise ValueError(f"bits: 32 or 8, not {bits}")
+    params = _listed(params)
     kind = torch.float32 if bits == 32 else torch.uint8
     new = lambda: [torch.zeros(p.shape, dtype=kind, device=p.device) for p in params]
     scales = lambda: [torch.zeros(-(-p.numel() // 256), dtype=torch.uint8, device=p.device) for p in params] if bits == 8 else []

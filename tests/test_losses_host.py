@@ -37,3 +37,14 @@ def test_forms_and_bits_by_name():
     assert [x.shape for x in s["m"]] == [(300, 2), (0,)] and [x.shape for x in s["v_scale"]] == [(3,), (0,)] and s["m"][0].dtype == torch.uint8
     s = zk.adamw_state([torch.zeros(5, dtype=torch.bfloat16)])
     assert s["m"][0].dtype == torch.float32 and s["m_scale"] == []
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_from_a_generator(bits):
+    """A network's parameters come one by one: every list has a tensor for each."""
+    torch = pytest.importorskip("torch")
+    params = [torch.zeros(300, 2), torch.zeros(5)]
+    got, want = zk.adamw_state((p for p in params), bits), zk.adamw_state(params, bits)
+    assert len(got["m"]) == 2
+    for k in ("m", "v", "m_scale", "v_scale"):
+        assert [(t.shape, t.dtype) for t in got[k]] == [(t.shape, t.dtype) for t in want[k]]
