@@ -156,3 +156,21 @@ def test_a_margin_is_rounded_once(lib, ctx, T, n):
         assert abs(got["margin"].item() - want) <= 1.01 * U * abs(want) + noise
         assert abs(got["loss"].item() - want ** 2) <= 1.01 * 2 * U * want ** 2 + (2 * abs(want) + noise) * noise
         assert torch.all(got["logp"][:-1] == ref.item()) and got["logp"][-1] == 0
+
+
+@pytest.mark.parametrize("shape", PATHS + [(1030, 3500), (192, 131072)], ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_log_probabilities_of_logits_far_from_zero(lib, ctx, shape, dtype):
+    """logp is the token's distance from the row's largest entry less log_sum, with no rounding of either's size.  A thread adds at most 8 (32 + 1) terms;
+    1 / temperature is rounded where it is in 32 bits, and logp once."""
+    T, V = shape
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (3000 + torch.randn((T, V), generator=g, device="cuda") * (64 if dtype == "bf16" else 4)).to(TYPES[dtype])
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    for tau in (0.7, 1.3):
+        row = Row64(x, y, torch.tensor(tau).item())
+        row.sum_err = (2 * math.log(V) + 22 + 264) * U
+        row.log_sum_err = row.sum_err + U * row.log_sum.abs()
+        row.logp_err = row.sum_err + U * row.logp.abs()
+        for got in (lib.token_logprobs(ctx, x, y, temperature=tau), lib.policy_loss(ctx, x, y, row.logp.float(), row.logp.float(), temperature=tau)):
+            row.check({k: got[k] for k in ("logp", "log_sum") if k in got})
