@@ -92,42 +92,59 @@ __device__ __forceinline__ RowStats row_stats(const LossArgs& a, float c, float 
     return s;
 }
 
-// em = exp(d) - 1 and exp(d) - 1 - d: where d is small by the series, which is off by d^3 / 60 < 2^-35 of it; the difference in 64 bits by 2^-52 of 1,
+// em = exp(d) - 1, of grown = exp(d), and exp(d) - 1 - d: where d is small by the series, which is off by d^3 / 60 < 2^-35 of it; the difference in 64 bits by 2^-52 of 1,
 // 2^-31 of it at most.
-__device__ __forceinline__ double divergence_of(double d, double& em) {
+__device__ __forceinline__ double divergence_of(double d, double grown, double& em) {
     const double small = d * d * fma(d, fma(d, 1. / 24, 1. / 6), .5);
     const bool near = fabs(d) < 0x1p-10;
-    em = near ? small + d : exp(d) - 1;
+    em = near ? small + d : grown - 1;
     return near ? small : em < INF ? em - d : em;       // (d may be infinite: a token that cannot be)
+}
+
+// A number that the lane next door has, of each pair of lanes.
+__device__ __forceinline__ double next_door(double x) {
+    const auto swap = [](int w) { return __builtin_amdgcn_mov_dpp(w, 0xB1, 0xF, 0xF, true); };
+    return __hiloint2double(swap(__double2hiint(x)), swap(__double2loint(x)));
 }
 
 // What the policy loss has of a row beside its logits, asked for before they are looked at.
 struct PolicyRow {
-    double w;
-    float adv, old, ref;
+    float w, adv, old, ref;
 };
 template <int MODE>
 __device__ __forceinline__ PolicyRow policy_of(const LossArgs& a, uint64_t r) {
-    if constexpr (MODE != ROWS_POLICY) return {0., 0.f, 0.f, 0.f};
-    return {a.weight ? (double)a.weight[r] : a.every, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
+    if constexpr (MODE != ROWS_POLICY) return {0.f, 0.f, 0.f, 0.f};
+    return {a.weight ? a.weight[r] : 1.f, a.advantage[r], a.old_logp[r], a.ref_logp ? a.ref_logp[r] : 0.f};
 }
 // One row's share of the policy loss; returns dlogp.  In 64 bits up to the three terms and dlogp, which are rounded once, with the weight in them: a
 // ratio or a divergence beyond 2^128 may have a weight that brings it back, and the terms' sum may be much smaller than they are (the
-// loss of 4096 x 131072 16-bit entries, terms of 0.6 and a sum of 0.01: off by 1.2e-9, with shares in 32 bits by 1.4e-9).  Short rows pay for it: 2^20
-// rows of 32 with a reference 102 us, in 32 bits 89; rows of 16384 51 and 50.
+// loss of 4096 x 131072 16-bit entries, terms of 0.6 and a sum of 0.01: off by 1.2e-9, with shares in 32 bits by 1.4e-9).  What is loaded is widened
+// here and not where it is asked for, which would wait for it (4096 x 1024 32-bit entries 12.0 us, 12.6 that way).  PAIRS: of two lanes, which have the same
+// row, one takes the ratio's exponential and the other the divergence's, where the vector operations show (2^20 rows of 32 with a reference
+// 97 us; both in every lane 101, in 32 bits 89).
+template <bool PAIRS = false>
 __device__ __forceinline__ float policy_row(const LossArgs& a, const PolicyRow& row, double logp, float (&term)[3]) {
-    const double w = row.w, adv = row.adv;
-    if (w == 0) {           // whatever the rest is
+    const double w = a.weight ? (double)row.w : a.every, adv = row.adv;
+    if (row.w == 0) {           // whatever the rest is
         term[0] = term[1] = term[2] = 0.f;
         return 0.f;
     }
-    const double ratio = exp(logp - (double)row.old);
+    double ratio, grown = 0.;
+    if constexpr (PAIRS) {
+        const bool odd = threadIdx.x & 1;
+        const double mine = exp(odd ? (double)row.ref - logp : logp - (double)row.old), other = next_door(mine);
+        ratio = odd ? other : mine;
+        grown = odd ? mine : other;
+    } else {
+        ratio = exp(logp - (double)row.old);
+        if (a.ref_logp) grown = exp((double)row.ref - logp);
+    }
     const bool up = adv > 0 && ratio > a.high, down = adv < 0 && ratio < a.low, clipped = up || down;
     const double gain = adv == 0 ? 0. : (up ? a.high : down ? a.low : ratio) * adv;
     double slope = clipped || adv == 0 ? 0. : -adv * ratio, div = 0.;
     if (a.ref_logp) {
         double em;
-        div = divergence_of((double)row.ref - logp, em);
+        div = divergence_of((double)row.ref - logp, grown, em);
         if (a.kl != 0) slope = fma(-a.kl, em, slope);
     }
     term[0] = (float)(w * (a.kl != 0 ? fma(a.kl, div, -gain) : -gain));     // (a divergence without end that nobody asked for stays out)
@@ -435,7 +452,7 @@ __global__ __launch_bounds__(256) void k_loss_small(LossArgs a, const float* dlo
             sum = lanes_reduce<G, false>(sum);
             st = row_stats(a, c, sum, y, xy);
             if (MODE == ROWS_POLICY) {
-                dlogp = policy_row(a, given, st.logp, term);
+                dlogp = policy_row<true>(a, given, st.logp, term);
                 co_inv = dlogp * a.inv_tau / sum;
             }
         }
