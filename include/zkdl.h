@@ -642,7 +642,8 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
 /* zkdl_token_logprobs: logp, and top and log_sum for the backward pass (both may be NULL). */
 int zkdl_token_logprobs(zkdl_ctx* ctx, const zkdl_mat* logits, const void* tokens, int tokens_dtype, float temperature, float* logp,
                         float* top, float* log_sum);
-/* zkdl_token_logprobs_backward: dlogits from dlogp, with top and log_sum as returned. */
+/* zkdl_token_logprobs_backward: dlogits from dlogp, with top and log_sum as zkdl_token_logprobs returns them at the same temperature: top is the
+ * largest logit times 1 / temperature, both rounded to 32 bits, and so is every product it is taken from, so that the largest entry's exponent is 0. */
 int zkdl_token_logprobs_backward(zkdl_ctx* ctx, const float* dlogp, const zkdl_mat* logits, const void* tokens, int tokens_dtype,
                                  const float* top, const float* log_sum, float temperature, const zkdl_mat* dlogits);
 
@@ -652,7 +653,8 @@ int zkdl_token_logprobs_backward(zkdl_ctx* ctx, const float* dlogp, const zkdl_m
  *   sums[0] = sum_t w (kl k - gain),  sums[1] = sum_t w k,  sums[2] = sum_t w [clipped]  over the rows that count,
  *   dlogp = w ((clipped ? 0 : -r A) + kl (1 - exp(d))),
  * clipped where A > 0 and r > 1 + clip_high or A < 0 and r < 1 - clip_low.  weight: w, or NULL for 1 / T; a row of weight 0 adds nothing and has
- * no gradient whatever else is given for it.
+ * no gradient whatever else is given for it.  Ratio, divergence and gain are in 64 bits; a row's terms and its dlogp are rounded once to 32, with the
+ * weight in them.  k is infinite where logp or ref_logp alone is (not NaN).
  * 0 <= clip_low <= 1, clip_high >= 0 and finite, kl finite and 0 without ref_logp.  sums: 3 floats.  logp, dlogits may be NULL. */
 typedef struct {
     const float *old_logp, *advantage, *ref_logp, *weight;

@@ -72,9 +72,10 @@ __device__ __forceinline__ float below_top(float x, float times, float top) {
     return u - top;
 }
 
-// log_sum and logp in 64 bits: in 32 their last places are a millionth at 10, which a loss has in every ratio and, of sums that cancel, in its first
-// places (policy, 2000 x 4001 16-bit entries, a loss of 0.03: off by 2.9e-9, from log-probabilities in 32 bits by 7.8e-9).  The logarithm is the
-// exponent and that of a number next to 1, which 32 bits hold to 2^-25.
+// The logarithm of a row's sum, and what is taken from it, in 64 bits: in 32 the last places of log_sum and logp are a millionth at 10, which a loss has in
+// every ratio and, of sums that cancel, in its first places (policy, 2000 x 4001 16-bit entries, a loss of 0.03: off by 2.1e-9, from log-probabilities
+// rounded to 32 bits by 5.6e-9).  The logarithm is the exponent and that of a number next to 1, which 32 bits hold to 2^-25.  The sum itself is in 32
+// bits, and so is k, whose rounding all terms share: both stay in logp (4096 x 131072 entries: off by -5e-8 on average over the rows).
 struct RowStats {
     float top, log_sum;
     double logp;
@@ -278,7 +279,7 @@ __device__ __forceinline__ void put_zeros(T* to, uint32_t mine, uint32_t turn, b
 // blocks of 512 threads with 128 registers each, and half of the LDS, have room in a compute unit up to rows of 256 kB, and one of them has
 // memory at work while the other computes.  (As many instances as there are lengths: with a count that the kernel learns when it runs, the
 // vectors' registers were copied and spilled.)  Bound by memory: log-probabilities of 4096 x 32768 16-bit entries, a quarter of the rows
-// not read, 38.3 us (5.2 TB/s); the policy's gradient of 4096 x 131072, a quarter zeros, 356 us (5.3 TB/s), of 4096 x 16384 50 us (5.4 TB/s).
+// not read, 38.3 us (5.2 TB/s); the policy's gradient of 4096 x 131072, a quarter zeros, 360 us (5.2 TB/s), of 4096 x 16384 49 us (5.5 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int loss_threads(int G) { return G < 256 ? 256 : G; }
 // vectors in registers, by what else a thread holds, and in LDS, of which a compute unit has 160 kB
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(loss_threads(G), G == 512 ? 4 : 1) void k_loss_rows
 // ---------------------------------------------------------------------------
 // Rows of up to 8 G entries for G = 8, 16 or 32 lanes: as many rows in a wave as fit, a vector of eight (or what there is) a lane.
 // ROWS_SLOPE: the gradient from dlogp, top and log_sum alone.  2^20 rows of 128 32-bit entries: log-probabilities 112 us (4.8 TB/s), gradient
-// 191 us (5.6 TB/s), policy 225 us.
+// 191 us (5.6 TB/s), policy 223 us.
 // ---------------------------------------------------------------------------
 template <int G, bool MAX>
 __device__ __forceinline__ float lanes_reduce(float x) {
@@ -718,7 +719,7 @@ __global__ __launch_bounds__(256) void k_loss_slope(LossArgs a, const float* dlo
 struct PairArgs {
     uint64_t rows, pairs;
     Ints tokens, offsets;
-    const double* logp;
+    const double* logp;         // (as they came out of the rows: what rounding took from each would be in the margin, where the sums cancel)
     const float *ref_logp, *weight;
     int form, average;
     float every, beta, target, smoothing;
