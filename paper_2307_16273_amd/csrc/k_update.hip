@@ -242,8 +242,16 @@ __device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
     return x;
 }
 
+// 1 ulp.  The instruction takes what is below 2^-126 for 0, which leaves nothing to divide by where eps is as small as such a root: SMALL.
+template <bool SMALL>
+__device__ __forceinline__ float root_of(float v) {
+    if (!SMALL) return __builtin_amdgcn_sqrtf(v);
+    const bool small = v < FLT_MIN;
+    const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
+    return small ? r * 0x1p-32f : r;
+}
 // BITS: of the states.  A thread has eight adjacent entries of every 2048; 32 threads have a block of an 8-bit state.  FULL: the tensor does not end in
-// the chunk, so that no load waits for a branch.
+// the chunk, so that no load waits for a branch.  SMALL: roots of subnormal numbers (2 to 3 % of the time where they are not asked for).
 struct AdamJob {
     double b1, b2, c1, c2;      // m <- b1 m + c1 grad, v <- b2 v + (c2 grad)^2: the gradients' factor is in c1 and c2
     AdamRates rates;
@@ -265,7 +273,7 @@ __device__ __forceinline__ void store_entries(T* p, int n, const float (&f)[8]) 
     if constexpr (FULL) store8(p, f);
     else l8_store(p, n, f);
 }
-template <class P, class G, int BITS, bool FULL>
+template <class P, class G, int BITS, bool FULL, bool SMALL>
 __device__ __forceinline__ void adam_chunk(const AdamJob& a, const typename AdamArgs<BITS>::Tensor& t, uint64_t at) {
     P* const param = (P*)t.param;
     const G* const grad = (const G*)t.grad;
@@ -321,7 +329,7 @@ __device__ __forceinline__ void adam_chunk(const AdamJob& a, const typename Adam
                 const double d = (double)g[q], d2 = a.c2 * d;
                 m[q] = (float)fma(a.c1, d, b1 * (double)m[q]);
                 v[q] = (float)fma(d2, d2, b2 * (double)v[q]);
-                const float below = fmaf(__builtin_amdgcn_sqrtf(v[q]), a.rates.root, a.eps);
+                const float below = fmaf(root_of<SMALL>(v[q]), a.rates.root, a.eps);
                 p[q] = fmaf(-a.rates.rate * m[q], __builtin_amdgcn_rcpf(below), p[q] * a.rates.keep);
                 if (BITS == 8 && (FULL || q < n[k])) {
                     tm = max(tm, l8_mag(m[q]));
@@ -379,8 +387,8 @@ __device__ __forceinline__ void adam_chunk(const AdamJob& a, const typename Adam
     }
 }
 
-// BITS: of the states
-template <class P, class G, int BITS>
+// BITS: of the states; SMALL: as in adam_chunk
+template <class P, class G, int BITS, bool SMALL>
 __global__ __launch_bounds__(256) void k_adamw(AdamArgs<BITS> a) {
     __shared__ AdamRates s_rates;
     const uint32_t i = tensor_of(a.first, a.count, blockIdx.x);
@@ -409,8 +417,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamArgs<BITS> a) {
     if constexpr (BITS == 8) key = mix(mix(mix(mix(a.seed_lo) ^ a.seed_hi) ^ step) ^ t.number);
     const uint64_t at = (uint64_t)(blockIdx.x - a.first[i]) * ADAM_CHUNK + threadIdx.x * 8;
     const AdamJob job = {a.beta1, a.beta2, (1 - a.beta1) * factor, a.root2 * factor, rates, a.eps, key, go};
-    if ((uint64_t)(blockIdx.x - a.first[i] + 1) * ADAM_CHUNK <= t.n) adam_chunk<P, G, BITS, true>(job, t, at);
-    else adam_chunk<P, G, BITS, false>(job, t, at);
+    if ((uint64_t)(blockIdx.x - a.first[i] + 1) * ADAM_CHUNK <= t.n) adam_chunk<P, G, BITS, true, SMALL>(job, t, at);
+    else adam_chunk<P, G, BITS, false, SMALL>(job, t, at);
 }
 
 template <class F>
@@ -471,6 +479,8 @@ void adamw(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const 
     a.rate = rates.rate;
     a.root = rates.root;
     a.keep = rates.keep;
+    // a subnormal v, below 2^-126, divided by 1 - beta2^t, which is 1 - beta2 at least, has a root below 2^-26 of eps: half a unit of 32 bits is not reached
+    const bool small = how->eps * a.root2 < 0x1p-37;
     // tensors of the same types share launches
     const int types[3] = {ZKDL_F32, ZKDL_F16, ZKDL_BF16};
     uint32_t there = 0;
@@ -485,7 +495,8 @@ void adamw(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const 
             if (!a.count) return;
             by_type(types[k / 3], [&](auto p) {
                 by_type(types[k % 3], [&](auto g) {
-                    hipLaunchKernelGGL((k_adamw<decltype(p), decltype(g), BITS>), dim3(a.first[a.count]), dim3(256), 0, ctx->stream, a);
+                    const auto kernel = small ? k_adamw<decltype(p), decltype(g), BITS, true> : k_adamw<decltype(p), decltype(g), BITS, false>;
+                    hipLaunchKernelGGL(kernel, dim3(a.first[a.count]), dim3(256), 0, ctx->stream, a);
                 });
             });
             a.count = 0;

@@ -115,6 +115,27 @@ def test_adamw_32(lib, ctx, shapes, ptype, gtype):
                 check_params(params[i], want, move, p)
 
 
+@pytest.mark.parametrize("eps", [1e-8, 1e-20, 1e-30, 1e-37])
+def test_second_moments_below_the_normal_numbers(lib, ctx, eps):
+    """Gradients from 1 down to 1e-23 and 0: v goes down to 0 through the subnormal numbers, and its root with it."""
+    g = gen(31)
+    n = 3000
+    d = torch.randn(n, generator=g) * 10.0 ** (-(torch.arange(n) % 24).float())
+    d[::50] = 0
+    p, m, v = torch.randn(n, generator=g) * 1e-3, torch.zeros(n), torch.zeros(n)
+    how = dict(lr=0.01, beta1=0.9, beta2=0.999, eps=eps, decay=0.0)
+    want, move, m64, v64 = adam64(p, d, m, v, 1, factor=1.0, **how)
+    assert ((v64.float() > 0) & (v64.float() < 2.0 ** -126)).sum() > 100
+    for bits in (32, 8):
+        w, state = p.cuda(), lib.adamw_state([p.cuda()], bits)
+        lib.adamw_step(ctx, [w], [d.cuda()], state, 1, **how)
+        # the 64-bit moments of either side may round to neighbouring numbers of 32 bits, of which subnormal ones are far apart
+        (near, far) = (adam64(p, d * s, m, v, 1, factor=1.0, **how)[1] for s in (1 - 2.0 ** -50, 1 + 2.0 ** -50))
+        slack = torch.maximum((near - move).abs(), (far - move).abs())
+        err = 2 * U * p.double().abs() + 12 * U * move.abs() + U * want.abs() + 2.0 ** -148 + slack
+        assert torch.all((w.cpu().double() - want).abs() <= err)
+
+
 def mix(x):
     x = x ^ x >> 16
     x = x * 0x9E3779B1 & M32
