@@ -127,11 +127,11 @@ struct AdamArgs {
     Tensor t[TENSORS];
     uint32_t first[TENSORS + 1];
     uint32_t count, seed_lo, seed_hi, step;
-    double lr, decay, beta1, beta2, root2;      // root2: (1 - beta2)^(1/2)
+    double lr, decay, beta1, beta2, root2, scale;       // root2: (1 - beta2)^(1/2); scale: of rate, root and eps
     const int64_t* step_ptr;
     const float *lr_ptr, *factor;
     float eps;
-    float rate, root, keep;     // lr / (1 - beta1^t), (1 - beta2^t)^(-1/2), 1 - lr decay
+    float rate, root, keep;     // scale lr / (1 - beta1^t), scale (1 - beta2^t)^(-1/2), 1 - lr decay
 };
 static_assert(sizeof(AdamArgs<32>) <= 4096 - 256 && sizeof(AdamArgs<8>) <= 4096 - 256, "a launch's arguments");
 
@@ -147,10 +147,10 @@ static __host__ __device__ inline double power_of(double b, uint32_t t) {       
     }
     return r;
 }
-static __host__ __device__ inline AdamRates adam_rates(double lr, double decay, double beta1, double beta2, uint32_t t) {
+static __host__ __device__ inline AdamRates adam_rates(double lr, double decay, double beta1, double beta2, double scale, uint32_t t) {
     AdamRates r;
-    r.rate = (float)(lr / (1 - power_of(beta1, t)));
-    r.root = (float)(1 / sqrt(1 - power_of(beta2, t)));
+    r.rate = (float)(scale * lr / (1 - power_of(beta1, t)));
+    r.root = (float)(scale / sqrt(1 - power_of(beta2, t)));
     r.keep = (float)fma(-lr, decay, 1.0);       // (rounded once, on either side)
     return r;
 }
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamArgs<BITS> a) {
         step = go ? (uint32_t)v : 1;
     }
     if (a.step_ptr || a.lr_ptr) {
-        if (threadIdx.x == 0) s_rates = adam_rates(a.lr_ptr ? (double)*a.lr_ptr : a.lr, a.decay, a.beta1, a.beta2, step);
+        if (threadIdx.x == 0) s_rates = adam_rates(a.lr_ptr ? (double)*a.lr_ptr : a.lr, a.decay, a.beta1, a.beta2, a.scale, step);
         __syncthreads();
         rates = s_rates;
     }
@@ -474,8 +474,9 @@ void adamw(zkdl_ctx* ctx, const zkdl_adamw_tensor* tensors, size_t count, const 
     a.step_ptr = how->step_ptr;
     a.lr_ptr = how->lr_ptr;
     a.factor = how->factor;
-    a.eps = (float)how->eps;
-    const AdamRates rates = adam_rates(a.lr, a.decay, a.beta1, a.beta2, a.step);
+    a.scale = how->eps < 0x1p64 ? 1 : 0x1p-64;      // the reciprocal of what is above 2^126 would be 0
+    a.eps = (float)(how->eps * a.scale);
+    const AdamRates rates = adam_rates(a.lr, a.decay, a.beta1, a.beta2, a.scale, a.step);
     a.rate = rates.rate;
     a.root = rates.root;
     a.keep = rates.keep;

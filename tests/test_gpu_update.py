@@ -136,6 +136,20 @@ def test_second_moments_below_the_normal_numbers(lib, ctx, eps):
         assert torch.all((w.cpu().double() - want).abs() <= err)
 
 
+@pytest.mark.parametrize("eps", [1e15, 1e25, 1e38, 3e38])
+def test_an_eps_as_large_as_numbers_go(lib, ctx, eps):
+    """A step is as long as the definition's, from numbers of the host and of the device.  (v stays in the range of 32 bits.)"""
+    n = 300
+    for d, lr in ((torch.full((n,), 1e18), 1.0), (torch.linspace(1e16, 5e18, n), 1e6)):
+        zero = torch.zeros(n)
+        how = dict(beta1=0.9, beta2=0.999, eps=eps, decay=0.0)
+        want, move, _, _ = adam64(zero, d, zero, zero, 1, factor=1.0, lr=lr, **how)
+        for at in (1, torch.tensor(1, device="cuda")):
+            w, state = torch.zeros(n, device="cuda"), lib.adamw_state([zero.cuda()])
+            lib.adamw_step(ctx, [w], [d.cuda()], state, at, lr, **how)
+            assert torch.all((w.cpu().double() - want).abs() <= 13 * U * move.abs() + 2.0 ** -149)
+
+
 def mix(x):
     x = x ^ x >> 16
     x = x * 0x9E3779B1 & M32
