@@ -635,7 +635,7 @@ int zkdl_matmul_i8_backward(zkdl_ctx* ctx, const zkdl_mat* dy, const zkdl_mat* a
  * Entries of -infinity (a masked vocabulary) have p = 0; rows that hold a NaN, +infinity or nothing but -infinity give NaN.  Where u is beyond
  * the range of 32 bits (masks of the lowest value at a temperature below 1) top is infinite; the rest holds.
  * dlogits: the gradient of the logits, logits' type and shape, dlogits_j = dlogp ([j = token] - p_j) / temperature; a row whose dlogp
- * is 0 has zeros whatever it holds.  temperature: positive, normal, finite; so is its reciprocal.  Sums in 32 bits and more, in an
+ * is 0 has zeros whatever it holds.  temperature: 2^-126 .. 2^120.  Sums in 32 bits and more, in an
  * order that depends on the sizes and the row's place alone.  Float arrays without a type are 32-bit and hold T entries where nothing else is said.
  * Conventions (stream, scratch, graphs, outputs that overlap nothing) and errors as for the 8-bit layers. */
 

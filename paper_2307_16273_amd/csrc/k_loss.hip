@@ -877,7 +877,8 @@ int launch_parts(zkdl_ctx* ctx, const LossArgs& a, L8Mat<const T> x) {
 }
 
 bool ints_ok(int dtype) { return dtype == ZKDL_I32 || dtype == ZKDL_I64; }
-bool good_tau(float tau) { return tau >= FLT_MIN && tau <= FLT_MAX && 1.f / tau >= FLT_MIN && 1.f / tau <= FLT_MAX; }
+// Above 2^120 a term would be there whose distance from the largest logit is beyond 32 bits.
+bool good_tau(float tau) { return tau >= FLT_MIN && tau <= 0x1p120f && 1.f / tau <= FLT_MAX; }
 bool rows_ok(const zkdl_mat* m) { return l8_mat_ok(m, false) && l8_is_float(m->dtype) && m->stack == 1 && (m->rows == 0 || m->cols > 0); }
 bool slope_ok(const zkdl_mat* d, const zkdl_mat* x) { return !d || (l8_mat_ok(d, true) && d->dtype == x->dtype && l8_same_shape(d, x)); }
 

@@ -174,3 +174,28 @@ def test_log_probabilities_of_logits_far_from_zero(lib, ctx, shape, dtype):
         row.logp_err = row.sum_err + U * row.logp.abs()
         for got in (lib.token_logprobs(ctx, x, y, temperature=tau), lib.policy_loss(ctx, x, y, row.logp.float(), row.logp.float(), temperature=tau)):
             row.check({k: got[k] for k in ("logp", "log_sum") if k in got})
+
+
+@pytest.mark.parametrize("shape", PATHS, ids=str)
+def test_temperatures_from_one_end_to_the_other(lib, ctx, shape):
+    """Logits a few temperatures apart, and among them the largest and the lowest, whose distance is no 32-bit number.  Beyond 2^120 such a distance would count
+    for something: refused."""
+    T, V = shape
+    g = gen(T * V + 1)
+    for tau in (2.0 ** -126, 2.0 ** -124 / 3, 1e-20, 1e20, 1e35, 2.0 ** 120):
+        tau = torch.tensor(tau).item()
+        x, y = (2 * tau * torch.randn((T, V), generator=g).double()).float(), torch.randint(0, V, (T,), generator=g)
+        x[1, 0], x[1, V // 2], x[2, 3] = torch.finfo(torch.float32).max, torch.finfo(torch.float32).min, torch.finfo(torch.float32).min
+        row = Row64(x, y, tau)
+        row.sum_err = (2 * math.log(V) + 22 + 264) * U
+        row.log_sum_err = row.sum_err + U * row.log_sum.abs()
+        row.logp_err = row.sum_err + U * row.logp.abs() * 4
+        got = lib.token_logprobs(ctx, x.cuda(), y.cuda(), temperature=tau)
+        finite = row.logp.abs() < 3e38      # (a distance of more temperatures than 32 bits hold is infinite)
+        assert torch.all(((got["logp"].double() - row.logp).abs() <= row.logp_err) | ~finite) and torch.all(got["logp"][~finite] == -math.inf)
+        assert torch.all((got["log_sum"].double() - row.log_sum).abs() <= row.log_sum_err)
+    for tau in (2.0 ** 120 * (1 + 2.0 ** -23), 8e37, 2.0 ** -125 / 3, 2.0 ** -127):
+        for call in (lambda: lib.token_logprobs(ctx, x.cuda(), y.cuda(), temperature=tau),
+                     lambda: lib.preference_loss(ctx, x.cuda(), y.cuda(), torch.tensor([0, 1, T]).cuda(), temperature=tau)):
+            with pytest.raises(lib.ZkdlError):
+                call()
